@@ -8,6 +8,9 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
+from typing import List
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -19,7 +22,8 @@ CAPI_CLIENT = os.path.join(PKG, "fused_step_capi")  # next to libdaso.so (found 
 CAPI_CLUSTER_SRC = os.path.join(ROOT, "tests", "c", "daso_cluster_capi.c")
 CAPI_CLUSTER = os.path.join(PKG, "daso_cluster_capi")
 
-SOURCES = ["daso_kernels.hip", "daso_api.hip", "daso_host.cpp", "daso_schedule.cpp"]
+SOURCES = ["daso_kernels.hip", "daso_api.hip", "daso_host.cpp", "daso_schedule.cpp",
+           "daso_train_host.cpp", "daso_norm.hip", "daso_loss.hip", "daso_muon.hip"]
 # The bench's bandwidth-ceiling probes (the step's access pattern without its
 # arithmetic): a library of their own, outside the C ABI.
 PROBE_SOURCE = "daso_ceiling.hip"
@@ -45,20 +49,32 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found: the DASO library needs ROCm's hipcc to build")
 
 
-def build(verbose: bool = False) -> str:
-    """Compile every source into libdaso.so next to this file; returns its path."""
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), *HIP_FLAGS, "-I", INCLUDE, "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", tmp]
+def _run(cmd: List[str], verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError(f"hipcc failed with status {res.returncode}")
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed with status {res.returncode}")
     errs = [ln for ln in res.stderr.splitlines() if "warning" in ln and "packed-fp32-ops" not in ln]
     if verbose and errs:
         sys.stderr.write("\n".join(errs) + "\n")
+
+
+def build(verbose: bool = False) -> str:
+    """Compile every source into libdaso.so next to this file; returns its path."""
+    tmp = LIB + ".tmp"
+    compile_flags = [f for f in HIP_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as objs:
+        def compiled(source: str) -> str:
+            obj = os.path.join(objs, source + ".o")
+            _run([hipcc(), *compile_flags, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", obj], verbose)
+            return obj
+
+        # one source at a time is a minute, of which the step's kernels are the most
+        with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 1)) as pool:
+            found = list(pool.map(compiled, SOURCES))
+        _run([hipcc(), *HIP_FLAGS, *found, "-o", tmp], verbose)
     os.replace(tmp, LIB)
     build_probes(verbose)
     if os.path.exists(CAPI_CLIENT_SRC):

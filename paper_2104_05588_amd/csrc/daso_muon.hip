@@ -1,0 +1,616 @@
+// Newton-Schulz orthogonalisation and the optimizer step that uses it (daso_train.h).
+//
+// A step on X (m x n, m <= n) is three products: the gram matrix A = X X^T and its square,
+// both symmetric, of which only the tiles on and below the diagonal are computed and
+// stored twice, and X' = a X + B X with B = b A + c A^2.  m^2 n + m^3 + 2 m^2 n
+// multiply-adds in place of 4 m^2 n + 2 m^3.  All three are taken as A B^T with the
+// contraction contiguous, so X is kept transposed as well; the epilogue that
+// computes X' writes both.
+//
+// Numbers.  With |X|_F <= 1 at the start and the polynomial's range, entries of X, A and B stay
+// below 4 for the coefficients in use; they are stored times 2^11 as binary16.  A step
+// raises weak directions by up to a (3.4 and more, some 480 times in five steps), so X,
+// which the sum a X + B X carries forward, keeps 22 bits (hi + lo) always.  In the
+// products an error of B or of X's operand form only reaches the result through a strong
+// direction, which the steps do not raise: there 11 bits are enough for a bf16 result,
+// while fp32 results take hi hi + hi lo + lo hi.  One error of 11 bits does not average out:
+// where the rows of X are near orthogonal, A and B are near diagonal, and a X + B X takes the
+// difference of two near numbers.  So what the rounding of the diagonals left over is kept
+// in 32 bits (`rest`) and put into the products' epilogues, at the cost of one multiply-add.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+
+#include "daso_planes.h"
+#include "daso_product.h"
+#include "daso_train_host.h"
+
+namespace daso {
+namespace {
+
+using host::SchulzGroup;
+using host::SchulzRound;
+using product::f4;
+using product::half8;
+
+constexpr float kScale = 2048.0f, kUnscale = 1.0f / 2048.0f;
+
+// What the final product needs of a matrix of a flat buffer.
+struct Entry {
+  int64_t start;
+  float step;  // lr * scale
+  float pad;
+};
+static_assert(sizeof(Entry) == 16, "the table of a round counts 16 bytes an entry");
+
+// ------------------------------------------------------------------------- epilogues
+// v = alpha * C + beta * (in_hi + in_lo) as planes, and transposed where `t_always` or the
+// tile lies off the diagonal of a symmetric result.  With in one plane, `rest` is what its
+// diagonal lacks (square) or what that of the left operand does.
+struct PlanesOut {
+  struct Params {
+    const _Float16 *in_hi, *in_lo;
+    _Float16 *hi, *lo, *t_hi, *t_lo;
+    int64_t ld, batch, t_ld, t_batch;  // of in, hi and lo; of t_hi and t_lo
+    float alpha, beta;
+    int32_t t_always;
+    const float* rest;   // rest_ld a matrix; null: nothing is lacking
+    float* rest_out;     // of the result's diagonal
+    int32_t rest_ld;
+    int32_t square;      // C = in in^T; else C = left in
+  };
+  template <class Tile>
+  __device__ static void tile(const Params& p, const product::Args& args, const product::Place& at, f4 (&acc)[Tile::kBlocks][8],
+                              char* lds) {
+    product::by_blocks<Tile, PlanesOut>(p, args, at, acc, lds);
+  }
+  __device__ static void block(const Params& p, const product::Place& at, const f4 (&c)[8], int row,
+                               int col, char* stage, int lane) {
+    const bool turn = p.t_hi != nullptr && (p.t_always || at.tm != at.tn);
+    char* plane = stage + product::kStageFloats;
+    const int64_t base = at.batch * p.batch;
+    const float* rest = p.rest != nullptr ? p.rest + int64_t(at.batch) * p.rest_ld : nullptr;
+    product::by_rows(c, stage, lane, [&](int r, int k, float(&v)[8]) {
+      const int64_t to = base + int64_t(row + r) * p.ld + col + k;
+      if (p.in_hi != nullptr) {
+        const half8 h = *(const half8*)(p.in_hi + to);
+        half8 l = (half8)(_Float16)0.0f;
+        if (p.in_lo != nullptr) l = *(const half8*)(p.in_lo + to);
+        const float left = rest != nullptr ? rest[row + r] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float in = static_cast<float>(h[i]) + static_cast<float>(l[i]), more = left;
+          if (rest != nullptr && p.square) {
+            more += rest[col + k + i];
+            in += row + r == col + k + i ? left : 0.0f;
+          }
+          v[i] = fmaf(p.beta, in, p.alpha * fmaf(more, in, v[i]));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= p.alpha;
+      }
+      half8 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        _Float16 a, b;
+        product::split(v[i], &a, &b);
+        hi[i] = a, lo[i] = b;
+        if (p.rest_out != nullptr && row + r == col + k + i)
+          p.rest_out[int64_t(at.batch) * p.rest_ld + row + r] = v[i] - static_cast<float>(a);
+      }
+      *(half8*)(p.hi + to) = hi;
+      if (p.lo != nullptr) *(half8*)(p.lo + to) = lo;
+      if (turn) {
+        *(half8*)(plane + product::plane_at(r, k)) = hi;
+        if (p.t_lo != nullptr) *(half8*)(plane + product::kStagePlane + product::plane_at(r, k)) = lo;
+      }
+    });
+    if (!turn) return;
+    product::wait_lds();
+    __builtin_amdgcn_wave_barrier();
+    const int64_t t_base = at.batch * p.t_batch;
+    product::by_columns(plane, lane, [&](int k, int r, half8 v) {
+      *(half8*)(p.t_hi + t_base + int64_t(col + k) * p.t_ld + row + r) = v;
+    });
+    if (p.t_lo != nullptr)
+      product::by_columns(plane + product::kStagePlane, lane, [&](int k, int r, half8 v) {
+        *(half8*)(p.t_lo + t_base + int64_t(col + k) * p.t_ld + row + r) = v;
+      });
+  }
+};
+
+// The last step's X' = a X + C in the source's orientation: written as it is, or taken as
+// the update of a matrix of the flat parameter buffer.
+struct LastOut {
+  enum Kind { kF32, kBf16, kStep };
+  struct Params {
+    const _Float16 *in_hi, *in_lo;
+    int64_t ld, batch;
+    float alpha, beta;
+    int32_t kind;
+    int32_t rows, cols;
+    void* out;  // kF32, kBf16
+    int64_t out_ld, out_batch;
+    const Entry* table;  // kStep: of the group's matrices
+    float* params;
+    uint16_t* wire;
+    float keep;  // 1 - lr * weight_decay
+    const float* rest;  // as above, of the square operand, which is the right one where `right`
+    int32_t rest_ld, right;
+  };
+  template <class Tile>
+  __device__ static void tile(const Params& p, const product::Args& args, const product::Place& at, f4 (&acc)[Tile::kBlocks][8],
+                              char* lds) {
+    product::by_blocks<Tile, LastOut>(p, args, at, acc, lds);
+  }
+  __device__ static void block(const Params& p, const product::Place& at, const f4 (&c)[8], int row,
+                               int col, char* stage, int lane) {
+    const int64_t base = at.batch * p.batch;
+    int64_t out = p.out_batch * at.batch, out_ld = p.out_ld;
+    float step = 0.0f;
+    if (p.kind == kStep) {
+      const Entry e = p.table[at.batch];
+      out = e.start, out_ld = p.cols, step = e.step;
+    }
+    const size_t esz = p.kind == kBf16 ? 2 : 4;
+    char* first = p.kind == kStep ? (char*)p.params : (char*)p.out;
+    const bool wide = ((reinterpret_cast<uintptr_t>(first + out * esz) | (out_ld * esz)) & 15) == 0 &&
+                      (p.wire == nullptr || ((out | out_ld) & 7) == 0);
+    const float* rest = p.rest != nullptr ? p.rest + int64_t(at.batch) * p.rest_ld : nullptr;
+    product::by_rows(c, stage, lane, [&](int r, int k, float(&v)[8]) {
+      const int64_t from = base + int64_t(row + r) * p.ld + col + k;
+      const half8 h = *(const half8*)(p.in_hi + from), l = *(const half8*)(p.in_lo + from);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float in = static_cast<float>(h[i]) + static_cast<float>(l[i]);
+        const float more = rest != nullptr ? rest[p.right ? col + k + i : row + r] : 0.0f;
+        v[i] = fmaf(p.beta, in, p.alpha * fmaf(more, in, v[i])) * kUnscale;
+      }
+      const int32_t rr = row + r, cc = col + k;
+      if (rr >= p.rows || cc >= p.cols) return;
+      const int64_t to = out + int64_t(rr) * out_ld + cc;
+      const int32_t left = p.cols - cc;
+      if (p.kind == kStep) {
+        if (wide && left >= 8) {
+          float x[8];
+          load8(p.params + to, x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = x[i] * p.keep - step * v[i];
+          store8(p.params + to, x);
+          if (p.wire != nullptr) store8(p.wire + to, x);
+        } else {
+          for (int i = 0; i < 8 && i < left; ++i) {
+            const float x = p.params[to + i] * p.keep - step * v[i];
+            p.params[to + i] = x;
+            if (p.wire != nullptr) p.wire[to + i] = to_bf16(x);
+          }
+        }
+      } else if (p.kind == kF32) {
+        float* o = (float*)p.out + to;
+        if (wide && left >= 8) store8(o, v);
+        else
+          for (int i = 0; i < 8 && i < left; ++i) o[i] = v[i];
+      } else {
+        uint16_t* o = (uint16_t*)p.out + to;
+        if (wide && left >= 8) store8(o, v);
+        else
+          for (int i = 0; i < 8 && i < left; ++i) o[i] = to_bf16(v[i]);
+      }
+    });
+  }
+};
+
+// ------------------------------------------------------------------------- before the products
+// The matrices of a round as kernel arguments.
+struct RoundTable {
+  int64_t start[host::kRoundMatrices];
+  float step[host::kRoundMatrices];
+  int32_t count;
+  int32_t groups;
+  int32_t first[host::kRoundGroups + 1];  // the first matrix of each group
+  int64_t elems[host::kRoundGroups];
+  float* source[host::kRoundGroups];
+};
+
+__device__ inline int group_of(const int32_t* first, int32_t groups, int matrix) {
+  int k = 0;
+  while (k + 1 < groups && matrix >= first[k + 1]) ++k;
+  return k;
+}
+
+struct MomentumArgs {
+  const float* grads[DASO_MAX_G];
+  float* momentum;
+  Entry* table;
+  double* sums;  // kSumParts a matrix
+  int32_t g, nesterov;
+  float mu;
+};
+
+// gbar, m' and u of a part of a matrix, and the part's sum of u^2.  Sums in binary64: the
+// order of 64 parts and 256 threads then does not show.
+__global__ __launch_bounds__(256) void momentum_kernel(MomentumArgs a, RoundTable t) {
+  __shared__ double shared[4];
+  const int matrix = blockIdx.y, k = group_of(t.first, t.groups, matrix);
+  const int64_t elems = t.elems[k], start = t.start[matrix];
+  float* u = t.source[k] + (matrix - t.first[k]) * elems;
+  const int64_t each = ((elems + gridDim.x - 1) / gridDim.x + 3) / 4 * 4;
+  const int64_t lo = each * blockIdx.x, hi = lo + each < elems ? lo + each : elems;
+  const float gf = static_cast<float>(a.g);
+  double sum = 0;
+  auto one = [&](float s, float m, float* m_out) {
+    const float gbar = a.g > 1 ? s / gf : s;
+    const float mm = a.mu * m + gbar;
+    *m_out = mm;
+    const float v = a.nesterov ? gbar + a.mu * mm : mm;
+    sum += static_cast<double>(v) * v;
+    return v;
+  };
+  if (((start | elems) & 3) == 0) {
+    for (int64_t i = lo + 4 * threadIdx.x; i < hi; i += 1024) {
+      f4v s = *(const f4v*)(a.grads[0] + start + i);
+      for (int r = 1; r < a.g; ++r) s += *(const f4v*)(a.grads[r] + start + i);
+      f4v m = *(const f4v*)(a.momentum + start + i), v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float mm;
+        v[j] = one(s[j], m[j], &mm);
+        m[j] = mm;
+      }
+      *(f4v*)(a.momentum + start + i) = m;
+      *(f4v*)(u + i) = v;
+    }
+  } else {
+    for (int64_t i = lo + threadIdx.x; i < hi; i += 256) {
+      float s = a.grads[0][start + i];
+      for (int r = 1; r < a.g; ++r) s += a.grads[r][start + i];
+      float mm;
+      u[i] = one(s, a.momentum[start + i], &mm);
+      a.momentum[start + i] = mm;
+    }
+  }
+  sum = group_sum(sum, shared);
+  if (threadIdx.x == 0) {
+    a.sums[matrix * host::kSumParts + blockIdx.x] = sum;
+    if (blockIdx.x == 0) a.table[matrix] = {start, t.step[matrix], 0.0f};
+  }
+}
+
+// The sum of squares of a part of a matrix that is only read.
+template <class T>
+__global__ __launch_bounds__(256) void squares_kernel(const T* src, int64_t batch_stride, int64_t stride, int32_t rows,
+                                                      int32_t cols, double* sums) {
+  __shared__ double shared[4];
+  const T* p = src + blockIdx.y * batch_stride;
+  const int32_t each = (rows + gridDim.x - 1) / gridDim.x;
+  const int32_t lo = each * blockIdx.x, hi = lo + each < rows ? lo + each : rows;
+  double sum = 0;
+  const bool wide = ((reinterpret_cast<uintptr_t>(p) | (stride * sizeof(T))) & 15) == 0;
+  const int32_t whole = wide ? cols / 8 * 8 : 0;
+  for (int32_t r = lo + (threadIdx.x >> 6); r < hi; r += 4) {
+    const T* q = p + r * stride;
+    for (int32_t c = (threadIdx.x & 63) * 8; c < whole; c += 512) {
+      float v[8];
+      load8(q + c, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += static_cast<double>(v[i]) * v[i];
+    }
+    for (int32_t c = whole + (threadIdx.x & 63); c < cols; c += 64) {
+      const double v = load1(q + c);
+      sum += v * v;
+    }
+  }
+  sum = group_sum(sum, shared);
+  if (threadIdx.x == 0) sums[blockIdx.y * host::kSumParts + blockIdx.x] = sum;
+}
+
+struct LayOut {
+  int32_t groups;
+  int32_t parts;  // sums of a matrix
+  int64_t first_tile[host::kRoundGroups + 1];
+  int32_t first_matrix[host::kRoundGroups];
+  PlanesArgs p[host::kRoundGroups];
+  const double* sums;
+  float eps;
+};
+
+// X = u / (|u| + eps) as planes, straight and transposed.
+template <class T>
+__global__ __launch_bounds__(256) void normalise_kernel(LayOut a) {
+  __shared__ uint16_t lds[2][64][66];
+  const int64_t id = blockIdx.x + int64_t(blockIdx.y) * gridDim.x;
+  if (id >= a.first_tile[a.groups]) return;
+  int k = 0;
+  while (k + 1 < a.groups && id >= a.first_tile[k + 1]) ++k;
+  const PlanesArgs& p = a.p[k];
+  const int64_t t = id - a.first_tile[k], across = p.cols_p / 64, per = across * (p.rows_p / 64);
+  const int64_t batch = t / per;
+  const double* s = a.sums + (a.first_matrix[k] + batch) * host::kSumParts;
+  double sum = 0;
+  for (int i = 0; i < a.parts; ++i) sum += s[i];
+  const float scale = static_cast<float>(kScale / (sqrt(sum) + a.eps));
+  planes_tile<T, false>(p, batch, static_cast<int>((t % per) / across), static_cast<int>(t % across), scale, lds);
+}
+
+// ------------------------------------------------------------------------- host
+_Float16* plane(char* ws, size_t at) { return reinterpret_cast<_Float16*>(ws + at); }
+
+int32_t parts_of(int64_t elems) {
+  const int64_t p = (elems + 8191) / 8192;
+  return static_cast<int32_t>(p < 1 ? 1 : p > host::kSumParts ? host::kSumParts : p);
+}
+
+// Planes of X from the sources' matrices.  src: null for the round's own copies.
+template <class T>
+hipError_t normalise(const SchulzRound& r, char* ws, const T* src, int64_t src_batch, int64_t src_stride, int32_t parts,
+                     float eps, bool full, hipStream_t stream) {
+  LayOut a = {};
+  a.groups = static_cast<int32_t>(r.groups.size());
+  a.parts = parts;
+  a.eps = eps;
+  a.sums = reinterpret_cast<const double*>(ws + host::kRoundMatrices * sizeof(Entry));
+  for (int32_t k = 0; k < a.groups; ++k) {
+    const SchulzGroup& g = r.groups[k];
+    PlanesArgs& p = a.p[k];
+    p.src = src != nullptr ? (const void*)src : (const void*)(ws + g.source);
+    p.stride = src != nullptr ? src_stride : g.cols;
+    p.batch_stride = src != nullptr ? src_batch : g.rows * g.cols;
+    p.rows = static_cast<int32_t>(g.rows), p.cols = static_cast<int32_t>(g.cols);
+    p.rows_p = static_cast<int32_t>(g.tall ? g.n : g.m), p.cols_p = static_cast<int32_t>(g.tall ? g.m : g.n);
+    for (int i = 0; i < 2; ++i) {
+      uint16_t* x = reinterpret_cast<uint16_t*>(ws + g.x[0][i]);
+      uint16_t* xt = reinterpret_cast<uint16_t*>(ws + g.xt[0][i]);
+      p.d[i] = g.tall ? xt : x;
+      p.t[i] = g.tall ? x : xt;
+    }
+    // the transpose's low plane is read by products in 22 bits and by a tall matrix's last step
+    if (!full && !g.tall) p.t[1] = nullptr;
+    a.first_matrix[k] = g.first;
+    a.first_tile[k + 1] = a.first_tile[k] + int64_t(p.rows_p / 64) * (p.cols_p / 64) * g.count;
+  }
+  const int64_t tiles = a.first_tile[a.groups], row = int64_t(1) << 20;
+  return launch(&normalise_kernel<T>, dim3(static_cast<uint32_t>(tiles < row ? tiles : row), static_cast<uint32_t>((tiles + row - 1) / row)),
+                dim3(256), stream, a);
+}
+
+// Operands of a product: X's or the square's planes, in one segment or three.
+void operands(product::Args& p, const _Float16* a_hi, const _Float16* a_lo, const _Float16* b_hi, const _Float16* b_lo,
+              bool full) {
+  p.segments = full ? 3 : 1;
+  p.a[0] = a_hi, p.b[0] = b_hi;
+  p.a[1] = a_hi, p.b[1] = b_lo;
+  p.a[2] = a_lo, p.b[2] = b_hi;
+}
+
+// The steps of one round, from planes in buffer 0 to `last`, whose Params lack only what
+// the steps know.
+hipError_t schulz_steps(const SchulzRound& r, char* ws, int32_t steps, const float* coefficients, bool full,
+                        const std::vector<LastOut::Params>& last, hipStream_t stream) {
+  const int32_t groups = static_cast<int32_t>(r.groups.size());
+  for (int32_t s = 0; s < steps; ++s) {
+    const float a = coefficients[3 * s], b = coefficients[3 * s + 1], c = coefficients[3 * s + 2];
+    const int from = s & 1, to = from ^ 1;
+    const bool end = s + 1 == steps;
+    product::Launch<PlanesOut> gram = {}, poly = {}, next = {};
+    product::Launch<LastOut> final_ = {};
+    gram.count = poly.count = next.count = final_.count = groups;
+    for (int32_t k = 0; k < groups; ++k) {
+      const SchulzGroup& g = r.groups[k];
+      const int32_t m = static_cast<int32_t>(g.m), n = static_cast<int32_t>(g.n);
+      _Float16 *x[2], *xt[2], *y[2], *yt[2], *q[2], *w[2];
+      for (int i = 0; i < 2; ++i) {
+        x[i] = plane(ws, g.x[from][i]), xt[i] = plane(ws, g.xt[from][i]);
+        y[i] = plane(ws, g.x[to][i]), yt[i] = plane(ws, g.xt[to][i]);
+        q[i] = plane(ws, g.gram[i]), w[i] = plane(ws, g.poly[i]);
+      }
+      // A = X X^T
+      product::Args& pa = gram.args[k];
+      operands(pa, x[0], x[1], x[0], x[1], full);
+      pa.lda = pa.ldb = n, pa.batch_a = pa.batch_b = int64_t(m) * n;
+      pa.steps = n / 64, pa.M = pa.N = m, pa.tri = 1, pa.batch = g.count;
+      PlanesOut::Params& ga = gram.out[k];
+      ga.hi = ga.t_hi = q[0], ga.lo = ga.t_lo = full ? q[1] : nullptr;
+      ga.ld = ga.t_ld = m, ga.batch = ga.t_batch = int64_t(m) * m;
+      ga.alpha = kUnscale;
+      float *rest_q = full ? nullptr : reinterpret_cast<float*>(ws + g.rest[0]), *rest_w = full ? nullptr : reinterpret_cast<float*>(ws + g.rest[1]);
+      ga.rest_out = rest_q, ga.rest_ld = m;
+      // B = b A + c A A^T
+      product::Args& pb = poly.args[k];
+      operands(pb, q[0], q[1], q[0], q[1], full);
+      pb.lda = pb.ldb = m, pb.batch_a = pb.batch_b = int64_t(m) * m;
+      pb.steps = m / 64, pb.M = pb.N = m, pb.tri = 1, pb.batch = g.count;
+      PlanesOut::Params& gb = poly.out[k];
+      gb = ga;
+      gb.in_hi = q[0], gb.in_lo = full ? q[1] : nullptr;
+      gb.hi = gb.t_hi = w[0], gb.lo = gb.t_lo = full ? w[1] : nullptr;
+      gb.alpha = c * kUnscale, gb.beta = b;
+      gb.rest = rest_q, gb.rest_out = rest_w, gb.square = 1;
+      // X' = a X + B X, as B (X^T)^T; the last step of a tall matrix as X^T B
+      if (!end || !g.tall) {
+        product::Args& pc = end ? final_.args[k] : next.args[k];
+        operands(pc, w[0], w[1], xt[0], xt[1], full);
+        pc.lda = pc.ldb = m, pc.batch_a = int64_t(m) * m, pc.batch_b = int64_t(m) * n;
+        pc.steps = m / 64, pc.M = m, pc.N = n, pc.batch = g.count;
+      } else {
+        product::Args& pc = final_.args[k];
+        operands(pc, xt[0], xt[1], w[0], w[1], full);
+        pc.lda = pc.ldb = m, pc.batch_a = int64_t(m) * n, pc.batch_b = int64_t(m) * m;
+        pc.steps = m / 64, pc.M = n, pc.N = m, pc.batch = g.count;
+      }
+      if (!end) {
+        PlanesOut::Params& gc = next.out[k];
+        gc.in_hi = x[0], gc.in_lo = x[1];
+        gc.hi = y[0], gc.lo = y[1], gc.t_hi = yt[0], gc.t_lo = full || g.tall ? yt[1] : nullptr;
+        gc.ld = n, gc.batch = gc.t_batch = int64_t(m) * n, gc.t_ld = m;
+        gc.alpha = kUnscale, gc.beta = a, gc.t_always = 1;
+        gc.rest = rest_w, gc.rest_ld = m;
+      } else {
+        LastOut::Params& gc = final_.out[k];
+        gc = last[k];
+        gc.in_hi = g.tall ? xt[0] : x[0], gc.in_lo = g.tall ? xt[1] : x[1];
+        gc.ld = g.tall ? m : n, gc.batch = int64_t(m) * n;
+        gc.alpha = kUnscale, gc.beta = a;
+        gc.rest = rest_w, gc.rest_ld = m, gc.right = g.tall ? 1 : 0;
+        gc.rows = static_cast<int32_t>(g.rows), gc.cols = static_cast<int32_t>(g.cols);
+      }
+    }
+    hipError_t e = product::launch_products<false>(gram, stream);
+    if (e == hipSuccess) e = product::launch_products<false>(poly, stream);
+    if (e == hipSuccess) e = end ? product::launch_products<false>(final_, stream) : product::launch_products<false>(next, stream);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+size_t most_bytes(const std::vector<SchulzRound>& rounds) {
+  size_t most = 0;
+  for (const SchulzRound& r : rounds) most = r.bytes > most ? r.bytes : most;
+  return most;
+}
+
+std::vector<host::Shape> shapes_of(const daso_orthogonalize_args& s) {
+  if (s.rows == 0 || s.cols == 0) return {};
+  return std::vector<host::Shape>(static_cast<size_t>(s.batch), host::Shape{s.rows, s.cols});
+}
+std::vector<host::Shape> shapes_of(const daso_muon_args& s) {
+  std::vector<host::Shape> v;
+  for (int32_t i = 0; i < s.nmatrices; ++i) v.push_back({s.matrices[i].rows, s.matrices[i].cols});
+  return v;
+}
+
+template <class T>
+hipError_t orthogonalize_round(const daso_orthogonalize_args& s, const SchulzRound& r, hipStream_t stream) {
+  char* ws = static_cast<char*>(s.workspace);
+  const SchulzGroup& g = r.groups[0];  // one shape
+  const int64_t at = r.matrices[0];
+  const T* src = static_cast<const T*>(s.src) + at * s.src_batch_stride;
+  const int64_t rows = s.rows;
+  const int32_t parts = static_cast<int32_t>(std::min<int64_t>(parts_of(rows * s.cols), rows));
+  double* sums = reinterpret_cast<double*>(ws + host::kRoundMatrices * sizeof(Entry));
+  hipError_t e = launch(&squares_kernel<T>, dim3(parts, g.count), dim3(256), stream, src, s.src_batch_stride, s.src_stride,
+                        static_cast<int32_t>(rows), static_cast<int32_t>(s.cols), sums);
+  if (e != hipSuccess) return e;
+  const bool full = s.out_type == DASO_TYPE_F32;
+  e = normalise<T>(r, ws, src, s.src_batch_stride, s.src_stride, parts, s.eps, full, stream);
+  if (e != hipSuccess) return e;
+  LastOut::Params last = {};
+  last.kind = full ? LastOut::kF32 : LastOut::kBf16;
+  last.out = static_cast<char*>(s.out) + at * s.out_batch_stride * static_cast<int64_t>(host::bytes_of(s.out_type));
+  last.out_ld = s.out_stride, last.out_batch = s.out_batch_stride;
+  return schulz_steps(r, ws, s.steps, s.coefficients, full, {last}, stream);
+}
+
+hipError_t muon_round(const daso_muon_args& s, const SchulzRound& r, hipStream_t stream) {
+  char* ws = static_cast<char*>(s.workspace);
+  Entry* table = reinterpret_cast<Entry*>(ws);
+  MomentumArgs a = {};
+  for (int32_t k = 0; k < s.g; ++k) a.grads[k] = s.grads[k];
+  a.momentum = s.momentum;
+  a.table = table;
+  a.sums = reinterpret_cast<double*>(ws + host::kRoundMatrices * sizeof(Entry));
+  a.g = s.g, a.nesterov = (s.flags & DASO_MUON_NESTEROV) ? 1 : 0, a.mu = s.mu;
+  RoundTable t = {};
+  t.count = static_cast<int32_t>(r.matrices.size());
+  t.groups = static_cast<int32_t>(r.groups.size());
+  int64_t most = 0;
+  for (int32_t k = 0; k < t.groups; ++k) {
+    const SchulzGroup& g = r.groups[k];
+    t.first[k] = g.first;
+    t.elems[k] = g.rows * g.cols;
+    t.source[k] = reinterpret_cast<float*>(ws + g.source);
+    most = std::max(most, t.elems[k]);
+  }
+  t.first[t.groups] = t.count;
+  for (int32_t i = 0; i < t.count; ++i) {
+    const daso_matrix& m = s.matrices[r.matrices[i]];
+    t.start[i] = m.start;
+    t.step[i] = s.lr * m.scale;
+  }
+  const int32_t parts = parts_of(most);
+  hipError_t e = launch(&momentum_kernel, dim3(parts, t.count), dim3(256), stream, a, t);
+  if (e != hipSuccess) return e;
+  e = normalise<float>(r, ws, nullptr, 0, 0, parts, s.eps, true, stream);
+  if (e != hipSuccess) return e;
+  std::vector<LastOut::Params> last(r.groups.size());
+  for (int32_t k = 0; k < t.groups; ++k) {
+    LastOut::Params& p = last[k];
+    p = {};
+    p.kind = LastOut::kStep;
+    p.table = table + r.groups[k].first;
+    p.params = s.params, p.wire = s.wire;
+    p.keep = 1.0f - s.lr * s.weight_decay;
+  }
+  return schulz_steps(r, ws, s.steps, s.coefficients, true, last, stream);
+}
+
+}  // namespace
+}  // namespace daso
+
+using daso::host::SchulzRound;
+
+extern "C" {
+
+int daso_orthogonalize_workspace(const daso_orthogonalize_args* args, size_t* bytes) {
+  if (args == nullptr || bytes == nullptr) return DASO_EINVAL;
+  const int rc = daso::host::check_orthogonalize_sizes(*args);
+  if (rc != DASO_OK) return rc;
+  try {
+    *bytes = daso::most_bytes(daso::host::plan_rounds(daso::shapes_of(*args), false));
+  } catch (const std::bad_alloc&) {
+    return DASO_EHIP;
+  }
+  return DASO_OK;
+}
+
+int daso_orthogonalize(const daso_orthogonalize_args* args, hipStream_t stream) {
+  if (args == nullptr) return DASO_EINVAL;
+  const daso_orthogonalize_args& s = *args;
+  int rc = daso::host::check_orthogonalize(s);
+  if (rc != DASO_OK || s.batch == 0 || s.rows == 0 || s.cols == 0) return rc;
+  try {
+    const std::vector<SchulzRound> rounds = daso::host::plan_rounds(daso::shapes_of(s), false);
+    if ((rc = daso::host::check_workspace(s.workspace, s.workspace_bytes, daso::most_bytes(rounds))) != DASO_OK) return rc;
+    if ((rc = daso::current_device(stream)) != DASO_OK) return rc;
+    for (const SchulzRound& r : rounds) {
+      const hipError_t e = s.type == DASO_TYPE_F32 ? daso::orthogonalize_round<float>(s, r, stream)
+                                                   : daso::orthogonalize_round<uint16_t>(s, r, stream);
+      if (e != hipSuccess) return DASO_EHIP;
+    }
+  } catch (const std::bad_alloc&) {
+    return DASO_EHIP;
+  }
+  return DASO_OK;
+}
+
+int daso_muon_workspace(const daso_muon_args* args, size_t* bytes) {
+  if (args == nullptr || bytes == nullptr) return DASO_EINVAL;
+  try {
+    const int rc = daso::host::check_muon_sizes(*args);
+    if (rc != DASO_OK) return rc;
+    *bytes = daso::most_bytes(daso::host::plan_rounds(daso::shapes_of(*args), true));
+  } catch (const std::bad_alloc&) {
+    return DASO_EHIP;
+  }
+  return DASO_OK;
+}
+
+int daso_muon_step(const daso_muon_args* args, hipStream_t stream) {
+  if (args == nullptr) return DASO_EINVAL;
+  const daso_muon_args& s = *args;
+  try {
+    int rc = daso::host::check_muon(s);
+    if (rc != DASO_OK || s.n == 0 || s.nmatrices == 0) return rc;
+    const std::vector<SchulzRound> rounds = daso::host::plan_rounds(daso::shapes_of(s), true);
+    if ((rc = daso::host::check_workspace(s.workspace, s.workspace_bytes, daso::most_bytes(rounds))) != DASO_OK) return rc;
+    if ((rc = daso::current_device(stream)) != DASO_OK) return rc;
+    for (const SchulzRound& r : rounds)
+      if (daso::muon_round(s, r, stream) != hipSuccess) return DASO_EHIP;
+  } catch (const std::bad_alloc&) {
+    return DASO_EHIP;
+  }
+  return DASO_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,502 @@
+// Matrix products of 16-bit planes on the matrix cores: C = sum over segments of
+// A_s B_s^T, both operands with their contraction contiguous, 32-bit sums, and an
+// epilogue that takes C in blocks of 64 x 32 while it is still in registers.
+//
+// A value that needs more than 11 bits of significand is held as two binary16 planes,
+// hi + lo (22 bits), and a product of such values as the segments hi hi, hi lo, lo hi;
+// what is left out is below 2^-22 of the product of the magnitudes.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+namespace daso {
+namespace product {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMaxSegments = 3;
+constexpr int kStepElems = 64;     // contraction elements a step: 128 bytes of a row, one cache line
+constexpr int kLeastSteps = 2;     // the pipeline's depth: a product takes at least this many steps
+constexpr int kBlockRows = 64, kBlockCols = 32;  // what an epilogue is handed at a time
+// LDS of a wavefront's own for its epilogue: a block in 32 bits, and two planes of it in 16.
+constexpr int kStageFloats = kBlockRows * kBlockCols * 4;
+constexpr int kStagePlane = kBlockRows * kBlockCols * 2 + (kBlockRows / 8) * 16;
+constexpr int kWaveStage = kStageFloats + 2 * kStagePlane;
+constexpr int64_t kMaxLd = int64_t(1) << 22;  // row offsets within a tile stay in 32 bits
+constexpr int kMaxProblems = 8;               // products of one launch
+
+// Operands: rows of `ld` elements, 16-byte aligned, ld a multiple of 8, of which the first
+// steps * 64 are contracted (zeros beyond the true length).  Rows from M (N) on are not
+// read: a tile that reaches past them reads the last row again, and its epilogue leaves
+// what comes of it.
+struct Args {
+  const void* a[kMaxSegments];
+  const void* b[kMaxSegments];
+  int64_t lda, ldb, batch_a, batch_b;  // in elements
+  int32_t segments, steps;             // steps of 64 a segment
+  int32_t M, N;
+  int32_t tiles_m, tiles_n;            // tiles_m x tiles_n, or with tri the tiles on and below the diagonal
+  int32_t tri;
+  int32_t batch;
+};
+
+inline int64_t tile_count(const Args& p) {
+  const int64_t per = p.tri ? int64_t(p.tiles_m) * (p.tiles_m + 1) / 2 : int64_t(p.tiles_m) * p.tiles_n;
+  return per * p.batch;
+}
+
+#if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)
+
+#define DASO_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+#define DASO_GLOBAL(p) ((const __attribute__((address_space(1))) void*)(p))
+
+template <bool BF16>
+__device__ inline f4 mfma(half8 a, half8 b, f4 c) {
+  if constexpr (BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8, a), __builtin_bit_cast(bhalf8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+template <int N>
+__device__ inline void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ inline void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// The workgroup meets; nothing is moved across by the compiler.
+__device__ inline void meet() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+struct Place {
+  int tm, tn, batch;
+};
+
+// The tile `id` of a product.  Tiles are counted in bands of four tile rows, so that the
+// rows and columns that neighbouring tiles read stay in an L2.
+__device__ inline Place place_of(const Args& p, int64_t id) {
+  Place at;
+  if (p.tri) {
+    const int per = p.tiles_m * (p.tiles_m + 1) / 2;
+    at.batch = static_cast<int>(id / per);
+    const int t = static_cast<int>(id - int64_t(at.batch) * per);
+    int i = static_cast<int>((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+    while (i * (i + 1) / 2 > t) --i;
+    while ((i + 1) * (i + 2) / 2 <= t) ++i;
+    at.tm = i;
+    at.tn = t - i * (i + 1) / 2;
+  } else {
+    const int per = p.tiles_m * p.tiles_n;
+    at.batch = static_cast<int>(id / per);
+    const int t = static_cast<int>(id - int64_t(at.batch) * per);
+    constexpr int kBand = 4;
+    const int band = t / (kBand * p.tiles_n), first = band * kBand;
+    const int rows = min(p.tiles_m - first, kBand), in = t - first * p.tiles_n;
+    at.tm = first + in % rows;
+    at.tn = in / rows;
+  }
+  return at;
+}
+
+// The operand's bytes at step t of all segments.
+__device__ inline const char* step_of(const char* s0, const char* s1, const char* s2, int t, int steps) {
+  const char* base = s0;
+  if (t >= steps) {
+    base = s1;
+    t -= steps;
+    if (t >= steps) {
+      base = s2;
+      t -= steps;
+    }
+  }
+  return base + int64_t(t) * 128;
+}
+
+// LDS holds operand rows of 128 bytes; the 16-byte piece c of row r lies in place
+// c ^ (r / 2 % 8) of the row, so that 16 lanes that read one piece of 16 rows touch all
+// 64 banks once.  Loads go straight to LDS, in lane order, so it is the source address
+// that is permuted: a wavefront's load still takes whole lines.
+
+// 256 x 256 a workgroup of 8 wavefronts.  A step's operands are four pieces of 128 rows
+// (A0 A1 B0 B1, 16 KB each, two steps in LDS), and a step is four phases, one quarter
+// (128 x 128) of the tile each, in an order in which a phase changes one piece only.  A piece
+// is loaded again, for the step after the next, two phases after its last read: six
+// phases before it is wanted.  Each phase is a part that reads LDS and issues loads and a
+// part of 16 matrix instructions, and the two wavefronts of a SIMD take them in
+// opposite turns, one barrier apart, so that one of them is always computing.
+// Measured on 8192^3: 2285 cycles a step where the matrix instructions alone take 2048.  In
+// time the clock decides: under this load it falls to 1.4 to 1.6 GHz, for the power that
+// the matrix cores draw.  16x16x32 instructions draw less than 32x32x16 ones (registers
+// only: 1950 and 1670 TFLOP/s), and the whole runs at 1235 TFLOP/s, with 32x32x16 at 1040.
+struct Tile256 {
+  static constexpr int kRows = 256, kCols = 256, kThreads = 512, kLds = 8 * kWaveStage > 131072 ? 8 * kWaveStage : 131072;
+  static constexpr int kBlocks = 4;  // blocks of 64 x 32 a wavefront
+  static constexpr int kOccupancy = 2;
+
+  __device__ static void block_at(int wave, int b, int* row, int* col) {
+    *row = (b >> 1) * 128 + (wave >> 2) * 64;
+    *col = (b & 1) * 128 + (wave & 3) * 32;
+  }
+
+  template <bool BF16>
+  __device__ static void run(const Args& p, const Place& at, char* lds, f4 (&acc)[kBlocks][8]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t skip_a = (at.batch * p.batch_a + int64_t(at.tm) * kRows * p.lda) * 2;
+    const int64_t skip_b = (at.batch * p.batch_b + int64_t(at.tn) * kCols * p.ldb) * 2;
+    const char *a0 = (const char*)p.a[0] + skip_a, *a1 = (const char*)p.a[1] + skip_a, *a2 = (const char*)p.a[2] + skip_a;
+    const char *b0 = (const char*)p.b[0] + skip_b, *b1 = (const char*)p.b[1] + skip_b, *b2 = (const char*)p.b[2] + skip_b;
+    const int last_a = min(kRows, p.M - at.tm * kRows) - 1, last_b = min(kCols, p.N - at.tn * kCols) - 1;
+    const int steps = p.steps, total = p.steps * p.segments;
+    uint32_t from_a[2][2], from_b[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = (wave * 2 + j) * 8 + (lane >> 3), c = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+        from_a[h][j] = static_cast<uint32_t>(min(h * 128 + r, last_a)) * (static_cast<uint32_t>(p.lda) * 2) + c;
+        from_b[h][j] = static_cast<uint32_t>(min(h * 128 + r, last_b)) * (static_cast<uint32_t>(p.ldb) * 2) + c;
+      }
+    auto load_a = [&](int t, int h) {
+      char* to = lds + (t & 1) * 65536 + h * 16384 + wave * 2048;
+      const char* g = step_of(a0, a1, a2, t, steps);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(g + from_a[h][j]), DASO_LDS(to + j * 1024), 16, 0, 0);
+    };
+    auto load_b = [&](int t, int h) {
+      char* to = lds + (t & 1) * 65536 + 32768 + h * 16384 + wave * 2048;
+      const char* g = step_of(b0, b1, b2, t, steps);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(g + from_b[h][j]), DASO_LDS(to + j * 1024), 16, 0, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[i][j] = (f4)0.0f;
+    const int wm = wave >> 2, wn = wave & 3, r16 = lane & 15, kq = lane >> 4;
+    half8 a[8], bl[4], br[4], bnext[4];
+    int at_a[2], at_b[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      const int c = ((kk * 4 + kq) ^ ((r16 >> 1) & 7)) * 16;
+      at_a[kk] = (wm * 64 + r16) * 128 + c;
+      at_b[kk] = 32768 + (wn * 32 + r16) * 128 + c;
+    }
+    auto read_a = [&](int t, int h) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          a[kk * 4 + i] = *(const half8*)(lds + (t & 1) * 65536 + at_a[kk] + h * 16384 + i * 2048);
+    };
+    auto read_b = [&](int t, int h, half8* b) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          b[kk * 2 + j] = *(const half8*)(lds + (t & 1) * 65536 + at_b[kk] + h * 16384 + j * 2048);
+    };
+    // the operands are handed over as (b, a), so that a lane holds four neighbouring
+    // columns of one row of C
+    auto compute = [&](f4* c, const half8* b) {
+      wait_lds();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) c[i * 2 + j] = mfma<BF16>(b[kk * 2 + j], a[kk * 4 + i], c[i * 2 + j]);
+      __builtin_amdgcn_s_setprio(0);
+      meet();
+    };
+    load_b(0, 0), load_a(0, 0), load_b(0, 1), load_a(0, 1), load_b(1, 0), load_a(1, 0), load_b(1, 1);
+    wait_loads<10>();
+    meet();
+    if (wm == 1) meet();
+    read_b(0, 0, bnext);
+    // kLeft: steps after this one, 2 for two or more.  Each wait leaves in flight what was
+    // issued after the piece that the next phase reads.
+    auto step = [&](int k, auto left) {
+      constexpr int kLeft = decltype(left)::value;
+      read_a(k, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bl[i] = bnext[i];
+      if constexpr (kLeft > 0) load_a(k + 1, 1), wait_loads<10>();
+      else wait_loads<2>();
+      meet();
+      compute(acc[0], bl);
+      read_b(k, 1, br);
+      if constexpr (kLeft > 1) load_b(k + 2, 0), wait_loads<10>();
+      else wait_loads<kLeft == 1 ? 8 : 0>();
+      meet();
+      compute(acc[1], br);
+      read_a(k, 1);
+      if constexpr (kLeft > 1) load_a(k + 2, 0), wait_loads<10>();
+      else if constexpr (kLeft == 1) wait_loads<6>();
+      meet();
+      compute(acc[3], br);
+      if constexpr (kLeft > 0) read_b(k + 1, 0, bnext);
+      if constexpr (kLeft > 1) load_b(k + 2, 1), wait_loads<10>();
+      else if constexpr (kLeft == 1) wait_loads<4>();
+      meet();
+      compute(acc[2], bl);
+    };
+    int k = 0;
+    for (; k + 2 < total; ++k) step(k, Left<2>());
+    step(k, Left<1>());
+    step(k + 1, Left<0>());
+    if (wm == 0) meet();
+  }
+
+ private:
+  template <int N>
+  struct Left {
+    static constexpr int value = N;
+  };
+};
+
+// 128 x 128 a workgroup of 4 wavefronts, two workgroups a CU, for results too small to
+// give every CU a larger tile.  Two steps in LDS; a step's last quarter runs while the
+// next step's first operands are read.
+struct Tile128 {
+  static constexpr int kRows = 128, kCols = 128, kThreads = 256, kLds = 4 * kWaveStage > 65536 ? 4 * kWaveStage : 65536;
+  static constexpr int kBlocks = 2;
+  static constexpr int kOccupancy = 2;
+
+  __device__ static void block_at(int wave, int b, int* row, int* col) {
+    *row = (wave >> 1) * 64;
+    *col = (wave & 1) * 64 + b * 32;
+  }
+
+  template <bool BF16>
+  __device__ static void run(const Args& p, const Place& at, char* lds, f4 (&acc)[kBlocks][8]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t skip_a = (at.batch * p.batch_a + int64_t(at.tm) * kRows * p.lda) * 2;
+    const int64_t skip_b = (at.batch * p.batch_b + int64_t(at.tn) * kCols * p.ldb) * 2;
+    const char *a0 = (const char*)p.a[0] + skip_a, *a1 = (const char*)p.a[1] + skip_a, *a2 = (const char*)p.a[2] + skip_a;
+    const char *b0 = (const char*)p.b[0] + skip_b, *b1 = (const char*)p.b[1] + skip_b, *b2 = (const char*)p.b[2] + skip_b;
+    const int last_a = min(kRows, p.M - at.tm * kRows) - 1, last_b = min(kCols, p.N - at.tn * kCols) - 1;
+    const int steps = p.steps, total = p.steps * p.segments;
+    uint32_t from_a[4], from_b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = (wave * 4 + j) * 8 + (lane >> 3), c = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+      from_a[j] = static_cast<uint32_t>(min(r, last_a)) * (static_cast<uint32_t>(p.lda) * 2) + c;
+      from_b[j] = static_cast<uint32_t>(min(r, last_b)) * (static_cast<uint32_t>(p.ldb) * 2) + c;
+    }
+    auto load = [&](int t) {
+      char* to = lds + (t & 1) * 32768 + wave * 4096;
+      const char *ga = step_of(a0, a1, a2, t, steps), *gb = step_of(b0, b1, b2, t, steps);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(ga + from_a[j]), DASO_LDS(to + j * 1024), 16, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(gb + from_b[j]), DASO_LDS(to + 16384 + j * 1024), 16, 0, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[i][j] = (f4)0.0f;
+    const int wm = wave >> 1, wn = wave & 1, r16 = lane & 15, kq = lane >> 4;
+    half8 a[2][4], b[2][4];
+    auto read = [&](int t, int kk) {
+      const int c = ((kk * 4 + kq) ^ ((r16 >> 1) & 7)) * 16;
+      const char* s = lds + (t & 1) * 32768;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[kk][i] = *(const half8*)(s + (wm * 64 + r16) * 128 + c + i * 2048);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[kk][j] = *(const half8*)(s + 16384 + (wn * 64 + r16) * 128 + c + j * 2048);
+    };
+    auto compute = [&](int kk) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[j >> 1][i * 2 + (j & 1)] = mfma<BF16>(b[kk][j], a[kk][i], acc[j >> 1][i * 2 + (j & 1)]);
+    };
+    load(0), load(1);
+    wait_loads<8>();
+    meet();
+    read(0, 0);
+    for (int k = 0; k < total; ++k) {
+      read(k, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(0);
+      __builtin_amdgcn_sched_barrier(0);
+      wait_loads<0>();
+      wait_lds();
+      meet();
+      if (k + 2 < total) load(k + 2);
+      if (k + 1 < total) read(k + 1, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
+// ------------------------------------------------------------------------- epilogues
+// A block in `stage` (the wavefront's own 8 KB of LDS): rows of 32 floats, 16-byte pieces
+// permuted as above.  Calls f(row, col, v) with eight neighbouring columns of a row, four
+// lanes a row, rows 16 at a time.
+template <class F>
+__device__ inline void by_rows(const f4 (&c)[8], char* stage, int lane, F f) {
+  const int r16 = lane & 15, kq = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = i * 16 + r16;
+      *(f4*)(stage + row * 128 + (((j * 4 + kq) ^ ((row >> 1) & 7)) * 16)) = c[i * 2 + j];
+    }
+  wait_lds();
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int pass = 0; pass < 4; ++pass) {
+    const int row = pass * 16 + (lane >> 2), piece = (lane & 3) * 2, s = (row >> 1) & 7;
+    const f4 lo = *(const f4*)(stage + row * 128 + ((piece ^ s) * 16));
+    const f4 hi = *(const f4*)(stage + row * 128 + (((piece + 1) ^ s) * 16));
+    float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    f(row, piece * 4, v);
+  }
+}
+
+// Where a staged plane of 16-bit values (64 x 32) keeps (row, col): rows of 64 bytes, with 16
+// more after every eighth, so that eight lanes that read rows eight apart meet no bank twice.
+__device__ inline int plane_at(int row, int col) { return row * 64 + (row >> 3) * 16 + col * 2; }
+
+// A staged plane by columns: calls f(col, row, v) with eight neighbouring rows of a column,
+// eight lanes a column, columns 8 at a time.
+template <class F>
+__device__ inline void by_columns(const char* plane, int lane, F f) {
+#pragma unroll
+  for (int pass = 0; pass < 4; ++pass) {
+    const int col = pass * 8 + (lane >> 3), row = (lane & 7) * 8;
+    half8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = *(const _Float16*)(plane + plane_at(row + i, col));
+    f(col, row, v);
+  }
+}
+
+// v as hi + lo.  A value that binary16 has no finite form of keeps its infinity or NaN in
+// hi, with nothing in lo.
+__device__ inline void split(float v, _Float16* hi, _Float16* lo) {
+  const _Float16 h = static_cast<_Float16>(v);
+  const float rest = v - static_cast<float>(h);
+  *hi = h;
+  *lo = static_cast<_Float16>(__builtin_fabsf(rest) < __builtin_inff() ? rest : 0.0f);
+}
+
+// Hands the tile's blocks to E::block(params, place, c, row, col, stage, lane), each at (row, col)
+// of C, those that begin inside the result's extent.
+template <class Tile, class E>
+__device__ inline void by_blocks(const typename E::Params& out, const Args& p, const Place& at, f4 (&acc)[Tile::kBlocks][8],
+                                 char* lds) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  char* stage = lds + wave * kWaveStage;
+#pragma unroll
+  for (int b = 0; b < Tile::kBlocks; ++b) {
+    int row, col;
+    Tile::block_at(wave, b, &row, &col);
+    row += at.tm * Tile::kRows;
+    col += at.tn * Tile::kCols;
+    if (row < p.M && col < p.N) E::block(out, at, acc[b], row, col, stage, lane);
+  }
+}
+
+// The products of one launch, told apart by their tiles.  An epilogue E has a plain struct
+// E::Params and tile<Tile>(params, args, place, acc, lds), by the whole workgroup.
+template <class E>
+struct Launch {
+  int32_t count;
+  int64_t first[kMaxProblems + 1];  // the first tile of each product; the last entry: of none
+  Args args[kMaxProblems];
+  typename E::Params out[kMaxProblems];
+};
+
+template <class Tile, bool BF16, class E>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kOccupancy) void product_kernel(Launch<E> all) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  int64_t id = blockIdx.x + int64_t(blockIdx.y) * gridDim.x;
+  const int64_t total = all.first[all.count];
+  if (id >= total) return;
+  // workgroups go to the 8 XCDs in turn: each XCD is given a run of consecutive tiles
+  const int64_t q = total / 8, r = total % 8, x = id % 8, y = id / 8;
+  id = x * q + (x < r ? x : r) + y;
+  int k = 0;
+  while (k + 1 < all.count && id >= all.first[k + 1]) ++k;
+  const Args& p = all.args[k];
+  const Place at = place_of(p, id - all.first[k]);
+  f4 acc[Tile::kBlocks][8];
+  Tile::template run<BF16>(p, at, lds, acc);
+  E::template tile<Tile>(all.out[k], p, at, acc, lds);
+}
+
+template <class Tile, bool BF16, class E>
+hipError_t launch_tiles(Launch<E>& all, hipStream_t stream) {
+  all.first[0] = 0;
+  for (int32_t k = 0; k < all.count; ++k) {
+    Args& p = all.args[k];
+    p.tiles_m = (p.M + Tile::kRows - 1) / Tile::kRows;
+    p.tiles_n = (p.N + Tile::kCols - 1) / Tile::kCols;
+    all.first[k + 1] = all.first[k] + tile_count(p);
+  }
+  const int64_t total = all.first[all.count];
+  if (total == 0) return hipSuccess;
+  constexpr int64_t kRow = int64_t(1) << 20;  // a multiple of 8; work-items of a row stay in 32 bits
+  const dim3 grid(static_cast<uint32_t>(total < kRow ? total : kRow), static_cast<uint32_t>((total + kRow - 1) / kRow));
+  auto* kernel = product_kernel<Tile, BF16, E>;
+  // once a device, before the first launch there
+  static std::atomic<uint64_t> allowed{0};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (dev >= 64 || (allowed.load(std::memory_order_relaxed) & bit) == 0) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Tile::kLds);
+    if (e != hipSuccess) return e;
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+  }
+  void* list[] = {&all};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(Tile::kThreads), list, Tile::kLds, stream);
+}
+
+// Whether the launch is better off in tiles of 256 x 256.  A CU takes a 256 tile's step in
+// about the time in which two workgroups on it take 1.3 steps of a 128 tile each.
+template <class E>
+bool large_tiles(const Launch<E>& all) {
+  int64_t t256 = 0, t128 = 0;
+  for (int32_t k = 0; k < all.count; ++k) {
+    Args p = all.args[k];
+    p.tiles_m = (p.M + 255) / 256, p.tiles_n = (p.N + 255) / 256;
+    t256 += tile_count(p);
+    p.tiles_m = (p.M + 127) / 128, p.tiles_n = (p.N + 127) / 128;
+    t128 += tile_count(p);
+  }
+  const int64_t rounds256 = (t256 + 255) / 256, rounds128 = (t128 + 511) / 512;
+  return rounds256 * 13 <= rounds128 * 10;
+}
+
+template <bool BF16, class E>
+hipError_t launch_products(Launch<E>& all, hipStream_t stream) {
+  return large_tiles(all) ? launch_tiles<Tile256, BF16, E>(all, stream) : launch_tiles<Tile128, BF16, E>(all, stream);
+}
+
+#endif
+
+}  // namespace product
+}  // namespace daso

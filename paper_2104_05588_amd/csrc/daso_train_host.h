@@ -1,0 +1,65 @@
+// Host-only argument checks of daso_train.h (no HIP calls).  Each returns DASO_OK or the
+// status that the entry point returns; workspaces are checked by the entry points, which
+// know their size.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include <vector>
+
+#include "daso_train.h"
+
+namespace daso {
+namespace host {
+
+inline size_t bytes_of(int32_t type) { return type == DASO_TYPE_BF16 ? 2 : 4; }
+
+int check_layer_norm(const daso_layer_norm_args& s);
+int check_layer_norm_backward(const daso_layer_norm_backward_args& s);
+int check_loss(const daso_loss_args& s, bool backward);
+int check_orthogonalize(const daso_orthogonalize_args& s);
+int check_muon(const daso_muon_args& s);
+// The shapes and counts alone, for the *_workspace functions.
+int check_layer_norm_backward_sizes(const daso_layer_norm_backward_args& s);
+int check_loss_sizes(const daso_loss_args& s);
+int check_orthogonalize_sizes(const daso_orthogonalize_args& s);
+int check_muon_sizes(const daso_muon_args& s);
+int check_workspace(const void* p, size_t bytes, size_t need);
+
+// ------------------------------------------------------------------ Newton-Schulz plan
+// Matrices of one shape that take their steps together.  Inside, X is m x n with m <= n,
+// both padded with zeros to multiples of 64.
+struct SchulzGroup {
+  int64_t rows, cols;
+  int64_t m, n;           // padded
+  bool tall;              // X is the transpose
+  int32_t count;          // matrices
+  int32_t first;          // place of the first among the round's matrices
+  // byte offsets in the workspace; planes: [0] hi, [1] lo
+  size_t source;          // fp32 copies of what is orthogonalised, rows x cols (muon only)
+  size_t x[2][2], xt[2][2], gram[2], poly[2];  // x, xt: [buffer][plane]
+  size_t rest[2];         // what the one plane of gram and of poly leaves of their diagonals
+};
+
+// What is worked on at a time: groups of up to kRoundElems elements in all.
+struct SchulzRound {
+  std::vector<SchulzGroup> groups;
+  std::vector<int32_t> matrices;  // indexes into the caller's list, group by group
+  size_t bytes;                   // of workspace
+};
+
+constexpr int64_t kRoundElems = int64_t(1) << 26;  // 20 bytes of workspace each, and the squares
+constexpr int32_t kRoundMatrices = 128;            // as many as kernel arguments hold
+constexpr int32_t kRoundGroups = 8;
+constexpr int32_t kSumParts = 64;                  // partial sums of squares a matrix
+constexpr size_t kRoundHead = size_t(kRoundMatrices) * (16 + 8 * kSumParts);  // table and partial sums
+
+struct Shape {
+  int64_t rows, cols;
+};
+// Rounds over the given matrices, in order of first appearance of their shapes.
+std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with_source);
+
+}  // namespace host
+}  // namespace daso

@@ -1,0 +1,549 @@
+"""The training operators on the GPU against the 64-bit oracle.
+
+Tolerances follow from the arithmetic.  u = 2^-24 is the rounding of one 32-bit operation.  A
+sum of k terms in any order is off by at most (k - 1) u times the sum of their magnitudes;
+here sums are trees of short runs, and k u is a bound with room.  A result rounded to bf16 is off by
+2^-9 of itself more.  Values carried as one binary16 plane are off by 2^-11 of themselves at
+most, as two by 2^-22, and by 2^-25 of the plane's scale where they are tiny."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2104_05588_amd as daso  # noqa: E402
+from oracle import train_oracle as O  # noqa: E402
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(), reason="no GPU")]
+
+U = 2.0 ** -24
+QUINTIC = (3.4445, -4.7750, 2.0315)
+
+
+def announce(*what):
+    print("[case]", *what, flush=True)
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def np64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def close(got, want, tol, what):
+    got = np64(got)
+    assert got.shape == want.shape, what
+    off = np.abs(got - want)
+    bad = ~(off <= tol)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, worst {np.nanmax(off / tol):.3g} of the tolerance"
+
+
+def rounded(want, bf16):
+    return np.abs(want) * 2.0 ** -8 + 2.0 ** -133 if bf16 else np.abs(want) * U
+
+
+def wide(t, pad, shift=0):
+    """t's values on the GPU, in rows that lie `pad` elements further apart, `shift` elements into storage."""
+    rows, d = t.shape
+    store = torch.full((rows * (d + pad) + shift + 1,), 7.0, dtype=t.dtype, device="cuda")
+    v = store[shift:shift + rows * (d + pad)].view(rows, d + pad)[:, :d]
+    v.copy_(t)
+    return v
+
+
+# ------------------------------------------------------------------------- layer norm
+NORM_SIZES = [(1, 1), (1, 64), (3, 33), (5, 512), (7, 513), (64, 1024), (9, 1601), (130, 2048), (33, 2049), (6, 4096),
+              (5, 4100), (3, 8192), (3, 8193), (2, 20000), (2500, 40), (4099, 96)]
+
+
+@pytest.mark.parametrize("rows,d", NORM_SIZES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("pad,shift,affine", [(0, 0, True), (5, 1, True), (8, 0, False)])
+def test_layer_norm(rows, d, dtype, pad, shift, affine):
+    announce("layer_norm", rows, d, dtype, pad, shift, affine)
+    g, bf16 = gen(rows * 7919 + d), dtype == torch.bfloat16
+    host = (torch.randn(rows, d, generator=g) * 2 + torch.randn(1, d, generator=g)).to(dtype)
+    x = wide(host, pad, shift)
+    w = torch.randn(d, generator=g).cuda() if affine else None
+    b = torch.randn(d, generator=g).cuda() if affine else None
+    y, mean, rstd = daso.layer_norm(x, w, b, eps=1e-5)
+    xh = np64(host)
+    want, want_mean, want_rstd = O.layer_norm(xh, None if w is None else np64(w), None if b is None else np64(b), 1e-5)
+    # the mean is off by k u of the mean magnitude, k = 50 for runs of 32 and the tree; the variance by as much of itself and
+    # the mean's error squared, rstd by half of that
+    k = 50 + d / 256
+    tol_mean = k * U * np.abs(xh).mean(axis=1) + 1e-30
+    close(mean, want_mean, tol_mean, "mean")
+    rel = k * U + (tol_mean * want_rstd) ** 2
+    close(rstd, want_rstd, 2 * rel * want_rstd, "rstd")
+    wa = 1.0 if w is None else np.abs(np64(w))
+    xhat = np.abs(xh - want_mean[:, None]) * want_rstd[:, None]
+    tol = (2 * rel[:, None] + 6 * U) * xhat * wa + 2 * (tol_mean * want_rstd)[:, None] * wa + 4 * U * np.abs(want)
+    close(y, want, tol + rounded(want, bf16), "y")
+
+    dyh = (torch.randn(rows, d, generator=g) * 0.1).to(dtype)
+    dy = wide(dyh, pad, shift)
+    dx, dw, db = daso.layer_norm_backward(dy, x, w, mean, rstd)
+    want_dx, want_dw, want_db = O.layer_norm_backward(np64(dyh), xh, None if w is None else np64(w), np64(mean), np64(rstd))
+    gm = np.abs(np64(dyh)) * wa
+    # (x - mean) is rounded where x is large: an error of u |x| rstd in xhat
+    xe = 4 * U * (np.abs(xh) + np.abs(np64(mean))[:, None]) * np64(rstd)[:, None]
+    s1, s2 = gm.mean(axis=1, keepdims=True), (gm * (xhat + xe)).mean(axis=1, keepdims=True)
+    tol = np64(rstd)[:, None] * (k * U * (gm + s1 + (xhat + 1) * s2) + xe * s2 + xhat * (gm * xe).mean(axis=1, keepdims=True))
+    close(dx, want_dx, tol + rounded(want_dx, bf16), "dx")
+    kr = 40 + rows / 64
+    close(dw, want_dw, (np.abs(np64(dyh)) * (kr * U * xhat + xe)).sum(axis=0) + 1e-30, "dweight")
+    close(db, want_db, kr * U * np.abs(np64(dyh)).sum(axis=0) + 1e-30, "dbias")
+
+
+def test_layer_norm_in_place_parts_and_empty():
+    announce("layer_norm in place")
+    x = torch.randn(37, 256, generator=gen(1)).cuda()
+    y, mean, rstd = daso.layer_norm(x)
+    again, _, _ = daso.layer_norm(x.clone(), out=(z := x.clone()))
+    assert again is z and torch.equal(again, y)
+    dy = torch.randn(37, 256, generator=gen(2)).cuda()
+    dx, dw, db = daso.layer_norm_backward(dy, x, None, mean, rstd)
+    dx2, dw2, none = daso.layer_norm_backward(dy, x, None, mean, rstd, bias=False)
+    assert none is None and torch.equal(dx, dx2) and torch.equal(dw, dw2)
+    flat = torch.full((600,), 3.0, device="cuda")
+    same = dy.clone()
+    dx3, _, _ = daso.layer_norm_backward(same, x, None, mean, rstd, dx=same, dweight=flat[3:259], dbias=flat[300:556])
+    assert torch.equal(dx3, dx) and torch.equal(flat[3:259], dw) and torch.equal(flat[300:556], db)
+    assert (flat[:3] == 3).all() and (flat[259:300] == 3).all() and (flat[556:] == 3).all()
+    empty = torch.empty(0, 256, device="cuda")
+    y0, m0, r0 = daso.layer_norm(empty)
+    assert y0.shape == (0, 256) and m0.numel() == 0
+    _, dw0, db0 = daso.layer_norm_backward(empty, empty, None, m0, r0)
+    assert not dw0.any() and not db0.any()
+
+
+def test_layer_norm_special_values():
+    announce("layer_norm special values")
+    x = torch.zeros(5, 128)
+    x[0] = 3.0                      # constant: y is the bias
+    x[1, 5] = float("inf")
+    x[2, 7] = float("nan")
+    x[3] = torch.linspace(-1e-20, 1e-20, 128)
+    x[4] = torch.linspace(0.9, 1.1, 128) * 1e18
+    b = torch.randn(128, generator=gen(3))
+    y, _, rstd = daso.layer_norm(x.cuda(), None, b.cuda(), eps=1e-5)
+    y = y.cpu()
+    assert torch.equal(y[0], b) and torch.isnan(y[1]).all() and torch.isnan(y[2]).all()
+    assert torch.allclose(y[3], b, atol=1e-6)
+    assert torch.isfinite(y[4]).all() and abs((y[4] - b).double().std(unbiased=False) - 1) < 1e-5
+    assert not torch.equal(rstd[3:4].cpu(), torch.zeros(1))
+
+
+# ------------------------------------------------------------------------- the loss
+def loss_case(n, v, d, dtype, ignored, seed, scale=0.3):
+    g = gen(seed)
+    h = torch.randn(n, d, generator=g).to(dtype)
+    w = (torch.randn(v, d, generator=g) * scale / d ** 0.5 * 4).to(dtype)
+    t = torch.randint(0, v, (n,), generator=g)
+    if ignored >= 1:
+        t[:] = -100
+    elif ignored > 0:
+        t[torch.rand(n, generator=g) < ignored] = -100
+    s = torch.rand(n, generator=g) + 0.1
+    s[torch.rand(n, generator=g) < 0.1] = 0.0
+    return h, w, t, s
+
+
+def check_loss(h, w, t, s, hd, wd, grad_dtype=None, dhidden=None, dweight=None):
+    n, d = h.shape
+    bf16 = h.dtype == torch.bfloat16
+    h64, w64 = np64(h), np64(w)
+    want_loss, want_lse = O.linear_cross_entropy(h64, w64, t.numpy())
+    mag = np.abs(h64) @ np.abs(w64).T
+    # logits: a sum of d exact products, of planes that lack 2^-21 of a product for fp32
+    ze = (d * U + (0 if bf16 else 2.0 ** -20)) * mag.max(axis=1)
+    tol = 2 * ze + 2.0 ** -20 + 8 * U * (np.abs(want_lse) + mag.max(axis=1))
+    td, sd = t.cuda(), s.cuda()
+    loss, lse = daso.linear_cross_entropy(hd, wd, td)
+    close(lse, want_lse, tol, "lse")
+    close(loss, want_loss, tol, "loss")
+    assert not loss.cpu()[t == -100].any()
+    if dweight is None:
+        dweight = torch.full(w.shape, float("nan"), dtype=grad_dtype or h.dtype, device="cuda")
+    dh, dw = daso.linear_cross_entropy_backward(sd, hd, wd, td, lse, dhidden=dhidden, dweight=dweight)
+    assert dw is dweight
+    want_dh, want_dw, dz = O.linear_cross_entropy_backward(s.numpy(), h64, w64, t.numpy())
+    # dz: p is off by its logit's and the log-sum-exp's error, and both are rounded
+    sa = np.where(t.numpy() == -100, 0, np.abs(s.numpy()))[:, None]
+    p = np.abs(dz) + (np.arange(w.shape[0])[None] == t.numpy()[:, None]) * sa  # s p or more
+    pe = p * (ze + tol + 2.0 ** -18)[:, None]
+    top = 2.0 ** -38 * max(float(s.max()), 1e-30)
+    for got, want, left, right, wide_type, mags in (
+            (dh, want_dh, np.abs(dz), np.abs(w64), bf16, pe), (dw, want_dw, np.abs(dz).T, np.abs(h64), dw.dtype == torch.bfloat16, pe.T)):
+        planes = 2.0 ** -11 if wide_type else 2.0 ** -20
+        terms = left.shape[1]
+        off = ((planes + terms * U) * left + mags + top * (left > 0)) @ right + 2.0 ** -36 * left.sum(axis=1, keepdims=True) * right.max()
+        close(got, want, off + rounded(want, wide_type) + 1e-30, "dhidden" if got is dh else "dweight")
+    return loss, lse, dh, dw
+
+
+LOSS_SIZES = [(1, 1, 1), (1, 2, 64), (2, 100, 33), (17, 127, 128), (64, 128, 64), (65, 129, 65), (128, 1000, 192), (200, 257, 512),
+              (300, 2049, 130), (513, 777, 320), (1, 5000, 256), (1025, 65, 96)]
+
+
+@pytest.mark.parametrize("n,v,d", LOSS_SIZES)
+@pytest.mark.parametrize("dtype,grad", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32),
+                                        (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("ignored", [0.0, 0.4, 1.0])
+def test_loss(n, v, d, dtype, grad, ignored):
+    announce("loss", n, v, d, dtype, grad, ignored)
+    h, w, t, s = loss_case(n, v, d, dtype, ignored, n + 31 * v + 7 * d)
+    loss, lse, dh, dw = check_loss(h, w, t, s, h.cuda(), w.cuda(), grad)
+    if ignored >= 1:
+        assert not loss.any() and not dh.any() and not dw.any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (3, 0), (0, 1)])
+def test_loss_strides_and_alignment(dtype, pad, shift):
+    announce("loss strides", dtype, pad, shift)
+    h, w, t, s = loss_case(150, 333, 192, dtype, 0.2, 5)
+    flat = torch.full((333 * (192 + pad) + 9,), 5.0, device="cuda")
+    dw = flat[shift:shift + 333 * (192 + pad)].view(333, 192 + pad)[:, :192]
+    dh = torch.full((150, 192 + pad), 5.0, dtype=dtype, device="cuda")[:, :192]
+    check_loss(h, w, t, s, wide(h, pad, shift), wide(w, pad, shift), dhidden=dh, dweight=dw)
+    kept = torch.ones(flat.numel(), dtype=torch.bool, device="cuda")
+    kept[shift:shift + 333 * (192 + pad)].view(333, 192 + pad)[:, :192] = False
+    assert (flat[kept] == 5).all()
+
+
+def test_loss_over_several_pieces_of_the_vocabulary():
+    """More tokens times classes than one piece holds: dhidden is summed over pieces."""
+    n, v, d = 9000, 16500, 64
+    announce("loss in pieces", n, v, d)
+    h, w, t, s = loss_case(n, v, d, torch.bfloat16, 0.1, 11)
+    hd, wd, td, sd = h.cuda(), w.cuda(), t.cuda(), s.cuda()
+    loss, lse = daso.linear_cross_entropy(hd, wd, td)
+    dh, dw = daso.linear_cross_entropy_backward(sd, hd, wd, td, lse, dweight=torch.empty(v, d, device="cuda"))
+    # the same definition in 64 bits on the GPU
+    z = hd.double() @ wd.double().t()
+    want_lse = torch.logsumexp(z, 1)
+    live = td != -100
+    want_loss = torch.where(live, want_lse - z.gather(1, td.clamp(min=0)[:, None])[:, 0], 0.0)
+    dz = torch.softmax(z, 1)
+    dz.scatter_add_(1, td.clamp(min=0)[:, None], torch.full_like(td, -1)[:, None].double())
+    dz *= torch.where(live, sd.double(), 0.0)[:, None]
+    mag = hd.double().abs() @ wd.double().abs().t()
+    top = float(mag.max())
+    tol = 2 * d * U * top + 2.0 ** -20 + 16 * U * top
+    assert (lse.double() - want_lse).abs().max() <= tol and (loss.double() - want_loss).abs().max() <= tol
+    want_dh, want_dw = dz @ wd.double(), dz.t() @ hd.double()
+    az = dz.abs() + 1e-12
+    bound = (az * (2.0 ** -11 + v * U + 4 * tol)) @ wd.double().abs() + want_dh.abs() * 2.0 ** -8
+    assert ((dh.double() - want_dh).abs() <= bound).all()
+    bound = (az * (2.0 ** -20 + n * U + 4 * tol)).t() @ hd.double().abs()
+    assert ((dw.double() - want_dw).abs() <= bound).all()
+
+
+def test_loss_special_targets_and_values():
+    announce("loss special values")
+    h, w, t, s = loss_case(70, 200, 128, torch.bfloat16, 0.0, 3)
+    t[3], t[4], t[5] = 200, -7, 199
+    loss, lse = daso.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    nan = torch.isnan(loss.cpu())
+    assert nan[3] and nan[4] and nan.sum() == 2 and torch.isfinite(lse).all()
+    # one sure token: p - 1 is not the difference of rounded numbers
+    h, w, t, s = loss_case(64, 150, 64, torch.float32, 0.0, 4)
+    h[0] = w[t[0]] * 40
+    check_loss(h, w, t, s, h.cuda(), w.cuda())
+    # any class may be the one that is ignored
+    t = torch.zeros(64, dtype=torch.int64)
+    loss, _ = daso.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda(), ignore_index=0)
+    assert not loss.any()
+    # NaN and infinities stay in their rows
+    h, w, t, s = loss_case(70, 200, 128, torch.bfloat16, 0.0, 6)
+    h[7, 3], h[9, 2] = float("nan"), float("inf")
+    hd, wd, td = h.cuda(), w.cuda(), t.cuda()
+    loss, lse = daso.linear_cross_entropy(hd, wd, td)
+    bad = ~torch.isfinite(loss.cpu())
+    assert bad[7] and bad[9] and bad.sum() == 2
+    td[7] = td[9] = -100
+    loss, lse = daso.linear_cross_entropy(hd, wd, td)
+    assert torch.isfinite(loss).all()
+    dh, _ = daso.linear_cross_entropy_backward(s.cuda(), hd, wd, td, lse)
+    assert not dh[7].any() and not dh[9].any() and torch.isfinite(dh).all()
+    # magnitudes from one end of the types to the other
+    for size in (1e-30, 1e15):
+        h, w, t, s = loss_case(40, 60, 64, torch.float32, 0.0, 8)
+        check_loss(h * size, w / size, t, s * 1e-6, (h * size).cuda(), (w / size).cuda())
+
+
+def test_loss_without_tokens():
+    announce("loss without tokens")
+    h, w = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(100, 64, dtype=torch.bfloat16, device="cuda")
+    t, s = torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda")
+    loss, lse = daso.linear_cross_entropy(h, w, t)
+    assert loss.numel() == 0
+    dh, dw = daso.linear_cross_entropy_backward(s, h, w, t, lse, dweight=torch.full((100, 64), 9.0, device="cuda"))
+    assert dh.shape == (0, 64) and not dw.any()
+
+
+# ------------------------------------------------------------------------- Newton-Schulz
+def schulz_tolerance(want, bf16, steps):
+    """Relative, in the 2-norm.  A step rounds three operands and its result; what that does to the
+    strong directions it does not raise (the derivative of the step there is below 4).  Weak
+    directions are raised by at most 3.5 a step, from X0 of norm 1 carried to 2^-22."""
+    plane = 2.0 ** -11 if bf16 else 2.0 ** -21
+    weak = 2.0 ** -22 * 3.5 ** steps / max(np.linalg.norm(want), 1e-30)
+    return 4 * steps * plane + weak + (2.0 ** -8 if bf16 else U)
+
+
+SCHULZ_SIZES = [(1, 1, 1), (1, 1, 50), (2, 33, 1), (3, 24, 24), (1, 64, 576), (2, 65, 64), (1, 100, 300), (2, 300, 100), (1, 129, 257),
+                (2, 256, 256), (1, 500, 640), (1, 640, 500), (3, 128, 1024)]
+
+
+@pytest.mark.parametrize("batch,rows,cols", SCHULZ_SIZES)
+@pytest.mark.parametrize("dtype,out", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32), (torch.float32, torch.bfloat16),
+                                       (torch.bfloat16, torch.float32)])
+def test_orthogonalize(batch, rows, cols, dtype, out):
+    announce("orthogonalize", batch, rows, cols, dtype, out)
+    u = (torch.randn(batch, rows, cols, generator=gen(rows * 100 + cols)) * 1e-3).to(dtype)
+    got = daso.orthogonalize(u.cuda(), out=torch.full(u.shape, float("nan"), dtype=out, device="cuda"))
+    for i in range(batch):
+        want = O.newton_schulz(np64(u[i]), [QUINTIC] * 5)
+        off = np.linalg.norm(np64(got[i]) - want) / np.linalg.norm(want)
+        assert off <= schulz_tolerance(want, out == torch.bfloat16, 5), (i, off)
+
+
+def test_orthogonalize_weak_directions():
+    """Singular values over six decades, some of them zero: the weak ones are raised from values."""
+    announce("orthogonalize weak directions")
+    q1, _ = torch.linalg.qr(torch.randn(192, 192, generator=gen(1), dtype=torch.float64))
+    q2, _ = torch.linalg.qr(torch.randn(320, 320, generator=gen(2), dtype=torch.float64))
+    sigma = torch.logspace(0, -6, 192, dtype=torch.float64)
+    sigma[150:] = 0
+    u = (q1 * sigma) @ q2[:192]
+    for out in (torch.float32, torch.bfloat16):
+        for v in (u, u.t()):
+            host = v.float().contiguous()
+            want = O.newton_schulz(np64(host), [QUINTIC] * 5)
+            got = daso.orthogonalize(host.cuda(), out=torch.empty(host.shape, dtype=out, device="cuda"))
+            off = np.linalg.norm(np64(got) - want) / np.linalg.norm(want)
+            assert off <= schulz_tolerance(want, out == torch.bfloat16, 5), (out, off)
+
+
+def test_orthogonalize_steps_strides_and_special_values():
+    announce("orthogonalize steps")
+    u = torch.randn(2, 48, 80, generator=gen(9))
+    for steps, c in ((1, [QUINTIC]), (3, [(2.0, -1.5, 0.5), QUINTIC, (1.5, -0.5, 0.0)]), (16, [(1.5, -0.5, 0.0)] * 16)):
+        got = daso.orthogonalize(u.cuda(), steps=steps, coefficients=c)
+        for i in range(2):
+            want = O.newton_schulz(np64(u[i]), c)
+            assert np.linalg.norm(np64(got[i]) - want) <= schulz_tolerance(want, False, min(steps, 6)) * np.linalg.norm(want) * max(1, steps / 5)
+    store = torch.full((2, 50, 91), 4.0, device="cuda")
+    view = store[:, 1:49, 3:83]
+    view.copy_(u)
+    got = daso.orthogonalize(view)
+    assert torch.equal(got, daso.orthogonalize(u.cuda()))
+    assert daso.orthogonalize(view, out=view) is view
+    assert torch.equal(view, got)
+    assert (store[:, 0] == 4).all() and (store[:, 49] == 4).all() and (store[:, :, :3] == 4).all() and (store[:, :, 83:] == 4).all()
+    zero = torch.zeros(3, 40, 30)
+    zero[1] = torch.randn(40, 30, generator=gen(4))
+    zero[2, 3, 4] = float("nan")
+    got = daso.orthogonalize(zero.cuda()).cpu()
+    assert not got[0].any() and torch.isfinite(got[1]).all() and torch.isnan(got[2]).any()
+    for size in (1e-18, 1e18):
+        same = daso.orthogonalize((u * size).cuda(), eps=0.0)
+        want = O.newton_schulz(np64(u[0]), [QUINTIC] * 5, 0.0)
+        assert np.linalg.norm(np64(same[0]) - want) <= schulz_tolerance(want, False, 5) * np.linalg.norm(want)
+    assert daso.orthogonalize(torch.empty(0, 4, 5, device="cuda")).shape == (0, 4, 5)
+
+
+# ------------------------------------------------------------------------- the step
+def muon_case(mats, n, g, seed):
+    r = gen(seed)
+    grads = [torch.randn(n, generator=r) * 1e-3 for _ in range(g)]
+    return grads, torch.randn(n, generator=r) * 0.02, torch.randn(n, generator=r) * 5e-3
+
+
+@pytest.mark.parametrize("g", [1, 3, 4, 8])
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("mats,n", [
+    ([(0, 16, 16)], 256),
+    ([(5, 24, 40), (1000, 40, 24), (2000, 24, 40), (3001, 1, 7)], 3100),
+    ([(0, 128, 64), (8192, 64, 128), (16384, 96, 96), (25600, 33, 65)], 30000),
+    ([(k * 1500, 30 + k % 11, 36 - k % 7) for k in range(40)], 61500),   # more shapes than one round takes
+    ([(k * 80, 8, 10) for k in range(150)], 12000),                       # more matrices than one round takes
+])
+def test_muon_step(mats, n, g, nesterov):
+    announce("muon_step", len(mats), n, g, nesterov)
+    grads, x, m = muon_case(mats, n, g, n + g)
+    lr, mu, wd = 0.02, 0.95, 0.1
+    xd, md, wire = x.cuda(), m.cuda(), torch.full((n,), 7.0, dtype=torch.bfloat16, device="cuda")
+    daso.muon_step([t.cuda() for t in grads], xd, md, mats, lr, mu, wd, nesterov, wire=wire)
+    scaled = [(s, r, c, max(1.0, r / c) ** 0.5) for s, r, c in mats]
+    f = np.float32
+    want_x, want_m = O.muon_step([np64(t) for t in grads], np64(x), np64(m), scaled, float(f(lr)), float(f(mu)), float(f(wd)), nesterov,
+                                 [QUINTIC] * 5)
+    inside = np.zeros(n, bool)
+    for s, r, c in mats:
+        inside[s:s + r * c] = True
+    mag = np.abs(np64(m)) + sum(np.abs(np64(t)) for t in grads)
+    close(md, want_m, (g + 4) * U * mag, "momentum")
+    got_x = np64(xd)
+    assert np.array_equal(got_x[~inside], np64(x)[~inside]) and np.array_equal(np64(md)[~inside], np64(m)[~inside])
+    assert (wire.cpu()[torch.from_numpy(~inside)] == 7).all()
+    for s, r, c, scale in scaled:
+        cut = slice(s, s + r * c)
+        step = (want_x - np64(x) * (1 - lr * wd))[cut]
+        tol = schulz_tolerance(step / (lr * scale), False, 5) * np.linalg.norm(step) + 4 * U * np.linalg.norm(np64(x)[cut])
+        assert np.linalg.norm(got_x[cut] - want_x[cut]) <= tol
+        assert torch.equal(wire[cut].cpu(), xd[cut].cpu().to(torch.bfloat16))
+
+
+def test_muon_momentum_matches_the_fused_step():
+    """The average and the momentum are the fused step's, bit for bit."""
+    announce("muon momentum")
+    n = 64 * 96
+    for g in (1, 3, 4, 7):
+        grads, x, m = muon_case([(0, 64, 96)], n, g, g)
+        gd, md, m2 = [t.cuda() for t in grads], m.cuda(), m.cuda()
+        daso.muon_step(gd, x.cuda(), md, [(0, 64, 96)], 0.1, 0.9)
+        daso.fused_sync_step(gd, x.cuda(), m2, [], [(0, n, 1)], 0.1, 0.9)
+        assert torch.equal(md, m2)
+
+
+def test_muon_scales_and_prepared_step():
+    announce("muon prepared")
+    mats, n = [(0, 64, 32), (2048, 32, 64)], 4096
+    grads, x, m = muon_case(mats, n, 2, 1)
+    gd = [t.cuda() for t in grads]
+    steps = {}
+    for adjust in (None, "spectral", "rms"):
+        xd = x.cuda()
+        daso.muon_step(gd, xd, m.cuda(), mats, 0.1, 0.9, adjust=adjust)
+        steps[adjust] = (xd - x.cuda()).cpu().double()
+    for (s, r, c) in mats:
+        cut = slice(s, s + r * c)
+        for adjust in ("spectral", "rms"):
+            want = steps[None][cut] * daso.muon_scale(r, c, adjust)
+            assert torch.allclose(steps[adjust][cut], want, rtol=1e-4, atol=1e-7)
+    xd, md = x.cuda(), m.cuda()
+    step = daso.MuonStep(gd, xd, md, mats, 0.1, 0.9)
+    step(), step()
+    x2, m2 = x.cuda(), m.cuda()
+    for _ in range(2):
+        daso.muon_step(gd, x2, m2, mats, 0.1, 0.9)
+    assert torch.equal(xd, x2) and torch.equal(md, m2)
+
+
+# ------------------------------------------------------------------------- streams, graphs, repeats
+def all_operators(seed=0):
+    """A closure over fixed inputs that runs every operator into the same outputs."""
+    g = gen(seed)
+    x = torch.randn(300, 384, generator=g).to(torch.bfloat16).cuda()
+    dy = torch.randn(300, 384, generator=g).to(torch.bfloat16).cuda()
+    h, w, t, s = loss_case(300, 700, 384, torch.bfloat16, 0.1, seed + 1)
+    h, w, t, s = h.cuda(), w.cuda(), t.cuda(), s.cuda()
+    u = torch.randn(2, 200, 300, generator=g).cuda()
+    mats = [(0, 96, 64), (6144, 64, 96)]
+    grads, p0, m0 = muon_case(mats, 12288, 4, seed)
+    gd, p0, m0 = [v.cuda() for v in grads], p0.cuda(), m0.cuda()
+
+    def go(stream=None):
+        y, mean, rstd = daso.layer_norm(x, stream=stream)
+        dx, dg, db = daso.layer_norm_backward(dy, x, None, mean, rstd, stream=stream)
+        loss, lse = daso.linear_cross_entropy(h, w, t, stream=stream)
+        dh, dw = daso.linear_cross_entropy_backward(s, h, w, t, lse, stream=stream,
+                                                    dweight=None)
+        o32 = daso.orthogonalize(u, stream=stream)
+        with torch.cuda.stream(stream) if stream is not None else torch.cuda.stream(torch.cuda.current_stream()):
+            p, m = p0.clone(), m0.clone()
+        daso.muon_step(gd, p, m, mats, 0.1, 0.9, stream=stream)
+        return [y, mean, rstd, dx, dg, db, loss, lse, dh, dw, o32, p, m]
+    return go
+
+
+def test_repeats_and_streams_give_the_same_bits():
+    announce("repeats and streams")
+    go = all_operators()
+    first = go()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, go()))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = go(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, other))
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    both = [go(a), go(b)]
+    torch.cuda.synchronize()
+    for out in both:
+        assert all(torch.equal(p, q) for p, q in zip(first, out))
+
+
+def test_graph_capture_and_replays():
+    announce("graph capture")
+    go = all_operators(5)
+    want = [t.clone() for t in go()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = go()
+    for k in range(4):
+        for t in held:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, held)), k
+        eager = go()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, eager)), k
+
+
+# ------------------------------------------------------------------------- refusals
+def test_refusals():
+    announce("refusals")
+    f = torch.zeros(4, 8, device="cuda")
+    b = f.to(torch.bfloat16)
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    w = torch.zeros(5, 8, device="cuda")
+    v = torch.zeros(4, device="cuda")
+    for match, call in [
+        ("device tensor", lambda: daso.layer_norm(f.cpu())),
+        ("dtype", lambda: daso.layer_norm(f.double())),
+        ("matrix", lambda: daso.layer_norm(f[0])),
+        ("contiguous", lambda: daso.layer_norm(f.t())),
+        ("8 elements", lambda: daso.layer_norm(f, v)),
+        ("shape", lambda: daso.layer_norm(f, out=f[:3])),
+        ("dtype", lambda: daso.layer_norm_backward(b, f, None, v, v)),
+        ("4 elements", lambda: daso.layer_norm_backward(f, f, None, v[:3], v)),
+        ("dtype", lambda: daso.linear_cross_entropy(f, w.to(torch.bfloat16), t)),
+        ("features", lambda: daso.linear_cross_entropy(f, w[:, :7], t)),
+        ("dtype", lambda: daso.linear_cross_entropy(f, w, t.int())),
+        ("shape", lambda: daso.linear_cross_entropy_backward(v, f, w, t, v, dweight=w[:4])),
+        ("dimensions", lambda: daso.orthogonalize(v)),
+        ("contiguous", lambda: daso.orthogonalize(f.t())),
+        ("shape", lambda: daso.orthogonalize(f, out=w)),
+        ("steps", lambda: daso.orthogonalize(f, steps=0)),
+        ("coefficients", lambda: daso.orthogonalize(f, steps=2, coefficients=[(1, 2, 3)])),
+        ("adjust", lambda: daso.muon_step([f.view(-1)], w.view(-1)[:32].clone(), v.repeat(8), [(0, 4, 8)], 0.1, adjust="no")),
+    ]:
+        with pytest.raises(ValueError, match=match):
+            call()
+    flat, mom = torch.zeros(64, device="cuda"), torch.zeros(64, device="cuda")
+    grad = torch.ones(64, device="cuda")
+    for status, call in [
+        ("EINVAL", lambda: daso.layer_norm(f, eps=-1.0)),
+        ("EALIAS", lambda: daso.layer_norm(flat.view(8, 8)[:4], out=flat.view(8, 8)[1:5])),
+        ("EINVAL", lambda: daso.muon_step([grad], flat, mom, [(0, 8, 9)], 0.1)),
+        ("EINVAL", lambda: daso.muon_step([grad], flat, mom, [(0, 4, 4), (8, 4, 4)], 0.1)),
+        ("EINVAL", lambda: daso.muon_step([grad], flat, mom, [(0, 0, 4)], 0.1)),
+        ("EINVAL", lambda: daso.muon_step([grad], flat, mom, [(0, 4, 4)], float("nan"))),
+        ("EALIAS", lambda: daso.muon_step([grad], flat, flat, [(0, 4, 4)], 0.1)),
+        ("EALIAS", lambda: daso.orthogonalize(flat.view(8, 8)[:6], out=flat.view(8, 8)[2:])),
+        ("EINVAL", lambda: daso.linear_cross_entropy(f[:, :0], w[:, :0], t)),
+    ]:
+        with pytest.raises(daso.DasoError, match=status):
+            call()
+    torch.cuda.synchronize()
+    assert not flat.any() and not mom.any()

@@ -1,0 +1,204 @@
+"""The training operators' C ABI without a GPU: exports, struct layouts, the stated workspaces, and
+bad arguments rejected before any HIP call.  Fake device addresses are never dereferenced:
+these calls are all refused, and the tests skip where a GPU is visible."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+
+from paper_2104_05588_amd import _lib as L
+from paper_2104_05588_amd import _train as T
+from paper_2104_05588_amd import build as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "daso_train.h")
+A, MB = 0x10000000, 1 << 20
+OK, EINVAL, EALIGN, EALIAS, ENOSPACE = L.DASO_OK, L.DASO_EINVAL, L.DASO_EALIGN, L.DASO_EALIAS, L.DASO_ENOSPACE
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(L.LIB_PATH):
+        B.build()
+    return T._load()
+
+
+def no_gpu():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("argument-check tests use fake device addresses; run them without a GPU")
+
+
+def test_header_and_exports(lib):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"^\s*int\s+(daso_\w+)\s*\(", text, flags=re.M))
+    assert names == set(T.EXPORTED_TRAIN)
+    for name in names:
+        assert hasattr(lib, name), name
+
+
+def test_struct_layouts_match_header(tmp_path):
+    structs = [T.daso_layer_norm_args, T.daso_layer_norm_backward_args, T.daso_loss_args, T.daso_orthogonalize_args,
+               T.daso_matrix, T.daso_muon_args]
+    src = ["#include <stdio.h>", "#include <stddef.h>", '#include "daso_train.h"', "int main(void) {"]
+    for st in structs:
+        src.append(f'  printf("{st.__name__} size %zu\\n", sizeof({st.__name__}));')
+        src += [f'  printf("{st.__name__} {f[0]} %zu\\n", offsetof({st.__name__}, {f[0]}));' for f in st._fields_]
+    c = tmp_path / "layout.c"
+    c.write_text("\n".join(src + ["  return 0; }"]) + "\n")
+    exe = tmp_path / "layout"
+    subprocess.run(["gcc", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROOT, "include"), "-I", "/opt/rocm/include", str(c), "-o",
+                    str(exe)], check=True)
+    found = {st.__name__: st for st in structs}
+    lines = subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split("\n")
+    assert len(lines) > 60
+    for line in filter(None, lines):
+        st, f, v = line.split()
+        assert int(v) == (ctypes.sizeof(found[st]) if f == "size" else getattr(found[st], f).offset), line
+
+
+def made(struct, base, **over):
+    a = struct()
+    for k, v in {**base, **over}.items():
+        setattr(a, k, v)
+    return a
+
+
+def call(fn, a):
+    return fn(ctypes.byref(a), None)
+
+
+def need(fn, a, *more):
+    n = ctypes.c_size_t(12345)
+    return fn(ctypes.byref(a), *more, ctypes.byref(n)), n.value
+
+
+def refused(fn, struct, base, cases):
+    for over, status in cases:
+        assert call(fn, made(struct, base, **over)) == status, over
+
+
+def test_layer_norm_rejects(lib):
+    no_gpu()
+    base = dict(rows=10, d=64, type=1, eps=1e-5, x=A, x_stride=64, weight=A + MB, bias=A + 2 * MB, y=A + 3 * MB, y_stride=64,
+                mean=A + 4 * MB, rstd=A + 5 * MB)
+    refused(lib.daso_layer_norm, T.daso_layer_norm_args, base, [
+        (dict(rows=-1), EINVAL), (dict(d=-1), EINVAL), (dict(d=65537, x_stride=65537, y_stride=65537), EINVAL), (dict(type=2), EINVAL),
+        (dict(eps=-1e-9), EINVAL), (dict(eps=float("nan")), EINVAL), (dict(eps=float("inf")), EINVAL), (dict(x=None), EINVAL),
+        (dict(y=None), EINVAL), (dict(x_stride=63), EINVAL), (dict(y_stride=0), EINVAL), (dict(x_stride=1 << 60), EINVAL),
+        (dict(x=A + 1), EALIGN), (dict(weight=A + MB + 2), EALIGN), (dict(mean=A + 4 * MB + 2), EALIGN),
+        (dict(y=A, y_stride=65), EALIAS), (dict(y=A + 64), EALIAS), (dict(mean=A + 8), EALIAS), (dict(mean=A + 3 * MB + 100), EALIAS),
+        (dict(rstd=A + 4 * MB), EALIAS), (dict(y=A + MB), EALIAS),
+        (dict(rows=0, x=None, y=None), OK), (dict(d=0), OK)])
+    assert lib.daso_layer_norm(None, None) == EINVAL
+
+
+def test_layer_norm_backward_rejects(lib):
+    no_gpu()
+    base = dict(rows=10, d=64, type=0, dy=A, dy_stride=64, x=A + MB, x_stride=70, weight=A + 2 * MB, mean=A + 3 * MB, rstd=A + 4 * MB,
+                dx=A + 5 * MB, dx_stride=64, dweight=A + 6 * MB, dbias=A + 7 * MB, workspace=A + 8 * MB, workspace_bytes=MB)
+    rc, n = need(lib.daso_layer_norm_backward_workspace, made(T.daso_layer_norm_backward_args, base))
+    assert rc == OK and 0 < n <= MB and n % (2 * 64 * 4) == 0
+    refused(lib.daso_layer_norm_backward, T.daso_layer_norm_backward_args, base, [
+        (dict(reserved=1), EINVAL), (dict(dy=None), EINVAL), (dict(x=None), EINVAL), (dict(mean=None), EINVAL), (dict(rstd=None), EINVAL),
+        (dict(dy_stride=63), EINVAL), (dict(dx_stride=63), EINVAL), (dict(dx=A + 5 * MB + 2), EALIGN), (dict(dweight=A + 6 * MB + 1), EALIGN),
+        (dict(dx=A, dx_stride=65), EALIAS), (dict(dx=A + MB), EALIAS), (dict(dweight=A + 2 * MB), EALIAS), (dict(dbias=A + 6 * MB), EALIAS),
+        (dict(workspace_bytes=n - 1), ENOSPACE), (dict(workspace=None), EINVAL), (dict(workspace=A + 8 * MB + 16), EALIGN),
+        (dict(d=0), OK), (dict(rows=0, dweight=None, dbias=None), OK), (dict(dx=None, dweight=None, dbias=None), OK)])
+    assert need(lib.daso_layer_norm_backward_workspace, made(T.daso_layer_norm_backward_args, base, rows=0)) == (OK, 0)
+    assert lib.daso_layer_norm_backward_workspace(None, None) == EINVAL
+
+
+def test_loss_rejects(lib):
+    no_gpu()
+    G = 1 << 30
+    base = dict(tokens=100, vocab=1000, d=128, type=1, dweight_type=0, hidden=A, hidden_stride=128, weight=A + G, weight_stride=128,
+                targets=A + 2 * G, ignore_index=-100, loss=A + 3 * G, lse=A + 4 * G, dloss=A + 5 * G, dhidden=A + 6 * G, dhidden_stride=128,
+                dweight=A + 7 * G, dweight_stride=128, workspace=A + 8 * G, workspace_bytes=G)
+    both = [
+        (dict(tokens=-1), EINVAL), (dict(tokens=(4 << 20) + 1), EINVAL), (dict(vocab=0), EINVAL), (dict(d=0), EINVAL), (dict(vocab=(1 << 20) + 1), EINVAL),
+        (dict(type=7), EINVAL), (dict(dweight_type=-1), EINVAL), (dict(hidden=None), EINVAL), (dict(weight=None), EINVAL),
+        (dict(targets=None), EINVAL), (dict(lse=None), EINVAL), (dict(hidden_stride=127), EINVAL), (dict(weight_stride=5 << 20), EINVAL),
+        (dict(hidden=A + 1), EALIGN), (dict(targets=A + 2 * G + 4), EALIGN), (dict(workspace_bytes=1000), ENOSPACE)]
+    refused(lib.daso_linear_cross_entropy, T.daso_loss_args, base, both + [
+        (dict(loss=None), EINVAL), (dict(loss=A), EALIAS), (dict(lse=A + 3 * G + 4), EALIAS), (dict(tokens=0, hidden=None), OK)])
+    refused(lib.daso_linear_cross_entropy_backward, T.daso_loss_args, base, both + [
+        (dict(dloss=None), EINVAL), (dict(dhidden_stride=100), EINVAL), (dict(dweight_stride=100), EINVAL), (dict(dhidden=A), EALIAS),
+        (dict(dweight=A + G), EALIAS), (dict(dweight=A + 6 * G), EALIAS), (dict(dhidden=A + 5 * G), EALIAS),
+        (dict(dhidden=None, dweight=None), OK), (dict(tokens=0, dweight=None), OK)])
+    sizes = [need(lib.daso_linear_cross_entropy_workspace, made(T.daso_loss_args, base, vocab=v), 1)[1] for v in (1000, 10000, 100000)]
+    assert sizes == sorted(sizes)
+    # more tokens do not grow the planes of dz without bound: 2^26 values of four planes, and what grows with each side alone
+    _, n = need(lib.daso_linear_cross_entropy_workspace, made(T.daso_loss_args, base, tokens=65536, vocab=50257), 1)
+    assert n < 4 * 2 * (1 << 26) * 1.3 + 65536 * 128 * 16 + 50257 * 128 * 8
+    assert need(lib.daso_linear_cross_entropy_workspace, made(T.daso_loss_args, base, tokens=0), 0) == (OK, 0)
+
+
+def coefficients(steps):
+    return (ctypes.c_float * (3 * steps))(*[3.4445, -4.775, 2.0315] * steps)
+
+
+def test_orthogonalize_rejects(lib):
+    no_gpu()
+    G = 1 << 30
+    c, bad = coefficients(5), coefficients(5)
+    bad[4] = float("inf")
+    base = dict(batch=2, rows=100, cols=64, type=1, out_type=0, src=A, src_batch_stride=6400, src_stride=64, out=A + G,
+                out_batch_stride=6400, out_stride=64, steps=5, eps=1e-7, coefficients=c, workspace=A + 2 * G, workspace_bytes=G)
+    rc, n = need(lib.daso_orthogonalize_workspace, made(T.daso_orthogonalize_args, base))
+    assert rc == OK and n % 256 == 0
+    refused(lib.daso_orthogonalize, T.daso_orthogonalize_args, base, [
+        (dict(batch=-1), EINVAL), (dict(rows=(1 << 20) + 1), EINVAL), (dict(type=3), EINVAL), (dict(steps=0), EINVAL), (dict(steps=17), EINVAL),
+        (dict(coefficients=bad), EINVAL), (dict(coefficients=None), EINVAL), (dict(eps=-1.0), EINVAL), (dict(src=None), EINVAL),
+        (dict(src_stride=63), EINVAL), (dict(src_batch_stride=6399), EINVAL), (dict(out_batch_stride=100), EINVAL), (dict(out=A + G + 2), EALIGN),
+        (dict(out=A), EALIAS), (dict(out=A + 64), EALIAS), (dict(workspace_bytes=n - 1), ENOSPACE), (dict(workspace=A + 2 * G + 128), EALIGN),
+        (dict(batch=0, src=None), OK), (dict(rows=0), OK)])
+
+
+def test_muon_rejects(lib):
+    no_gpu()
+    G = 1 << 30
+    c = coefficients(5)
+
+    def mats(*rows):
+        arr = (T.daso_matrix * max(len(rows), 1))()
+        for m, r in zip(arr, rows):
+            m.start, m.rows, m.cols, m.scale = r[:4]
+            m.reserved = r[4] if len(r) > 4 else 0
+        return arr
+
+    def ptrs(*xs):
+        return (ctypes.c_void_p * len(xs))(*xs)
+
+    base = dict(n=10000, g=2, nmatrices=2, grads=ptrs(A, A + G), params=A + 2 * G, momentum=A + 3 * G, wire=A + 4 * G,
+                matrices=mats((0, 50, 40, 1.0), (4000, 60, 100, 1.0)), lr=0.1, mu=0.9, weight_decay=0.0, eps=1e-7, coefficients=c, steps=5,
+                flags=1, workspace=A + 5 * G, workspace_bytes=G)
+    rc, n = need(lib.daso_muon_workspace, made(T.daso_muon_args, base))
+    assert rc == OK and n > 0
+    one = (0, 50, 40, 1.0)
+    refused(lib.daso_muon_step, T.daso_muon_args, base, [
+        (dict(n=-1), EINVAL), (dict(g=0), EINVAL), (dict(g=65), EINVAL), (dict(nmatrices=-1), EINVAL), (dict(matrices=None), EINVAL),
+        (dict(matrices=mats(one, (1999, 2, 2, 1.0))), EINVAL), (dict(matrices=mats(one, (9000, 60, 100, 1.0))), EINVAL),
+        (dict(matrices=mats(one, (-1, 2, 2, 1.0))), EINVAL), (dict(matrices=mats(one, (3000, 0, 2, 1.0))), EINVAL),
+        (dict(matrices=mats(one, (3000, 2, 2, float("nan")))), EINVAL), (dict(matrices=mats(one, (3000, 2, 2, 1.0, 1))), EINVAL),
+        (dict(flags=2), EINVAL), (dict(lr=float("inf")), EINVAL), (dict(steps=0), EINVAL), (dict(grads=None), EINVAL), (dict(grads=ptrs(A, None)), EINVAL),
+        (dict(params=None), EINVAL), (dict(params=A + 2 * G + 4), EALIGN), (dict(grads=ptrs(A, A + G + 8)), EALIGN), (dict(momentum=A + 2 * G), EALIAS),
+        (dict(params=A + 16), EALIAS), (dict(wire=A + 3 * G + 16), EALIAS), (dict(workspace_bytes=n - 1), ENOSPACE),
+        (dict(n=0, nmatrices=0), OK), (dict(nmatrices=0), OK)])
+
+
+def test_rounds_bound_the_workspace(lib):
+    """Many matrices are taken in rounds: the workspace stops growing with their number."""
+    mats = (T.daso_matrix * 1000)()
+    for i, m in enumerate(mats):
+        m.start, m.rows, m.cols, m.scale = i << 20, 1024, 1024, 1.0
+    a = T.daso_muon_args()
+    a.n, a.g, a.matrices = 1000 << 20, 1, mats
+    sizes = []
+    for k in (1, 10, 64, 128, 1000):
+        a.nmatrices = k
+        sizes.append(need(lib.daso_muon_workspace, a)[1])
+    assert sizes[0] < sizes[1] < sizes[2] and sizes[2] == sizes[3] == sizes[4]
+    assert sizes[2] < (1 << 26) * 29 + MB
