@@ -33,13 +33,12 @@ using product::half8;
 
 constexpr float kProbScale = 16384.0f;  // dz / dloss in [-1, 1] as binary16
 
-// Powers of two and their reciprocals, worked out on the device.
+// Powers of two from the largest finite magnitudes of hidden, weight and dloss, and their reciprocals.
+enum Tensor { kHidden, kWeight, kGrad };
+constexpr int kTopParts = 512;  // workgroups that look for one
 struct Scales {
-  uint32_t top[3];  // bits of the largest finite magnitude: hidden, weight, dloss
-  uint32_t pad;
-  float hidden, hidden_inv;  // hidden * scale <= 2^15
-  float weight, weight_inv;
-  float grad, grad_inv;  // |dloss| * grad_inv <= 1
+  uint32_t top[3][kTopParts];  // bits of the magnitudes
+  float to[3], inv[3];         // hidden and weight times `to` are below 2^15, dloss times `inv` is at most 1
 };
 
 // What the backward epilogue needs of a token.
@@ -52,13 +51,17 @@ struct Row {
 
 __device__ inline float power_of_two(int e) { return __builtin_bit_cast(float, uint32_t(min(max(e, -126), 127) + 127) << 23); }
 
-__global__ void clear_kernel(Scales* s) {
-  if (threadIdx.x < 3) s->top[threadIdx.x] = 0;
-}
+struct TopArgs {
+  struct {
+    const void* src;
+    int64_t stride, rows, cols;
+    int32_t type;
+  } of[3];
+  Scales* out;
+};
 
-// The largest finite magnitude of a matrix.
 template <class T>
-__global__ __launch_bounds__(256) void top_kernel(const T* src, int64_t stride, int64_t rows, int64_t cols, uint32_t* top) {
+__device__ inline float top_of(const T* src, int64_t stride, int64_t rows, int64_t cols) {
   const int64_t wave = (blockIdx.x * 256 + threadIdx.x) >> 6, waves = gridDim.x * 4;
   const int lane = threadIdx.x & 63;
   const bool wide = ((reinterpret_cast<uintptr_t>(src) | (stride * sizeof(T))) & 15) == 0;
@@ -66,64 +69,124 @@ __global__ __launch_bounds__(256) void top_kernel(const T* src, int64_t stride, 
   float m = 0.0f;
   auto take = [&](float v) {
     v = __builtin_fabsf(v);
-    if (v < __builtin_inff()) m = fmaxf(m, v);
+    m = fmaxf(m, v < __builtin_inff() ? v : 0.0f);
   };
-  for (int64_t r = wave; r < rows; r += waves) {
-    const T* p = src + r * stride;
-    for (int64_t c = lane * 8; c < whole; c += 512) {
-      float v[8];
-      load8(p + c, v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) take(v[i]);
-    }
-    for (int64_t c = whole + lane; c < cols; c += 64) take(load1(p + c));
+  if (cols == 1) {  // a vector
+    for (int64_t r = wave * 64 + lane; r < rows; r += waves * 64) take(load1(src + r * stride));
+    return wave_max(m);
   }
-  m = wave_max(m);
-  if (lane == 0 && m > 0.0f) atomicMax(top, __builtin_bit_cast(uint32_t, m));
+  // four rows at a time, for loads in flight
+  for (int64_t r = wave; r < rows; r += 4 * waves) {
+    for (int64_t c = lane * 8; c < whole; c += 512) {
+      float v[4][8] = {};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (r + k * waves < rows) load8(src + (r + k * waves) * stride + c, v[k]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) take(v[k][i]);
+    }
+    for (int64_t c = whole + lane; c < cols; c += 64) {
+      float v[4] = {};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (r + k * waves < rows) v[k] = load1(src + (r + k * waves) * stride + c);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) take(v[k]);
+    }
+  }
+  return wave_max(m);
 }
 
-__global__ void scales_kernel(Scales* s) {
-  if (threadIdx.x != 0) return;
-  const auto exponent = [](uint32_t bits) { return bits == 0 ? 0 : static_cast<int>(max(bits >> 23, 1u)) - 127; };
-  const int h = min(max(14 - exponent(s->top[0]), -126), 126), w = min(max(14 - exponent(s->top[1]), -126), 126);
-  s->hidden = power_of_two(h), s->hidden_inv = power_of_two(-h);
-  s->weight = power_of_two(w), s->weight_inv = power_of_two(-w);
-  const int g = min(max(exponent(s->top[2]) + 1, -126), 126);
-  s->grad = power_of_two(g), s->grad_inv = power_of_two(-g);
+// Workgroup (x, y): part x of tensor y.
+__global__ __launch_bounds__(256) void tops_kernel(TopArgs a) {
+  __shared__ float shared[4];
+  const auto& s = a.of[blockIdx.y];
+  const float m = s.type == DASO_TYPE_BF16 ? top_of((const uint16_t*)s.src, s.stride, s.rows, s.cols)
+                                           : top_of((const float*)s.src, s.stride, s.rows, s.cols);
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    a.out->top[blockIdx.y][blockIdx.x] = __builtin_bit_cast(uint32_t, fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3])));
 }
 
-__global__ __launch_bounds__(256) void rows_kernel(Row* out, int64_t padded, int64_t tokens, int64_t vocab, const float* lse,
-                                                   const float* dloss, const int64_t* targets, int64_t ignore,
-                                                   const Scales* s) {
-  const int64_t i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= padded) return;
+// The exponent of a tensor's scale, by a workgroup of 256.
+__device__ inline int scale_exponent(const Scales* s, int tensor, uint32_t* shared) {
+  uint32_t m = max(s->top[tensor][threadIdx.x], s->top[tensor][threadIdx.x + 256]);
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), k)));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = max(max(shared[0], shared[1]), max(shared[2], shared[3]));
+  const int e = m == 0 ? 0 : static_cast<int>(max(m >> 23, 1u)) - 127;
+  return min(max(tensor == kGrad ? e + 1 : 14 - e, -126), 126);
+}
+static_assert(kTopParts == 512, "two parts a thread");
+
+// What comes before the products of a pass, in one launch: planes of hidden and weight, and the
+// backward pass's rows.
+constexpr int kMaxPlanes = 4;
+struct PrepareArgs {
+  int32_t count;
+  int64_t first[kMaxPlanes + 2];  // workgroups of each job: the planes, then the rows
+  PlanesArgs planes[kMaxPlanes];
+  int32_t tensor[kMaxPlanes];
+  int32_t raw[kMaxPlanes];
+  Scales* scales;                 // null: none are needed
+  Row* rows;
+  int64_t padded, tokens, vocab;
+  const float *lse, *dloss;
+  const int64_t* targets;
+  int64_t ignore;
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
+  __shared__ uint16_t lds[2][64][66];
+  __shared__ uint32_t shared[4];
+  const int64_t id = blockIdx.x + int64_t(blockIdx.y) * gridDim.x;
+  if (id >= a.first[a.count + 1]) return;
+  if (id == 0 && a.scales != nullptr) {
+    for (int t = 0; t < 3; ++t) {
+      const int e = scale_exponent(a.scales, t, shared);
+      if (threadIdx.x == 0) a.scales->to[t] = power_of_two(e), a.scales->inv[t] = power_of_two(-e);
+    }
+  }
+  if (id < a.first[a.count]) {
+    int k = 0;
+    while (id >= a.first[k + 1]) ++k;
+    const PlanesArgs& p = a.planes[k];
+    const int64_t t = id - a.first[k], across = p.cols_p / 64;
+    const int tr = static_cast<int>(t / across), tc = static_cast<int>(t % across);
+    if (a.raw[k]) planes_tile<T, true>(p, 0, tr, tc, 1.0f, lds);
+    else planes_tile<T, false>(p, 0, tr, tc, power_of_two(scale_exponent(a.scales, a.tensor[k], shared)), lds);
+    return;
+  }
+  const float inv = power_of_two(-scale_exponent(a.scales, kGrad, shared));
+  const int64_t i = (id - a.first[a.count]) * 256 + threadIdx.x;
+  if (i >= a.padded) return;
   Row r = {0.0f, 0.0f, -1, 0};
-  if (i < tokens) {
-    const int64_t t = targets[i];
-    if (t >= 0 && t < vocab && t != ignore) {
-      r.lse = lse[i];
-      r.g = dloss[i] * s->grad_inv * kProbScale;
+  if (i < a.tokens) {
+    const int64_t t = a.targets[i];
+    if (t >= 0 && t < a.vocab && t != a.ignore) {
+      r.lse = a.lse[i];
+      r.g = a.dloss[i] * inv * kProbScale;
       r.target = static_cast<int32_t>(t);
-    } else if (t != ignore) {
+    } else if (t != a.ignore) {
       r.g = __builtin_nanf("");
       r.target = 0;
     }
   }
-  out[i] = r;
-}
-
-template <class T, bool RAW>
-__global__ __launch_bounds__(256) void planes_kernel(PlanesArgs p, const float* scale) {
-  __shared__ uint16_t lds[2][64][66];
-  const int64_t id = blockIdx.x + int64_t(blockIdx.y) * gridDim.x, across = p.cols_p / 64;
-  if (id >= across * (p.rows_p / 64)) return;
-  planes_tile<T, RAW>(p, 0, static_cast<int>(id / across), static_cast<int>(id % across), RAW ? 1.0f : *scale, lds);
+  a.rows[i] = r;
 }
 
 // ------------------------------------------------------------------------- forward epilogue
 // For each row the maximum and the sum of exponentials of the tile's columns, and the logit of
 // the target where the tile has it.
 struct LseOut {
+  static constexpr auto kKind = product::kWhole;
   struct Params {
     float2* parts;  // [tile column][token]
     float* at_target;
@@ -135,7 +198,7 @@ struct LseOut {
                               char* lds) {
     constexpr int kAcross = Tile::kThreads / 128;  // wavefronts side by side, of two rows of them
     constexpr int kBands = Tile::kBlocks / 2;      // runs of 64 rows a wavefront holds
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = product::thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, kq = lane >> 4, wn = wave % kAcross;
     float2* shared = (float2*)lds;  // [row][kAcross]
     const float inv = out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f;
@@ -223,6 +286,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* parts, int32_t 
 // ------------------------------------------------------------------------- backward epilogues
 // dz of a piece's columns as planes, straight and transposed; columns beyond the vocabulary are zero.
 struct ProbOut {
+  static constexpr auto kKind = product::kBlocks;
   struct Params {
     const Row* rows;
     _Float16 *hi, *lo, *t_hi, *t_lo;  // any may be null but hi's or t_hi's
@@ -231,64 +295,55 @@ struct ProbOut {
     int32_t padded_rows;             // tokens with padding: the planes are contracted over both
     const float *inv_a, *inv_b;
   };
-  template <class Tile>
-  __device__ static void tile(const Params& out, const product::Args&, const product::Place& at, f4 (&acc)[Tile::kBlocks][8],
-                              char* lds) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __device__ static void block(const Params& out, const product::Place&, const f4 (&acc)[8], int row0, int col0, char* hi, int lane) {
+    if (row0 >= out.padded_rows || col0 >= out.padded) return;
     const int r16 = lane & 15, kq = lane >> 4;
-    char* hi = lds + wave * product::kWaveStage;
     char* lo = hi + product::kStagePlane;
     const float inv = out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f;
     const bool two = out.lo != nullptr || out.t_lo != nullptr;
 #pragma unroll
-    for (int b = 0; b < Tile::kBlocks; ++b) {
-      int row0, col0;
-      Tile::block_at(wave, b, &row0, &col0);
-      row0 += at.tm * Tile::kRows, col0 += at.tn * Tile::kCols;
-      if (row0 >= out.padded_rows || col0 >= out.padded) continue;
+    for (int i = 0; i < 4; ++i) {
+      const Row r = out.rows[row0 + i * 16 + r16];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const Row r = out.rows[row0 + i * 16 + r16];
+      for (int j = 0; j < 2; ++j) {
+        const int col = col0 + j * 16 + kq * 4;
+        half4 h, l;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int col = col0 + j * 16 + kq * 4;
-          half4 h, l;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float v = __expf(acc[b][i * 2 + j][e] * inv - r.lse) - (out.first + col + e == r.target ? 1.0f : 0.0f);
-            v = r.target >= 0 && col + e < out.columns ? v * r.g : 0.0f;
-            _Float16 a, c;
-            product::split(v, &a, &c);
-            h[e] = a, l[e] = c;
-          }
-          *(half4*)(hi + product::plane_at(i * 16 + r16, j * 16 + kq * 4)) = h;
-          if (two) *(half4*)(lo + product::plane_at(i * 16 + r16, j * 16 + kq * 4)) = l;
+        for (int e = 0; e < 4; ++e) {
+          float v = __expf(acc[i * 2 + j][e] * inv - r.lse) - (out.first + col + e == r.target ? 1.0f : 0.0f);
+          v = r.target >= 0 && col + e < out.columns ? v * r.g : 0.0f;
+          _Float16 a, c;
+          product::split(v, &a, &c);
+          h[e] = a, l[e] = c;
         }
+        *(half4*)(hi + product::plane_at(i * 16 + r16, j * 16 + kq * 4)) = h;
+        if (two) *(half4*)(lo + product::plane_at(i * 16 + r16, j * 16 + kq * 4)) = l;
       }
-      product::wait_lds();
-      __builtin_amdgcn_wave_barrier();
-      const auto straight = [&](const char* plane, _Float16* to) {
-#pragma unroll
-        for (int pass = 0; pass < 4; ++pass) {
-          const int r = pass * 16 + (lane >> 2), c = (lane & 3) * 8;
-          *(half8*)(to + int64_t(row0 + r) * out.ld + col0 + c) = *(const half8*)(plane + product::plane_at(r, c));
-        }
-      };
-      const auto turned = [&](const char* plane, _Float16* to) {
-        product::by_columns(plane, lane, [&](int c, int r, half8 v) {
-          *(half8*)(to + int64_t(col0 + c) * out.t_ld + row0 + r) = v;
-        });
-      };
-      if (out.hi != nullptr) straight(hi, out.hi);
-      if (out.lo != nullptr) straight(lo, out.lo);
-      if (out.t_hi != nullptr) turned(hi, out.t_hi);
-      if (out.t_lo != nullptr) turned(lo, out.t_lo);
     }
+    product::wait_lds();
+    __builtin_amdgcn_wave_barrier();
+    const auto straight = [&](const char* plane, _Float16* to) {
+#pragma unroll
+      for (int pass = 0; pass < product::kPasses; ++pass) {
+        const int r = product::pass_row(pass, lane), c = product::pass_col(lane);
+        *(half8*)(to + int64_t(row0 + r) * out.ld + col0 + c) = *(const half8*)(plane + product::plane_at(r, c));
+      }
+    };
+    const auto turned = [&](const char* plane, _Float16* to) {
+      product::by_columns(plane, lane, [&](int c, int r, half8 v) {
+        *(half8*)(to + int64_t(col0 + c) * out.t_ld + row0 + r) = v;
+      });
+    };
+    if (out.hi != nullptr) straight(hi, out.hi);
+    if (out.lo != nullptr) straight(lo, out.lo);
+    if (out.t_hi != nullptr) turned(hi, out.t_hi);
+    if (out.t_lo != nullptr) turned(lo, out.t_lo);
   }
 };
 
 // A gradient: (C * grad * inv / kProbScale) [+ sum], as the sum so far or as the result.
 struct GradOut {
+  static constexpr auto kKind = product::kStaged;
   struct Params {
     const float *grad, *inv;
     const float* before;  // the sum of the pieces so far, or null
@@ -298,38 +353,42 @@ struct GradOut {
     int32_t bf16;
     int32_t rows, cols;
   };
-  template <class Tile>
-  __device__ static void tile(const Params& p, const product::Args& args, const product::Place& at, f4 (&acc)[Tile::kBlocks][8],
-                              char* lds) {
-    product::by_blocks<Tile, GradOut>(p, args, at, acc, lds);
-  }
-  __device__ static void block(const Params& p, const product::Place&, const f4 (&c)[8], int row, int col, char* stage, int lane) {
+  __device__ static void block(const Params& p, const product::Place&, int row, int col, char* stage, int lane) {
     const float factor = *p.grad * (1.0f / kProbScale), inv = *p.inv;
     const bool wide = ((reinterpret_cast<uintptr_t>(p.out) | (p.ld * (p.bf16 ? 2 : 4))) & 15) == 0;
-    product::by_rows(c, stage, lane, [&](int r, int k, float(&v)[8]) {
-      const int32_t rr = row + r, cc = col + k, left = p.cols - cc;
-      if (rr >= p.rows || left <= 0) return;
+    const int cc = col + product::pass_col(lane), left = p.cols - cc;
+    if (left <= 0) return;
+    float before[product::kPasses][8] = {};
+    if (p.before != nullptr) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = v[i] * inv * factor;
-      if (p.before != nullptr) {
-        float b[8];
-        load8(p.before + int64_t(rr) * p.before_ld + cc, b);  // padded to whole vectors
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += b[i];
+      for (int pass = 0; pass < product::kPasses; ++pass) {
+        const int rr = row + product::pass_row(pass, lane);
+        if (rr < p.rows) load8(p.before + int64_t(rr) * p.before_ld + cc, before[pass]);  // padded to whole vectors
       }
+    }
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) {
+      const int rr = row + product::pass_row(pass, lane);
+      if (rr >= p.rows) continue;
+      float v[8];
+      product::pass_values(stage, pass, lane, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = v[i] * inv * factor + before[pass][i];
       const int64_t to = int64_t(rr) * p.ld + cc;
-      if (p.bf16) {
-        uint16_t* o = (uint16_t*)p.out + to;
-        if (wide && left >= 8) store8(o, v);
-        else
-          for (int i = 0; i < 8 && i < left; ++i) o[i] = to_bf16(v[i]);
+      uint16_t* o16 = p.bf16 ? (uint16_t*)p.out + to : nullptr;
+      float* o32 = p.bf16 ? nullptr : (float*)p.out + to;
+      if (wide && left >= 8) {
+        if (o16 != nullptr) store8(o16, v);
+        else store8(o32, v);
       } else {
-        float* o = (float*)p.out + to;
-        if (wide && left >= 8) store8(o, v);
-        else
-          for (int i = 0; i < 8 && i < left; ++i) o[i] = v[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (i >= left) continue;
+          if (o16 != nullptr) o16[i] = to_bf16(v[i]);
+          else o32[i] = v[i];
+        }
       }
-    });
+    }
   }
 };
 
@@ -352,7 +411,7 @@ struct Plan {
   int64_t n_p, d_p, v_p;          // padded tokens, features, classes
   int64_t piece, pieces;          // classes of a piece (but the last), pieces
   bool f32, copy_h, copy_w;       // operands of the logits that are copied
-  size_t scales, parts, at_target, rows, h[2], w[2], ht[2], wt[2], p[2], pt[2], sum;
+  size_t scales, sums, sums_bytes, parts, at_target, rows, h[2], w[2], ht[2], wt[2], p[2], pt[2], sum;
   size_t bytes;
 };
 
@@ -399,29 +458,12 @@ Plan plan_of(const daso_loss_args& s, bool backward) {
     for (int i = 0; i < 2; ++i) q.p[i] = take(2 * q.n_p * width), q.pt[i] = take(2 * q.n_p * width);
     q.sum = take(q.pieces > 1 ? 4 * q.n_p * q.d_p : 0);
   }
+  // the largest product's steps, in tiles of 128 and three segments
+  const int64_t nt = (q.n_p + 127) / 128, dt = (q.d_p + 127) / 128, width = std::min(q.v_p, q.piece), vt = (width + 127) / 128;
+  q.sums_bytes = backward ? host::sums_bytes(3 * std::max(nt * vt * (q.d_p / 64), dt * (nt * (width / 64) + vt * (q.n_p / 64)))) : 0;
+  q.sums = take(static_cast<int64_t>(q.sums_bytes));
   q.bytes = to;
   return q;
-}
-
-hipError_t lay_out(const void* src, int32_t type, int64_t stride, int64_t rows, int64_t cols, int64_t rows_p, int64_t cols_p,
-                   bool raw, const float* scale, char* d0, char* d1, char* t0, char* t1, hipStream_t stream) {
-  PlanesArgs p = {};
-  p.src = src, p.stride = stride;
-  p.rows = static_cast<int32_t>(rows), p.cols = static_cast<int32_t>(cols);
-  p.rows_p = static_cast<int32_t>(rows_p), p.cols_p = static_cast<int32_t>(cols_p);
-  p.d[0] = (uint16_t*)d0, p.d[1] = (uint16_t*)d1, p.t[0] = (uint16_t*)t0, p.t[1] = (uint16_t*)t1;
-  const int64_t tiles = (rows_p / 64) * (cols_p / 64), row = int64_t(1) << 20;
-  const dim3 grid(static_cast<uint32_t>(std::min(tiles, row)), static_cast<uint32_t>((tiles + row - 1) / row));
-  if (raw) return launch(&planes_kernel<uint16_t, true>, grid, dim3(256), stream, p, scale);
-  if (type == DASO_TYPE_BF16) return launch(&planes_kernel<uint16_t, false>, grid, dim3(256), stream, p, scale);
-  return launch(&planes_kernel<float, false>, grid, dim3(256), stream, p, scale);
-}
-
-hipError_t top_of(const void* src, int32_t type, int64_t stride, int64_t rows, int64_t cols, uint32_t* top, hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(std::min<int64_t>((rows + 3) / 4, 2048)));
-  if (type == DASO_TYPE_BF16)
-    return launch(&top_kernel<uint16_t>, grid, dim3(256), stream, (const uint16_t*)src, stride, rows, cols, top);
-  return launch(&top_kernel<float>, grid, dim3(256), stream, (const float*)src, stride, rows, cols, top);
 }
 
 // The operands of the logits, for the classes from `first`.
@@ -441,43 +483,67 @@ void logits(product::Args& a, const Plan& q, const Operands& o, int64_t tokens, 
   a.M = static_cast<int32_t>(tokens), a.N = static_cast<int32_t>(classes), a.batch = 1;
 }
 
-// Scales, and the planes of hidden and weight that the pass needs.
-hipError_t operands_of(const daso_loss_args& s, const Plan& q, bool backward, Operands* o, hipStream_t stream) {
+void add_planes(PrepareArgs& a, int32_t tensor, bool raw, const void* src, int64_t stride, int64_t rows, int64_t cols,
+                int64_t rows_p, int64_t cols_p, char* d0, char* d1, char* t0, char* t1) {
+  PlanesArgs& p = a.planes[a.count];
+  p.src = src, p.stride = stride;
+  p.rows = static_cast<int32_t>(rows), p.cols = static_cast<int32_t>(cols);
+  p.rows_p = static_cast<int32_t>(rows_p), p.cols_p = static_cast<int32_t>(cols_p);
+  p.d[0] = (uint16_t*)d0, p.d[1] = (uint16_t*)d1, p.t[0] = (uint16_t*)t0, p.t[1] = (uint16_t*)t1;
+  a.tensor[a.count] = tensor, a.raw[a.count] = raw ? 1 : 0;
+  a.first[a.count + 1] = a.first[a.count] + (rows_p / 64) * (cols_p / 64);
+  ++a.count;
+}
+
+// Scales, the planes of hidden and weight that the pass needs, and the backward pass's rows.
+hipError_t prepare(const daso_loss_args& s, const Plan& q, bool backward, Operands* o, hipStream_t stream) {
   char* ws = static_cast<char*>(s.workspace);
   Scales* sc = reinterpret_cast<Scales*>(ws + q.scales);
   hipError_t e = hipSuccess;
-  if (q.f32 || backward) {
-    e = launch(&clear_kernel, dim3(1), dim3(64), stream, sc);
-    if (e == hipSuccess) e = top_of(s.hidden, s.type, s.hidden_stride, s.tokens, s.d, &sc->top[0], stream);
-    if (e == hipSuccess) e = top_of(s.weight, s.type, s.weight_stride, s.vocab, s.d, &sc->top[1], stream);
-    // in rows of 512, so that long ones are taken by many wavefronts
-    const int64_t rows = s.tokens / 512, rest = s.tokens - rows * 512;
-    if (e == hipSuccess && backward && rows > 0) e = top_of(s.dloss, DASO_TYPE_F32, 512, rows, 512, &sc->top[2], stream);
-    if (e == hipSuccess && backward && rest > 0) e = top_of(s.dloss + rows * 512, DASO_TYPE_F32, rest, 1, rest, &sc->top[2], stream);
-    if (e == hipSuccess) e = launch(&scales_kernel, dim3(1), dim3(64), stream, sc);
+  const bool scaled = q.f32 || backward;
+  if (scaled) {
+    TopArgs t = {};
+    t.of[kHidden] = {s.hidden, s.hidden_stride, s.tokens, s.d, s.type};
+    t.of[kWeight] = {s.weight, s.weight_stride, s.vocab, s.d, s.type};
+      t.of[kGrad] = {s.dloss, 1, backward ? s.tokens : 0, 1, DASO_TYPE_F32};
+    t.out = sc;
+    e = launch(&tops_kernel, dim3(kTopParts, 3), dim3(256), stream, t);
   }
-  const bool need_ht = backward && s.dweight != nullptr, need_wt = backward && s.dhidden != nullptr;
-  char *h[2] = {ws + q.h[0], ws + q.h[1]}, *w[2] = {ws + q.w[0], ws + q.w[1]};
+  PrepareArgs a = {};
+  const auto place = [ws](size_t at, bool wanted) { return wanted ? ws + at : nullptr; };
+  const bool ht = backward && s.dweight != nullptr, wt = backward && s.dhidden != nullptr;
+  const auto hidden = [&](bool raw, char* d0, char* d1, char* t0, char* t1) {
+    add_planes(a, kHidden, raw, s.hidden, s.hidden_stride, s.tokens, s.d, q.n_p, q.d_p, d0, d1, t0, t1);
+  };
+  const auto weight = [&](bool raw, char* d0, char* d1, char* t0, char* t1) {
+    add_planes(a, kWeight, raw, s.weight, s.weight_stride, s.vocab, s.d, q.v_p, q.d_p, d0, d1, t0, t1);
+  };
   if (q.f32) {
-    char *ht0 = need_ht ? ws + q.ht[0] : nullptr, *ht1 = need_ht ? ws + q.ht[1] : nullptr;
-    char *wt0 = need_wt ? ws + q.wt[0] : nullptr, *wt1 = need_wt ? ws + q.wt[1] : nullptr;
-    if (e == hipSuccess)
-      e = lay_out(s.hidden, s.type, s.hidden_stride, s.tokens, s.d, q.n_p, q.d_p, false, &sc->hidden, h[0], h[1], ht0, ht1, stream);
-    if (e == hipSuccess)
-      e = lay_out(s.weight, s.type, s.weight_stride, s.vocab, s.d, q.v_p, q.d_p, false, &sc->weight, w[0], w[1], wt0, wt1, stream);
+    weight(false, ws + q.w[0], ws + q.w[1], place(q.wt[0], wt), place(q.wt[1], wt));
+    hidden(false, ws + q.h[0], ws + q.h[1], place(q.ht[0], ht), place(q.ht[1], ht));
   } else {
-    if (e == hipSuccess && q.copy_h)
-      e = lay_out(s.hidden, s.type, s.hidden_stride, s.tokens, s.d, q.n_p, q.d_p, true, nullptr, h[0], nullptr, nullptr, nullptr, stream);
-    if (e == hipSuccess && q.copy_w)
-      e = lay_out(s.weight, s.type, s.weight_stride, s.vocab, s.d, q.v_p, q.d_p, true, nullptr, w[0], nullptr, nullptr, nullptr, stream);
-    if (e == hipSuccess && need_ht)
-      e = lay_out(s.hidden, s.type, s.hidden_stride, s.tokens, s.d, q.n_p, q.d_p, false, &sc->hidden, nullptr, nullptr, ws + q.ht[0], nullptr, stream);
-    if (e == hipSuccess && need_wt)
-      e = lay_out(s.weight, s.type, s.weight_stride, s.vocab, s.d, q.v_p, q.d_p, false, &sc->weight, nullptr, nullptr, ws + q.wt[0], nullptr, stream);
+    if (q.copy_w) weight(true, ws + q.w[0], nullptr, nullptr, nullptr);
+    if (q.copy_h) hidden(true, ws + q.h[0], nullptr, nullptr, nullptr);
+    if (wt) weight(false, nullptr, nullptr, ws + q.wt[0], nullptr);
+    if (ht) hidden(false, nullptr, nullptr, ws + q.ht[0], nullptr);
   }
-  o->h[0] = q.copy_h ? h[0] : (const char*)s.hidden;
-  o->w[0] = q.copy_w ? w[0] : (const char*)s.weight;
-  o->h[1] = h[1], o->w[1] = w[1];
+  a.first[a.count + 1] = a.first[a.count];
+  if (backward) {
+    a.first[a.count + 1] += (q.n_p + 255) / 256;
+    a.rows = reinterpret_cast<Row*>(ws + q.rows);
+    a.padded = q.n_p, a.tokens = s.tokens, a.vocab = s.vocab;
+    a.lse = s.lse, a.dloss = s.dloss, a.targets = s.targets, a.ignore = s.ignore_index;
+  }
+  a.scales = scaled ? sc : nullptr;
+  const int64_t groups = a.first[a.count + 1], row = int64_t(1) << 20;
+  if (e == hipSuccess && groups > 0) {
+    const dim3 grid(static_cast<uint32_t>(std::min(groups, row)), static_cast<uint32_t>((groups + row - 1) / row));
+    e = s.type == DASO_TYPE_BF16 ? launch(&prepare_kernel<uint16_t>, grid, dim3(256), stream, a)
+                                 : launch(&prepare_kernel<float>, grid, dim3(256), stream, a);
+  }
+  o->h[0] = q.copy_h ? ws + q.h[0] : (const char*)s.hidden;
+  o->w[0] = q.copy_w ? ws + q.w[0] : (const char*)s.weight;
+  o->h[1] = ws + q.h[1], o->w[1] = ws + q.w[1];
   o->h_ld = q.copy_h ? q.d_p : s.hidden_stride;
   o->w_ld = q.copy_w ? q.d_p : s.weight_stride;
   return e;
@@ -485,9 +551,10 @@ hipError_t operands_of(const daso_loss_args& s, const Plan& q, bool backward, Op
 
 hipError_t forward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
   char* ws = static_cast<char*>(s.workspace);
+  const product::Sums sums = {reinterpret_cast<float*>(ws + q.sums), q.sums_bytes};
   const Scales* sc = reinterpret_cast<const Scales*>(ws + q.scales);
   Operands o;
-  hipError_t e = operands_of(s, q, false, &o, stream);
+  hipError_t e = prepare(s, q, false, &o, stream);
   if (e != hipSuccess) return e;
   product::Launch<LseOut> all = {};
   all.count = 1;
@@ -496,11 +563,11 @@ hipError_t forward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
   out.parts = reinterpret_cast<float2*>(ws + q.parts);
   out.at_target = reinterpret_cast<float*>(ws + q.at_target);
   out.targets = s.targets;
-  out.inv_a = q.f32 ? &sc->hidden_inv : nullptr, out.inv_b = q.f32 ? &sc->weight_inv : nullptr;
+  out.inv_a = q.f32 ? &sc->inv[kHidden] : nullptr, out.inv_b = q.f32 ? &sc->inv[kWeight] : nullptr;
   const bool large = product::large_tiles(all);
   const int64_t across = large ? product::Tile256::kCols : product::Tile128::kCols;
-  if (q.f32) e = product::launch_products<false>(all, stream);
-  else e = product::launch_products<true>(all, stream);
+  if (q.f32) e = product::launch_products<false>(all, sums, stream);
+  else e = product::launch_products<true>(all, sums, stream);
   if (e != hipSuccess) return e;
   return launch(&join_kernel, dim3(static_cast<uint32_t>((s.tokens + 31) / 32)), dim3(256), stream, (const float2*)out.parts,
                 static_cast<int32_t>((s.vocab + across - 1) / across), s.tokens, s.vocab, s.targets, s.ignore_index,
@@ -509,13 +576,12 @@ hipError_t forward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
 
 hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
   char* ws = static_cast<char*>(s.workspace);
+  const product::Sums sums = {reinterpret_cast<float*>(ws + q.sums), q.sums_bytes};
   const Scales* sc = reinterpret_cast<const Scales*>(ws + q.scales);
   Operands o;
-  hipError_t e = operands_of(s, q, true, &o, stream);
+  hipError_t e = prepare(s, q, true, &o, stream);
   if (e != hipSuccess) return e;
   Row* rows = reinterpret_cast<Row*>(ws + q.rows);
-  e = launch(&rows_kernel, dim3(static_cast<uint32_t>((q.n_p + 255) / 256)), dim3(256), stream, rows, q.n_p, s.tokens, s.vocab,
-             (const float*)s.lse, s.dloss, s.targets, s.ignore_index, sc);
   const bool dh = s.dhidden != nullptr, dw = s.dweight != nullptr, dw32 = s.dweight_type == DASO_TYPE_F32;
   const auto at = [ws](size_t off) { return reinterpret_cast<_Float16*>(ws + off); };
   for (int64_t k = 0; k < q.pieces && e == hipSuccess; ++k) {
@@ -531,8 +597,8 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
     out.ld = width, out.t_ld = q.n_p;
     out.first = static_cast<int32_t>(first), out.columns = static_cast<int32_t>(classes), out.padded = static_cast<int32_t>(width);
     out.padded_rows = static_cast<int32_t>(q.n_p);
-    out.inv_a = q.f32 ? &sc->hidden_inv : nullptr, out.inv_b = q.f32 ? &sc->weight_inv : nullptr;
-    e = q.f32 ? product::launch_products<false>(prob, stream) : product::launch_products<true>(prob, stream);
+    out.inv_a = q.f32 ? &sc->inv[kHidden] : nullptr, out.inv_b = q.f32 ? &sc->inv[kWeight] : nullptr;
+    e = q.f32 ? product::launch_products<false>(prob, sums, stream) : product::launch_products<true>(prob, sums, stream);
     if (e != hipSuccess) break;
     product::Launch<GradOut> grads = {};
     if (dh) {
@@ -546,7 +612,7 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
       a.lda = width, a.ldb = q.v_p, a.steps = static_cast<int32_t>(width / 64);
       a.M = static_cast<int32_t>(s.tokens), a.N = static_cast<int32_t>(s.d), a.batch = 1;
       GradOut::Params& g = grads.out[grads.count++];
-      g.grad = &sc->grad, g.inv = &sc->weight_inv;
+      g.grad = &sc->to[kGrad], g.inv = &sc->inv[kWeight];
       float* sum = reinterpret_cast<float*>(ws + q.sum);
       if (k > 0) g.before = sum, g.before_ld = q.d_p;
       g.rows = a.M, g.cols = a.N;
@@ -563,12 +629,12 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
       a.lda = a.ldb = q.n_p, a.steps = static_cast<int32_t>(q.n_p / 64);
       a.M = static_cast<int32_t>(classes), a.N = static_cast<int32_t>(s.d), a.batch = 1;
       GradOut::Params& g = grads.out[grads.count++];
-      g.grad = &sc->grad, g.inv = &sc->hidden_inv;
+      g.grad = &sc->to[kGrad], g.inv = &sc->inv[kHidden];
       g.out = static_cast<char*>(s.dweight) + first * s.dweight_stride * static_cast<int64_t>(host::bytes_of(s.dweight_type));
       g.ld = s.dweight_stride, g.bf16 = !dw32;
       g.rows = a.M, g.cols = a.N;
     }
-    e = product::launch_products<false>(grads, stream);
+    e = product::launch_products<false>(grads, sums, stream);
   }
   return e;
 }

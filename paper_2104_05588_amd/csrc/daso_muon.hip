@@ -60,44 +60,42 @@ struct PlanesOut {
     int32_t rest_ld;
     int32_t square;      // C = in in^T; else C = left in
   };
-  template <class Tile>
-  __device__ static void tile(const Params& p, const product::Args& args, const product::Place& at, f4 (&acc)[Tile::kBlocks][8],
-                              char* lds) {
-    product::by_blocks<Tile, PlanesOut>(p, args, at, acc, lds);
-  }
-  __device__ static void block(const Params& p, const product::Place& at, const f4 (&c)[8], int row,
-                               int col, char* stage, int lane) {
+  static constexpr auto kKind = product::kStaged;
+  __device__ static void block(const Params& p, const product::Place& at, int row, int col, char* stage, int lane) {
     const bool turn = p.t_hi != nullptr && (p.t_always || at.tm != at.tn);
     char* plane = stage + product::kStageFloats;
     const int64_t base = at.batch * p.batch;
     const float* rest = p.rest != nullptr ? p.rest + int64_t(at.batch) * p.rest_ld : nullptr;
-    product::by_rows(c, stage, lane, [&](int r, int k, float(&v)[8]) {
+    const int k = product::pass_col(lane);
+    half8 in_hi[product::kPasses], in_lo[product::kPasses];
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) {
+      in_hi[pass] = in_lo[pass] = (half8)(_Float16)0.0f;
+      const int64_t to = base + int64_t(row + product::pass_row(pass, lane)) * p.ld + col + k;
+      if (p.in_hi != nullptr) in_hi[pass] = *(const half8*)(p.in_hi + to);
+      if (p.in_lo != nullptr) in_lo[pass] = *(const half8*)(p.in_lo + to);
+    }
+    float right[8];  // what the operands' diagonals lack: of the left one by rows, of the right one by columns
+#pragma unroll
+    for (int i = 0; i < 8; ++i) right[i] = rest != nullptr && p.square ? rest[col + k + i] : 0.0f;
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) {
+      const int r = product::pass_row(pass, lane);
       const int64_t to = base + int64_t(row + r) * p.ld + col + k;
-      if (p.in_hi != nullptr) {
-        const half8 h = *(const half8*)(p.in_hi + to);
-        half8 l = (half8)(_Float16)0.0f;
-        if (p.in_lo != nullptr) l = *(const half8*)(p.in_lo + to);
-        const float left = rest != nullptr ? rest[row + r] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float in = static_cast<float>(h[i]) + static_cast<float>(l[i]), more = left;
-          if (rest != nullptr && p.square) {
-            more += rest[col + k + i];
-            in += row + r == col + k + i ? left : 0.0f;
-          }
-          v[i] = fmaf(p.beta, in, p.alpha * fmaf(more, in, v[i]));
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= p.alpha;
-      }
+      const float left = rest != nullptr ? rest[row + r] : 0.0f;
+      const int at_diagonal = row + r - col - k;  // which of the eight lies on it
+      float v[8];
+      product::pass_values(stage, pass, lane, v);
       half8 hi, lo;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
+        float in = static_cast<float>(in_hi[pass][i]) + static_cast<float>(in_lo[pass][i]);
+        if (p.square && i == at_diagonal) in += left;
+        v[i] = fmaf(p.beta, in, p.alpha * fmaf(left + right[i], in, v[i]));
         _Float16 a, b;
         product::split(v[i], &a, &b);
         hi[i] = a, lo[i] = b;
-        if (p.rest_out != nullptr && row + r == col + k + i)
+        if (p.rest_out != nullptr && i == at_diagonal)
           p.rest_out[int64_t(at.batch) * p.rest_ld + row + r] = v[i] - static_cast<float>(a);
       }
       *(half8*)(p.hi + to) = hi;
@@ -106,17 +104,17 @@ struct PlanesOut {
         *(half8*)(plane + product::plane_at(r, k)) = hi;
         if (p.t_lo != nullptr) *(half8*)(plane + product::kStagePlane + product::plane_at(r, k)) = lo;
       }
-    });
+    }
     if (!turn) return;
     product::wait_lds();
     __builtin_amdgcn_wave_barrier();
     const int64_t t_base = at.batch * p.t_batch;
-    product::by_columns(plane, lane, [&](int k, int r, half8 v) {
-      *(half8*)(p.t_hi + t_base + int64_t(col + k) * p.t_ld + row + r) = v;
+    product::by_columns(plane, lane, [&](int c, int r, half8 v) {
+      *(half8*)(p.t_hi + t_base + int64_t(col + c) * p.t_ld + row + r) = v;
     });
     if (p.t_lo != nullptr)
-      product::by_columns(plane + product::kStagePlane, lane, [&](int k, int r, half8 v) {
-        *(half8*)(p.t_lo + t_base + int64_t(col + k) * p.t_ld + row + r) = v;
+      product::by_columns(plane + product::kStagePlane, lane, [&](int c, int r, half8 v) {
+        *(half8*)(p.t_lo + t_base + int64_t(col + c) * p.t_ld + row + r) = v;
       });
   }
 };
@@ -140,13 +138,8 @@ struct LastOut {
     const float* rest;  // as above, of the square operand, which is the right one where `right`
     int32_t rest_ld, right;
   };
-  template <class Tile>
-  __device__ static void tile(const Params& p, const product::Args& args, const product::Place& at, f4 (&acc)[Tile::kBlocks][8],
-                              char* lds) {
-    product::by_blocks<Tile, LastOut>(p, args, at, acc, lds);
-  }
-  __device__ static void block(const Params& p, const product::Place& at, const f4 (&c)[8], int row,
-                               int col, char* stage, int lane) {
+  static constexpr auto kKind = product::kStaged;
+  __device__ static void block(const Params& p, const product::Place& at, int row, int col, char* stage, int lane) {
     const int64_t base = at.batch * p.batch;
     int64_t out = p.out_batch * at.batch, out_ld = p.out_ld;
     float step = 0.0f;
@@ -155,50 +148,53 @@ struct LastOut {
       out = e.start, out_ld = p.cols, step = e.step;
     }
     const size_t esz = p.kind == kBf16 ? 2 : 4;
-    char* first = p.kind == kStep ? (char*)p.params : (char*)p.out;
-    const bool wide = ((reinterpret_cast<uintptr_t>(first + out * esz) | (out_ld * esz)) & 15) == 0 &&
+    char* to_all = p.kind == kStep ? (char*)p.params : (char*)p.out;
+    const bool wide = ((reinterpret_cast<uintptr_t>(to_all + out * esz) | (out_ld * esz)) & 15) == 0 &&
                       (p.wire == nullptr || ((out | out_ld) & 7) == 0);
     const float* rest = p.rest != nullptr ? p.rest + int64_t(at.batch) * p.rest_ld : nullptr;
-    product::by_rows(c, stage, lane, [&](int r, int k, float(&v)[8]) {
-      const int64_t from = base + int64_t(row + r) * p.ld + col + k;
-      const half8 h = *(const half8*)(p.in_hi + from), l = *(const half8*)(p.in_lo + from);
+    const int k = product::pass_col(lane), cc = col + k, left = p.cols - cc;
+    half8 in_hi[product::kPasses], in_lo[product::kPasses];
+    float x[product::kPasses][8];
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) {
+      const int rr = row + product::pass_row(pass, lane);
+      const int64_t from = base + int64_t(rr) * p.ld + cc;
+      in_hi[pass] = *(const half8*)(p.in_hi + from), in_lo[pass] = *(const half8*)(p.in_lo + from);
+      if (p.kind != kStep || rr >= p.rows || left <= 0) continue;
+      const float* q = p.params + out + int64_t(rr) * out_ld + cc;
+      if (wide && left >= 8) load8(q, x[pass]);
+      else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[pass][i] = i < left ? q[i] : 0.0f;
+    }
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) {
+      const int rr = row + product::pass_row(pass, lane);
+      float v[8];
+      product::pass_values(stage, pass, lane, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float in = static_cast<float>(h[i]) + static_cast<float>(l[i]);
-        const float more = rest != nullptr ? rest[p.right ? col + k + i : row + r] : 0.0f;
+        const float in = static_cast<float>(in_hi[pass][i]) + static_cast<float>(in_lo[pass][i]);
+        const float more = rest != nullptr ? rest[p.right ? cc + i : rr] : 0.0f;
         v[i] = fmaf(p.beta, in, p.alpha * fmaf(more, in, v[i])) * kUnscale;
+        if (p.kind == kStep) v[i] = x[pass][i] * p.keep - step * v[i];
       }
-      const int32_t rr = row + r, cc = col + k;
-      if (rr >= p.rows || cc >= p.cols) return;
+      if (rr >= p.rows || left <= 0) continue;
       const int64_t to = out + int64_t(rr) * out_ld + cc;
-      const int32_t left = p.cols - cc;
-      if (p.kind == kStep) {
-        if (wide && left >= 8) {
-          float x[8];
-          load8(p.params + to, x);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = x[i] * p.keep - step * v[i];
-          store8(p.params + to, x);
-          if (p.wire != nullptr) store8(p.wire + to, x);
-        } else {
-          for (int i = 0; i < 8 && i < left; ++i) {
-            const float x = p.params[to + i] * p.keep - step * v[i];
-            p.params[to + i] = x;
-            if (p.wire != nullptr) p.wire[to + i] = to_bf16(x);
-          }
-        }
-      } else if (p.kind == kF32) {
-        float* o = (float*)p.out + to;
-        if (wide && left >= 8) store8(o, v);
-        else
-          for (int i = 0; i < 8 && i < left; ++i) o[i] = v[i];
+      float* o32 = p.kind == kStep ? p.params + to : p.kind == kF32 ? (float*)p.out + to : nullptr;
+      uint16_t* o16 = p.kind == kStep ? (p.wire != nullptr ? p.wire + to : nullptr) : p.kind == kBf16 ? (uint16_t*)p.out + to : nullptr;
+      if (wide && left >= 8) {
+        if (o32 != nullptr) store8(o32, v);
+        if (o16 != nullptr) store8(o16, v);
       } else {
-        uint16_t* o = (uint16_t*)p.out + to;
-        if (wide && left >= 8) store8(o, v);
-        else
-          for (int i = 0; i < 8 && i < left; ++i) o[i] = to_bf16(v[i]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (i >= left) continue;
+          if (o32 != nullptr) o32[i] = v[i];
+          if (o16 != nullptr) o16[i] = to_bf16(v[i]);
+        }
       }
-    });
+    }
   }
 };
 
@@ -229,8 +225,7 @@ struct MomentumArgs {
   float mu;
 };
 
-// gbar, m' and u of a part of a matrix, and the part's sum of u^2.  Sums in binary64: the
-// order of 64 parts and 256 threads then does not show.
+// gbar, m' and u of a part of a matrix, and the part's sum of u^2, in binary64.
 __global__ __launch_bounds__(256) void momentum_kernel(MomentumArgs a, RoundTable t) {
   __shared__ double shared[4];
   const int matrix = blockIdx.y, k = group_of(t.first, t.groups, matrix);
@@ -327,9 +322,9 @@ __global__ __launch_bounds__(256) void normalise_kernel(LayOut a) {
   const PlanesArgs& p = a.p[k];
   const int64_t t = id - a.first_tile[k], across = p.cols_p / 64, per = across * (p.rows_p / 64);
   const int64_t batch = t / per;
+  __shared__ double shared[4];
   const double* s = a.sums + (a.first_matrix[k] + batch) * host::kSumParts;
-  double sum = 0;
-  for (int i = 0; i < a.parts; ++i) sum += s[i];
+  const double sum = group_sum(static_cast<int>(threadIdx.x) < a.parts ? s[threadIdx.x] : 0.0, shared);
   const float scale = static_cast<float>(kScale / (sqrt(sum) + a.eps));
   planes_tile<T, false>(p, batch, static_cast<int>((t % per) / across), static_cast<int>(t % across), scale, lds);
 }
@@ -389,6 +384,7 @@ void operands(product::Args& p, const _Float16* a_hi, const _Float16* a_lo, cons
 hipError_t schulz_steps(const SchulzRound& r, char* ws, int32_t steps, const float* coefficients, bool full,
                         const std::vector<LastOut::Params>& last, hipStream_t stream) {
   const int32_t groups = static_cast<int32_t>(r.groups.size());
+  const product::Sums sums = {reinterpret_cast<float*>(ws + r.sums), r.sums_bytes};
   for (int32_t s = 0; s < steps; ++s) {
     const float a = coefficients[3 * s], b = coefficients[3 * s + 1], c = coefficients[3 * s + 2];
     const int from = s & 1, to = from ^ 1;
@@ -456,9 +452,9 @@ hipError_t schulz_steps(const SchulzRound& r, char* ws, int32_t steps, const flo
         gc.rows = static_cast<int32_t>(g.rows), gc.cols = static_cast<int32_t>(g.cols);
       }
     }
-    hipError_t e = product::launch_products<false>(gram, stream);
-    if (e == hipSuccess) e = product::launch_products<false>(poly, stream);
-    if (e == hipSuccess) e = end ? product::launch_products<false>(final_, stream) : product::launch_products<false>(next, stream);
+    hipError_t e = product::launch_products<false>(gram, sums, stream);
+    if (e == hipSuccess) e = product::launch_products<false>(poly, sums, stream);
+    if (e == hipSuccess) e = end ? product::launch_products<false>(final_, sums, stream) : product::launch_products<false>(next, sums, stream);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -2,8 +2,8 @@
 // into registers, its statistics are summed there (the variance from the differences to
 // the mean, not from squares), and it is written once.
 //
-// A row of up to 2048 elements is a wavefront's, of up to 8192 a workgroup's of 256 threads; a
-// team of threads keeps the weights in registers and walks over rows.  In the backward pass it
+// A row of up to 2048 elements (1024 in the backward pass, whose registers hold five rows' worth) is a
+// wavefront's, of up to 8192 a workgroup's of 256 threads; a team of threads keeps the weights in registers and walks over rows.  In the backward pass it
 // also keeps its columns' sums for dweight and dbias, which end up as one partial row a
 // workgroup; a second kernel adds those in order.  Longer rows are read again for each of
 // their passes, from L2.
@@ -18,6 +18,7 @@ namespace daso {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kForwardGroups = 1024;  // most workgroups of a forward pass
 constexpr int kPartialGroups = 512;  // most workgroups of a backward pass: two a CU
 
 struct Forward {
@@ -62,8 +63,12 @@ struct Slice {
       }
     }
   }
-  // of any alignment; `none` where there is no such vector or element
-  __device__ static void load_any(const float* p, int d, int t, float none, float (&v)[N]) {
+  // a vector of any alignment; `none` where there is no such vector
+  __device__ static void load_vector(const float* p, int d, int t, float none, float (&v)[N]) {
+    if (WIDE && p != nullptr && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+      load(p, d, t, v);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kRuns; ++i)
 #pragma unroll
@@ -88,6 +93,47 @@ struct Slice {
       }
     }
   }
+  // elements as they lie in memory: a row that is on its way takes no more registers than that
+  template <class T>
+  struct Raw {
+    static constexpr int kWords = N * sizeof(T) / 16;
+    typedef uint32_t word __attribute__((ext_vector_type(4)));
+    union {
+      word words[WIDE ? kWords : 1];
+      T elems[WIDE ? 1 : N];
+    };
+    __device__ void load(const T* row, int d, int t) {
+#pragma unroll
+      for (int i = 0; i < kRuns; ++i) {
+        const int c = column(i, t);
+        if constexpr (WIDE) {
+          constexpr int kEach = kWords / kRuns;  // 16 bytes each, of a run
+#pragma unroll
+          for (int k = 0; k < kEach; ++k) words[i * kEach + k] = c < d ? ((const word*)(row + c))[k] : word{0, 0, 0, 0};
+        } else {
+          elems[i] = c < d ? row[c] : T(0);
+        }
+      }
+    }
+    __device__ void get(float (&v)[N]) const {
+      if constexpr (!WIDE) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = load1(&elems[i]);
+      } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const uint32_t w = words[i / 4][i % 4];
+          v[i] = __builtin_bit_cast(float, w);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const uint32_t w = words[i / 8][i / 2 % 4];
+          v[i] = __builtin_bit_cast(float, i % 2 ? w & 0xffff0000u : w << 16);
+        }
+      }
+    }
+  };
   __device__ static bool inside(int e, int d, int t) { return column(e / kRun, t) + e % kRun < d; }
 };
 
@@ -103,13 +149,18 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(Forward a) {
   __shared__ float shared[kThreads / 64];
   const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   constexpr int kTeams = kThreads / TEAM;
+  const int64_t step = int64_t(gridDim.x) * kTeams;
+  int64_t r = blockIdx.x * int64_t(kTeams) + team;
   float w[N], b[N];
-  S::load_any(a.weight, a.d, t, 1.0f, w);
-  S::load_any(a.bias, a.d, t, 0.0f, b);
+  typename S::template Raw<T> next;
+  if (r < a.rows) next.load((const T*)a.x + r * a.x_stride, a.d, t);
+  S::load_vector(a.weight, a.d, t, 1.0f, w);
+  S::load_vector(a.bias, a.d, t, 0.0f, b);
   const float df = static_cast<float>(a.d);
-  for (int64_t r = blockIdx.x * int64_t(kTeams) + team; r < a.rows; r += int64_t(gridDim.x) * kTeams) {
+  for (; r < a.rows; r += step) {
     float v[N], sum = 0.0f, square = 0.0f;
-    S::load((const T*)a.x + r * a.x_stride, a.d, t, v);
+    next.get(v);
+    if (r + step < a.rows) next.load((const T*)a.x + (r + step) * a.x_stride, a.d, t);
 #pragma unroll
     for (int i = 0; i < N; ++i) sum += v[i];
     const float mean = team_sum<TEAM>(sum, shared) / df;
@@ -162,15 +213,25 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(Backward a) {
   __shared__ float meet[kTeams > 1 ? kTeams : 1][TEAM * S::kRun];
   const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   float w[N], dw[N], db[N];
-  S::load_any(a.weight, a.d, t, 1.0f, w);
+  S::load_vector(a.weight, a.d, t, 1.0f, w);
 #pragma unroll
   for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.0f;
   const float inv = 1.0f / static_cast<float>(a.d);
-  for (int64_t r = blockIdx.x * int64_t(kTeams) + team; r < a.rows; r += int64_t(gridDim.x) * kTeams) {
+  const int64_t step = int64_t(gridDim.x) * kTeams;
+  int64_t r = blockIdx.x * int64_t(kTeams) + team;
+  typename S::template Raw<T> next_x, next_g;
+  float next_mean = 0.0f, next_rstd = 0.0f;
+  const auto fetch = [&](int64_t row) {
+    next_x.load((const T*)a.x + row * a.x_stride, a.d, t);
+    next_g.load((const T*)a.dy + row * a.dy_stride, a.d, t);
+    next_mean = a.mean[row], next_rstd = a.rstd[row];
+  };
+  if (r < a.rows) fetch(r);
+  for (; r < a.rows; r += step) {
     float x[N], g[N], s1 = 0.0f, s2 = 0.0f;
-    S::load((const T*)a.x + r * a.x_stride, a.d, t, x);
-    S::load((const T*)a.dy + r * a.dy_stride, a.d, t, g);
-    const float mean = a.mean[r], rstd = a.rstd[r];
+    next_x.get(x), next_g.get(g);
+    const float mean = next_mean, rstd = next_rstd;
+    if (r + step < a.rows) fetch(r + step);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       x[i] = S::inside(i, a.d, t) ? (x[i] - mean) * rstd : 0.0f;
@@ -251,24 +312,28 @@ __global__ __launch_bounds__(kThreads) void columns_long_kernel(Backward a, int3
   a.partial[int64_t(share) * 2 * a.d + a.d + c] = db;
 }
 
-// dweight and dbias from the partial rows, in order: 64 columns a workgroup, 16 shares of
-// the rows.
-__global__ __launch_bounds__(1024) void partials_kernel(const float* partial, int32_t count, int32_t d, float* dweight,
-                                                        float* dbias) {
-  __shared__ float shared[16][64];
-  const int in = threadIdx.x & 63, share = threadIdx.x >> 6;
-  const int64_t c = blockIdx.x * 64 + in, width = 2 * int64_t(d);
-  float v = 0.0f;
+// dweight and dbias from the partial rows, in order: 16 columns a workgroup, 16 shares of
+// the rows with eight loads in flight each.
+__global__ __launch_bounds__(256) void partials_kernel(const float* partial, int32_t count, int32_t d, float* dweight,
+                                                       float* dbias) {
+  __shared__ float shared[16][16];
+  const int in = threadIdx.x & 15, share = threadIdx.x >> 4;
+  const int64_t c = blockIdx.x * 16 + in, width = 2 * int64_t(d);
+  float v[8] = {};
   if (c < width)
-    for (int32_t k = share; k < count; k += 16) v += partial[k * width + c];
-  shared[share][in] = v;
+    for (int32_t k = share; k < count; k += 128)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (k + 16 * i < count) v[i] += partial[(k + 16 * i) * width + c];
+  shared[share][in] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   __syncthreads();
   if (share != 0 || c >= width) return;
-  for (int k = 1; k < 16; ++k) v += shared[k][in];
+  float sum = shared[0][in];
+  for (int k = 1; k < 16; ++k) sum += shared[k][in];
   if (c < d) {
-    if (dweight != nullptr) dweight[c] = v;
+    if (dweight != nullptr) dweight[c] = sum;
   } else if (dbias != nullptr) {
-    dbias[c - d] = v;
+    dbias[c - d] = sum;
   }
 }
 
@@ -277,18 +342,18 @@ bool aligned16(const void* p, int64_t stride, size_t esz) {
   return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(stride * static_cast<int64_t>(esz))) & 15) == 0;
 }
 
-int team_of(int64_t d) { return d <= 2048 ? 64 : kThreads; }
+constexpr int64_t kWaveForward = 2048, kWaveBackward = 1024;  // longest rows of a wavefront
 bool is_long(int64_t d) { return d > 8192; }
 
 // Workgroups of a pass whose teams walk over rows.
-int64_t groups_of(int64_t rows, int64_t d, int64_t most) {
-  const int64_t teams = kThreads / team_of(d);
+int64_t groups_of(int64_t rows, int64_t d, int64_t wave_d, int64_t most) {
+  const int64_t teams = d <= wave_d ? kThreads / 64 : 1;
   return std::min((rows + teams - 1) / teams, most);
 }
 
 template <class T, bool WIDE>
 hipError_t forward(const Forward& a, hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(groups_of(a.rows, a.d, 2048))), block(kThreads);
+  const dim3 grid(static_cast<uint32_t>(groups_of(a.rows, a.d, kWaveForward, kForwardGroups))), block(kThreads);
   if (a.d <= 512) return launch(&forward_kernel<T, 64, 8, WIDE>, grid, block, stream, a);
   if (a.d <= 1024) return launch(&forward_kernel<T, 64, 16, WIDE>, grid, block, stream, a);
   if (a.d <= 2048) return launch(&forward_kernel<T, 64, 32, WIDE>, grid, block, stream, a);
@@ -302,7 +367,7 @@ hipError_t backward(const Backward& a, int32_t groups, hipStream_t stream) {
   const dim3 grid(static_cast<uint32_t>(groups)), block(kThreads);
   if (a.d <= 512) return launch(&backward_kernel<T, 64, 8, WIDE>, grid, block, stream, a);
   if (a.d <= 1024) return launch(&backward_kernel<T, 64, 16, WIDE>, grid, block, stream, a);
-  if (a.d <= 2048) return launch(&backward_kernel<T, 64, 32, WIDE>, grid, block, stream, a);
+  if (a.d <= 2048) return launch(&backward_kernel<T, 256, 8, WIDE>, grid, block, stream, a);
   if (a.d <= 4096) return launch(&backward_kernel<T, 256, 16, WIDE>, grid, block, stream, a);
   if (a.d <= 8192) return launch(&backward_kernel<T, 256, 32, WIDE>, grid, block, stream, a);
   hipError_t e = hipSuccess;
@@ -316,7 +381,7 @@ hipError_t backward(const Backward& a, int32_t groups, hipStream_t stream) {
 
 // Partial rows of a backward pass.
 int32_t partial_rows(int64_t rows, int64_t d) {
-  return static_cast<int32_t>(is_long(d) ? std::min<int64_t>(rows, 64) : groups_of(rows, d, kPartialGroups));
+  return static_cast<int32_t>(is_long(d) ? std::min<int64_t>(rows, 64) : groups_of(rows, d, kWaveBackward, kPartialGroups));
 }
 
 size_t backward_bytes(const daso_layer_norm_backward_args& s) {
@@ -375,7 +440,7 @@ int daso_layer_norm_backward(const daso_layer_norm_backward_args* args, hipStrea
       err = wide ? daso::backward<float, true>(a, groups, stream) : daso::backward<float, false>(a, groups, stream);
   }
   if (err == hipSuccess && sums)
-    err = daso::launch(&daso::partials_kernel, dim3(static_cast<uint32_t>((2 * s.d + 63) / 64)), dim3(1024), stream, (const float*)partial,
+    err = daso::launch(&daso::partials_kernel, dim3(static_cast<uint32_t>((2 * s.d + 15) / 16)), dim3(256), stream, (const float*)partial,
                        groups, d, s.dweight, s.dbias);
   return err == hipSuccess ? DASO_OK : DASO_EHIP;
 }

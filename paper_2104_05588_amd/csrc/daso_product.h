@@ -12,6 +12,8 @@
 
 #include <atomic>
 
+#include "daso_train_host.h"
+
 namespace daso {
 namespace product {
 
@@ -65,6 +67,14 @@ __device__ inline f4 mfma(half8 a, half8 b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
+// The thread's number, opaque to the compiler: what follows from it is worked out where it is
+// used, and not kept in registers over the products (where it would not fit).
+__device__ inline int thread_here() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
 template <int N>
 __device__ inline void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -83,26 +93,23 @@ struct Place {
 
 // The tile `id` of a product.  Tiles are counted in bands of four tile rows, so that the
 // rows and columns that neighbouring tiles read stay in an L2.
-__device__ inline Place place_of(const Args& p, int64_t id) {
+__device__ inline Place place_of(const Args& p, int id) {
   Place at;
+  const uint32_t per = static_cast<uint32_t>(p.tri ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n);
+  at.batch = static_cast<int>(static_cast<uint32_t>(id) / per);
+  const int t = id - at.batch * static_cast<int>(per);
   if (p.tri) {
-    const int per = p.tiles_m * (p.tiles_m + 1) / 2;
-    at.batch = static_cast<int>(id / per);
-    const int t = static_cast<int>(id - int64_t(at.batch) * per);
     int i = static_cast<int>((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
     while (i * (i + 1) / 2 > t) --i;
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
-    at.tm = i;
-    at.tn = t - i * (i + 1) / 2;
+    at.tm = __builtin_amdgcn_readfirstlane(i);
+    at.tn = t - at.tm * (at.tm + 1) / 2;
   } else {
-    const int per = p.tiles_m * p.tiles_n;
-    at.batch = static_cast<int>(id / per);
-    const int t = static_cast<int>(id - int64_t(at.batch) * per);
     constexpr int kBand = 4;
-    const int band = t / (kBand * p.tiles_n), first = band * kBand;
-    const int rows = min(p.tiles_m - first, kBand), in = t - first * p.tiles_n;
-    at.tm = first + in % rows;
-    at.tn = in / rows;
+    const int band = static_cast<int>(static_cast<uint32_t>(t) / static_cast<uint32_t>(kBand * p.tiles_n)), first = band * kBand;
+    const uint32_t rows = static_cast<uint32_t>(min(p.tiles_m - first, kBand)), in = static_cast<uint32_t>(t - first * p.tiles_n);
+    at.tm = first + static_cast<int>(in % rows);
+    at.tn = static_cast<int>(in / rows);
   }
   return at;
 }
@@ -148,14 +155,14 @@ struct Tile256 {
   }
 
   template <bool BF16>
-  __device__ static void run(const Args& p, const Place& at, char* lds, f4 (&acc)[kBlocks][8]) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __device__ static void run(const Args& p, const Place& at, int from, int to, char* lds, f4 (&acc)[kBlocks][8]) {
+    const int lane = thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t skip_a = (at.batch * p.batch_a + int64_t(at.tm) * kRows * p.lda) * 2;
     const int64_t skip_b = (at.batch * p.batch_b + int64_t(at.tn) * kCols * p.ldb) * 2;
     const char *a0 = (const char*)p.a[0] + skip_a, *a1 = (const char*)p.a[1] + skip_a, *a2 = (const char*)p.a[2] + skip_a;
     const char *b0 = (const char*)p.b[0] + skip_b, *b1 = (const char*)p.b[1] + skip_b, *b2 = (const char*)p.b[2] + skip_b;
     const int last_a = min(kRows, p.M - at.tm * kRows) - 1, last_b = min(kCols, p.N - at.tn * kCols) - 1;
-    const int steps = p.steps, total = p.steps * p.segments;
+    const int steps = p.steps;
     uint32_t from_a[2][2], from_b[2][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -166,18 +173,18 @@ struct Tile256 {
         from_b[h][j] = static_cast<uint32_t>(min(h * 128 + r, last_b)) * (static_cast<uint32_t>(p.ldb) * 2) + c;
       }
     auto load_a = [&](int t, int h) {
-      char* to = lds + (t & 1) * 65536 + h * 16384 + wave * 2048;
+      char* dst = lds + (t & 1) * 65536 + h * 16384 + wave * 2048;
       const char* g = step_of(a0, a1, a2, t, steps);
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(g + from_a[h][j]), DASO_LDS(to + j * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(g + from_a[h][j]), DASO_LDS(dst + j * 1024), 16, 0, 0);
     };
     auto load_b = [&](int t, int h) {
-      char* to = lds + (t & 1) * 65536 + 32768 + h * 16384 + wave * 2048;
+      char* dst = lds + (t & 1) * 65536 + 32768 + h * 16384 + wave * 2048;
       const char* g = step_of(b0, b1, b2, t, steps);
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(g + from_b[h][j]), DASO_LDS(to + j * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(g + from_b[h][j]), DASO_LDS(dst + j * 1024), 16, 0, 0);
     };
 #pragma unroll
     for (int i = 0; i < kBlocks; ++i)
@@ -221,11 +228,12 @@ struct Tile256 {
       __builtin_amdgcn_s_setprio(0);
       meet();
     };
-    load_b(0, 0), load_a(0, 0), load_b(0, 1), load_a(0, 1), load_b(1, 0), load_a(1, 0), load_b(1, 1);
+    load_b(from, 0), load_a(from, 0), load_b(from, 1), load_a(from, 1);
+    load_b(from + 1, 0), load_a(from + 1, 0), load_b(from + 1, 1);
     wait_loads<10>();
     meet();
     if (wm == 1) meet();
-    read_b(0, 0, bnext);
+    read_b(from, 0, bnext);
     // kLeft: steps after this one, 2 for two or more.  Each wait leaves in flight what was
     // issued after the piece that the next phase reads.
     auto step = [&](int k, auto left) {
@@ -253,8 +261,8 @@ struct Tile256 {
       meet();
       compute(acc[2], bl);
     };
-    int k = 0;
-    for (; k + 2 < total; ++k) step(k, Left<2>());
+    int k = from;
+    for (; k + 2 < to; ++k) step(k, Left<2>());
     step(k, Left<1>());
     step(k + 1, Left<0>());
     if (wm == 0) meet();
@@ -281,14 +289,14 @@ struct Tile128 {
   }
 
   template <bool BF16>
-  __device__ static void run(const Args& p, const Place& at, char* lds, f4 (&acc)[kBlocks][8]) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __device__ static void run(const Args& p, const Place& at, int from, int to, char* lds, f4 (&acc)[kBlocks][8]) {
+    const int lane = thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t skip_a = (at.batch * p.batch_a + int64_t(at.tm) * kRows * p.lda) * 2;
     const int64_t skip_b = (at.batch * p.batch_b + int64_t(at.tn) * kCols * p.ldb) * 2;
     const char *a0 = (const char*)p.a[0] + skip_a, *a1 = (const char*)p.a[1] + skip_a, *a2 = (const char*)p.a[2] + skip_a;
     const char *b0 = (const char*)p.b[0] + skip_b, *b1 = (const char*)p.b[1] + skip_b, *b2 = (const char*)p.b[2] + skip_b;
     const int last_a = min(kRows, p.M - at.tm * kRows) - 1, last_b = min(kCols, p.N - at.tn * kCols) - 1;
-    const int steps = p.steps, total = p.steps * p.segments;
+    const int steps = p.steps;
     uint32_t from_a[4], from_b[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -297,14 +305,14 @@ struct Tile128 {
       from_b[j] = static_cast<uint32_t>(min(r, last_b)) * (static_cast<uint32_t>(p.ldb) * 2) + c;
     }
     auto load = [&](int t) {
-      char* to = lds + (t & 1) * 32768 + wave * 4096;
+      char* dst = lds + (t & 1) * 32768 + wave * 4096;
       const char *ga = step_of(a0, a1, a2, t, steps), *gb = step_of(b0, b1, b2, t, steps);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(ga + from_a[j]), DASO_LDS(to + j * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(ga + from_a[j]), DASO_LDS(dst + j * 1024), 16, 0, 0);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(gb + from_b[j]), DASO_LDS(to + 16384 + j * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(DASO_GLOBAL(gb + from_b[j]), DASO_LDS(dst + 16384 + j * 1024), 16, 0, 0);
     };
 #pragma unroll
     for (int i = 0; i < kBlocks; ++i)
@@ -327,11 +335,11 @@ struct Tile128 {
         for (int j = 0; j < 4; ++j)
           acc[j >> 1][i * 2 + (j & 1)] = mfma<BF16>(b[kk][j], a[kk][i], acc[j >> 1][i * 2 + (j & 1)]);
     };
-    load(0), load(1);
+    load(from), load(from + 1);
     wait_loads<8>();
     meet();
-    read(0, 0);
-    for (int k = 0; k < total; ++k) {
+    read(from, 0);
+    for (int k = from; k < to; ++k) {
       read(k, 1);
       __builtin_amdgcn_sched_barrier(0);
       compute(0);
@@ -339,8 +347,8 @@ struct Tile128 {
       wait_loads<0>();
       wait_lds();
       meet();
-      if (k + 2 < total) load(k + 2);
-      if (k + 1 < total) read(k + 1, 0);
+      if (k + 2 < to) load(k + 2);
+      if (k + 1 < to) read(k + 1, 0);
       __builtin_amdgcn_sched_barrier(0);
       compute(1);
       __builtin_amdgcn_sched_barrier(0);
@@ -350,10 +358,8 @@ struct Tile128 {
 
 // ------------------------------------------------------------------------- epilogues
 // A block in `stage` (the wavefront's own 8 KB of LDS): rows of 32 floats, 16-byte pieces
-// permuted as above.  Calls f(row, col, v) with eight neighbouring columns of a row, four
-// lanes a row, rows 16 at a time.
-template <class F>
-__device__ inline void by_rows(const f4 (&c)[8], char* stage, int lane, F f) {
+// permuted as above.
+__device__ inline void stage_block(const f4 (&c)[8], char* stage, int lane) {
   const int r16 = lane & 15, kq = lane >> 4;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -362,16 +368,19 @@ __device__ inline void by_rows(const f4 (&c)[8], char* stage, int lane, F f) {
       const int row = i * 16 + r16;
       *(f4*)(stage + row * 128 + (((j * 4 + kq) ^ ((row >> 1) & 7)) * 16)) = c[i * 2 + j];
     }
-  wait_lds();
-  __builtin_amdgcn_wave_barrier();
+}
+
+// A staged block by rows, in four passes of 16 rows and four lanes a row: the row and the first of
+// the eight neighbouring columns that a lane has in a pass, and their values.
+constexpr int kPasses = 4;
+__device__ inline int pass_row(int pass, int lane) { return pass * 16 + (lane >> 2); }
+__device__ inline int pass_col(int lane) { return (lane & 3) * 8; }
+__device__ inline void pass_values(const char* stage, int pass, int lane, float (&v)[8]) {
+  const int row = pass_row(pass, lane), piece = (lane & 3) * 2, s = (row >> 1) & 7;
+  const f4 lo = *(const f4*)(stage + row * 128 + ((piece ^ s) * 16));
+  const f4 hi = *(const f4*)(stage + row * 128 + (((piece + 1) ^ s) * 16));
 #pragma unroll
-  for (int pass = 0; pass < 4; ++pass) {
-    const int row = pass * 16 + (lane >> 2), piece = (lane & 3) * 2, s = (row >> 1) & 7;
-    const f4 lo = *(const f4*)(stage + row * 128 + ((piece ^ s) * 16));
-    const f4 hi = *(const f4*)(stage + row * 128 + (((piece + 1) ^ s) * 16));
-    float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    f(row, piece * 4, v);
-  }
+  for (int i = 0; i < 4; ++i) v[i] = lo[i], v[4 + i] = hi[i];
 }
 
 // Where a staged plane of 16-bit values (64 x 32) keeps (row, col): rows of 64 bytes, with 16
@@ -401,64 +410,284 @@ __device__ inline void split(float v, _Float16* hi, _Float16* lo) {
   *lo = static_cast<_Float16>(__builtin_fabsf(rest) < __builtin_inff() ? rest : 0.0f);
 }
 
-// Hands the tile's blocks to E::block(params, place, c, row, col, stage, lane), each at (row, col)
-// of C, those that begin inside the result's extent.
-template <class Tile, class E>
-__device__ inline void by_blocks(const typename E::Params& out, const Args& p, const Place& at, f4 (&acc)[Tile::kBlocks][8],
-                                 char* lds) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  char* stage = lds + wave * kWaveStage;
-#pragma unroll
-  for (int b = 0; b < Tile::kBlocks; ++b) {
-    int row, col;
-    Tile::block_at(wave, b, &row, &col);
-    row += at.tm * Tile::kRows;
-    col += at.tn * Tile::kCols;
-    if (row < p.M && col < p.N) E::block(out, at, acc[b], row, col, stage, lane);
-  }
-}
+// The products of one launch.  An epilogue E has a plain struct E::Params and one of
+//   kStaged: block(params, place, row, col, stage, lane), by a wavefront: the staged 64 x 32 block at
+//            (row, col) of C, of those that begin inside the result
+//   kBlocks: block(params, place, c, row, col, stage, lane): the same with the block in registers, of all
+//            blocks of a tile
+//   kWhole:  tile<Tile>(params, args, place, acc, lds), by the whole workgroup; its tiles are never cut
+//
+// A launch has up to as many workgroups as fit the chip (kPlaces); an XCD's, to which they go in
+// turn, get a run of whole tiles, with about an eighth of all steps.  Of each product an XCD's
+// workgroups take tiles side by side, in rounds, so that what they read at a time is shared
+// in their L2.  What no whole round is left for is the XCD's pool.  Its tiles are dealt out, or,
+// where that would leave much of the XCD idle, each is cut along the contraction into parts of
+// about one length, and the parts are dealt out, first parts first, so that here too workgroups
+// side by side read the same steps.  The sums of parts are left in memory, and a second kernel adds
+// them, in order, and has the epilogue.  The cut, and so the order of sums, is fixed by
+// the sizes.
+enum EpilogueKind { kStaged, kBlocks, kWhole };
 
-// The products of one launch, told apart by their tiles.  An epilogue E has a plain struct
-// E::Params and tile<Tile>(params, args, place, acc, lds), by the whole workgroup.
+struct Run {
+  int32_t tile;    // the first of the XCD's tiles of a product
+  int32_t rounds;  // whole rounds of them
+  int32_t rest;    // tiles after those, in the pool
+  int32_t parts;   // that each of the pool's is cut into
+};
+
 template <class E>
 struct Launch {
   int32_t count;
-  int64_t first[kMaxProblems + 1];  // the first tile of each product; the last entry: of none
+  int32_t across;                   // workgroups an XCD
+  Run runs[8][kMaxProblems];
   Args args[kMaxProblems];
   typename E::Params out[kMaxProblems];
+  int32_t slot[8];                  // the first of an XCD's places for sums
+  float* sums;                      // a tile for each part of a pool that has cut tiles
 };
+
+// The call's memory for sums: a launch that would need more of it cuts nothing.
+struct Sums {
+  float* to;
+  size_t bytes;
+};
+
+// What cutting costs, in steps of a tile: the second kernel takes 10 to 30 us.
+constexpr int kPartCost256 = 16, kPartCost128 = 24;
+using host::kLeastPart;
+using host::kPoolParts;
+// Steps that are worth a workgroup of their own.
+constexpr int kLeastShare = 8;
+
+constexpr int kPlaces256 = host::kPlaces256, kPlaces128 = 2 * kPlaces256;
+
+inline __host__ __device__ int32_t steps_of(const Args& p) { return p.steps * p.segments; }
+
+template <class Tile, class E>
+__device__ inline void finish(const typename E::Params& out, const Args& p, const Place& at, f4 (&acc)[Tile::kBlocks][8], char* lds) {
+  if constexpr (E::kKind == kWhole) {
+    E::template tile<Tile>(out, p, at, acc, lds);
+  } else {
+    const int lane = thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char* stage = lds + wave * kWaveStage;
+    if constexpr (E::kKind == kStaged) {
+      // the blocks' own code is there once, and not once a block: unrolled, it would not fit the
+      // instruction cache
+#pragma unroll 1
+      for (int b = 0; b < Tile::kBlocks; ++b) {
+        int row, col;
+        Tile::block_at(wave, b, &row, &col);
+        row += at.tm * Tile::kRows, col += at.tn * Tile::kCols;
+        if (row >= p.M || col >= p.N) continue;
+#pragma unroll
+        for (int k = 0; k < Tile::kBlocks; ++k)
+          if (b == k) stage_block(acc[k], stage, lane);
+        wait_lds();
+        __builtin_amdgcn_wave_barrier();
+        E::block(out, at, row, col, stage, lane);
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < Tile::kBlocks; ++b) {
+        int row, col;
+        Tile::block_at(wave, b, &row, &col);
+        E::block(out, at, acc[b], row + at.tm * Tile::kRows, col + at.tn * Tile::kCols, stage, lane);
+      }
+    }
+  }
+}
 
 template <class Tile, bool BF16, class E>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kOccupancy) void product_kernel(Launch<E> all) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  int64_t id = blockIdx.x + int64_t(blockIdx.y) * gridDim.x;
-  const int64_t total = all.first[all.count];
-  if (id >= total) return;
-  // workgroups go to the 8 XCDs in turn: each XCD is given a run of consecutive tiles
-  const int64_t q = total / 8, r = total % 8, x = id % 8, y = id / 8;
-  id = x * q + (x < r ? x : r) + y;
-  int k = 0;
-  while (k + 1 < all.count && id >= all.first[k + 1]) ++k;
-  const Args& p = all.args[k];
-  const Place at = place_of(p, id - all.first[k]);
+  const int xcd = blockIdx.x & 7, across = all.across;
   f4 acc[Tile::kBlocks][8];
-  Tile::template run<BF16>(p, at, lds, acc);
-  E::template tile<Tile>(all.out[k], p, at, acc, lds);
+  // first the pool's parts, of which `part` is this workgroup's next (of all of them, and counted
+  // from `problem`'s first), then whole rounds
+  int problem = 0, place = blockIdx.x >> 3, part = place, round = -1;
+  for (;;) {
+    int tile, piece = 0, pieces = 1, slot = 0;
+    if (round < 0) {
+      for (; problem < all.count; ++problem) {
+        const Run& run = all.runs[xcd][problem];
+        if (part < run.rest * run.parts) break;
+        part -= run.rest * run.parts;
+      }
+      if (problem < all.count) {
+        const Run& run = all.runs[xcd][problem];
+        piece = static_cast<int>(static_cast<uint32_t>(part) / static_cast<uint32_t>(run.rest));
+        pieces = run.parts;
+        tile = run.tile + run.rounds * across + part - piece * run.rest;
+        slot = place;
+        part += across, place += across;
+      } else {
+        problem = round = 0;
+      }
+    }
+    if (round >= 0) {
+      for (; problem < all.count && round >= all.runs[xcd][problem].rounds; ++problem) round = 0;
+      if (problem >= all.count) break;
+      tile = all.runs[xcd][problem].tile + round * across + static_cast<int>(blockIdx.x >> 3);
+      ++round;
+    }
+    const Args& p = all.args[problem];
+    const int steps = steps_of(p), from = steps * piece / pieces, to = steps * (piece + 1) / pieces;
+    const Place at = place_of(p, tile);
+    Tile::template run<BF16>(p, at, from, to, lds, acc);
+    if (E::kKind != kWhole && pieces > 1) {
+      f4* left = (f4*)(all.sums + int64_t(all.slot[xcd] + slot) * (Tile::kRows * Tile::kCols)) + thread_here();
+#pragma unroll
+      for (int b = 0; b < Tile::kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) left[(b * 8 + i) * Tile::kThreads] = acc[b][i];
+    } else {
+      finish<Tile, E>(all.out[problem], p, at, acc, lds);
+    }
+    __syncthreads();  // LDS is free again
+  }
 }
 
-template <class Tile, bool BF16, class E>
-hipError_t launch_tiles(Launch<E>& all, hipStream_t stream) {
-  all.first[0] = 0;
+// What is left of tiles that were cut: workgroups (x, y) take blocks of the pools' tiles.
+constexpr int kJoinWaves = 4;
+
+template <class Tile, class E>
+__global__ __launch_bounds__(64 * kJoinWaves) void product_join_kernel(Launch<E> all) {
+  __shared__ __attribute__((aligned(1024))) char lds[kJoinWaves * kWaveStage];
+  // the tile, counted over the cut ones of the XCDs' pools, and the place of its first part's sums
+  int t = blockIdx.x, xcd = 0, problem = 0, slot = 0;
+  for (;; ++xcd, problem = 0) {
+    if (xcd == 8) return;
+    for (slot = 0; problem < all.count; ++problem) {
+      const Run& run = all.runs[xcd][problem];
+      if (run.parts > 1) {
+        if (t < run.rest) break;
+        t -= run.rest;
+      }
+      slot += run.rest * run.parts;
+    }
+    if (problem < all.count) break;
+  }
+  const Run& run = all.runs[xcd][problem];
+  const Args& p = all.args[problem];
+  const Place at = place_of(p, run.tile + run.rounds * all.across + t);
+  const int lane = threadIdx.x & 63, block = blockIdx.y * kJoinWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = block / Tile::kBlocks, b = block % Tile::kBlocks;
+  constexpr int64_t kTile = int64_t(Tile::kRows) * Tile::kCols / 4;  // in vectors
+  const f4* from = (const f4*)all.sums + int64_t(all.slot[xcd] + slot + t) * kTile + b * 8 * Tile::kThreads + wave * 64 + lane;
+  f4 c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = from[i * Tile::kThreads];
+  for (int k = 1; k < run.parts; ++k) {
+    from += run.rest * kTile;
+    f4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = from[i * Tile::kThreads];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] += v[i];
+  }
+  int row, col;
+  Tile::block_at(wave, b, &row, &col);
+  row += at.tm * Tile::kRows, col += at.tn * Tile::kCols;
+  char* stage = lds + (threadIdx.x >> 6) * kWaveStage;
+  if constexpr (E::kKind == kStaged) {
+    if (row >= p.M || col >= p.N) return;
+    stage_block(c, stage, lane);
+    wait_lds();
+    __builtin_amdgcn_wave_barrier();
+    E::block(all.out[problem], at, row, col, stage, lane);
+  } else {
+    E::block(all.out[problem], at, c, row, col, stage, lane);
+  }
+}
+
+// The steps that the busiest of `across` workgroups has of an XCD's pool, cut so that the longest
+// tile has `pieces` parts and the others parts of about its parts' length; 0: there is no room for the
+// parts.
+inline int64_t pool_steps(Run* runs, const Args* args, int32_t count, int32_t across, int32_t pieces) {
+  int64_t longest = 0, parts = 0, load[kPlaces128 / 8] = {}, most = 0;
+  for (int32_t k = 0; k < count; ++k)
+    if (runs[k].rest > 0 && steps_of(args[k]) > longest) longest = steps_of(args[k]);
+  for (int32_t k = 0; k < count; ++k) {
+    if (runs[k].rest == 0) continue;
+    const int64_t steps = steps_of(args[k]);
+    int64_t s = pieces > 1 ? (steps * pieces + longest / 2) / longest : 1;
+    if (s > steps / kLeastPart) s = steps / kLeastPart;
+    runs[k].parts = static_cast<int32_t>(s < 1 ? 1 : s);
+    for (int64_t i = 0; i < runs[k].rest * int64_t(runs[k].parts); ++i)
+      load[(parts + i) % across] += (steps + runs[k].parts - 1) / runs[k].parts;
+    parts += runs[k].rest * int64_t(runs[k].parts);
+  }
+  if (pieces > 1 && parts > int64_t(kPoolParts) * across) return 0;
+  for (int32_t i = 0; i < across; ++i) most = load[i] > most ? load[i] : most;
+  return most;
+}
+
+// Deals the launch's tiles to XCDs and plans their pools.  Returns the workgroups; *cut counts the
+// tiles that are cut.
+template <class Tile, class E>
+int deal(Launch<E>& all, const Sums& sums, int* cut) {
+  constexpr int kPlaces = Tile::kRows == 256 ? kPlaces256 : kPlaces128;
+  constexpr int kCost = Tile::kRows == 256 ? kPartCost256 : kPartCost128;
+  int64_t first[kMaxProblems + 1] = {}, units = 0;
   for (int32_t k = 0; k < all.count; ++k) {
     Args& p = all.args[k];
     p.tiles_m = (p.M + Tile::kRows - 1) / Tile::kRows;
     p.tiles_n = (p.N + Tile::kCols - 1) / Tile::kCols;
-    all.first[k + 1] = all.first[k] + tile_count(p);
+    first[k + 1] = first[k] + tile_count(p);
+    if (tile_count(p) > INT32_MAX / 2) return -1;
+    units += tile_count(p) * steps_of(p);
   }
-  const int64_t total = all.first[all.count];
-  if (total == 0) return hipSuccess;
-  constexpr int64_t kRow = int64_t(1) << 20;  // a multiple of 8; work-items of a row stay in 32 bits
-  const dim3 grid(static_cast<uint32_t>(total < kRow ? total : kRow), static_cast<uint32_t>((total + kRow - 1) / kRow));
+  *cut = 0;
+  if (first[all.count] == 0) return 0;
+  int64_t worth = (units / kLeastShare + 7) / 8;
+  if (E::kKind == kWhole) worth = (first[all.count] + 7) / 8;
+  all.across = static_cast<int32_t>(worth < 1 ? 1 : worth < kPlaces / 8 ? worth : kPlaces / 8);
+  int64_t tile = 0;  // of all products, the first that is not dealt yet
+  int64_t dealt = 0;
+  int32_t problem = 0, slots = 0;
+  for (int x = 0; x < 8; ++x) {
+    // tiles until the XCD's part of the steps is reached
+    const int64_t until = units * (x + 1) / 8;
+    for (int32_t k = 0; k < all.count; ++k) all.runs[x][k] = Run{0, 0, 0, 1};
+    while (tile < first[all.count] && (dealt < until || x == 7)) {
+      while (tile >= first[problem + 1]) ++problem;
+      const int64_t steps = steps_of(all.args[problem]), left = first[problem + 1] - tile;
+      int64_t take = x == 7 ? left : (until - dealt + steps / 2) / steps;
+      if (take > left) take = left;
+      if (take == 0) break;
+      Run& r = all.runs[x][problem];
+      r.tile = static_cast<int32_t>(tile - first[problem]);
+      r.rounds = static_cast<int32_t>(take / all.across);
+      r.rest = static_cast<int32_t>(take % all.across);
+      tile += take;
+      dealt += take * steps;
+    }
+    int32_t best = 1;
+    int64_t least = pool_steps(all.runs[x], all.args, all.count, all.across, 1);
+    if (E::kKind != kWhole)
+      for (int32_t s = 2; s <= 16; ++s) {
+        const int64_t n = pool_steps(all.runs[x], all.args, all.count, all.across, s);
+        if (n > 0 && n + kCost < least) best = s, least = n + kCost;
+      }
+    pool_steps(all.runs[x], all.args, all.count, all.across, best);
+    all.slot[x] = slots;
+    if (best == 1) continue;
+    for (int32_t k = 0; k < all.count; ++k) slots += all.runs[x][k].rest * all.runs[x][k].parts;
+  }
+  if (size_t(slots) * Tile::kRows * Tile::kCols * sizeof(float) > sums.bytes)
+    for (int x = 0; x < 8; ++x) pool_steps(all.runs[x], all.args, all.count, all.across, 1);
+  all.sums = sums.to;
+  for (int x = 0; x < 8; ++x)
+    for (int32_t k = 0; k < all.count; ++k) *cut += all.runs[x][k].parts > 1 ? all.runs[x][k].rest : 0;
+  return all.across * 8;
+}
+
+template <class Tile, bool BF16, class E>
+hipError_t launch_tiles(Launch<E>& all, const Sums& sums, hipStream_t stream) {
+  int cut = 0;
+  const int groups = deal<Tile>(all, sums, &cut);
+  if (groups == 0) return hipSuccess;
+  if (groups < 0) return hipErrorInvalidValue;
   auto* kernel = product_kernel<Tile, BF16, E>;
   // once a device, before the first launch there
   static std::atomic<uint64_t> allowed{0};
@@ -472,28 +701,36 @@ hipError_t launch_tiles(Launch<E>& all, hipStream_t stream) {
     allowed.fetch_or(bit, std::memory_order_relaxed);
   }
   void* list[] = {&all};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(Tile::kThreads), list, Tile::kLds, stream);
+  e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(static_cast<uint32_t>(groups)), dim3(Tile::kThreads), list,
+                      Tile::kLds, stream);
+  if constexpr (E::kKind != kWhole) {
+    constexpr uint32_t kBlocksOfTile = Tile::kRows * Tile::kCols / (kBlockRows * kBlockCols);
+    if (e == hipSuccess && cut > 0)
+      e = hipLaunchKernel(reinterpret_cast<const void*>(&product_join_kernel<Tile, E>),
+                          dim3(static_cast<uint32_t>(cut), kBlocksOfTile / kJoinWaves), dim3(64 * kJoinWaves), list, 0, stream);
+  }
+  return e;
 }
 
-// Whether the launch is better off in tiles of 256 x 256.  A CU takes a 256 tile's step in
-// about the time in which two workgroups on it take 1.3 steps of a 128 tile each.
+// Whether the launch is better off in tiles of 256 x 256: by the steps that a CU takes.  A CU
+// takes a step of a 256 tile in about the time in which two workgroups on it take 1.4 steps of a
+// 128 tile each.
 template <class E>
 bool large_tiles(const Launch<E>& all) {
-  int64_t t256 = 0, t128 = 0;
+  int64_t u256 = 0, u128 = 0;
   for (int32_t k = 0; k < all.count; ++k) {
     Args p = all.args[k];
     p.tiles_m = (p.M + 255) / 256, p.tiles_n = (p.N + 255) / 256;
-    t256 += tile_count(p);
+    u256 += tile_count(p) * steps_of(p);
     p.tiles_m = (p.M + 127) / 128, p.tiles_n = (p.N + 127) / 128;
-    t128 += tile_count(p);
+    u128 += tile_count(p) * steps_of(p);
   }
-  const int64_t rounds256 = (t256 + 255) / 256, rounds128 = (t128 + 511) / 512;
-  return rounds256 * 13 <= rounds128 * 10;
+  return u256 > kPlaces256 * kLeastShare && u256 * 14 <= u128 * 5;
 }
 
 template <bool BF16, class E>
-hipError_t launch_products(Launch<E>& all, hipStream_t stream) {
-  return large_tiles(all) ? launch_tiles<Tile256, BF16, E>(all, stream) : launch_tiles<Tile128, BF16, E>(all, stream);
+hipError_t launch_products(Launch<E>& all, const Sums& sums, hipStream_t stream) {
+  return large_tiles(all) ? launch_tiles<Tile256, BF16, E>(all, sums, stream) : launch_tiles<Tile128, BF16, E>(all, sums, stream);
 }
 
 #endif

@@ -261,7 +261,7 @@ std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with
     }
   }
   for (SchulzRound& r : rounds) {
-    size_t to = kRoundHead;
+    size_t to = (kRoundTables + 255) / 256 * 256;
     const auto take = [&to](int64_t bytes) {
       const size_t from = to;
       to += (static_cast<size_t>(bytes) + 255) / 256 * 256;
@@ -274,6 +274,16 @@ std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with
       for (int p = 0; p < 2; ++p) g.gram[p] = take(2 * g.m * g.m * g.count), g.poly[p] = take(2 * g.m * g.m * g.count);
       for (int p = 0; p < 2; ++p) g.rest[p] = take(4 * g.m * g.count);
     }
+    // steps of the largest of a step's products, in tiles of 128 and three segments
+    int64_t gram = 0, poly = 0, next = 0;
+    for (const SchulzGroup& g : r.groups) {
+      const int64_t m = (g.m + 127) / 128, n = (g.n + 127) / 128;
+      gram += g.count * (m * (m + 1) / 2) * 3 * (g.n / 64);
+      poly += g.count * (m * (m + 1) / 2) * 3 * (g.m / 64);
+      next += g.count * (m * n) * 3 * (g.m / 64);
+    }
+    r.sums_bytes = sums_bytes(std::max({gram, poly, next}));
+    r.sums = take(static_cast<int64_t>(r.sums_bytes));
     r.bytes = to;
   }
   return rounds;

@@ -27,6 +27,18 @@ int check_orthogonalize_sizes(const daso_orthogonalize_args& s);
 int check_muon_sizes(const daso_muon_args& s);
 int check_workspace(const void* p, size_t bytes, size_t need);
 
+// ------------------------------------------------------------------ sums of cut tiles
+// Steps of a part of a tile, at the least, and the most parts of an XCD's pool, a workgroup
+// (daso_product.h).
+constexpr int kLeastPart = 6, kPoolParts = 3, kPlaces256 = 256;
+
+// Bytes of the sums that a launch of so many steps of 128 tiles may leave; a 256 tile's step counts
+// as four.
+inline size_t sums_bytes(int64_t steps128) {
+  const int64_t parts = steps128 / kLeastPart + 64, most = int64_t(kPoolParts) * kPlaces256 * 4;
+  return static_cast<size_t>(parts < most ? parts : most) * 128 * 128 * 4;
+}
+
 // ------------------------------------------------------------------ Newton-Schulz plan
 // Matrices of one shape that take their steps together.  Inside, X is m x n with m <= n,
 // both padded with zeros to multiples of 64.
@@ -46,14 +58,15 @@ struct SchulzGroup {
 struct SchulzRound {
   std::vector<SchulzGroup> groups;
   std::vector<int32_t> matrices;  // indexes into the caller's list, group by group
+  size_t sums, sums_bytes;        // the products' sums: byte offset, and room
   size_t bytes;                   // of workspace
 };
 
-constexpr int64_t kRoundElems = int64_t(1) << 26;  // 20 bytes of workspace each, and the squares
+constexpr int64_t kRoundElems = int64_t(1) << 27;  // 20 bytes of workspace each, and the squares
 constexpr int32_t kRoundMatrices = 128;            // as many as kernel arguments hold
 constexpr int32_t kRoundGroups = 8;
-constexpr int32_t kSumParts = 64;                  // partial sums of squares a matrix
-constexpr size_t kRoundHead = size_t(kRoundMatrices) * (16 + 8 * kSumParts);  // table and partial sums
+constexpr int32_t kSumParts = 256;                 // partial sums of squares a matrix, one a thread of who adds them
+constexpr size_t kRoundTables = size_t(kRoundMatrices) * (16 + 8 * kSumParts);  // table and partial sums
 
 struct Shape {
   int64_t rows, cols;
