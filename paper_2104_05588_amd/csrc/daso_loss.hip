@@ -187,6 +187,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
 // the target where the tile has it.
 struct LseOut {
   static constexpr auto kKind = product::kWhole;
+  static constexpr int kLds = 256 * 4 * sizeof(float2);
   struct Params {
     float2* parts;  // [tile column][token]
     float* at_target;
@@ -301,9 +302,12 @@ struct ProbOut {
     char* lo = hi + product::kStagePlane;
     const float inv = out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f;
     const bool two = out.lo != nullptr || out.t_lo != nullptr;
+    Row rows[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rows[i] = out.rows[row0 + i * 16 + r16];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const Row r = out.rows[row0 + i * 16 + r16];
+      const Row r = rows[i];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int col = col0 + j * 16 + kq * 4;
@@ -353,39 +357,49 @@ struct GradOut {
     int32_t bf16;
     int32_t rows, cols;
   };
-  __device__ static void block(const Params& p, const product::Place&, int row, int col, char* stage, int lane) {
-    const float factor = *p.grad * (1.0f / kProbScale), inv = *p.inv;
-    const bool wide = ((reinterpret_cast<uintptr_t>(p.out) | (p.ld * (p.bf16 ? 2 : 4))) & 15) == 0;
-    const int cc = col + product::pass_col(lane), left = p.cols - cc;
-    if (left <= 0) return;
-    float before[product::kPasses][8] = {};
-    if (p.before != nullptr) {
+  struct Inputs {
+    float before[product::kPasses][8];
+    float factor, inv;
+  };
+  __device__ static void fetch(const Params& p, const product::Place&, int row, int col, int lane, Inputs& in) {
+    const int r0 = row + product::pass_row(0, lane), cc = col + product::pass_col(lane);
+    in.factor = *p.grad * (1.0f / kProbScale), in.inv = *p.inv;
+    if (p.before == nullptr) return;
 #pragma unroll
-      for (int pass = 0; pass < product::kPasses; ++pass) {
-        const int rr = row + product::pass_row(pass, lane);
-        if (rr < p.rows) load8(p.before + int64_t(rr) * p.before_ld + cc, before[pass]);  // padded to whole vectors
-      }
-    }
+    for (int pass = 0; pass < product::kPasses; ++pass)  // padded to whole vectors
+      if (r0 + pass * product::kPassRows < p.rows && cc < p.cols) load8(p.before + int64_t(r0 + pass * product::kPassRows) * p.before_ld + cc, in.before[pass]);
+  }
+  template <class F>
+  __device__ static void block(const Params& p, const product::Place&, int row, int col, char* stage, int lane, const Inputs& in,
+                               F next) {
+    const int r0 = row + product::pass_row(0, lane), cc = col + product::pass_col(lane), left = p.cols - cc;
+    const bool wide = ((reinterpret_cast<uintptr_t>(p.out) | (p.ld * (p.bf16 ? 2 : 4))) & 15) == 0 && left >= 8;
+    float v[product::kPasses][8];
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass) {
-      const int rr = row + product::pass_row(pass, lane);
-      if (rr >= p.rows) continue;
-      float v[8];
-      product::pass_values(stage, pass, lane, v);
+      product::pass_values(stage, pass, lane, v[pass]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = v[i] * inv * factor + before[pass][i];
-      const int64_t to = int64_t(rr) * p.ld + cc;
-      uint16_t* o16 = p.bf16 ? (uint16_t*)p.out + to : nullptr;
-      float* o32 = p.bf16 ? nullptr : (float*)p.out + to;
-      if (wide && left >= 8) {
-        if (o16 != nullptr) store8(o16, v);
-        else store8(o32, v);
+      for (int i = 0; i < 8; ++i) {
+        v[pass][i] = v[pass][i] * in.inv * in.factor;
+        if (p.before != nullptr) v[pass][i] += in.before[pass][i];
+      }
+    }
+    next();
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) {
+      if (r0 + pass * product::kPassRows >= p.rows || left <= 0) continue;
+      const int64_t to = (r0 + pass * product::kPassRows) * p.ld + cc;
+      float* const o32 = (float*)p.out + to;
+      uint16_t* const o16 = (uint16_t*)p.out + to;
+      if (wide) {
+        if (p.bf16) store8(o16, v[pass]);
+        else store8(o32, v[pass]);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if (i >= left) continue;
-          if (o16 != nullptr) o16[i] = to_bf16(v[i]);
-          else o32[i] = v[i];
+          if (p.bf16) o16[i] = to_bf16(v[pass][i]);
+          else o32[i] = v[pass][i];
         }
       }
     }
@@ -460,7 +474,8 @@ Plan plan_of(const daso_loss_args& s, bool backward) {
   }
   // the largest product's steps, in tiles of 128 and three segments
   const int64_t nt = (q.n_p + 127) / 128, dt = (q.d_p + 127) / 128, width = std::min(q.v_p, q.piece), vt = (width + 127) / 128;
-  q.sums_bytes = backward ? host::sums_bytes(3 * std::max(nt * vt * (q.d_p / 64), dt * (nt * (width / 64) + vt * (q.n_p / 64)))) : 0;
+  q.sums_bytes = host::sums_bytes(3 * std::max(nt * (backward ? vt : (q.v_p + 127) / 128) * (q.d_p / 64),
+                                               backward ? dt * (nt * (width / 64) + vt * (q.n_p / 64)) : 0));
   q.sums = take(static_cast<int64_t>(q.sums_bytes));
   q.bytes = to;
   return q;
@@ -564,8 +579,7 @@ hipError_t forward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
   out.at_target = reinterpret_cast<float*>(ws + q.at_target);
   out.targets = s.targets;
   out.inv_a = q.f32 ? &sc->inv[kHidden] : nullptr, out.inv_b = q.f32 ? &sc->inv[kWeight] : nullptr;
-  const bool large = product::large_tiles(all);
-  const int64_t across = large ? product::Tile256::kCols : product::Tile128::kCols;
+  const int64_t across = product::large_tiles(all) ? 256 : 128;
   if (q.f32) e = product::launch_products<false>(all, sums, stream);
   else e = product::launch_products<true>(all, sums, stream);
   if (e != hipSuccess) return e;

@@ -61,61 +61,84 @@ struct PlanesOut {
     int32_t square;      // C = in in^T; else C = left in
   };
   static constexpr auto kKind = product::kStaged;
-  __device__ static void block(const Params& p, const product::Place& at, int row, int col, char* stage, int lane) {
-    const bool turn = p.t_hi != nullptr && (p.t_always || at.tm != at.tn);
-    char* plane = stage + product::kStageFloats;
-    const int64_t base = at.batch * p.batch;
-    const float* rest = p.rest != nullptr ? p.rest + int64_t(at.batch) * p.rest_ld : nullptr;
-    const int k = product::pass_col(lane);
-    half8 in_hi[product::kPasses], in_lo[product::kPasses];
+  struct Inputs {
+    half8 hi[product::kPasses], lo[product::kPasses];
+    float left[product::kPasses], right[8];  // what the operands' diagonals lack, by rows and by columns
+  };
+  __device__ static void fetch(const Params& p, const product::Place& at, int row, int col, int lane, Inputs& in) {
+    const int64_t from = at.batch * p.batch + int64_t(row + product::pass_row(0, lane)) * p.ld + col + product::pass_col(lane);
+    const half8 none = (half8)(_Float16)0.0f;
+    if (p.in_hi != nullptr) {
 #pragma unroll
-    for (int pass = 0; pass < product::kPasses; ++pass) {
-      in_hi[pass] = in_lo[pass] = (half8)(_Float16)0.0f;
-      const int64_t to = base + int64_t(row + product::pass_row(pass, lane)) * p.ld + col + k;
-      if (p.in_hi != nullptr) in_hi[pass] = *(const half8*)(p.in_hi + to);
-      if (p.in_lo != nullptr) in_lo[pass] = *(const half8*)(p.in_lo + to);
+      for (int pass = 0; pass < product::kPasses; ++pass) in.hi[pass] = *(const half8*)(p.in_hi + from + pass * product::kPassRows * p.ld);
+    } else {
+#pragma unroll
+      for (int pass = 0; pass < product::kPasses; ++pass) in.hi[pass] = none;
     }
-    float right[8];  // what the operands' diagonals lack: of the left one by rows, of the right one by columns
+    if (p.in_lo != nullptr) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) right[i] = rest != nullptr && p.square ? rest[col + k + i] : 0.0f;
+      for (int pass = 0; pass < product::kPasses; ++pass) in.lo[pass] = *(const half8*)(p.in_lo + from + pass * product::kPassRows * p.ld);
+    } else {
+#pragma unroll
+      for (int pass = 0; pass < product::kPasses; ++pass) in.lo[pass] = none;
+    }
+    const float* rest = p.rest + int64_t(at.batch) * p.rest_ld;
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass)
+      in.left[pass] = p.rest != nullptr ? rest[row + product::pass_row(pass, lane)] : 0.0f;
+    const bool square = p.rest != nullptr && p.square;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) in.right[i] = square ? rest[col + product::pass_col(lane) + i] : 0.0f;
+  }
+  template <class F>
+  __device__ static void block(const Params& p, const product::Place& at, int row, int col, char* stage, int lane, const Inputs& in,
+                               F next) {
+    const bool turn = p.t_hi != nullptr && (p.t_always || at.tm != at.tn), t_lo = p.t_lo != nullptr;
+    const int k = product::pass_col(lane);
+    float v[product::kPasses][8];  // (all of them, before the planes take their place in LDS)
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) product::pass_values(stage, pass, lane, v[pass]);
+    product::wait_lds();
+    __builtin_amdgcn_wave_barrier();
+    half8 hi[product::kPasses], lo[product::kPasses];
+    float missing[product::kPasses];
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass) {
-      const int r = product::pass_row(pass, lane);
-      const int64_t to = base + int64_t(row + r) * p.ld + col + k;
-      const float left = rest != nullptr ? rest[row + r] : 0.0f;
-      const int at_diagonal = row + r - col - k;  // which of the eight lies on it
-      float v[8];
-      product::pass_values(stage, pass, lane, v);
-      half8 hi, lo;
+      const int at_diagonal = row + product::pass_row(pass, lane) - col - k;  // which of the eight lies on it
+      missing[pass] = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        float in = static_cast<float>(in_hi[pass][i]) + static_cast<float>(in_lo[pass][i]);
-        if (p.square && i == at_diagonal) in += left;
-        v[i] = fmaf(p.beta, in, p.alpha * fmaf(left + right[i], in, v[i]));
+        float x = static_cast<float>(in.hi[pass][i]) + static_cast<float>(in.lo[pass][i]);
+        if (p.square) x += i == at_diagonal ? in.left[pass] : 0.0f;
+        x = fmaf(p.beta, x, p.alpha * fmaf(in.left[pass] + in.right[i], x, v[pass][i]));
         _Float16 a, b;
-        product::split(v[i], &a, &b);
-        hi[i] = a, lo[i] = b;
-        if (p.rest_out != nullptr && i == at_diagonal)
-          p.rest_out[int64_t(at.batch) * p.rest_ld + row + r] = v[i] - static_cast<float>(a);
+        product::split(x, &a, &b);
+        hi[pass][i] = a, lo[pass][i] = b;
+        missing[pass] = i == at_diagonal ? x - static_cast<float>(a) : missing[pass];
       }
-      *(half8*)(p.hi + to) = hi;
-      if (p.lo != nullptr) *(half8*)(p.lo + to) = lo;
+    }
+    next();
+    const int64_t to = at.batch * p.batch + int64_t(row + product::pass_row(0, lane)) * p.ld + col + k;
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) {
+      const int r = product::pass_row(pass, lane), at_diagonal = row + r - col - k;
+      if (p.rest_out != nullptr && at_diagonal >= 0 && at_diagonal < 8)
+        p.rest_out[int64_t(at.batch) * p.rest_ld + row + r] = missing[pass];
+      *(half8*)(p.hi + to + pass * product::kPassRows * p.ld) = hi[pass];
+      if (p.lo != nullptr) *(half8*)(p.lo + to + pass * product::kPassRows * p.ld) = lo[pass];
       if (turn) {
-        *(half8*)(plane + product::plane_at(r, k)) = hi;
-        if (p.t_lo != nullptr) *(half8*)(plane + product::kStagePlane + product::plane_at(r, k)) = lo;
+        *(half8*)(stage + product::plane_at(r, k)) = hi[pass];
+        if (t_lo) *(half8*)(stage + product::kStagePlane + product::plane_at(r, k)) = lo[pass];
       }
     }
     if (!turn) return;
     product::wait_lds();
     __builtin_amdgcn_wave_barrier();
-    const int64_t t_base = at.batch * p.t_batch;
-    product::by_columns(plane, lane, [&](int c, int r, half8 v) {
-      *(half8*)(p.t_hi + t_base + int64_t(col + c) * p.t_ld + row + r) = v;
-    });
-    if (p.t_lo != nullptr)
-      product::by_columns(plane + product::kStagePlane, lane, [&](int c, int r, half8 v) {
-        *(half8*)(p.t_lo + t_base + int64_t(col + c) * p.t_ld + row + r) = v;
-      });
+    const int64_t t_base = at.batch * p.t_batch + int64_t(col) * p.t_ld + row;
+    product::by_columns(stage, lane, [&](int c, int r, half8 x) { *(half8*)(p.t_hi + t_base + c * p.t_ld + r) = x; });
+    if (t_lo)
+      product::by_columns(stage + product::kStagePlane, lane,
+                          [&](int c, int r, half8 x) { *(half8*)(p.t_lo + t_base + c * p.t_ld + r) = x; });
   }
 };
 
@@ -139,59 +162,83 @@ struct LastOut {
     int32_t rest_ld, right;
   };
   static constexpr auto kKind = product::kStaged;
-  __device__ static void block(const Params& p, const product::Place& at, int row, int col, char* stage, int lane) {
-    const int64_t base = at.batch * p.batch;
-    int64_t out = p.out_batch * at.batch, out_ld = p.out_ld;
-    float step = 0.0f;
-    if (p.kind == kStep) {
-      const Entry e = p.table[at.batch];
-      out = e.start, out_ld = p.cols, step = e.step;
-    }
-    const size_t esz = p.kind == kBf16 ? 2 : 4;
-    char* to_all = p.kind == kStep ? (char*)p.params : (char*)p.out;
-    const bool wide = ((reinterpret_cast<uintptr_t>(to_all + out * esz) | (out_ld * esz)) & 15) == 0 &&
-                      (p.wire == nullptr || ((out | out_ld) & 7) == 0);
-    const float* rest = p.rest != nullptr ? p.rest + int64_t(at.batch) * p.rest_ld : nullptr;
-    const int k = product::pass_col(lane), cc = col + k, left = p.cols - cc;
-    half8 in_hi[product::kPasses], in_lo[product::kPasses];
-    float x[product::kPasses][8];
+  struct Inputs {
+    half8 hi[product::kPasses], lo[product::kPasses];
+    float x[product::kPasses][8];  // kStep: the parameters
+    float left[product::kPasses], right[8];
+    Entry entry;
+  };
+  // Where a matrix's result lies, and whether eight of its elements may be taken at a time.
+  __device__ static bool place(const Params& p, int batch, const Entry& e, int64_t* out, int64_t* ld) {
+    *out = p.kind == kStep ? e.start : p.out_batch * batch;
+    *ld = p.kind == kStep ? p.cols : p.out_ld;
+    const int64_t esz = p.kind == kBf16 ? 2 : 4;
+    const uintptr_t first = reinterpret_cast<uintptr_t>(p.kind == kStep ? (void*)p.params : p.out);
+    return ((first + *out * esz) & 15) == 0 && ((*ld * esz) & 15) == 0 && (p.wire == nullptr || ((*out | *ld) & 7) == 0);
+  }
+  __device__ static void fetch(const Params& p, const product::Place& at, int row, int col, int lane, Inputs& in) {
+    const int k = product::pass_col(lane), r0 = row + product::pass_row(0, lane), cc = col + k;
+    const int64_t from = at.batch * p.batch + int64_t(r0) * p.ld + cc;
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass) {
-      const int rr = row + product::pass_row(pass, lane);
-      const int64_t from = base + int64_t(rr) * p.ld + cc;
-      in_hi[pass] = *(const half8*)(p.in_hi + from), in_lo[pass] = *(const half8*)(p.in_lo + from);
-      if (p.kind != kStep || rr >= p.rows || left <= 0) continue;
-      const float* q = p.params + out + int64_t(rr) * out_ld + cc;
-      if (wide && left >= 8) load8(q, x[pass]);
+      in.hi[pass] = *(const half8*)(p.in_hi + from + pass * product::kPassRows * p.ld);
+      in.lo[pass] = *(const half8*)(p.in_lo + from + pass * product::kPassRows * p.ld);
+    }
+    const float* rest = p.rest + int64_t(at.batch) * p.rest_ld;
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) in.left[pass] = p.rest != nullptr && !p.right ? rest[r0 + pass * product::kPassRows] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) in.right[i] = p.rest != nullptr && p.right ? rest[cc + i] : 0.0f;
+    if (p.kind != kStep) return;
+    in.entry = p.table[at.batch];
+    int64_t out, ld;
+    const bool wide = place(p, at.batch, in.entry, &out, &ld) && cc + 8 <= p.cols;
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) {
+      if (r0 + pass * product::kPassRows >= p.rows) continue;
+      const float* q = p.params + out + (r0 + pass * product::kPassRows) * ld + cc;
+      if (wide) load8(q, in.x[pass]);
       else
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[pass][i] = i < left ? q[i] : 0.0f;
+        for (int i = 0; i < 8; ++i) in.x[pass][i] = cc + i < p.cols ? q[i] : 0.0f;
     }
+  }
+  template <class F>
+  __device__ static void block(const Params& p, const product::Place& at, int row, int col, char* stage, int lane, const Inputs& in,
+                               F next) {
+    const int r0 = row + product::pass_row(0, lane), cc = col + product::pass_col(lane);
+    int64_t out, ld;
+    const bool wide = place(p, at.batch, in.entry, &out, &ld) && cc + 8 <= p.cols;
+    const float step = p.kind == kStep ? in.entry.step : 0.0f;
+    float* const o32 = p.kind == kStep ? p.params : (float*)p.out;
+    uint16_t* const o16 = p.kind == kStep ? p.wire : (uint16_t*)p.out;
+    const bool has32 = p.kind != kBf16, has16 = p.kind == kBf16 || (p.kind == kStep && p.wire != nullptr);
+    float v[product::kPasses][8];
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass) {
-      const int rr = row + product::pass_row(pass, lane);
-      float v[8];
-      product::pass_values(stage, pass, lane, v);
+      product::pass_values(stage, pass, lane, v[pass]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float in = static_cast<float>(in_hi[pass][i]) + static_cast<float>(in_lo[pass][i]);
-        const float more = rest != nullptr ? rest[p.right ? cc + i : rr] : 0.0f;
-        v[i] = fmaf(p.beta, in, p.alpha * fmaf(more, in, v[i])) * kUnscale;
-        if (p.kind == kStep) v[i] = x[pass][i] * p.keep - step * v[i];
+        const float x = static_cast<float>(in.hi[pass][i]) + static_cast<float>(in.lo[pass][i]);
+        float& o = v[pass][i];
+        o = fmaf(p.beta, x, p.alpha * fmaf(in.left[pass] + in.right[i], x, o)) * kUnscale;
+        if (p.kind == kStep) o = in.x[pass][i] * p.keep - step * o;
       }
-      if (rr >= p.rows || left <= 0) continue;
-      const int64_t to = out + int64_t(rr) * out_ld + cc;
-      float* o32 = p.kind == kStep ? p.params + to : p.kind == kF32 ? (float*)p.out + to : nullptr;
-      uint16_t* o16 = p.kind == kStep ? (p.wire != nullptr ? p.wire + to : nullptr) : p.kind == kBf16 ? (uint16_t*)p.out + to : nullptr;
-      if (wide && left >= 8) {
-        if (o32 != nullptr) store8(o32, v);
-        if (o16 != nullptr) store8(o16, v);
+    }
+    next();
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass) {
+      if (r0 + pass * product::kPassRows >= p.rows) continue;
+      const int64_t to = out + (r0 + pass * product::kPassRows) * ld + cc;
+      if (wide) {
+        if (has32) store8(o32 + to, v[pass]);
+        if (has16) store8(o16 + to, v[pass]);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (i >= left) continue;
-          if (o32 != nullptr) o32[i] = v[i];
-          if (o16 != nullptr) o16[i] = to_bf16(v[i]);
+          if (cc + i >= p.cols) continue;
+          if (has32) o32[to + i] = v[pass][i];
+          if (has16) o16[to + i] = to_bf16(v[pass][i]);
         }
       }
     }

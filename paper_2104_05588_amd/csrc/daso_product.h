@@ -27,10 +27,10 @@ constexpr int kMaxSegments = 3;
 constexpr int kStepElems = 64;     // contraction elements a step: 128 bytes of a row, one cache line
 constexpr int kLeastSteps = 2;     // the pipeline's depth: a product takes at least this many steps
 constexpr int kBlockRows = 64, kBlockCols = 32;  // what an epilogue is handed at a time
-// LDS of a wavefront's own for its epilogue: a block in 32 bits, and two planes of it in 16.
-constexpr int kStageFloats = kBlockRows * kBlockCols * 4;
+// LDS of a wavefront's own for its epilogue: a block in 32 bits, or two planes of it in 16.
 constexpr int kStagePlane = kBlockRows * kBlockCols * 2 + (kBlockRows / 8) * 16;
-constexpr int kWaveStage = kStageFloats + 2 * kStagePlane;
+constexpr int kWaveStage = 2 * kStagePlane;
+static_assert(kWaveStage >= kBlockRows * kBlockCols * 4, "a staged block fits");
 constexpr int64_t kMaxLd = int64_t(1) << 22;  // row offsets within a tile stay in 32 bits
 constexpr int kMaxProblems = 8;               // products of one launch
 
@@ -145,7 +145,8 @@ __device__ inline const char* step_of(const char* s0, const char* s1, const char
 // the matrix cores draw.  16x16x32 instructions draw less than 32x32x16 ones (registers
 // only: 1950 and 1670 TFLOP/s), and the whole runs at 1235 TFLOP/s, with 32x32x16 at 1040.
 struct Tile256 {
-  static constexpr int kRows = 256, kCols = 256, kThreads = 512, kLds = 8 * kWaveStage > 131072 ? 8 * kWaveStage : 131072;
+  static constexpr int kRows = 256, kCols = 256, kThreads = 512, kLds = 131072;
+  static_assert(kLds >= 8 * kWaveStage, "the epilogue's LDS");
   static constexpr int kBlocks = 4;  // blocks of 64 x 32 a wavefront
   static constexpr int kOccupancy = 2;
 
@@ -275,13 +276,16 @@ struct Tile256 {
   };
 };
 
-// 128 x 128 a workgroup of 4 wavefronts, two workgroups a CU, for results too small to
-// give every CU a larger tile.  Two steps in LDS; a step's last quarter runs while the
-// next step's first operands are read.
+// 128 x 128 a workgroup of 4 wavefronts, for results too small to give every CU a larger tile.  Two
+// steps in LDS, two workgroups a CU, which hide each other's waits; a step's second half runs
+// while the next step's first operands are read.  (A ring of four steps, with one workgroup a CU, was
+// no faster where there are few: 33 us against 27 for 16 tiles of 32 steps, which wait for what one
+// CU gets of memory.)
 struct Tile128 {
-  static constexpr int kRows = 128, kCols = 128, kThreads = 256, kLds = 4 * kWaveStage > 65536 ? 4 * kWaveStage : 65536;
+  static constexpr int kRows = 128, kCols = 128, kThreads = 256, kLds = 65536;
   static constexpr int kBlocks = 2;
   static constexpr int kOccupancy = 2;
+  static_assert(kLds >= 4 * kWaveStage, "the epilogue's LDS");
 
   __device__ static void block_at(int wave, int b, int* row, int* col) {
     *row = (wave >> 1) * 64;
@@ -372,8 +376,8 @@ __device__ inline void stage_block(const f4 (&c)[8], char* stage, int lane) {
 
 // A staged block by rows, in four passes of 16 rows and four lanes a row: the row and the first of
 // the eight neighbouring columns that a lane has in a pass, and their values.
-constexpr int kPasses = 4;
-__device__ inline int pass_row(int pass, int lane) { return pass * 16 + (lane >> 2); }
+constexpr int kPasses = 4, kPassRows = 16;
+__device__ inline int pass_row(int pass, int lane) { return pass * kPassRows + (lane >> 2); }
 __device__ inline int pass_col(int lane) { return (lane & 3) * 8; }
 __device__ inline void pass_values(const char* stage, int pass, int lane, float (&v)[8]) {
   const int row = pass_row(pass, lane), piece = (lane & 3) * 2, s = (row >> 1) & 7;
@@ -411,11 +415,13 @@ __device__ inline void split(float v, _Float16* hi, _Float16* lo) {
 }
 
 // The products of one launch.  An epilogue E has a plain struct E::Params and one of
-//   kStaged: block(params, place, row, col, stage, lane), by a wavefront: the staged 64 x 32 block at
-//            (row, col) of C, of those that begin inside the result
+//   kStaged: fetch(params, place, row, col, lane) what is needed of memory, as Inputs, and
+//            block(params, place, row, col, stage, lane, inputs, next), by a wavefront: the staged
+//            block at (row, col) of C, of those that begin inside the result; next is called
+//            once, after the last use of the inputs and before the first store
 //   kBlocks: block(params, place, c, row, col, stage, lane): the same with the block in registers, of all
 //            blocks of a tile
-//   kWhole:  tile<Tile>(params, args, place, acc, lds), by the whole workgroup; its tiles are never cut
+//   kWhole:  tile<Tile>(params, args, place, acc, lds), by the whole workgroup, in kLds bytes of LDS
 //
 // A launch has up to as many workgroups as fit the chip (kPlaces); an XCD's, to which they go in
 // turn, get a run of whole tiles, with about an eighth of all steps.  Of each product an XCD's
@@ -452,8 +458,12 @@ struct Sums {
   size_t bytes;
 };
 
-// What cutting costs, in steps of a tile: the second kernel takes 10 to 30 us.
-constexpr int kPartCost256 = 16, kPartCost128 = 24;
+// What cutting costs, in steps of a tile: the parts' sums are written and read again, 256 KB each
+// for a 256 tile, and the second kernel takes 8 us and more.  A launch of few workgroups has the
+// shortest second kernel, and its steps are the longest, since few CUs ask for memory.
+// (4096 x 4096 orthogonalised in bf16, 136 tiles of 64 steps on 256 CUs: 1.94 ms at a cost of 16,
+// which cuts them, 1.63 at 28, which does not; the gradients of a loss, 256 steps: 2.2 ms cut, 2.8 not.)
+constexpr int kPartCost256 = 28, kPartCost128 = 24, kPartCostFew = 10;
 using host::kLeastPart;
 using host::kPoolParts;
 // Steps that are worth a workgroup of their own.
@@ -464,27 +474,58 @@ constexpr int kPlaces256 = host::kPlaces256, kPlaces128 = 2 * kPlaces256;
 inline __host__ __device__ int32_t steps_of(const Args& p) { return p.steps * p.segments; }
 
 template <class Tile, class E>
-__device__ inline void finish(const typename E::Params& out, const Args& p, const Place& at, f4 (&acc)[Tile::kBlocks][8], char* lds) {
+__device__ inline void finish(const typename E::Params& params, const Args& p, const Place& at, f4 (&acc)[Tile::kBlocks][8], char* lds) {
+  const typename E::Params out = params;  // read once
   if constexpr (E::kKind == kWhole) {
     E::template tile<Tile>(out, p, at, acc, lds);
   } else {
     const int lane = thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     char* stage = lds + wave * kWaveStage;
     if constexpr (E::kKind == kStaged) {
-      // the blocks' own code is there once, and not once a block: unrolled, it would not fit the
-      // instruction cache
+      const auto block_at = [&](int b, int* row, int* col) {
+        Tile::block_at(wave, b, row, col);
+        *row += at.tm * Tile::kRows, *col += at.tn * Tile::kCols;
+        return b < Tile::kBlocks && *row < p.M && *col < p.N;
+      };
+      typename E::Inputs in;
+      if constexpr (Tile::kBlocks > 2) {
+        // The blocks' code is there once: unrolled, with the next block's inputs on their way, it took more
+        // registers than there are, and 6% more time over a GPT-medium's matrices.
 #pragma unroll 1
-      for (int b = 0; b < Tile::kBlocks; ++b) {
-        int row, col;
-        Tile::block_at(wave, b, &row, &col);
-        row += at.tm * Tile::kRows, col += at.tn * Tile::kCols;
-        if (row >= p.M || col >= p.N) continue;
+        for (int b = 0; b < Tile::kBlocks; ++b) {
+          int row, col;
+          if (!block_at(b, &row, &col)) continue;
+          E::fetch(out, at, row, col, lane, in);
 #pragma unroll
-        for (int k = 0; k < Tile::kBlocks; ++k)
-          if (b == k) stage_block(acc[k], stage, lane);
-        wait_lds();
-        __builtin_amdgcn_wave_barrier();
-        E::block(out, at, row, col, stage, lane);
+          for (int k = 0; k < Tile::kBlocks; ++k)
+            if (b == k) stage_block(acc[k], stage, lane);
+          wait_lds();
+          __builtin_amdgcn_wave_barrier();
+          E::block(out, at, row, col, stage, lane, in, [] {});
+        }
+        return;
+      }
+      // A block's inputs are fetched before the stores of the block before it: fetched later, they
+      // would be waited for with the stores, which take as long again.
+      int row, col;
+      bool has = block_at(0, &row, &col);
+      if (has) E::fetch(out, at, row, col, lane, in);
+#pragma unroll
+      for (int b = 0; b < Tile::kBlocks; ++b) {
+        int next_row, next_col;
+        const bool next = block_at(b + 1, &next_row, &next_col);
+        const auto fetch_next = [&] {
+          if (next) E::fetch(out, at, next_row, next_col, lane, in);
+        };
+        if (has) {
+          stage_block(acc[b], stage, lane);
+          wait_lds();
+          __builtin_amdgcn_wave_barrier();
+          E::block(out, at, row, col, stage, lane, in, fetch_next);
+        } else {
+          fetch_next();
+        }
+        has = next, row = next_row, col = next_col;
       }
     } else {
 #pragma unroll
@@ -530,11 +571,11 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kOccupancy) void product_kern
       tile = all.runs[xcd][problem].tile + round * across + static_cast<int>(blockIdx.x >> 3);
       ++round;
     }
-    const Args& p = all.args[problem];
+    const Args p = all.args[problem];
     const int steps = steps_of(p), from = steps * piece / pieces, to = steps * (piece + 1) / pieces;
     const Place at = place_of(p, tile);
     Tile::template run<BF16>(p, at, from, to, lds, acc);
-    if (E::kKind != kWhole && pieces > 1) {
+    if (pieces > 1) {
       f4* left = (f4*)(all.sums + int64_t(all.slot[xcd] + slot) * (Tile::kRows * Tile::kCols)) + thread_here();
 #pragma unroll
       for (int b = 0; b < Tile::kBlocks; ++b)
@@ -547,57 +588,87 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kOccupancy) void product_kern
   }
 }
 
-// What is left of tiles that were cut: workgroups (x, y) take blocks of the pools' tiles.
-constexpr int kJoinWaves = 4;
+// The cut tile t, counted over the XCDs' pools.
+struct CutTile {
+  int problem, tile, parts, rest;  // the parts' sums are `rest` places apart
+  int slot;                        // the place of the first part's, -1: there is no such tile
+};
 
-template <class Tile, class E>
-__global__ __launch_bounds__(64 * kJoinWaves) void product_join_kernel(Launch<E> all) {
-  __shared__ __attribute__((aligned(1024))) char lds[kJoinWaves * kWaveStage];
-  // the tile, counted over the cut ones of the XCDs' pools, and the place of its first part's sums
-  int t = blockIdx.x, xcd = 0, problem = 0, slot = 0;
-  for (;; ++xcd, problem = 0) {
-    if (xcd == 8) return;
-    for (slot = 0; problem < all.count; ++problem) {
-      const Run& run = all.runs[xcd][problem];
+template <class E>
+__device__ inline CutTile cut_tile(const Launch<E>& all, int t) {
+  for (int xcd = 0; xcd < 8; ++xcd) {
+    int slot = all.slot[xcd];
+    for (int k = 0; k < all.count; ++k) {
+      const Run& run = all.runs[xcd][k];
       if (run.parts > 1) {
-        if (t < run.rest) break;
+        if (t < run.rest) return {k, run.tile + run.rounds * all.across + t, run.parts, run.rest, slot + t};
         t -= run.rest;
       }
       slot += run.rest * run.parts;
     }
-    if (problem < all.count) break;
   }
-  const Run& run = all.runs[xcd][problem];
-  const Args& p = all.args[problem];
-  const Place at = place_of(p, run.tile + run.rounds * all.across + t);
-  const int lane = threadIdx.x & 63, block = blockIdx.y * kJoinWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wave = block / Tile::kBlocks, b = block % Tile::kBlocks;
+  return {0, 0, 0, 0, -1};
+}
+
+template <class Tile>
+__device__ inline void add_parts(const float* sums, const CutTile& cut, int b, int thread, f4 (&c)[8]) {
   constexpr int64_t kTile = int64_t(Tile::kRows) * Tile::kCols / 4;  // in vectors
-  const f4* from = (const f4*)all.sums + int64_t(all.slot[xcd] + slot + t) * kTile + b * 8 * Tile::kThreads + wave * 64 + lane;
-  f4 c[8];
+  const f4* from = (const f4*)sums + cut.slot * kTile + b * 8 * Tile::kThreads + thread;
 #pragma unroll
   for (int i = 0; i < 8; ++i) c[i] = from[i * Tile::kThreads];
-  for (int k = 1; k < run.parts; ++k) {
-    from += run.rest * kTile;
+  for (int k = 1; k < cut.parts; ++k) {
+    from += cut.rest * kTile;
     f4 v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = from[i * Tile::kThreads];
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] += v[i];
   }
+}
+
+// What is left of tiles that were cut: workgroups (x, y) take blocks of tile x.
+constexpr int kJoinWaves = 4;
+
+template <class Tile, class E>
+__global__ __launch_bounds__(64 * kJoinWaves) void product_join_kernel(Launch<E> all) {
+  __shared__ __attribute__((aligned(1024))) char lds[kJoinWaves * kWaveStage];
+  const CutTile cut = cut_tile(all, blockIdx.x);
+  if (cut.slot < 0) return;
+  const Args& p = all.args[cut.problem];
+  const Place at = place_of(p, cut.tile);
+  const int lane = threadIdx.x & 63, block = blockIdx.y * kJoinWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = block / Tile::kBlocks, b = block % Tile::kBlocks;
   int row, col;
   Tile::block_at(wave, b, &row, &col);
   row += at.tm * Tile::kRows, col += at.tn * Tile::kCols;
+  if (E::kKind == kStaged && (row >= p.M || col >= p.N)) return;
+  const typename E::Params out = all.out[cut.problem];
+  f4 c[8];
+  add_parts<Tile>(all.sums, cut, b, wave * 64 + lane, c);
   char* stage = lds + (threadIdx.x >> 6) * kWaveStage;
   if constexpr (E::kKind == kStaged) {
-    if (row >= p.M || col >= p.N) return;
+    typename E::Inputs in;
+    E::fetch(out, at, row, col, lane, in);
     stage_block(c, stage, lane);
     wait_lds();
     __builtin_amdgcn_wave_barrier();
-    E::block(all.out[problem], at, row, col, stage, lane);
+    E::block(out, at, row, col, stage, lane, in, [] {});
   } else {
-    E::block(all.out[problem], at, c, row, col, stage, lane);
+    E::block(out, at, c, row, col, stage, lane);
   }
+}
+
+// The same for an epilogue of whole tiles: a workgroup a tile.
+template <class Tile, class E>
+__global__ __launch_bounds__(Tile::kThreads) void product_join_whole_kernel(Launch<E> all) {
+  __shared__ __attribute__((aligned(1024))) char lds[E::kLds];
+  const CutTile cut = cut_tile(all, blockIdx.x);
+  if (cut.slot < 0) return;
+  const Args& p = all.args[cut.problem];
+  f4 acc[Tile::kBlocks][8];
+#pragma unroll
+  for (int b = 0; b < Tile::kBlocks; ++b) add_parts<Tile>(all.sums, cut, b, threadIdx.x, acc[b]);
+  E::template tile<Tile>(all.out[cut.problem], p, place_of(p, cut.tile), acc, lds);
 }
 
 // The steps that the busiest of `across` workgroups has of an XCD's pool, cut so that the longest
@@ -624,15 +695,14 @@ inline int64_t pool_steps(Run* runs, const Args* args, int32_t count, int32_t ac
 
 // Deals the launch's tiles to XCDs and plans their pools.  Returns the workgroups; *cut counts the
 // tiles that are cut.
-template <class Tile, class E>
+template <int kSide, class E>
 int deal(Launch<E>& all, const Sums& sums, int* cut) {
-  constexpr int kPlaces = Tile::kRows == 256 ? kPlaces256 : kPlaces128;
-  constexpr int kCost = Tile::kRows == 256 ? kPartCost256 : kPartCost128;
+  constexpr int kPlaces = kSide == 256 ? kPlaces256 : kPlaces128;
   int64_t first[kMaxProblems + 1] = {}, units = 0;
   for (int32_t k = 0; k < all.count; ++k) {
     Args& p = all.args[k];
-    p.tiles_m = (p.M + Tile::kRows - 1) / Tile::kRows;
-    p.tiles_n = (p.N + Tile::kCols - 1) / Tile::kCols;
+    p.tiles_m = (p.M + kSide - 1) / kSide;
+    p.tiles_n = (p.N + kSide - 1) / kSide;
     first[k + 1] = first[k] + tile_count(p);
     if (tile_count(p) > INT32_MAX / 2) return -1;
     units += tile_count(p) * steps_of(p);
@@ -640,8 +710,8 @@ int deal(Launch<E>& all, const Sums& sums, int* cut) {
   *cut = 0;
   if (first[all.count] == 0) return 0;
   int64_t worth = (units / kLeastShare + 7) / 8;
-  if (E::kKind == kWhole) worth = (first[all.count] + 7) / 8;
   all.across = static_cast<int32_t>(worth < 1 ? 1 : worth < kPlaces / 8 ? worth : kPlaces / 8);
+  const int cost = kSide == 256 ? kPartCost256 : all.across * 8 > kPlaces256 ? kPartCost128 : kPartCostFew;
   int64_t tile = 0;  // of all products, the first that is not dealt yet
   int64_t dealt = 0;
   int32_t problem = 0, slots = 0;
@@ -664,17 +734,16 @@ int deal(Launch<E>& all, const Sums& sums, int* cut) {
     }
     int32_t best = 1;
     int64_t least = pool_steps(all.runs[x], all.args, all.count, all.across, 1);
-    if (E::kKind != kWhole)
-      for (int32_t s = 2; s <= 16; ++s) {
-        const int64_t n = pool_steps(all.runs[x], all.args, all.count, all.across, s);
-        if (n > 0 && n + kCost < least) best = s, least = n + kCost;
-      }
+    for (int32_t s = 2; s <= 16; ++s) {
+      const int64_t n = pool_steps(all.runs[x], all.args, all.count, all.across, s);
+      if (n > 0 && n + cost < least) best = s, least = n + cost;
+    }
     pool_steps(all.runs[x], all.args, all.count, all.across, best);
     all.slot[x] = slots;
     if (best == 1) continue;
     for (int32_t k = 0; k < all.count; ++k) slots += all.runs[x][k].rest * all.runs[x][k].parts;
   }
-  if (size_t(slots) * Tile::kRows * Tile::kCols * sizeof(float) > sums.bytes)
+  if (size_t(slots) * kSide * kSide * sizeof(float) > sums.bytes)
     for (int x = 0; x < 8; ++x) pool_steps(all.runs[x], all.args, all.count, all.across, 1);
   all.sums = sums.to;
   for (int x = 0; x < 8; ++x)
@@ -683,11 +752,7 @@ int deal(Launch<E>& all, const Sums& sums, int* cut) {
 }
 
 template <class Tile, bool BF16, class E>
-hipError_t launch_tiles(Launch<E>& all, const Sums& sums, hipStream_t stream) {
-  int cut = 0;
-  const int groups = deal<Tile>(all, sums, &cut);
-  if (groups == 0) return hipSuccess;
-  if (groups < 0) return hipErrorInvalidValue;
+hipError_t launch_tiles(Launch<E>& all, int groups, int cut, hipStream_t stream) {
   auto* kernel = product_kernel<Tile, BF16, E>;
   // once a device, before the first launch there
   static std::atomic<uint64_t> allowed{0};
@@ -703,13 +768,15 @@ hipError_t launch_tiles(Launch<E>& all, const Sums& sums, hipStream_t stream) {
   void* list[] = {&all};
   e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(static_cast<uint32_t>(groups)), dim3(Tile::kThreads), list,
                       Tile::kLds, stream);
-  if constexpr (E::kKind != kWhole) {
+  if (e != hipSuccess || cut == 0) return e;
+  if constexpr (E::kKind == kWhole) {
+    return hipLaunchKernel(reinterpret_cast<const void*>(&product_join_whole_kernel<Tile, E>), dim3(static_cast<uint32_t>(cut)),
+                           dim3(Tile::kThreads), list, 0, stream);
+  } else {
     constexpr uint32_t kBlocksOfTile = Tile::kRows * Tile::kCols / (kBlockRows * kBlockCols);
-    if (e == hipSuccess && cut > 0)
-      e = hipLaunchKernel(reinterpret_cast<const void*>(&product_join_kernel<Tile, E>),
-                          dim3(static_cast<uint32_t>(cut), kBlocksOfTile / kJoinWaves), dim3(64 * kJoinWaves), list, 0, stream);
+    return hipLaunchKernel(reinterpret_cast<const void*>(&product_join_kernel<Tile, E>),
+                           dim3(static_cast<uint32_t>(cut), kBlocksOfTile / kJoinWaves), dim3(64 * kJoinWaves), list, 0, stream);
   }
-  return e;
 }
 
 // Whether the launch is better off in tiles of 256 x 256: by the steps that a CU takes.  A CU
@@ -730,7 +797,12 @@ bool large_tiles(const Launch<E>& all) {
 
 template <bool BF16, class E>
 hipError_t launch_products(Launch<E>& all, const Sums& sums, hipStream_t stream) {
-  return large_tiles(all) ? launch_tiles<Tile256, BF16, E>(all, sums, stream) : launch_tiles<Tile128, BF16, E>(all, sums, stream);
+  int cut = 0;
+  const bool large = large_tiles(all);
+  const int groups = large ? deal<256>(all, sums, &cut) : deal<128>(all, sums, &cut);
+  if (groups == 0) return hipSuccess;
+  if (groups < 0) return hipErrorInvalidValue;
+  return large ? launch_tiles<Tile256, BF16, E>(all, groups, cut, stream) : launch_tiles<Tile128, BF16, E>(all, groups, cut, stream);
 }
 
 #endif

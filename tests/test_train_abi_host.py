@@ -201,4 +201,4 @@ def test_rounds_bound_the_workspace(lib):
         a.nmatrices = k
         sizes.append(need(lib.daso_muon_workspace, a)[1])
     assert sizes[0] < sizes[1] < sizes[2] and sizes[2] == sizes[3] == sizes[4]
-    assert sizes[2] < (1 << 27) * 29 + 65 * MB
+    assert sizes[2] < (1 << 27) * 29 + 260 * MB
