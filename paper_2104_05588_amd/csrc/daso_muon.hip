@@ -19,6 +19,7 @@
 // in 32 bits (`rest`) and put into the products' epilogues, at the cost of one multiply-add.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <new>
 
@@ -376,6 +377,277 @@ __global__ __launch_bounds__(256) void normalise_kernel(LayOut a) {
   planes_tile<T, false>(p, batch, static_cast<int>((t % per) / across), static_cast<int>(t % across), scale, lds);
 }
 
+// ------------------------------------------------------------------------- small matrices
+// All steps of a matrix whose shorter side is at most 64, in one workgroup of 8 wavefronts, from its
+// norm to its result: sixteen launches of a few microseconds each become one.
+//
+// X (m x n, m padded to 64) stays in registers in 32 bits, in the layout in which the matrix
+// instructions leave X' = a X + B X: a wavefront has every eighth group of 16 columns.  Its planes,
+// for the products, are in LDS: one layout serves both X X^T, whose operands run along n, and B X,
+// whose operand runs along m and is read with the transposing LDS loads.  Rows are padded by 16 bytes,
+// which makes their distance an odd number of 16-byte pieces: 16 lanes that read one piece of 16
+// rows meet no bank twice.  The gram matrix and B take turns in one place of LDS, 2 of their 16
+// tiles a wavefront, and stay in 32 bits in the registers of the wavefront that computed them.
+// With one plane (bf16 results), what the planes' diagonals lack is kept as above.
+using host::kGramStride;
+using host::kSmallGroups;
+using host::kSmallM;
+using host::small_stride;
+constexpr int kSmallThreads = 512;
+
+struct SmallArgs {
+  int32_t groups;
+  int32_t first[host::kRoundGroups + 1];  // workgroups of each group of matrices
+  struct {
+    const void* src;
+    int64_t stride, batch_stride;
+    int32_t rows, cols;
+    LastOut::Params out;
+  } of[host::kRoundGroups];
+  int32_t steps;
+  float eps;
+  float coefficients[3 * DASO_MAX_SCHULZ_STEPS];
+};
+
+// Four values down a column: the transposing LDS load.  The lanes of a group of 16 give the places of
+// four rows, four lanes a row, of 16 neighbouring values; lane l gets those of column l.
+typedef short short4v __attribute__((ext_vector_type(4)));
+__device__ inline product::half4 read_turned(const char* p) {
+  return __builtin_bit_cast(product::half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)DASO_LDS(p)));
+}
+
+template <class T, bool FULL>
+__global__ __launch_bounds__(kSmallThreads, 2) void small_kernel(SmallArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  int g = 0;
+  while (g + 1 < a.groups && static_cast<int>(blockIdx.x) >= a.first[g + 1]) ++g;
+  const auto& of = a.of[g];
+  const int batch = static_cast<int>(blockIdx.x) - a.first[g];
+  const bool tall = of.rows > of.cols;
+  const int m = tall ? of.cols : of.rows, n = tall ? of.rows : of.cols;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, kq = lane >> 4;
+  const int stride = small_stride(n), plane = kSmallM * stride, n_steps = (n + 63) / 64;
+  char* x_lds = lds;
+  char* gram = lds + (FULL ? 2 : 1) * plane;  // planes of kSmallM * kGramStride
+  float* rest = (float*)(gram + (FULL ? 2 : 1) * kSmallM * kGramStride);  // 64; and 8 doubles behind it
+  double* sums = (double*)(rest + kSmallM);
+
+  // X: x[i][j] has row j * 16 + r16 of columns (wave + 8 i) * 16 + kq * 4 ..
+  f4 x[kSmallGroups][4];
+  const T* src = (const T*)of.src + batch * of.batch_stride;
+  // four neighbouring columns at a time, where they lie so: one by one, each load would touch 64 lines
+  const bool wide = !tall && ((reinterpret_cast<uintptr_t>(src) | (of.stride * sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
+#pragma unroll
+  for (int i = 0; i < kSmallGroups; ++i) {
+    const int col = (wave + 8 * i) * 16 + kq * 4;
+    if ((wave + 8 * i) * 16 >= n) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = j * 16 + r16;
+      if (wide && col + 4 <= n) {
+        x[i][j] = (f4)0.0f;
+        if (row < m) x[i][j] = load4(src + row * of.stride + col);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[i][j][e] = row < m && col + e < n ? load1(src + (tall ? (col + e) * of.stride + row : row * of.stride + col + e)) : 0.0f;
+      }
+    }
+  }
+  double square = 0;
+#pragma unroll
+  for (int i = 0; i < kSmallGroups; ++i) {
+    if ((wave + 8 * i) * 16 >= n) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) square += static_cast<double>(x[i][j][e]) * x[i][j][e];
+  }
+  const float scale = static_cast<float>(kScale / (sqrt(group_sum(square, sums)) + a.eps));
+#pragma unroll
+  for (int i = 0; i < kSmallGroups; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[i][j] *= scale;
+  // columns between n and the last step's end are read as zeros
+  for (int k = threadIdx.x; k < kSmallM * 8; k += kSmallThreads) {
+    const int row = k >> 3, at = (n_steps * 64 - 64 + (k & 7) * 8) * 2;
+#pragma unroll
+    for (int p = 0; p < (FULL ? 2 : 1); ++p) *(half8*)(x_lds + p * plane + row * stride + at) = (half8)(_Float16)0.0f;
+  }
+  __syncthreads();
+
+  const auto put = [&](char* to, int next_plane, const f4& v) {
+    product::half4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      _Float16 hi, lo;
+      product::split(v[e], &hi, &lo);
+      h[e] = hi, l[e] = lo;
+    }
+    *(product::half4*)to = h;
+    if constexpr (FULL) *(product::half4*)(to + next_plane) = l;
+    return h;
+  };
+  const auto multiply = [&](const half8 (&b)[FULL ? 2 : 1], const half8 (&c)[FULL ? 2 : 1], f4 acc) {
+    if constexpr (FULL) {
+      acc = product::mfma<false>(b[1], c[0], acc);
+      acc = product::mfma<false>(b[0], c[1], acc);
+    }
+    return product::mfma<false>(b[0], c[0], acc);
+  };
+  // tiles (wave / 2, wave % 2 * 2) and the one to its right of a square product of rows in LDS
+  const int ti = wave >> 1, tj = (wave & 1) * 2;
+  const auto square_product = [&](const char* rows, int row_stride, int next_plane, int k_steps, f4 (&c)[2]) {
+    c[0] = c[1] = (f4)0.0f;
+    // 64 of the contraction at a time: what is read of LDS is on its way together
+    for (int k = 0; k < k_steps; ++k) {
+      half8 left[2][FULL ? 2 : 1], right[2][2][FULL ? 2 : 1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int p = 0; p < (FULL ? 2 : 1); ++p) {
+          const char* at = rows + p * next_plane + k * 128 + h * 64 + kq * 16;
+          left[h][p] = *(const half8*)(at + (ti * 16 + r16) * row_stride);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) right[h][t][p] = *(const half8*)(at + ((tj + t) * 16 + r16) * row_stride);
+        }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) c[t] = multiply(right[h][t], left[h], c[t]);
+    }
+  };
+  // a square's tiles into their place, and what the diagonal's one plane lacks
+  const auto put_square = [&](const f4 (&c)[2]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int row = ti * 16 + r16, col = (tj + t) * 16 + kq * 4;
+      const product::half4 h = put(gram + row * kGramStride + col * 2, kSmallM * kGramStride, c[t]);
+      if constexpr (!FULL) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + e == row) rest[row] = c[t][e] - static_cast<float>(h[e]);
+      }
+    }
+  };
+
+  for (int step = 0; step < a.steps; ++step) {
+    const float ca = a.coefficients[3 * step], cb = a.coefficients[3 * step + 1], cc = a.coefficients[3 * step + 2];
+#pragma unroll
+    for (int i = 0; i < kSmallGroups; ++i) {
+      if ((wave + 8 * i) * 16 >= n) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) put(x_lds + (j * 16 + r16) * stride + ((wave + 8 * i) * 16 + kq * 4) * 2, plane, x[i][j]);
+    }
+    __syncthreads();
+    f4 gram_c[2], c[2];
+    square_product(x_lds, stride, plane, n_steps, gram_c);
+    gram_c[0] *= kUnscale, gram_c[1] *= kUnscale;
+    put_square(gram_c);
+    __syncthreads();
+    square_product(gram, kGramStride, kSmallM * kGramStride, 1, c);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int row = ti * 16 + r16, col = (tj + t) * 16 + kq * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float more = FULL ? 0.0f : rest[row] + rest[col + e];
+        c[t][e] = fmaf(cb, gram_c[t][e], cc * kUnscale * fmaf(more, gram_c[t][e], c[t][e]));
+      }
+    }
+    __syncthreads();  // the gram matrix and its rest have been read
+    put_square(c);
+    __syncthreads();
+    half8 left[2][4][FULL ? 2 : 1];
+    float more[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      more[j] = FULL ? 0.0f : rest[j * 16 + r16];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int p = 0; p < (FULL ? 2 : 1); ++p)
+          left[k][j][p] = *(const half8*)(gram + p * kSmallM * kGramStride + (j * 16 + r16) * kGramStride + k * 64 + kq * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < kSmallGroups; ++i) {
+      const int col = (wave + 8 * i) * 16;
+      if (col >= n) continue;
+      f4 y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = (f4)0.0f;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        half8 right[FULL ? 2 : 1];  // column r16 of X, rows k * 32 + kq * 8 ..
+#pragma unroll
+        for (int p = 0; p < (FULL ? 2 : 1); ++p) {
+          const char* at = x_lds + p * plane + (k * 32 + kq * 8 + (r16 >> 2)) * stride + (col + (r16 & 3) * 4) * 2;
+          const product::half4 lo = read_turned(at), hi = read_turned(at + 4 * stride);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) right[p][e] = lo[e], right[p][4 + e] = hi[e];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = multiply(right, left[k][j], y[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][j][e] = fmaf(ca, x[i][j][e], kUnscale * fmaf(more[j], x[i][j][e], y[j][e]));
+    }
+    __syncthreads();  // X's planes and B have been read
+  }
+
+  const LastOut::Params& out = of.out;
+  int64_t to = out.out_batch * batch, ld = out.out_ld;
+  float lr = 0.0f;
+  if (out.kind == LastOut::kStep) {
+    const Entry e = out.table[batch];
+    to = e.start, ld = of.cols, lr = e.step;
+  }
+  const int64_t esz = out.kind == LastOut::kBf16 ? 2 : 4;
+  const uintptr_t base = reinterpret_cast<uintptr_t>(out.kind == LastOut::kStep ? (void*)out.params : out.out);
+  const bool wide_out = !tall && ((base + to * esz) & (4 * esz - 1)) == 0 && ((to | ld) & 3) == 0;
+#pragma unroll
+  for (int i = 0; i < kSmallGroups; ++i) {
+    const int col = (wave + 8 * i) * 16 + kq * 4;
+    if ((wave + 8 * i) * 16 >= n) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = j * 16 + r16;
+      if (row >= m) continue;
+      f4 v = x[i][j] * kUnscale;
+      if (wide_out && col + 4 <= n) {
+        const int64_t at = to + row * ld + col;
+        if (out.kind == LastOut::kStep) {
+          v = load4(out.params + at) * out.keep - lr * v;
+          store4(out.params + at, v);
+          if (out.wire != nullptr) store4(out.wire + at, v);
+        } else if (out.kind == LastOut::kF32) {
+          store4((float*)out.out + at, v);
+        } else {
+          store4((uint16_t*)out.out + at, v);
+        }
+        continue;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (col + e >= n) continue;
+        const int64_t at = to + (tall ? (col + e) * ld + row : row * ld + col + e);
+        if (out.kind == LastOut::kStep) {
+          const float p = out.params[at] * out.keep - lr * v[e];
+          out.params[at] = p;
+          if (out.wire != nullptr) out.wire[at] = to_bf16(p);
+        } else if (out.kind == LastOut::kF32) {
+          ((float*)out.out)[at] = v[e];
+        } else {
+          ((uint16_t*)out.out)[at] = to_bf16(v[e]);
+        }
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------------------------- host
 _Float16* plane(char* ws, size_t at) { return reinterpret_cast<_Float16*>(ws + at); }
 
@@ -507,6 +779,57 @@ hipError_t schulz_steps(const SchulzRound& r, char* ws, int32_t steps, const flo
   return hipSuccess;
 }
 
+// The small matrices of a round, their groups' Params as for the products.
+template <class T>
+hipError_t small_steps(const SchulzRound& r, char* ws, const T* src, int64_t src_batch, int64_t src_stride, int32_t steps,
+                       const float* coefficients, float eps, bool full, const std::vector<LastOut::Params>& last,
+                       hipStream_t stream) {
+  SmallArgs a = {};
+  a.steps = steps, a.eps = eps;
+  for (int32_t i = 0; i < 3 * steps; ++i) a.coefficients[i] = coefficients[i];
+  int lds_bytes = 0;
+  for (size_t k = 0; k < r.groups.size(); ++k) {
+    const SchulzGroup& g = r.groups[k];
+    if (!g.small) continue;
+    auto& of = a.of[a.groups];
+    of.src = src != nullptr ? (const void*)src : (const void*)(ws + g.source);
+    of.stride = src != nullptr ? src_stride : g.cols;
+    of.batch_stride = src != nullptr ? src_batch : g.rows * g.cols;
+    of.rows = static_cast<int32_t>(g.rows), of.cols = static_cast<int32_t>(g.cols);
+    of.out = last[k];
+    a.first[a.groups + 1] = a.first[a.groups] + g.count;
+    ++a.groups;
+    lds_bytes = std::max(lds_bytes, host::small_lds(static_cast<int>(std::max(g.rows, g.cols)), full));
+  }
+  if (a.groups == 0) return hipSuccess;
+  const void* kernel = full ? reinterpret_cast<const void*>(&small_kernel<T, true>) : reinterpret_cast<const void*>(&small_kernel<T, false>);
+  static std::atomic<uint64_t> allowed[2];
+  const hipError_t e = product::allow_lds(kernel, 160 * 1024, allowed[full ? 1 : 0]);
+  if (e != hipSuccess) return e;
+  void* list[] = {&a};
+  return hipLaunchKernel(kernel, dim3(static_cast<uint32_t>(a.first[a.groups])), dim3(kSmallThreads), list,
+                         static_cast<size_t>(lds_bytes), stream);
+}
+
+// A round from its sources to its results.  parts: the sums of squares of a matrix.
+template <class T>
+hipError_t run_round(const SchulzRound& r, char* ws, const T* src, int64_t src_batch, int64_t src_stride, int32_t parts,
+                     int32_t steps, const float* coefficients, float eps, bool full, const std::vector<LastOut::Params>& last,
+                     hipStream_t stream) {
+  hipError_t e = small_steps<T>(r, ws, src, src_batch, src_stride, steps, coefficients, eps, full, last, stream);
+  SchulzRound large = r;
+  large.groups.clear();
+  std::vector<LastOut::Params> large_last;
+  for (size_t k = 0; k < r.groups.size(); ++k) {
+    if (r.groups[k].small) continue;
+    large.groups.push_back(r.groups[k]);
+    large_last.push_back(last[k]);
+  }
+  if (e != hipSuccess || large.groups.empty()) return e;
+  e = normalise<T>(large, ws, src, src_batch, src_stride, parts, eps, full, stream);
+  return e == hipSuccess ? schulz_steps(large, ws, steps, coefficients, full, large_last, stream) : e;
+}
+
 size_t most_bytes(const std::vector<SchulzRound>& rounds) {
   size_t most = 0;
   for (const SchulzRound& r : rounds) most = r.bytes > most ? r.bytes : most;
@@ -532,17 +855,17 @@ hipError_t orthogonalize_round(const daso_orthogonalize_args& s, const SchulzRou
   const int64_t rows = s.rows;
   const int32_t parts = static_cast<int32_t>(std::min<int64_t>(parts_of(rows * s.cols), rows));
   double* sums = reinterpret_cast<double*>(ws + host::kRoundMatrices * sizeof(Entry));
-  hipError_t e = launch(&squares_kernel<T>, dim3(parts, g.count), dim3(256), stream, src, s.src_batch_stride, s.src_stride,
-                        static_cast<int32_t>(rows), static_cast<int32_t>(s.cols), sums);
-  if (e != hipSuccess) return e;
+  if (!g.small) {
+    const hipError_t e = launch(&squares_kernel<T>, dim3(parts, g.count), dim3(256), stream, src, s.src_batch_stride, s.src_stride,
+                                static_cast<int32_t>(rows), static_cast<int32_t>(s.cols), sums);
+    if (e != hipSuccess) return e;
+  }
   const bool full = s.out_type == DASO_TYPE_F32;
-  e = normalise<T>(r, ws, src, s.src_batch_stride, s.src_stride, parts, s.eps, full, stream);
-  if (e != hipSuccess) return e;
   LastOut::Params last = {};
   last.kind = full ? LastOut::kF32 : LastOut::kBf16;
   last.out = static_cast<char*>(s.out) + at * s.out_batch_stride * static_cast<int64_t>(host::bytes_of(s.out_type));
   last.out_ld = s.out_stride, last.out_batch = s.out_batch_stride;
-  return schulz_steps(r, ws, s.steps, s.coefficients, full, {last}, stream);
+  return run_round<T>(r, ws, src, s.src_batch_stride, s.src_stride, parts, s.steps, s.coefficients, s.eps, full, {last}, stream);
 }
 
 hipError_t muon_round(const daso_muon_args& s, const SchulzRound& r, hipStream_t stream) {
@@ -574,8 +897,6 @@ hipError_t muon_round(const daso_muon_args& s, const SchulzRound& r, hipStream_t
   const int32_t parts = parts_of(most);
   hipError_t e = launch(&momentum_kernel, dim3(parts, t.count), dim3(256), stream, a, t);
   if (e != hipSuccess) return e;
-  e = normalise<float>(r, ws, nullptr, 0, 0, parts, s.eps, true, stream);
-  if (e != hipSuccess) return e;
   std::vector<LastOut::Params> last(r.groups.size());
   for (int32_t k = 0; k < t.groups; ++k) {
     LastOut::Params& p = last[k];
@@ -585,7 +906,7 @@ hipError_t muon_round(const daso_muon_args& s, const SchulzRound& r, hipStream_t
     p.params = s.params, p.wire = s.wire;
     p.keep = 1.0f - s.lr * s.weight_decay;
   }
-  return schulz_steps(r, ws, s.steps, s.coefficients, true, last, stream);
+  return run_round<float>(r, ws, nullptr, 0, 0, parts, s.steps, s.coefficients, s.eps, true, last, stream);
 }
 
 }  // namespace
@@ -600,7 +921,7 @@ int daso_orthogonalize_workspace(const daso_orthogonalize_args* args, size_t* by
   const int rc = daso::host::check_orthogonalize_sizes(*args);
   if (rc != DASO_OK) return rc;
   try {
-    *bytes = daso::most_bytes(daso::host::plan_rounds(daso::shapes_of(*args), false));
+    *bytes = daso::most_bytes(daso::host::plan_rounds(daso::shapes_of(*args), false, args->out_type == DASO_TYPE_F32));
   } catch (const std::bad_alloc&) {
     return DASO_EHIP;
   }
@@ -613,7 +934,7 @@ int daso_orthogonalize(const daso_orthogonalize_args* args, hipStream_t stream) 
   int rc = daso::host::check_orthogonalize(s);
   if (rc != DASO_OK || s.batch == 0 || s.rows == 0 || s.cols == 0) return rc;
   try {
-    const std::vector<SchulzRound> rounds = daso::host::plan_rounds(daso::shapes_of(s), false);
+    const std::vector<SchulzRound> rounds = daso::host::plan_rounds(daso::shapes_of(s), false, s.out_type == DASO_TYPE_F32);
     if ((rc = daso::host::check_workspace(s.workspace, s.workspace_bytes, daso::most_bytes(rounds))) != DASO_OK) return rc;
     if ((rc = daso::current_device(stream)) != DASO_OK) return rc;
     for (const SchulzRound& r : rounds) {
@@ -632,7 +953,7 @@ int daso_muon_workspace(const daso_muon_args* args, size_t* bytes) {
   try {
     const int rc = daso::host::check_muon_sizes(*args);
     if (rc != DASO_OK) return rc;
-    *bytes = daso::most_bytes(daso::host::plan_rounds(daso::shapes_of(*args), true));
+    *bytes = daso::most_bytes(daso::host::plan_rounds(daso::shapes_of(*args), true, true));
   } catch (const std::bad_alloc&) {
     return DASO_EHIP;
   }
@@ -645,7 +966,7 @@ int daso_muon_step(const daso_muon_args* args, hipStream_t stream) {
   try {
     int rc = daso::host::check_muon(s);
     if (rc != DASO_OK || s.n == 0 || s.nmatrices == 0) return rc;
-    const std::vector<SchulzRound> rounds = daso::host::plan_rounds(daso::shapes_of(s), true);
+    const std::vector<SchulzRound> rounds = daso::host::plan_rounds(daso::shapes_of(s), true, true);
     if ((rc = daso::host::check_workspace(s.workspace, s.workspace_bytes, daso::most_bytes(rounds))) != DASO_OK) return rc;
     if ((rc = daso::current_device(stream)) != DASO_OK) return rc;
     for (const SchulzRound& r : rounds)

@@ -56,6 +56,15 @@ __device__ inline void store8(uint16_t* p, const float (&v)[8]) {
   *(us8*)p = a;
 }
 
+// Four, from a place aligned to four elements.
+__device__ inline f4v load4(const float* p) { return *(const f4v*)p; }
+__device__ inline f4v load4(const uint16_t* p) {
+  const us4 a = *(const us4*)p;
+  return f4v{widen_bf16(a[0]), widen_bf16(a[1]), widen_bf16(a[2]), widen_bf16(a[3])};
+}
+__device__ inline void store4(float* p, const f4v& v) { *(f4v*)p = v; }
+__device__ inline void store4(uint16_t* p, const f4v& v) { *(us4*)p = us4{to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3])}; }
+
 // Sums over a wavefront, the same in every lane.
 template <class T>
 __device__ inline T wave_sum(T v) {

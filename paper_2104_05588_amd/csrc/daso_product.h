@@ -751,20 +751,24 @@ int deal(Launch<E>& all, const Sums& sums, int* cut) {
   return all.across * 8;
 }
 
-template <class Tile, bool BF16, class E>
-hipError_t launch_tiles(Launch<E>& all, int groups, int cut, hipStream_t stream) {
-  auto* kernel = product_kernel<Tile, BF16, E>;
-  // once a device, before the first launch there
-  static std::atomic<uint64_t> allowed{0};
+// Lets a kernel have more than 64 KB of LDS: once a device, before its first launch there.
+inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   const uint64_t bit = uint64_t(1) << (dev & 63);
-  if (dev >= 64 || (allowed.load(std::memory_order_relaxed) & bit) == 0) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Tile::kLds);
-    if (e != hipSuccess) return e;
-    allowed.fetch_or(bit, std::memory_order_relaxed);
-  }
+  if (dev < 64 && (done.load(std::memory_order_relaxed) & bit) != 0) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+template <class Tile, bool BF16, class E>
+hipError_t launch_tiles(Launch<E>& all, int groups, int cut, hipStream_t stream) {
+  auto* kernel = product_kernel<Tile, BF16, E>;
+  static std::atomic<uint64_t> allowed{0};
+  hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), Tile::kLds, allowed);
+  if (e != hipSuccess) return e;
   void* list[] = {&all};
   e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(static_cast<uint32_t>(groups)), dim3(Tile::kThreads), list,
                       Tile::kLds, stream);

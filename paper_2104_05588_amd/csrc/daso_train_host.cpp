@@ -222,7 +222,7 @@ int check_muon(const daso_muon_args& s) {
   return check_alias({flat(s.params, s.n, 4), flat(s.momentum, s.n, 4), flat(s.wire, s.n, 2)}, inputs, -1);
 }
 
-std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with_source) {
+std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with_source, bool full) {
   // shapes in order of first appearance, each with its matrices
   std::map<std::pair<int64_t, int64_t>, size_t> at;
   std::vector<std::pair<Shape, std::vector<int32_t>>> kinds;
@@ -239,7 +239,9 @@ std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with
   int64_t held = 0;
   for (const auto& kind : kinds) {
     const Shape& s = kind.first;
-    const int64_t m = padded(std::min(s.rows, s.cols)), n = padded(std::max(s.rows, s.cols)), each = m * n;
+    const int64_t m = padded(std::min(s.rows, s.cols)), n = padded(std::max(s.rows, s.cols));
+    const bool small = is_small(std::min(s.rows, s.cols), std::max(s.rows, s.cols), full);
+    const int64_t each = small ? 1024 : m * n;  // (small ones hold no planes)
     for (size_t done = 0; done < kind.second.size();) {
       int64_t room = 0;
       if (!rounds.empty() && rounds.back().groups.size() < size_t(kRoundGroups))
@@ -251,7 +253,7 @@ std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with
       }
       SchulzRound& r = rounds.back();
       SchulzGroup g = {};
-      g.rows = s.rows, g.cols = s.cols, g.m = m, g.n = n, g.tall = s.rows > s.cols;
+      g.rows = s.rows, g.cols = s.cols, g.m = m, g.n = n, g.tall = s.rows > s.cols, g.small = small;
       g.count = static_cast<int32_t>(std::min<int64_t>(room, int64_t(kind.second.size() - done)));
       g.first = static_cast<int32_t>(r.matrices.size());
       for (int32_t k = 0; k < g.count; ++k) r.matrices.push_back(kind.second[done + size_t(k)]);
@@ -269,6 +271,7 @@ std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with
     };
     for (SchulzGroup& g : r.groups) {
       if (with_source) g.source = take(4 * g.rows * g.cols * g.count);
+      if (g.small) continue;
       for (int b = 0; b < 2; ++b)
         for (int p = 0; p < 2; ++p) g.x[b][p] = take(2 * g.m * g.n * g.count), g.xt[b][p] = take(2 * g.m * g.n * g.count);
       for (int p = 0; p < 2; ++p) g.gram[p] = take(2 * g.m * g.m * g.count), g.poly[p] = take(2 * g.m * g.m * g.count);
@@ -277,12 +280,13 @@ std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with
     // steps of the largest of a step's products, in tiles of 128 and three segments
     int64_t gram = 0, poly = 0, next = 0;
     for (const SchulzGroup& g : r.groups) {
+      if (g.small) continue;
       const int64_t m = (g.m + 127) / 128, n = (g.n + 127) / 128;
       gram += g.count * (m * (m + 1) / 2) * 3 * (g.n / 64);
       poly += g.count * (m * (m + 1) / 2) * 3 * (g.m / 64);
       next += g.count * (m * n) * 3 * (g.m / 64);
     }
-    r.sums_bytes = sums_bytes(std::max({gram, poly, next}));
+    r.sums_bytes = next > 0 ? sums_bytes(std::max({gram, poly, next})) : 0;
     r.sums = take(static_cast<int64_t>(r.sums_bytes));
     r.bytes = to;
   }

@@ -46,6 +46,7 @@ struct SchulzGroup {
   int64_t rows, cols;
   int64_t m, n;           // padded
   bool tall;              // X is the transpose
+  bool small;             // all steps in one workgroup: no planes in the workspace
   int32_t count;          // matrices
   int32_t first;          // place of the first among the round's matrices
   // byte offsets in the workspace; planes: [0] hi, [1] lo
@@ -71,8 +72,19 @@ constexpr size_t kRoundTables = size_t(kRoundMatrices) * (16 + 8 * kSumParts);  
 struct Shape {
   int64_t rows, cols;
 };
-// Rounds over the given matrices, in order of first appearance of their shapes.
-std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with_source);
+// Rounds over the given matrices, in order of first appearance of their shapes.  full: products in 22 bits.
+std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with_source, bool full);
+
+// The matrices that one workgroup takes (daso_muon.hip): what they need of its LDS, and whether they fit.
+constexpr int kSmallM = 64, kSmallGroups = 5;                        // m, and groups of 128 columns of n, at most
+constexpr int kGramStride = kSmallM * 2 + 16;                        // bytes a row of the gram matrix
+constexpr int small_stride(int n) { return (n + 63) / 64 * 128 + 16; }  // bytes a row of X
+constexpr int small_lds(int n, bool full) {
+  return (full ? 2 : 1) * (kSmallM * small_stride(n) + kSmallM * kGramStride) + 1024;
+}
+constexpr bool is_small(int64_t m, int64_t n, bool full) {
+  return m <= kSmallM && n <= kSmallGroups * 128 && small_lds(static_cast<int>(n), full) <= 160 * 1024;
+}
 
 }  // namespace host
 }  // namespace daso
