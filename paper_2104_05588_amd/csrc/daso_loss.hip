@@ -4,7 +4,7 @@
 // Forward: one product hidden weight^T, whose epilogue reduces each 256 (or 128) columns of a
 // row to their maximum and their sum of exponentials; a second kernel joins them.
 // Backward, per piece of the vocabulary: the piece's logits again, whose epilogue turns them
-// into s (p - onehot), stored straight and transposed as 16-bit planes; then dhidden += dz weight
+// into s (p - onehot), stored as 16-bit planes; then dhidden += dz weight
 // and dweight = dz^T hidden, in one launch.  6 N V d multiply-adds at least, 8 with the logits taken
 // twice: keeping them would cost N V 4 bytes written and read, which takes as long as the
 // product at d = 1024 and grows the memory by N V.
@@ -285,13 +285,13 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* parts, int32_t 
 }
 
 // ------------------------------------------------------------------------- backward epilogues
-// dz of a piece's columns as planes, straight and transposed; columns beyond the vocabulary are zero.
+// dz of a piece's columns as planes; columns beyond the vocabulary are zero.
 struct ProbOut {
   static constexpr auto kKind = product::kBlocks;
   struct Params {
     const Row* rows;
-    _Float16 *hi, *lo, *t_hi, *t_lo;  // any may be null but hi's or t_hi's
-    int64_t ld, t_ld;
+    _Float16 *hi, *lo;  // lo may be null
+    int64_t ld;
     int32_t first, columns, padded;  // the piece: its first class, its classes, its columns with padding
     int32_t padded_rows;             // tokens with padding: the planes are contracted over both
     const float *inv_a, *inv_b;
@@ -301,7 +301,7 @@ struct ProbOut {
     const int r16 = lane & 15, kq = lane >> 4;
     char* lo = hi + product::kStagePlane;
     const float inv = out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f;
-    const bool two = out.lo != nullptr || out.t_lo != nullptr;
+    const bool two = out.lo != nullptr;
     Row rows[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) rows[i] = out.rows[row0 + i * 16 + r16];
@@ -333,19 +333,13 @@ struct ProbOut {
         *(half8*)(to + int64_t(row0 + r) * out.ld + col0 + c) = *(const half8*)(plane + product::plane_at(r, c));
       }
     };
-    const auto turned = [&](const char* plane, _Float16* to) {
-      product::by_columns(plane, lane, [&](int c, int r, half8 v) {
-        *(half8*)(to + int64_t(col0 + c) * out.t_ld + row0 + r) = v;
-      });
-    };
-    if (out.hi != nullptr) straight(hi, out.hi);
-    if (out.lo != nullptr) straight(lo, out.lo);
-    if (out.t_hi != nullptr) turned(hi, out.t_hi);
-    if (out.t_lo != nullptr) turned(lo, out.t_lo);
+    straight(hi, out.hi);
+    if (two) straight(lo, out.lo);
   }
 };
 
-// A gradient: (C * grad * inv / kProbScale) [+ sum], as the sum so far or as the result.
+// A gradient: (C * grad * inv / kProbScale) [+ sum], as the sum so far or as the result; or, where
+// `turned`, C^T of that.
 struct GradOut {
   static constexpr auto kKind = product::kStaged;
   struct Params {
@@ -355,7 +349,8 @@ struct GradOut {
     void* out;
     int64_t ld;
     int32_t bf16;
-    int32_t rows, cols;
+    int32_t rows, cols;  // of what is written
+    int32_t turned;
   };
   struct Inputs {
     float before[product::kPasses][8];
@@ -372,6 +367,26 @@ struct GradOut {
   template <class F>
   __device__ static void block(const Params& p, const product::Place&, int row, int col, char* stage, int lane, const Inputs& in,
                                F next) {
+    if (p.turned) {
+      // 8 columns of C in a pass, 8 lanes a column, 8 rows of it each
+      const int cc = row + (lane & 7) * 8, left = p.cols - cc;
+      const bool wide = ((reinterpret_cast<uintptr_t>(p.out) | (p.ld * (p.bf16 ? 2 : 4))) & 15) == 0 && left >= 8;
+      float v[4][8];
+#pragma unroll
+      for (int pass = 0; pass < 4; ++pass)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = (lane & 7) * 8 + i, c = pass * 8 + (lane >> 3);
+          v[pass][i] = *(const float*)(stage + r * 128 + (((c >> 2) ^ ((r >> 1) & 7)) * 16) + (c & 3) * 4) * in.inv * in.factor;
+        }
+      next();
+#pragma unroll
+      for (int pass = 0; pass < 4; ++pass) {
+        const int rr = col + pass * 8 + (lane >> 3);
+        if (rr < p.rows && left > 0) store_run(p, rr * p.ld + cc, left, wide, v[pass]);
+      }
+      return;
+    }
     const int r0 = row + product::pass_row(0, lane), cc = col + product::pass_col(lane), left = p.cols - cc;
     const bool wide = ((reinterpret_cast<uintptr_t>(p.out) | (p.ld * (p.bf16 ? 2 : 4))) & 15) == 0 && left >= 8;
     float v[product::kPasses][8];
@@ -388,19 +403,22 @@ struct GradOut {
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass) {
       if (r0 + pass * product::kPassRows >= p.rows || left <= 0) continue;
-      const int64_t to = (r0 + pass * product::kPassRows) * p.ld + cc;
-      float* const o32 = (float*)p.out + to;
-      uint16_t* const o16 = (uint16_t*)p.out + to;
-      if (wide) {
-        if (p.bf16) store8(o16, v[pass]);
-        else store8(o32, v[pass]);
-      } else {
+      store_run(p, (r0 + pass * product::kPassRows) * p.ld + cc, left, wide, v[pass]);
+    }
+  }
+  // Eight neighbouring values, or the `left` of them that there are.
+  __device__ static void store_run(const Params& p, int64_t to, int left, bool wide, const float (&v)[8]) {
+    float* const o32 = (float*)p.out + to;
+    uint16_t* const o16 = (uint16_t*)p.out + to;
+    if (wide) {
+      if (p.bf16) store8(o16, v);
+      else store8(o32, v);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (i >= left) continue;
-          if (p.bf16) o16[i] = to_bf16(v[pass][i]);
-          else o32[i] = v[pass][i];
-        }
+      for (int i = 0; i < 8; ++i) {
+        if (i >= left) continue;
+        if (p.bf16) o16[i] = to_bf16(v[i]);
+        else o32[i] = v[i];
       }
     }
   }
@@ -425,7 +443,7 @@ struct Plan {
   int64_t n_p, d_p, v_p;          // padded tokens, features, classes
   int64_t piece, pieces;          // classes of a piece (but the last), pieces
   bool f32, copy_h, copy_w;       // operands of the logits that are copied
-  size_t scales, sums, sums_bytes, parts, at_target, rows, h[2], w[2], ht[2], wt[2], p[2], pt[2], sum;
+  size_t scales, sums, sums_bytes, parts, at_target, rows, h[2], w[2], ht[2], wp[2], p[2], sum;
   size_t bytes;
 };
 
@@ -466,10 +484,10 @@ Plan plan_of(const daso_loss_args& s, bool backward) {
     q.rows = take(sizeof(Row) * q.n_p);
     for (int i = 0; i < planes; ++i) {
       q.ht[i] = take(2 * q.n_p * q.d_p);
-      q.wt[i] = take(2 * q.v_p * q.d_p);
+      q.wp[i] = q.f32 ? q.w[i] : take(2 * q.v_p * q.d_p);
     }
     const int64_t width = q.pieces > 1 ? q.piece : q.v_p;
-    for (int i = 0; i < 2; ++i) q.p[i] = take(2 * q.n_p * width), q.pt[i] = take(2 * q.n_p * width);
+    for (int i = 0; i < 2; ++i) q.p[i] = take(2 * q.n_p * width);
     q.sum = take(q.pieces > 1 ? 4 * q.n_p * q.d_p : 0);
   }
   // the largest product's steps, in tiles of 128 and three segments
@@ -526,7 +544,7 @@ hipError_t prepare(const daso_loss_args& s, const Plan& q, bool backward, Operan
   }
   PrepareArgs a = {};
   const auto place = [ws](size_t at, bool wanted) { return wanted ? ws + at : nullptr; };
-  const bool ht = backward && s.dweight != nullptr, wt = backward && s.dhidden != nullptr;
+  const bool ht = backward && s.dweight != nullptr, wp = backward && s.dhidden != nullptr;
   const auto hidden = [&](bool raw, char* d0, char* d1, char* t0, char* t1) {
     add_planes(a, kHidden, raw, s.hidden, s.hidden_stride, s.tokens, s.d, q.n_p, q.d_p, d0, d1, t0, t1);
   };
@@ -534,12 +552,12 @@ hipError_t prepare(const daso_loss_args& s, const Plan& q, bool backward, Operan
     add_planes(a, kWeight, raw, s.weight, s.weight_stride, s.vocab, s.d, q.v_p, q.d_p, d0, d1, t0, t1);
   };
   if (q.f32) {
-    weight(false, ws + q.w[0], ws + q.w[1], place(q.wt[0], wt), place(q.wt[1], wt));
+    weight(false, ws + q.w[0], ws + q.w[1], nullptr, nullptr);
     hidden(false, ws + q.h[0], ws + q.h[1], place(q.ht[0], ht), place(q.ht[1], ht));
   } else {
     if (q.copy_w) weight(true, ws + q.w[0], nullptr, nullptr, nullptr);
     if (q.copy_h) hidden(true, ws + q.h[0], nullptr, nullptr, nullptr);
-    if (wt) weight(false, nullptr, nullptr, ws + q.wt[0], nullptr);
+    if (wp) weight(false, ws + q.wp[0], nullptr, nullptr, nullptr);
     if (ht) hidden(false, nullptr, nullptr, ws + q.ht[0], nullptr);
   }
   a.first[a.count + 1] = a.first[a.count];
@@ -580,8 +598,8 @@ hipError_t forward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
   out.targets = s.targets;
   out.inv_a = q.f32 ? &sc->inv[kHidden] : nullptr, out.inv_b = q.f32 ? &sc->inv[kWeight] : nullptr;
   const int64_t across = product::large_tiles(all) ? 256 : 128;
-  if (q.f32) e = product::launch_products<false>(all, sums, stream);
-  else e = product::launch_products<true>(all, sums, stream);
+  if (q.f32) e = product::launch_products<false, false>(all, sums, stream);
+  else e = product::launch_products<true, false>(all, sums, stream);
   if (e != hipSuccess) return e;
   return launch(&join_kernel, dim3(static_cast<uint32_t>((s.tokens + 31) / 32)), dim3(256), stream, (const float2*)out.parts,
                 static_cast<int32_t>((s.vocab + across - 1) / across), s.tokens, s.vocab, s.targets, s.ignore_index,
@@ -606,49 +624,49 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
     logits(prob.args[0], q, o, s.tokens, first, classes);
     ProbOut::Params& out = prob.out[0];
     out.rows = rows;
-    out.hi = dh ? at(q.p[0]) : nullptr, out.lo = dh && q.f32 ? at(q.p[1]) : nullptr;
-    out.t_hi = dw ? at(q.pt[0]) : nullptr, out.t_lo = dw && (q.f32 || dw32) ? at(q.pt[1]) : nullptr;
-    out.ld = width, out.t_ld = q.n_p;
+    // dz in two planes where a product in 22 bits reads it
+    out.hi = at(q.p[0]), out.lo = q.f32 || (dw && dw32) ? at(q.p[1]) : nullptr;
+    out.ld = width;
     out.first = static_cast<int32_t>(first), out.columns = static_cast<int32_t>(classes), out.padded = static_cast<int32_t>(width);
     out.padded_rows = static_cast<int32_t>(q.n_p);
     out.inv_a = q.f32 ? &sc->inv[kHidden] : nullptr, out.inv_b = q.f32 ? &sc->inv[kWeight] : nullptr;
-    e = q.f32 ? product::launch_products<false>(prob, sums, stream) : product::launch_products<true>(prob, sums, stream);
+    e = q.f32 ? product::launch_products<false, false>(prob, sums, stream) : product::launch_products<true, false>(prob, sums, stream);
     if (e != hipSuccess) break;
+    // dhidden = dz weight and dweight^T = hidden^T dz, both with the right operand read turned
     product::Launch<GradOut> grads = {};
     if (dh) {
       product::Args& a = grads.args[grads.count];
-      const _Float16* w0 = at(q.wt[0]) + first;
-      const _Float16* w1 = at(q.wt[1]) + first;
+      const _Float16 *w0 = at(q.wp[0]) + first * q.d_p, *w1 = at(q.wp[1]) + first * q.d_p;
       a.segments = q.f32 ? 3 : 1;
       a.a[0] = at(q.p[0]), a.b[0] = w0;
       a.a[1] = at(q.p[0]), a.b[1] = w1;
       a.a[2] = at(q.p[1]), a.b[2] = w0;
-      a.lda = width, a.ldb = q.v_p, a.steps = static_cast<int32_t>(width / 64);
-      a.M = static_cast<int32_t>(s.tokens), a.N = static_cast<int32_t>(s.d), a.batch = 1;
+      a.lda = width, a.ldb = q.d_p, a.steps = static_cast<int32_t>(width / 64);
+      a.M = static_cast<int32_t>(s.tokens), a.N = static_cast<int32_t>(q.d_p), a.batch = 1;
       GradOut::Params& g = grads.out[grads.count++];
       g.grad = &sc->to[kGrad], g.inv = &sc->inv[kWeight];
       float* sum = reinterpret_cast<float*>(ws + q.sum);
       if (k > 0) g.before = sum, g.before_ld = q.d_p;
-      g.rows = a.M, g.cols = a.N;
+      g.rows = a.M;
       if (k + 1 < q.pieces) g.out = sum, g.ld = q.d_p, g.bf16 = 0, g.cols = static_cast<int32_t>(q.d_p);
-      else g.out = s.dhidden, g.ld = s.dhidden_stride, g.bf16 = s.type == DASO_TYPE_BF16;
+      else g.out = s.dhidden, g.ld = s.dhidden_stride, g.bf16 = s.type == DASO_TYPE_BF16, g.cols = static_cast<int32_t>(s.d);
     }
     if (dw) {
       product::Args& a = grads.args[grads.count];
       // dz in one plane or two; hidden in one (exact) where it is bf16
       a.segments = q.f32 ? 3 : dw32 ? 2 : 1;
-      a.a[0] = at(q.pt[0]), a.b[0] = at(q.ht[0]);
-      a.a[1] = at(q.pt[1]), a.b[1] = at(q.ht[0]);
-      a.a[2] = at(q.pt[0]), a.b[2] = at(q.ht[1]);
-      a.lda = a.ldb = q.n_p, a.steps = static_cast<int32_t>(q.n_p / 64);
-      a.M = static_cast<int32_t>(classes), a.N = static_cast<int32_t>(s.d), a.batch = 1;
+      a.a[0] = at(q.ht[0]), a.b[0] = at(q.p[0]);
+      a.a[1] = at(q.ht[0]), a.b[1] = at(q.p[1]);
+      a.a[2] = at(q.ht[1]), a.b[2] = at(q.p[0]);
+      a.lda = q.n_p, a.ldb = width, a.steps = static_cast<int32_t>(q.n_p / 64);
+      a.M = static_cast<int32_t>(s.d), a.N = static_cast<int32_t>(width), a.batch = 1;
       GradOut::Params& g = grads.out[grads.count++];
       g.grad = &sc->to[kGrad], g.inv = &sc->inv[kHidden];
       g.out = static_cast<char*>(s.dweight) + first * s.dweight_stride * static_cast<int64_t>(host::bytes_of(s.dweight_type));
       g.ld = s.dweight_stride, g.bf16 = !dw32;
-      g.rows = a.M, g.cols = a.N;
+      g.rows = static_cast<int32_t>(classes), g.cols = a.M, g.turned = 1;
     }
-    e = product::launch_products<false>(grads, sums, stream);
+    e = product::launch_products<false, true>(grads, sums, stream);
   }
   return e;
 }

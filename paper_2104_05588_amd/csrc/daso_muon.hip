@@ -3,9 +3,7 @@
 // A step on X (m x n, m <= n) is three products: the gram matrix A = X X^T and its square,
 // both symmetric, of which only the tiles on and below the diagonal are computed and
 // stored twice, and X' = a X + B X with B = b A + c A^2.  m^2 n + m^3 + 2 m^2 n
-// multiply-adds in place of 4 m^2 n + 2 m^3.  All three are taken as A B^T with the
-// contraction contiguous, so X is kept transposed as well; the epilogue that
-// computes X' writes both.
+// multiply-adds in place of 4 m^2 n + 2 m^3.
 //
 // Numbers.  With |X|_F <= 1 at the start and the polynomial's range, entries of X, A and B stay
 // below 4 for the coefficients in use; they are stored times 2^11 as binary16.  A step
@@ -359,7 +357,7 @@ struct LayOut {
   float eps;
 };
 
-// X = u / (|u| + eps) as planes, straight and transposed.
+// X = u / (|u| + eps) as planes.
 template <class T>
 __global__ __launch_bounds__(256) void normalise_kernel(LayOut a) {
   __shared__ uint16_t lds[2][64][66];
@@ -408,13 +406,6 @@ struct SmallArgs {
   float eps;
   float coefficients[3 * DASO_MAX_SCHULZ_STEPS];
 };
-
-// Four values down a column: the transposing LDS load.  The lanes of a group of 16 give the places of
-// four rows, four lanes a row, of 16 neighbouring values; lane l gets those of column l.
-typedef short short4v __attribute__((ext_vector_type(4)));
-__device__ inline product::half4 read_turned(const char* p) {
-  return __builtin_bit_cast(product::half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)DASO_LDS(p)));
-}
 
 template <class T, bool FULL>
 __global__ __launch_bounds__(kSmallThreads, 2) void small_kernel(SmallArgs a) {
@@ -583,9 +574,7 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_kernel(SmallArgs a) {
 #pragma unroll
         for (int p = 0; p < (FULL ? 2 : 1); ++p) {
           const char* at = x_lds + p * plane + (k * 32 + kq * 8 + (r16 >> 2)) * stride + (col + (r16 & 3) * 4) * 2;
-          const product::half4 lo = read_turned(at), hi = read_turned(at + 4 * stride);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) right[p][e] = lo[e], right[p][4 + e] = hi[e];
+          right[p] = __builtin_shufflevector(product::read_turned(at), product::read_turned(at + 4 * stride), 0, 1, 2, 3, 4, 5, 6, 7);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = multiply(right, left[k][j], y[j]);
@@ -659,7 +648,7 @@ int32_t parts_of(int64_t elems) {
 // Planes of X from the sources' matrices.  src: null for the round's own copies.
 template <class T>
 hipError_t normalise(const SchulzRound& r, char* ws, const T* src, int64_t src_batch, int64_t src_stride, int32_t parts,
-                     float eps, bool full, hipStream_t stream) {
+                     float eps, bool only_step, hipStream_t stream) {
   LayOut a = {};
   a.groups = static_cast<int32_t>(r.groups.size());
   a.parts = parts;
@@ -673,14 +662,13 @@ hipError_t normalise(const SchulzRound& r, char* ws, const T* src, int64_t src_b
     p.batch_stride = src != nullptr ? src_batch : g.rows * g.cols;
     p.rows = static_cast<int32_t>(g.rows), p.cols = static_cast<int32_t>(g.cols);
     p.rows_p = static_cast<int32_t>(g.tall ? g.n : g.m), p.cols_p = static_cast<int32_t>(g.tall ? g.m : g.n);
+    // X, and for a tall matrix's last step, where that is the first, X^T, which the source then is
     for (int i = 0; i < 2; ++i) {
       uint16_t* x = reinterpret_cast<uint16_t*>(ws + g.x[0][i]);
-      uint16_t* xt = reinterpret_cast<uint16_t*>(ws + g.xt[0][i]);
-      p.d[i] = g.tall ? xt : x;
-      p.t[i] = g.tall ? x : xt;
+      if (g.tall) p.t[i] = x;
+      else p.d[i] = x;
+      if (g.tall && only_step) p.d[i] = reinterpret_cast<uint16_t*>(ws + g.xt[i]);
     }
-    // the transpose's low plane is read by products in 22 bits and by a tall matrix's last step
-    if (!full && !g.tall) p.t[1] = nullptr;
     a.first_matrix[k] = g.first;
     a.first_tile[k + 1] = a.first_tile[k] + int64_t(p.rows_p / 64) * (p.cols_p / 64) * g.count;
   }
@@ -709,17 +697,17 @@ hipError_t schulz_steps(const SchulzRound& r, char* ws, int32_t steps, const flo
     const int from = s & 1, to = from ^ 1;
     const bool end = s + 1 == steps;
     product::Launch<PlanesOut> gram = {}, poly = {}, next = {};
-    product::Launch<LastOut> final_ = {};
-    gram.count = poly.count = next.count = final_.count = groups;
+    product::Launch<LastOut> wide = {}, tall = {};
+    gram.count = poly.count = groups;
     for (int32_t k = 0; k < groups; ++k) {
       const SchulzGroup& g = r.groups[k];
       const int32_t m = static_cast<int32_t>(g.m), n = static_cast<int32_t>(g.n);
-      _Float16 *x[2], *xt[2], *y[2], *yt[2], *q[2], *w[2];
+      _Float16 *x[2], *xt[2], *y[2], *q[2], *w[2];
       for (int i = 0; i < 2; ++i) {
-        x[i] = plane(ws, g.x[from][i]), xt[i] = plane(ws, g.xt[from][i]);
-        y[i] = plane(ws, g.x[to][i]), yt[i] = plane(ws, g.xt[to][i]);
+        x[i] = plane(ws, g.x[from][i]), y[i] = plane(ws, g.x[to][i]), xt[i] = g.tall ? plane(ws, g.xt[i]) : nullptr;
         q[i] = plane(ws, g.gram[i]), w[i] = plane(ws, g.poly[i]);
       }
+      float *rest_q = full ? nullptr : reinterpret_cast<float*>(ws + g.rest[0]), *rest_w = full ? nullptr : reinterpret_cast<float*>(ws + g.rest[1]);
       // A = X X^T
       product::Args& pa = gram.args[k];
       operands(pa, x[0], x[1], x[0], x[1], full);
@@ -729,7 +717,6 @@ hipError_t schulz_steps(const SchulzRound& r, char* ws, int32_t steps, const flo
       ga.hi = ga.t_hi = q[0], ga.lo = ga.t_lo = full ? q[1] : nullptr;
       ga.ld = ga.t_ld = m, ga.batch = ga.t_batch = int64_t(m) * m;
       ga.alpha = kUnscale;
-      float *rest_q = full ? nullptr : reinterpret_cast<float*>(ws + g.rest[0]), *rest_w = full ? nullptr : reinterpret_cast<float*>(ws + g.rest[1]);
       ga.rest_out = rest_q, ga.rest_ld = m;
       // B = b A + c A A^T
       product::Args& pb = poly.args[k];
@@ -742,38 +729,42 @@ hipError_t schulz_steps(const SchulzRound& r, char* ws, int32_t steps, const flo
       gb.hi = gb.t_hi = w[0], gb.lo = gb.t_lo = full ? w[1] : nullptr;
       gb.alpha = c * kUnscale, gb.beta = b;
       gb.rest = rest_q, gb.rest_out = rest_w, gb.square = 1;
-      // X' = a X + B X, as B (X^T)^T; the last step of a tall matrix as X^T B
-      if (!end || !g.tall) {
-        product::Args& pc = end ? final_.args[k] : next.args[k];
-        operands(pc, w[0], w[1], xt[0], xt[1], full);
-        pc.lda = pc.ldb = m, pc.batch_a = int64_t(m) * m, pc.batch_b = int64_t(m) * n;
-        pc.steps = m / 64, pc.M = m, pc.N = n, pc.batch = g.count;
-      } else {
-        product::Args& pc = final_.args[k];
+      // X' = a X + B X, X being read turned; the last step of a tall matrix as X^T B
+      product::Args pc = {};
+      pc.lda = m, pc.steps = m / 64, pc.batch = g.count;
+      if (end && g.tall) {
         operands(pc, xt[0], xt[1], w[0], w[1], full);
-        pc.lda = pc.ldb = m, pc.batch_a = int64_t(m) * n, pc.batch_b = int64_t(m) * m;
-        pc.steps = m / 64, pc.M = n, pc.N = m, pc.batch = g.count;
+        pc.ldb = m, pc.batch_a = int64_t(m) * n, pc.batch_b = int64_t(m) * m, pc.M = n, pc.N = m;
+      } else {
+        operands(pc, w[0], w[1], x[0], x[1], full);
+        pc.ldb = n, pc.batch_a = int64_t(m) * m, pc.batch_b = int64_t(m) * n, pc.M = m, pc.N = n;
       }
       if (!end) {
-        PlanesOut::Params& gc = next.out[k];
+        PlanesOut::Params& gc = next.out[next.count];
         gc.in_hi = x[0], gc.in_lo = x[1];
-        gc.hi = y[0], gc.lo = y[1], gc.t_hi = yt[0], gc.t_lo = full || g.tall ? yt[1] : nullptr;
+        gc.hi = y[0], gc.lo = y[1];
         gc.ld = n, gc.batch = gc.t_batch = int64_t(m) * n, gc.t_ld = m;
-        gc.alpha = kUnscale, gc.beta = a, gc.t_always = 1;
+        if (g.tall && s + 2 == steps) gc.t_hi = xt[0], gc.t_lo = xt[1], gc.t_always = 1;
+        gc.alpha = kUnscale, gc.beta = a;
         gc.rest = rest_w, gc.rest_ld = m;
+        next.args[next.count++] = pc;
       } else {
-        LastOut::Params& gc = final_.out[k];
+        product::Launch<LastOut>& to_last = g.tall ? tall : wide;
+        LastOut::Params& gc = to_last.out[to_last.count];
         gc = last[k];
         gc.in_hi = g.tall ? xt[0] : x[0], gc.in_lo = g.tall ? xt[1] : x[1];
         gc.ld = g.tall ? m : n, gc.batch = int64_t(m) * n;
         gc.alpha = kUnscale, gc.beta = a;
         gc.rest = rest_w, gc.rest_ld = m, gc.right = g.tall ? 1 : 0;
         gc.rows = static_cast<int32_t>(g.rows), gc.cols = static_cast<int32_t>(g.cols);
+        to_last.args[to_last.count++] = pc;
       }
     }
-    hipError_t e = product::launch_products<false>(gram, sums, stream);
-    if (e == hipSuccess) e = product::launch_products<false>(poly, sums, stream);
-    if (e == hipSuccess) e = end ? product::launch_products<false>(final_, sums, stream) : product::launch_products<false>(next, sums, stream);
+    hipError_t e = product::launch_products<false, false>(gram, sums, stream);
+    if (e == hipSuccess) e = product::launch_products<false, false>(poly, sums, stream);
+    if (e == hipSuccess && next.count > 0) e = product::launch_products<false, true>(next, sums, stream);
+    if (e == hipSuccess && wide.count > 0) e = product::launch_products<false, true>(wide, sums, stream);
+    if (e == hipSuccess && tall.count > 0) e = product::launch_products<false, false>(tall, sums, stream);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -826,7 +817,7 @@ hipError_t run_round(const SchulzRound& r, char* ws, const T* src, int64_t src_b
     large_last.push_back(last[k]);
   }
   if (e != hipSuccess || large.groups.empty()) return e;
-  e = normalise<T>(large, ws, src, src_batch, src_stride, parts, eps, full, stream);
+  e = normalise<T>(large, ws, src, src_batch, src_stride, parts, eps, steps == 1, stream);
   return e == hipSuccess ? schulz_steps(large, ws, steps, coefficients, full, large_last, stream) : e;
 }
 

@@ -1,6 +1,7 @@
 // Matrix products of 16-bit planes on the matrix cores: C = sum over segments of
-// A_s B_s^T, both operands with their contraction contiguous, 32-bit sums, and an
-// epilogue that takes C in blocks of 64 x 32 while it is still in registers.
+// A_s B_s^T, A with its contraction contiguous and B either so or turned (as the rows of
+// B_s^T), 32-bit sums, and an epilogue that takes C in blocks of 64 x 32 while it is still
+// in registers.
 //
 // A value that needs more than 11 bits of significand is held as two binary16 planes,
 // hi + lo (22 bits), and a product of such values as the segments hi hi, hi lo, lo hi;
@@ -37,7 +38,7 @@ constexpr int kMaxProblems = 8;               // products of one launch
 // Operands: rows of `ld` elements, 16-byte aligned, ld a multiple of 8, of which the first
 // steps * 64 are contracted (zeros beyond the true length).  Rows from M (N) on are not
 // read: a tile that reaches past them reads the last row again, and its epilogue leaves
-// what comes of it.
+// what comes of it.  A turned B has steps * 64 rows, which are contracted, of N values; N is a multiple of 8.
 struct Args {
   const void* a[kMaxSegments];
   const void* b[kMaxSegments];
@@ -114,8 +115,8 @@ __device__ inline Place place_of(const Args& p, int id) {
   return at;
 }
 
-// The operand's bytes at step t of all segments.
-__device__ inline const char* step_of(const char* s0, const char* s1, const char* s2, int t, int steps) {
+// The operand's bytes at step t of all segments, whose steps are `step` bytes apart.
+__device__ inline const char* step_of(const char* s0, const char* s1, const char* s2, int t, int steps, int64_t step) {
   const char* base = s0;
   if (t >= steps) {
     base = s1;
@@ -125,13 +126,48 @@ __device__ inline const char* step_of(const char* s0, const char* s1, const char
       t -= steps;
     }
   }
-  return base + int64_t(t) * 128;
+  return base + t * step;
 }
 
 // LDS holds operand rows of 128 bytes; the 16-byte piece c of row r lies in place
 // c ^ (r / 2 % 8) of the row, so that 16 lanes that read one piece of 16 rows touch all
 // 64 banks once.  Loads go straight to LDS, in lane order, so it is the source address
 // that is permuted: a wavefront's load still takes whole lines.
+//
+// A turned B lies in LDS as it does in memory, 64 rows of 128 values a half, and is read with the
+// transposing LDS loads: 16 lanes read 16 neighbouring values of 4 rows, and lane l gets column l
+// of them.  Its 16-byte piece c of row r lies in place c ^ turned_place(r), so that the 32 pieces
+// which the four groups of 16 lanes read at once take all banks evenly.  (Writing such an operand
+// turned as a plane of its own instead cost 2 to 5 % of the whole: 4384 us against 4253 for the gradients
+// of 4096 x 1024 x 50304, 21.2 ms against 20.7 for a model's update of 302M elements.)
+__device__ inline int turned_place(int row) { return (row & 3) << 1 | ((row >> 3) & 1) << 3; }
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+__device__ inline half4 read_turned(const char* p) {
+  return __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)DASO_LDS(p)));
+}
+// Four operands, each of eight rows' values of a column: 4 rows from a place on and the 4 below them.
+// In one block with its wait: before the builtin the compiler would also wait for all loads that go
+// to LDS, which here are for later steps.
+__device__ inline void read_operands(const char* p0, const char* p1, const char* p2, const char* p3, half8 (&to)[4]) {
+  const auto at = [](const char* p) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(DASO_LDS(p))); };
+  half4 v[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %4, %10\n\t"
+      "ds_read_b64_tr_b16 %5, %10 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %6, %11\n\t"
+      "ds_read_b64_tr_b16 %7, %11 offset:1024\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+      : "v"(at(p0)), "v"(at(p1)), "v"(at(p2)), "v"(at(p3))
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) to[i] = __builtin_shufflevector(v[2 * i], v[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+}
 
 // 256 x 256 a workgroup of 8 wavefronts.  A step's operands are four pieces of 128 rows
 // (A0 A1 B0 B1, 16 KB each, two steps in LDS), and a step is four phases, one quarter
@@ -155,11 +191,12 @@ struct Tile256 {
     *col = (b & 1) * 128 + (wave & 3) * 32;
   }
 
-  template <bool BF16>
+  template <bool BF16, bool TURNED>
   __device__ static void run(const Args& p, const Place& at, int from, int to, char* lds, f4 (&acc)[kBlocks][8]) {
     const int lane = thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t skip_a = (at.batch * p.batch_a + int64_t(at.tm) * kRows * p.lda) * 2;
-    const int64_t skip_b = (at.batch * p.batch_b + int64_t(at.tn) * kCols * p.ldb) * 2;
+    const int64_t skip_b = (at.batch * p.batch_b + int64_t(at.tn) * kCols * (TURNED ? 1 : p.ldb)) * 2;
+    const int64_t step_b = TURNED ? p.ldb * 128 : 128;
     const char *a0 = (const char*)p.a[0] + skip_a, *a1 = (const char*)p.a[1] + skip_a, *a2 = (const char*)p.a[2] + skip_a;
     const char *b0 = (const char*)p.b[0] + skip_b, *b1 = (const char*)p.b[1] + skip_b, *b2 = (const char*)p.b[2] + skip_b;
     const int last_a = min(kRows, p.M - at.tm * kRows) - 1, last_b = min(kCols, p.N - at.tn * kCols) - 1;
@@ -171,18 +208,23 @@ struct Tile256 {
       for (int j = 0; j < 2; ++j) {
         const int r = (wave * 2 + j) * 8 + (lane >> 3), c = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
         from_a[h][j] = static_cast<uint32_t>(min(h * 128 + r, last_a)) * (static_cast<uint32_t>(p.lda) * 2) + c;
-        from_b[h][j] = static_cast<uint32_t>(min(h * 128 + r, last_b)) * (static_cast<uint32_t>(p.ldb) * 2) + c;
+        if constexpr (TURNED) {
+          const int k = (wave * 2 + j) * 4 + (lane >> 4), col = h * 128 + ((lane & 15) ^ turned_place(k)) * 8;
+          from_b[h][j] = static_cast<uint32_t>(k) * (static_cast<uint32_t>(p.ldb) * 2) + min(col, last_b - 7) * 2;
+        } else {
+          from_b[h][j] = static_cast<uint32_t>(min(h * 128 + r, last_b)) * (static_cast<uint32_t>(p.ldb) * 2) + c;
+        }
       }
     auto load_a = [&](int t, int h) {
       char* dst = lds + (t & 1) * 65536 + h * 16384 + wave * 2048;
-      const char* g = step_of(a0, a1, a2, t, steps);
+      const char* g = step_of(a0, a1, a2, t, steps, 128);
 #pragma unroll
       for (int j = 0; j < 2; ++j)
         __builtin_amdgcn_global_load_lds(DASO_GLOBAL(g + from_a[h][j]), DASO_LDS(dst + j * 1024), 16, 0, 0);
     };
     auto load_b = [&](int t, int h) {
       char* dst = lds + (t & 1) * 65536 + 32768 + h * 16384 + wave * 2048;
-      const char* g = step_of(b0, b1, b2, t, steps);
+      const char* g = step_of(b0, b1, b2, t, steps, step_b);
 #pragma unroll
       for (int j = 0; j < 2; ++j)
         __builtin_amdgcn_global_load_lds(DASO_GLOBAL(g + from_b[h][j]), DASO_LDS(dst + j * 1024), 16, 0, 0);
@@ -193,12 +235,14 @@ struct Tile256 {
       for (int j = 0; j < 8; ++j) acc[i][j] = (f4)0.0f;
     const int wm = wave >> 2, wn = wave & 3, r16 = lane & 15, kq = lane >> 4;
     half8 a[8], bl[4], br[4], bnext[4];
-    int at_a[2], at_b[2];
+    int at_a[2], at_b[2];  // by kk; of a turned B by the 16 columns
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
       const int c = ((kk * 4 + kq) ^ ((r16 >> 1) & 7)) * 16;
       at_a[kk] = (wm * 64 + r16) * 128 + c;
-      at_b[kk] = 32768 + (wn * 32 + r16) * 128 + c;
+      const int row = kq * 8 + (r16 >> 2), piece = wn * 4 + kk * 2 + ((r16 & 3) >> 1);
+      if constexpr (TURNED) at_b[kk] = 32768 + row * 256 + (piece ^ turned_place(row)) * 16 + (r16 & 1) * 8;
+      else at_b[kk] = 32768 + (wn * 32 + r16) * 128 + c;
     }
     auto read_a = [&](int t, int h) {
 #pragma unroll
@@ -207,12 +251,16 @@ struct Tile256 {
         for (int i = 0; i < 4; ++i)
           a[kk * 4 + i] = *(const half8*)(lds + (t & 1) * 65536 + at_a[kk] + h * 16384 + i * 2048);
     };
-    auto read_b = [&](int t, int h, half8* b) {
+    auto read_b = [&](int t, int h, half8 (&b)[4]) {
+      const char* from = lds + (t & 1) * 65536 + h * 16384;
+      if constexpr (TURNED) {
+        read_operands(from + at_b[0], from + at_b[1], from + at_b[0] + 8192, from + at_b[1] + 8192, b);
+      } else {
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
+        for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          b[kk * 2 + j] = *(const half8*)(lds + (t & 1) * 65536 + at_b[kk] + h * 16384 + j * 2048);
+          for (int j = 0; j < 2; ++j) b[kk * 2 + j] = *(const half8*)(from + at_b[kk] + j * 2048);
+      }
     };
     // the operands are handed over as (b, a), so that a lane holds four neighbouring
     // columns of one row of C
@@ -246,8 +294,9 @@ struct Tile256 {
       else wait_loads<2>();
       meet();
       compute(acc[0], bl);
+      if constexpr (kLeft > 1) load_b(k + 2, 0);
       read_b(k, 1, br);
-      if constexpr (kLeft > 1) load_b(k + 2, 0), wait_loads<10>();
+      if constexpr (kLeft > 1) wait_loads<10>();
       else wait_loads<kLeft == 1 ? 8 : 0>();
       meet();
       compute(acc[1], br);
@@ -256,8 +305,9 @@ struct Tile256 {
       else if constexpr (kLeft == 1) wait_loads<6>();
       meet();
       compute(acc[3], br);
+      if constexpr (kLeft > 1) load_b(k + 2, 1);
       if constexpr (kLeft > 0) read_b(k + 1, 0, bnext);
-      if constexpr (kLeft > 1) load_b(k + 2, 1), wait_loads<10>();
+      if constexpr (kLeft > 1) wait_loads<10>();
       else if constexpr (kLeft == 1) wait_loads<4>();
       meet();
       compute(acc[2], bl);
@@ -292,11 +342,12 @@ struct Tile128 {
     *col = (wave & 1) * 64 + b * 32;
   }
 
-  template <bool BF16>
+  template <bool BF16, bool TURNED>
   __device__ static void run(const Args& p, const Place& at, int from, int to, char* lds, f4 (&acc)[kBlocks][8]) {
     const int lane = thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t skip_a = (at.batch * p.batch_a + int64_t(at.tm) * kRows * p.lda) * 2;
-    const int64_t skip_b = (at.batch * p.batch_b + int64_t(at.tn) * kCols * p.ldb) * 2;
+    const int64_t skip_b = (at.batch * p.batch_b + int64_t(at.tn) * kCols * (TURNED ? 1 : p.ldb)) * 2;
+    const int64_t step_b = TURNED ? p.ldb * 128 : 128;
     const char *a0 = (const char*)p.a[0] + skip_a, *a1 = (const char*)p.a[1] + skip_a, *a2 = (const char*)p.a[2] + skip_a;
     const char *b0 = (const char*)p.b[0] + skip_b, *b1 = (const char*)p.b[1] + skip_b, *b2 = (const char*)p.b[2] + skip_b;
     const int last_a = min(kRows, p.M - at.tm * kRows) - 1, last_b = min(kCols, p.N - at.tn * kCols) - 1;
@@ -306,11 +357,16 @@ struct Tile128 {
     for (int j = 0; j < 4; ++j) {
       const int r = (wave * 4 + j) * 8 + (lane >> 3), c = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
       from_a[j] = static_cast<uint32_t>(min(r, last_a)) * (static_cast<uint32_t>(p.lda) * 2) + c;
-      from_b[j] = static_cast<uint32_t>(min(r, last_b)) * (static_cast<uint32_t>(p.ldb) * 2) + c;
+      if constexpr (TURNED) {
+        const int k = (wave * 4 + j) * 4 + (lane >> 4), col = ((lane & 15) ^ turned_place(k)) * 8;
+        from_b[j] = static_cast<uint32_t>(k) * (static_cast<uint32_t>(p.ldb) * 2) + min(col, last_b - 7) * 2;
+      } else {
+        from_b[j] = static_cast<uint32_t>(min(r, last_b)) * (static_cast<uint32_t>(p.ldb) * 2) + c;
+      }
     }
     auto load = [&](int t) {
       char* dst = lds + (t & 1) * 32768 + wave * 4096;
-      const char *ga = step_of(a0, a1, a2, t, steps), *gb = step_of(b0, b1, b2, t, steps);
+      const char *ga = step_of(a0, a1, a2, t, steps, 128), *gb = step_of(b0, b1, b2, t, steps, step_b);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         __builtin_amdgcn_global_load_lds(DASO_GLOBAL(ga + from_a[j]), DASO_LDS(dst + j * 1024), 16, 0, 0);
@@ -329,8 +385,14 @@ struct Tile128 {
       const char* s = lds + (t & 1) * 32768;
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[kk][i] = *(const half8*)(s + (wm * 64 + r16) * 128 + c + i * 2048);
+      if constexpr (TURNED) {
+        const int row = kq * 8 + (r16 >> 2), piece = (wn * 8 + ((r16 & 3) >> 1)) ^ turned_place(row);
+        const char* from = s + 16384 + kk * 8192 + row * 256 + (r16 & 1) * 8;
+        read_operands(from + piece * 16, from + (piece ^ 2) * 16, from + (piece ^ 4) * 16, from + (piece ^ 6) * 16, b[kk]);
+      } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) b[kk][j] = *(const half8*)(s + 16384 + (wn * 64 + r16) * 128 + c + j * 2048);
+        for (int j = 0; j < 4; ++j) b[kk][j] = *(const half8*)(s + 16384 + (wn * 64 + r16) * 128 + c + j * 2048);
+      }
     };
     auto compute = [&](int kk) {
 #pragma unroll
@@ -538,7 +600,7 @@ __device__ inline void finish(const typename E::Params& params, const Args& p, c
   }
 }
 
-template <class Tile, bool BF16, class E>
+template <class Tile, bool BF16, bool TURNED, class E>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kOccupancy) void product_kernel(Launch<E> all) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int xcd = blockIdx.x & 7, across = all.across;
@@ -574,7 +636,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kOccupancy) void product_kern
     const Args p = all.args[problem];
     const int steps = steps_of(p), from = steps * piece / pieces, to = steps * (piece + 1) / pieces;
     const Place at = place_of(p, tile);
-    Tile::template run<BF16>(p, at, from, to, lds, acc);
+    Tile::template run<BF16, TURNED>(p, at, from, to, lds, acc);
     if (pieces > 1) {
       f4* left = (f4*)(all.sums + int64_t(all.slot[xcd] + slot) * (Tile::kRows * Tile::kCols)) + thread_here();
 #pragma unroll
@@ -763,9 +825,9 @@ inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>
   return e;
 }
 
-template <class Tile, bool BF16, class E>
+template <class Tile, bool BF16, bool TURNED, class E>
 hipError_t launch_tiles(Launch<E>& all, int groups, int cut, hipStream_t stream) {
-  auto* kernel = product_kernel<Tile, BF16, E>;
+  auto* kernel = product_kernel<Tile, BF16, TURNED, E>;
   static std::atomic<uint64_t> allowed{0};
   hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), Tile::kLds, allowed);
   if (e != hipSuccess) return e;
@@ -799,14 +861,15 @@ bool large_tiles(const Launch<E>& all) {
   return u256 > kPlaces256 * kLeastShare && u256 * 14 <= u128 * 5;
 }
 
-template <bool BF16, class E>
+template <bool BF16, bool TURNED, class E>
 hipError_t launch_products(Launch<E>& all, const Sums& sums, hipStream_t stream) {
   int cut = 0;
   const bool large = large_tiles(all);
   const int groups = large ? deal<256>(all, sums, &cut) : deal<128>(all, sums, &cut);
   if (groups == 0) return hipSuccess;
   if (groups < 0) return hipErrorInvalidValue;
-  return large ? launch_tiles<Tile256, BF16, E>(all, groups, cut, stream) : launch_tiles<Tile128, BF16, E>(all, groups, cut, stream);
+  return large ? launch_tiles<Tile256, BF16, TURNED, E>(all, groups, cut, stream)
+               : launch_tiles<Tile128, BF16, TURNED, E>(all, groups, cut, stream);
 }
 
 #endif

@@ -273,7 +273,8 @@ std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with
       if (with_source) g.source = take(4 * g.rows * g.cols * g.count);
       if (g.small) continue;
       for (int b = 0; b < 2; ++b)
-        for (int p = 0; p < 2; ++p) g.x[b][p] = take(2 * g.m * g.n * g.count), g.xt[b][p] = take(2 * g.m * g.n * g.count);
+        for (int p = 0; p < 2; ++p) g.x[b][p] = take(2 * g.m * g.n * g.count);
+      for (int p = 0; p < 2 && g.tall; ++p) g.xt[p] = take(2 * g.m * g.n * g.count);
       for (int p = 0; p < 2; ++p) g.gram[p] = take(2 * g.m * g.m * g.count), g.poly[p] = take(2 * g.m * g.m * g.count);
       for (int p = 0; p < 2; ++p) g.rest[p] = take(4 * g.m * g.count);
     }

@@ -51,7 +51,7 @@ struct SchulzGroup {
   int32_t first;          // place of the first among the round's matrices
   // byte offsets in the workspace; planes: [0] hi, [1] lo
   size_t source;          // fp32 copies of what is orthogonalised, rows x cols (muon only)
-  size_t x[2][2], xt[2][2], gram[2], poly[2];  // x, xt: [buffer][plane]
+  size_t x[2][2], xt[2], gram[2], poly[2];  // x: [buffer][plane]; xt: of tall ones, for the last step
   size_t rest[2];         // what the one plane of gram and of poly leaves of their diagonals
 };
 
