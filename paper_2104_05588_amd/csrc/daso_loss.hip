@@ -435,9 +435,10 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(T* out, int64_t stride, 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // The backward pass takes the vocabulary in pieces of so many classes that a plane of dz
-// holds 2^26 values (128 MB): enough tiles for every CU, and small enough that the
-// planes are read back from the 256 MB cache in front of HBM.
-constexpr int64_t kPieceElems = int64_t(1) << 26;
+// holds 2^27 values, which bounds the workspace (256 MB a plane).  Each piece is two launches whose last
+// tiles leave CUs idle, and reads dhidden's sum so far: 8192 tokens x 50257 classes x 1024 with an fp32
+// dweight take 4.27 ms with 2^26, 4.09 with 2^27, 3.98 with 2^28, and twice the memory each time.
+constexpr int64_t kPieceElems = int64_t(1) << 27;
 
 struct Plan {
   int64_t n_p, d_p, v_p;          // padded tokens, features, classes
@@ -487,7 +488,8 @@ Plan plan_of(const daso_loss_args& s, bool backward) {
       q.wp[i] = q.f32 ? q.w[i] : take(2 * q.v_p * q.d_p);
     }
     const int64_t width = q.pieces > 1 ? q.piece : q.v_p;
-    for (int i = 0; i < 2; ++i) q.p[i] = take(2 * q.n_p * width);
+    const int dz_planes = q.f32 || (s.dweight != nullptr && s.dweight_type == DASO_TYPE_F32) ? 2 : 1;
+    for (int i = 0; i < dz_planes; ++i) q.p[i] = take(2 * q.n_p * width);
     q.sum = take(q.pieces > 1 ? 4 * q.n_p * q.d_p : 0);
   }
   // the largest product's steps, in tiles of 128 and three segments
@@ -625,7 +627,7 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
     ProbOut::Params& out = prob.out[0];
     out.rows = rows;
     // dz in two planes where a product in 22 bits reads it
-    out.hi = at(q.p[0]), out.lo = q.f32 || (dw && dw32) ? at(q.p[1]) : nullptr;
+    out.hi = at(q.p[0]), out.lo = q.p[1] != 0 ? at(q.p[1]) : nullptr;
     out.ld = width;
     out.first = static_cast<int32_t>(first), out.columns = static_cast<int32_t>(classes), out.padded = static_cast<int32_t>(width);
     out.padded_rows = static_cast<int32_t>(q.n_p);

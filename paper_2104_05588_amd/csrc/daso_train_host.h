@@ -63,7 +63,8 @@ struct SchulzRound {
   size_t bytes;                   // of workspace
 };
 
-constexpr int64_t kRoundElems = int64_t(1) << 27;  // 20 bytes of workspace each, and the squares
+// (an update of 302M elements takes 20.7 ms, with 2^26 21.5, with 2^25 22.1, with 2^28 20.65)
+constexpr int64_t kRoundElems = int64_t(1) << 27;  // up to 16 bytes of workspace each, and the squares
 constexpr int32_t kRoundMatrices = 128;            // as many as kernel arguments hold
 constexpr int32_t kRoundGroups = 8;
 constexpr int32_t kSumParts = 256;                 // partial sums of squares a matrix, one a thread of who adds them
