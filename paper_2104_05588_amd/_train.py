@@ -94,23 +94,26 @@ def _load() -> ctypes.CDLL:
 
 # ------------------------------------------------------------- marshalling
 def _device_tensor(t: torch.Tensor, dtypes, what: str) -> torch.Tensor:
+    # (get_device costs a third of device.index, and is -1 off the device)
+    if t.is_cuda and t.dtype in dtypes and t.get_device() == torch.cuda.current_device():
+        return t
     if not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor")
     if t.device.index != torch.cuda.current_device():
         raise ValueError(f"{what} is on {t.device}, not on the current device cuda:{torch.cuda.current_device()}")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{what} must have dtype in {tuple(dtypes)}, got {t.dtype}")
-    return t
+    raise ValueError(f"{what} must have dtype in {tuple(dtypes)}, got {t.dtype}")
 
 
 def _rows(t: torch.Tensor, shape: Tuple[int, int], dtypes, what: str) -> Tuple[int, int]:
     """Address and row stride of a matrix whose rows are contiguous."""
     _device_tensor(t, dtypes, what)
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if (shape[1] > 1 and t.stride(1) != 1) or (shape[0] > 1 and t.stride(0) < shape[1]):
+    rows, cols = shape
+    row, col = t.stride()
+    if (cols > 1 and col != 1) or (rows > 1 and row < cols):
         raise ValueError(f"the rows of {what} must be contiguous and must not overlap")
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(shape[1], 1)
+    return t.data_ptr(), row if rows > 1 else max(cols, 1)
 
 
 def _flat(t: Optional[torch.Tensor], n: int, dtypes, what: str) -> Optional[int]:
@@ -124,7 +127,10 @@ def _flat(t: Optional[torch.Tensor], n: int, dtypes, what: str) -> Optional[int]
 
 def _on(stream: Optional[torch.cuda.Stream]):
     """What is allocated for a call belongs to the stream that the call runs on."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _workspace(name: str, args, *more) -> Optional[torch.Tensor]:
@@ -154,17 +160,18 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     """y, mean and rstd of the layer norm of each row of x [rows, d] (bf16 or fp32, rows
     contiguous); weight and bias are fp32 [d]; mean and rstd fp32 [rows].  `out` may be x."""
     rows, d = _matrix_of(x, "x")
-    a = daso_layer_norm_args()
-    a.rows, a.d, a.eps = rows, d, float(eps)
-    a.x, a.x_stride = _rows(x, (rows, d), _FLOATS, "x")
-    a.type = _TYPES[x.dtype]
-    a.weight, a.bias = _flat(weight, d, _F32, "weight"), _flat(bias, d, _F32, "bias")
+    x_at, x_stride = _rows(x, (rows, d), _FLOATS, "x")
+    weight_at, bias_at = _flat(weight, d, _F32, "weight"), _flat(bias, d, _F32, "bias")
     with _on(stream):
-        y = torch.empty((rows, d), dtype=x.dtype, device=x.device) if out is None else out
-        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        a.y, a.y_stride = _rows(y, (rows, d), (x.dtype,), "out")
-        a.mean, a.rstd = mean.data_ptr(), rstd.data_ptr()
+        if out is None:
+            y = x.new_empty((rows, d))
+            y_at, y_stride = y.data_ptr(), max(d, 1)
+        else:
+            y = out
+            y_at, y_stride = _rows(y, (rows, d), (x.dtype,), "out")
+        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind()
+        a = daso_layer_norm_args(rows, d, _TYPES[x.dtype], eps, x_at, x_stride, weight_at, bias_at, y_at, y_stride,
+                                 mean.data_ptr(), rstd.data_ptr())
         L._check(_load().daso_layer_norm(ctypes.byref(a), L._stream_handle(stream)), "daso_layer_norm")
     return y, mean, rstd
 

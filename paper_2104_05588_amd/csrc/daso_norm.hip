@@ -312,23 +312,30 @@ __global__ __launch_bounds__(kThreads) void columns_long_kernel(Backward a, int3
   a.partial[int64_t(share) * 2 * a.d + a.d + c] = db;
 }
 
-// dweight and dbias from the partial rows, in order: 16 columns a workgroup, 16 shares of
-// the rows with eight loads in flight each.
-__global__ __launch_bounds__(256) void partials_kernel(const float* partial, int32_t count, int32_t d, float* dweight,
-                                                       float* dbias) {
+// dweight and dbias from the partial rows, in order: 16 columns a workgroup of 16 wavefronts, and 64
+// shares of the rows with eight loads in flight each, which is all of them.
+__global__ __launch_bounds__(1024) void partials_kernel(const float* partial, int32_t count, int32_t d, float* dweight,
+                                                        float* dbias) {
   __shared__ float shared[16][16];
   const int in = threadIdx.x & 15, share = threadIdx.x >> 4;
   const int64_t c = blockIdx.x * 16 + in, width = 2 * int64_t(d);
-  float v[8] = {};
-  if (c < width)
-    for (int32_t k = share; k < count; k += 128)
+  const float* const from = partial + min(c, width - 1);
+  float sum = 0.0f;
+  for (int32_t k = share; k < count; k += 512) {
+    float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + 16 * i < count) v[i] += partial[(k + 16 * i) * width + c];
-  shared[share][in] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    for (int i = 0; i < 8; ++i) v[i] = from[min(k + 64 * i, count - 1) * width];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = k + 64 * i < count ? v[i] : 0.0f;
+    sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  }
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if ((threadIdx.x & 63) < 16) shared[threadIdx.x >> 6][in] = sum;
   __syncthreads();
-  if (share != 0 || c >= width) return;
-  float sum = shared[0][in];
+  if (threadIdx.x >= 16 || c >= width) return;
+  sum = shared[0][in];
+#pragma unroll
   for (int k = 1; k < 16; ++k) sum += shared[k][in];
   if (c < d) {
     if (dweight != nullptr) dweight[c] = sum;
@@ -440,7 +447,7 @@ int daso_layer_norm_backward(const daso_layer_norm_backward_args* args, hipStrea
       err = wide ? daso::backward<float, true>(a, groups, stream) : daso::backward<float, false>(a, groups, stream);
   }
   if (err == hipSuccess && sums)
-    err = daso::launch(&daso::partials_kernel, dim3(static_cast<uint32_t>((2 * s.d + 15) / 16)), dim3(256), stream, (const float*)partial,
+    err = daso::launch(&daso::partials_kernel, dim3(static_cast<uint32_t>((2 * s.d + 15) / 16)), dim3(1024), stream, (const float*)partial,
                        groups, d, s.dweight, s.dbias);
   return err == hipSuccess ? DASO_OK : DASO_EHIP;
 }

@@ -138,8 +138,8 @@ __device__ inline const char* step_of(const char* s0, const char* s1, const char
 // transposing LDS loads: 16 lanes read 16 neighbouring values of 4 rows, and lane l gets column l
 // of them.  Its 16-byte piece c of row r lies in place c ^ turned_place(r), so that the 32 pieces
 // which the four groups of 16 lanes read at once take all banks evenly.  (Writing such an operand
-// turned as a plane of its own instead cost 2 to 5 % of the whole: 4384 us against 4253 for the gradients
-// of 4096 x 1024 x 50304, 21.2 ms against 20.7 for a model's update of 302M elements.)
+// turned as a plane of its own instead cost 2 to 5 % of the whole: 4384 us against 4253 for the loss and gradients
+// of 8192 x 50257 x 1024, 21.2 ms against 20.7 for a model's update of 302M elements.)
 __device__ inline int turned_place(int row) { return (row & 3) << 1 | ((row >> 3) & 1) << 3; }
 
 typedef short short4v __attribute__((ext_vector_type(4)));
