@@ -187,68 +187,108 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
 // the target where the tile has it.
 struct LseOut {
   static constexpr auto kKind = product::kWhole;
-  static constexpr int kLds = 256 * 4 * sizeof(float2);
   struct Params {
     float2* parts;  // [tile column][token]
     float* at_target;
     const int64_t* targets;
     const float *inv_a, *inv_b;  // null, or what takes the operands' scaling back
   };
+  // Strip i of a band: 16 rows of it a wavefront, 64 columns of which are in c (two blocks' two
+  // columns of 16).
+  template <class Tile>
+  __device__ static void strip(const Params& out, const product::Args& p, const product::Place& at, const f4& c0, const f4& c1,
+                               const f4& c2, const f4& c3, int band, int i, int32_t target, float inv, int wave, int lane,
+                               float2* to) {
+    const int kq = lane >> 4;
+    int row0, col0, col1;
+    Tile::block_at(wave, band * 2, &row0, &col0);
+    Tile::block_at(wave, band * 2 + 1, &row0, &col1);
+    const int row = at.tm * Tile::kRows + row0 + i * 16 + (lane & 15);
+    const f4 c[4] = {c0, c1, c2, c3};
+    float z[16], m = -__builtin_inff();
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int col = at.tn * Tile::kCols + (k < 2 ? col0 : col1) + (k & 1) * 16 + kq * 4 + e;
+        float v = c[k][e] * inv;
+        if (target == col) out.at_target[row] = v;
+        v = col < p.N ? v : -__builtin_inff();
+        z[k * 4 + e] = v;
+        m = fmaxf(m, v);
+      }
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    // columns that are all -inf, or none, add nothing; +inf or NaN make the sum NaN
+    const float base = m == -__builtin_inff() ? 0.0f : m;
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s += __expf(z[e] - base);
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (kq == 0) *to = make_float2(m, s);
+  }
+  // A row's parts of the wavefronts side by side.
+  template <int kAcross>
+  __device__ static void row_of(const Params& out, const product::Args& p, const product::Place& at, int row, const float2* from) {
+    if (row >= p.M) return;
+    float m = -__builtin_inff(), s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kAcross; ++w) m = fmaxf(m, from[w].x);
+    const float base = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+    for (int w = 0; w < kAcross; ++w) s += from[w].y * __expf(from[w].x - base);
+    out.parts[int64_t(at.tn) * p.M + row] = make_float2(m, s);
+  }
+  __device__ static float scale(const Params& out) { return out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f; }
+  // A row's target as a column of the product, or none.
+  __device__ static int32_t target_of(const Params& out, const product::Args& p, int row) {
+    const int64_t t = out.targets[min(row, p.M - 1)];
+    return row < p.M && t >= 0 && t < p.N ? static_cast<int32_t>(t) : -1;
+  }
+
   template <class Tile>
   __device__ static void tile(const Params& out, const product::Args& p, const product::Place& at, f4 (&acc)[Tile::kBlocks][8],
                               char* lds) {
     constexpr int kAcross = Tile::kThreads / 128;  // wavefronts side by side, of two rows of them
     constexpr int kBands = Tile::kBlocks / 2;      // runs of 64 rows a wavefront holds
     const int lane = product::thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r16 = lane & 15, kq = lane >> 4, wn = wave % kAcross;
     float2* shared = (float2*)lds;  // [row][kAcross]
-    const float inv = out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f;
+    const float inv = scale(out);
+    int32_t target[kBands][4];
+    int row0, col0;
+#pragma unroll
+    for (int k = 0; k < kBands * 4; ++k) {
+      Tile::block_at(wave, k / 4 * 2, &row0, &col0);
+      target[k / 4][k % 4] = target_of(out, p, at.tm * Tile::kRows + row0 + k % 4 * 16 + (lane & 15));
+    }
 #pragma unroll
     for (int band = 0; band < kBands; ++band)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        int row0, col0, col1;
         Tile::block_at(wave, band * 2, &row0, &col0);
-        Tile::block_at(wave, band * 2 + 1, &row0, &col1);
-        const int in = row0 + i * 16 + r16, row = at.tm * Tile::kRows + in;
-        const int64_t t = row < p.M ? out.targets[row] : -1;
-        float z[16], m = -__builtin_inff();
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int col = at.tn * Tile::kCols + (b ? col1 : col0) + j * 16 + kq * 4 + e;
-              float v = acc[band * 2 + b][i * 2 + j][e] * inv;
-              if (row < p.M && t == col && col < p.N) out.at_target[row] = v;
-              v = col < p.N ? v : -__builtin_inff();
-              z[(b * 2 + j) * 4 + e] = v;
-              m = fmaxf(m, v);
-            }
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        // columns that are all -inf, or none, add nothing; +inf or NaN make the sum NaN
-        const float base = m == -__builtin_inff() ? 0.0f : m;
-        float s = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s += __expf(z[e] - base);
-        s += __shfl_xor(s, 16);
-        s += __shfl_xor(s, 32);
-        if (kq == 0) shared[in * kAcross + wn] = make_float2(m, s);
+        strip<Tile>(out, p, at, acc[band * 2][i * 2], acc[band * 2][i * 2 + 1], acc[band * 2 + 1][i * 2], acc[band * 2 + 1][i * 2 + 1],
+                    band, i, target[band][i], inv, wave, lane, shared + (row0 + i * 16 + (lane & 15)) * kAcross + wave % kAcross);
       }
     __syncthreads();
-    for (int in = threadIdx.x; in < Tile::kRows; in += Tile::kThreads) {
-      const int row = at.tm * Tile::kRows + in;
-      if (row >= p.M) continue;
-      float m = -__builtin_inff(), s = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kAcross; ++w) m = fmaxf(m, shared[in * kAcross + w].x);
-      const float base = m == -__builtin_inff() ? 0.0f : m;
-#pragma unroll
-      for (int w = 0; w < kAcross; ++w) s += shared[in * kAcross + w].y * __expf(shared[in * kAcross + w].x - base);
-      out.parts[int64_t(at.tn) * p.M + row] = make_float2(m, s);
-    }
+    for (int in = threadIdx.x; in < Tile::kRows; in += Tile::kThreads)
+      row_of<kAcross>(out, p, at, at.tm * Tile::kRows + in, shared + in * kAcross);
+  }
+  // Strip `i` of `band` alone, of a tile whose values c are the sums of its parts.
+  template <class Tile>
+  __device__ static void part(const Params& out, const product::Args& p, const product::Place& at, const f4 (&c)[4], int band, int i) {
+    constexpr int kAcross = Tile::kThreads / 128;
+    __shared__ float2 shared[2 * 16 * kAcross];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int row0, col0;
+    Tile::block_at(wave, band * 2, &row0, &col0);
+    const int32_t target = target_of(out, p, at.tm * Tile::kRows + row0 + i * 16 + (lane & 15));
+    strip<Tile>(out, p, at, c[0], c[1], c[2], c[3], band, i, target, scale(out), wave, lane,
+                shared + (wave / kAcross * 16 + (lane & 15)) * kAcross + wave % kAcross);
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    Tile::block_at((threadIdx.x >> 4) * kAcross, band * 2, &row0, &col0);
+    row_of<kAcross>(out, p, at, at.tm * Tile::kRows + row0 + i * 16 + (threadIdx.x & 15), shared + threadIdx.x * kAcross);
   }
 };
 

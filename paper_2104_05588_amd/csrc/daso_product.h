@@ -511,6 +511,7 @@ struct Launch {
   Args args[kMaxProblems];
   typename E::Params out[kMaxProblems];
   int32_t slot[8];                  // the first of an XCD's places for sums
+  int32_t cut[8];                   // the XCDs' cut tiles before an XCD's
   float* sums;                      // a tile for each part of a pool that has cut tiles
 };
 
@@ -658,16 +659,18 @@ struct CutTile {
 
 template <class E>
 __device__ inline CutTile cut_tile(const Launch<E>& all, int t) {
-  for (int xcd = 0; xcd < 8; ++xcd) {
-    int slot = all.slot[xcd];
-    for (int k = 0; k < all.count; ++k) {
-      const Run& run = all.runs[xcd][k];
-      if (run.parts > 1) {
-        if (t < run.rest) return {k, run.tile + run.rounds * all.across + t, run.parts, run.rest, slot + t};
-        t -= run.rest;
-      }
-      slot += run.rest * run.parts;
+  int xcd = 0;
+#pragma unroll
+  for (int x = 1; x < 8; ++x) xcd += all.cut[x] <= t ? 1 : 0;
+  t -= all.cut[xcd];
+  int slot = all.slot[xcd];
+  for (int k = 0; k < all.count; ++k) {
+    const Run& run = all.runs[xcd][k];
+    if (run.parts > 1) {
+      if (t < run.rest) return {k, run.tile + run.rounds * all.across + t, run.parts, run.rest, slot + t};
+      t -= run.rest;
     }
+    slot += run.rest * run.parts;
   }
   return {0, 0, 0, 0, -1};
 }
@@ -720,17 +723,26 @@ __global__ __launch_bounds__(64 * kJoinWaves) void product_join_kernel(Launch<E>
   }
 }
 
-// The same for an epilogue of whole tiles: a workgroup a tile.
+// The same for an epilogue of whole tiles: workgroups (x, y) take strips of 16 rows of a
+// wavefront's 64, as little code as can be: it is fetched for this alone.  (A workgroup a tile, with all
+// of a thread's values: 10.8 us for 16 tiles of 128 in four parts each.)
 template <class Tile, class E>
 __global__ __launch_bounds__(Tile::kThreads) void product_join_whole_kernel(Launch<E> all) {
-  __shared__ __attribute__((aligned(1024))) char lds[E::kLds];
   const CutTile cut = cut_tile(all, blockIdx.x);
   if (cut.slot < 0) return;
   const Args& p = all.args[cut.problem];
-  f4 acc[Tile::kBlocks][8];
+  const int band = blockIdx.y >> 2, i = blockIdx.y & 3;
+  constexpr int64_t kTile = int64_t(Tile::kRows) * Tile::kCols / 4;  // in vectors
+  const f4* from = (const f4*)all.sums + cut.slot * kTile + (band * 16 + i * 2) * Tile::kThreads + threadIdx.x;
+  f4 c[4];
 #pragma unroll
-  for (int b = 0; b < Tile::kBlocks; ++b) add_parts<Tile>(all.sums, cut, b, threadIdx.x, acc[b]);
-  E::template tile<Tile>(all.out[cut.problem], p, place_of(p, cut.tile), acc, lds);
+  for (int k = 0; k < 4; ++k) c[k] = from[((k >> 1) * 8 + (k & 1)) * Tile::kThreads];
+  for (int s = 1; s < cut.parts; ++s) {
+    from += cut.rest * kTile;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) c[k] += from[((k >> 1) * 8 + (k & 1)) * Tile::kThreads];
+  }
+  E::template part<Tile>(all.out[cut.problem], p, place_of(p, cut.tile), c, band, i);
 }
 
 // The steps that the busiest of `across` workgroups has of an XCD's pool, cut so that the longest
@@ -808,8 +820,10 @@ int deal(Launch<E>& all, const Sums& sums, int* cut) {
   if (size_t(slots) * kSide * kSide * sizeof(float) > sums.bytes)
     for (int x = 0; x < 8; ++x) pool_steps(all.runs[x], all.args, all.count, all.across, 1);
   all.sums = sums.to;
-  for (int x = 0; x < 8; ++x)
+  for (int x = 0; x < 8; ++x) {
+    all.cut[x] = *cut;
     for (int32_t k = 0; k < all.count; ++k) *cut += all.runs[x][k].parts > 1 ? all.runs[x][k].rest : 0;
+  }
   return all.across * 8;
 }
 
@@ -836,8 +850,8 @@ hipError_t launch_tiles(Launch<E>& all, int groups, int cut, hipStream_t stream)
                       Tile::kLds, stream);
   if (e != hipSuccess || cut == 0) return e;
   if constexpr (E::kKind == kWhole) {
-    return hipLaunchKernel(reinterpret_cast<const void*>(&product_join_whole_kernel<Tile, E>), dim3(static_cast<uint32_t>(cut)),
-                           dim3(Tile::kThreads), list, 0, stream);
+    return hipLaunchKernel(reinterpret_cast<const void*>(&product_join_whole_kernel<Tile, E>),
+                           dim3(static_cast<uint32_t>(cut), Tile::kBlocks / 2 * 4), dim3(Tile::kThreads), list, 0, stream);
   } else {
     constexpr uint32_t kBlocksOfTile = Tile::kRows * Tile::kCols / (kBlockRows * kBlockCols);
     return hipLaunchKernel(reinterpret_cast<const void*>(&product_join_kernel<Tile, E>),
