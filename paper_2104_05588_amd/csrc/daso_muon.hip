@@ -291,9 +291,17 @@ __global__ __launch_bounds__(256) void momentum_kernel(MomentumArgs a, RoundTabl
   };
   if (((start | elems) & 3) == 0) {
     for (int64_t i = lo + 4 * threadIdx.x; i < hi; i += 1024) {
-      f4v s = *(const f4v*)(a.grads[0] + start + i);
-      for (int r = 1; r < a.g; ++r) s += *(const f4v*)(a.grads[r] + start + i);
-      f4v m = *(const f4v*)(a.momentum + start + i), v;
+      // four replicas' loads at a time are on their way together, with the momentum's
+      f4v m = *(const f4v*)(a.momentum + start + i), v, s = (f4v)0.0f;
+      for (int r = 0; r < a.g; r += 4) {
+        f4v x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (r + j < a.g) x[j] = *(const f4v*)(a.grads[r + j] + start + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (r + j < a.g) s = r + j == 0 ? x[j] : s + x[j];
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float mm;
