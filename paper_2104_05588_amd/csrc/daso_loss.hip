@@ -62,19 +62,29 @@ struct TopArgs {
 
 template <class T>
 __device__ inline float top_of(const T* src, int64_t stride, int64_t rows, int64_t cols) {
-  const int64_t wave = (blockIdx.x * 256 + threadIdx.x) >> 6, waves = gridDim.x * 4;
-  const int lane = threadIdx.x & 63;
-  const bool wide = ((reinterpret_cast<uintptr_t>(src) | (stride * sizeof(T))) & 15) == 0;
-  const int64_t whole = wide ? cols / 8 * 8 : 0;
   float m = 0.0f;
   auto take = [&](float v) {
     v = __builtin_fabsf(v);
     m = fmaxf(m, v < __builtin_inff() ? v : 0.0f);
   };
-  if (cols == 1) {  // a vector
-    for (int64_t r = wave * 64 + lane; r < rows; r += waves * 64) take(load1(src + r * stride));
+  if (stride == cols) {  // one run of elements, of which a thread takes eight in four places at a time
+    const int64_t n = rows * cols, whole = n / 8 * 8, id = blockIdx.x * 256 + threadIdx.x, step = gridDim.x * int64_t(2048);
+    for (int64_t i = id * 8; i < whole; i += 4 * step) {
+      float v[4][8] = {};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i + k * step < whole) load8(src + i + k * step, v[k]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) take(v[k][j]);
+    }
+    if (whole + id < n) take(load1(src + whole + id));
     return wave_max(m);
   }
+  const int64_t wave = (blockIdx.x * 256 + threadIdx.x) >> 6, waves = gridDim.x * 4;
+  const int lane = threadIdx.x & 63;
+  const int64_t whole = cols / 8 * 8;
   // four rows at a time, for loads in flight
   for (int64_t r = wave; r < rows; r += 4 * waves) {
     for (int64_t c = lane * 8; c < whole; c += 512) {
@@ -87,11 +97,11 @@ __device__ inline float top_of(const T* src, int64_t stride, int64_t rows, int64
 #pragma unroll
         for (int i = 0; i < 8; ++i) take(v[k][i]);
     }
-    for (int64_t c = whole + lane; c < cols; c += 64) {
+    if (whole + lane < cols) {
       float v[4] = {};
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (r + k * waves < rows) v[k] = load1(src + (r + k * waves) * stride + c);
+        if (r + k * waves < rows) v[k] = load1(src + (r + k * waves) * stride + whole + lane);
 #pragma unroll
       for (int k = 0; k < 4; ++k) take(v[k]);
     }

@@ -336,8 +336,7 @@ __global__ __launch_bounds__(256) void squares_kernel(const T* src, int64_t batc
   const int32_t each = (rows + gridDim.x - 1) / gridDim.x;
   const int32_t lo = each * blockIdx.x, hi = lo + each < rows ? lo + each : rows;
   double sum = 0;
-  const bool wide = ((reinterpret_cast<uintptr_t>(p) | (stride * sizeof(T))) & 15) == 0;
-  const int32_t whole = wide ? cols / 8 * 8 : 0;
+  const int32_t whole = cols / 8 * 8;
   for (int32_t r = lo + (threadIdx.x >> 6); r < hi; r += 4) {
     const T* q = p + r * stride;
     for (int32_t c = (threadIdx.x & 63) * 8; c < whole; c += 512) {

@@ -40,86 +40,80 @@ struct Backward {
   int32_t d;
 };
 
-// N elements of a row in a team of TEAM threads: eight neighbouring ones at a time where
-// WIDE (rows 16-byte aligned, d a multiple of 8), else one at a time.
-template <int TEAM, int N, bool WIDE>
+// N elements of a row in a team of TEAM threads, eight neighbouring ones at a time, at any
+// address.  Without WHOLE (d a multiple of 8) one thread of the team has the row's last, shorter run.
+template <int TEAM, int N, bool WHOLE>
 struct Slice {
-  static constexpr int kRun = WIDE ? 8 : 1, kRuns = N / kRun;
+  static constexpr int kRun = 8, kRuns = N / kRun;
   // the column of run i, element 0
   __device__ static int column(int i, int t) { return (i * TEAM + t) * kRun; }
+  __device__ static bool full(int c, int d) { return WHOLE ? c < d : c + kRun <= d; }
 
   template <class T>
   __device__ static void load(const T* row, int d, int t, float (&v)[N]) {
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
       const int c = column(i, t);
-      if constexpr (WIDE) {
-        float a[8] = {};
-        if (c < d) load8(row + c, a);
+      float a[8] = {};
+      if (full(c, d)) load8(row + c, a);
+      if (!WHOLE && c < d && c + kRun > d)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i * 8 + j] = a[j];
-      } else {
-        v[i] = c < d ? load1(row + c) : 0.0f;
-      }
+        for (int j = 0; j < kRun - 1; ++j)
+          if (c + j < d) a[j] = load1(row + c + j);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i * 8 + j] = a[j];
     }
   }
-  // a vector of any alignment; `none` where there is no such vector
+  // a vector, or `none` where there is no such vector
   __device__ static void load_vector(const float* p, int d, int t, float none, float (&v)[N]) {
-    if (WIDE && p != nullptr && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    if (p != nullptr) {
       load(p, d, t, v);
       return;
     }
 #pragma unroll
-    for (int i = 0; i < kRuns; ++i)
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) {
-        const int c = column(i, t) + j;
-        v[i * kRun + j] = p != nullptr && c < d ? p[c] : none;
-      }
+    for (int i = 0; i < N; ++i) v[i] = none;
   }
   template <class T>
   __device__ static void store(T* row, int d, int t, const float (&v)[N]) {
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
       const int c = column(i, t);
-      if (c >= d) continue;
-      if constexpr (WIDE) {
+      if (full(c, d)) {
         float a[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) a[j] = v[i * 8 + j];
         store8(row + c, a);
-      } else {
-        store1(row + c, v[i]);
+      } else if (!WHOLE && c < d) {
+#pragma unroll
+        for (int j = 0; j < kRun - 1; ++j)
+          if (c + j < d) store1(row + c + j, v[i * 8 + j]);
       }
     }
   }
   // elements as they lie in memory: a row that is on its way takes no more registers than that
   template <class T>
   struct Raw {
-    static constexpr int kWords = N * sizeof(T) / 16;
+    static constexpr int kEach = kRun * sizeof(T) / 16;  // 16 bytes each, of a run
     typedef uint32_t word __attribute__((ext_vector_type(4)));
-    union {
-      word words[WIDE ? kWords : 1];
-      T elems[WIDE ? 1 : N];
-    };
+    word words[kRuns * kEach];
+    T last[WHOLE ? 1 : kRun - 1];  // of the shorter run
     __device__ void load(const T* row, int d, int t) {
 #pragma unroll
       for (int i = 0; i < kRuns; ++i) {
         const int c = column(i, t);
-        if constexpr (WIDE) {
-          constexpr int kEach = kWords / kRuns;  // 16 bytes each, of a run
 #pragma unroll
-          for (int k = 0; k < kEach; ++k) words[i * kEach + k] = c < d ? ((const word*)(row + c))[k] : word{0, 0, 0, 0};
-        } else {
-          elems[i] = c < d ? row[c] : T(0);
-        }
+        for (int k = 0; k < kEach; ++k) words[i * kEach + k] = full(c, d) ? __builtin_bit_cast(word, load16(row + c + k * (16 / sizeof(T)))) : word{0, 0, 0, 0};
+      }
+      if constexpr (!WHOLE) {
+        const int c = d / kRun * kRun;
+        if (d / kRun % TEAM == t)
+#pragma unroll
+          for (int j = 0; j < kRun - 1; ++j)
+            if (c + j < d) last[j] = row[c + j];
       }
     }
-    __device__ void get(float (&v)[N]) const {
-      if constexpr (!WIDE) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = load1(&elems[i]);
-      } else if constexpr (sizeof(T) == 4) {
+    __device__ void get(float (&v)[N], int d, int t) const {
+      if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const uint32_t w = words[i / 4][i % 4];
@@ -132,6 +126,13 @@ struct Slice {
           v[i] = __builtin_bit_cast(float, i % 2 ? w & 0xffff0000u : w << 16);
         }
       }
+      if constexpr (!WHOLE) {
+#pragma unroll
+        for (int i = 0; i < kRuns; ++i)
+          if (d / (kRun * TEAM) == i && d / kRun % TEAM == t)
+#pragma unroll
+            for (int j = 0; j < kRun - 1; ++j) v[i * kRun + j] = j < d % kRun ? load1(&last[j]) : 0.0f;
+      }
     }
   };
   __device__ static bool inside(int e, int d, int t) { return column(e / kRun, t) + e % kRun < d; }
@@ -143,9 +144,9 @@ __device__ inline float team_sum(float v, float* shared) {
   else return group_sum(v, shared);
 }
 
-template <class T, int TEAM, int N, bool WIDE>
+template <class T, int TEAM, int N, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void forward_kernel(Forward a) {
-  using S = Slice<TEAM, N, WIDE>;
+  using S = Slice<TEAM, N, WHOLE>;
   __shared__ float shared[kThreads / 64];
   const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   constexpr int kTeams = kThreads / TEAM;
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(Forward a) {
   const float df = static_cast<float>(a.d);
   for (; r < a.rows; r += step) {
     float v[N], sum = 0.0f, square = 0.0f;
-    next.get(v);
+    next.get(v, a.d, t);
     if (r + step < a.rows) next.load((const T*)a.x + (r + step) * a.x_stride, a.d, t);
 #pragma unroll
     for (int i = 0; i < N; ++i) sum += v[i];
@@ -205,9 +206,9 @@ __global__ __launch_bounds__(kThreads) void forward_long_kernel(Forward a) {
   }
 }
 
-template <class T, int TEAM, int N, bool WIDE>
+template <class T, int TEAM, int N, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void backward_kernel(Backward a) {
-  using S = Slice<TEAM, N, WIDE>;
+  using S = Slice<TEAM, N, WHOLE>;
   constexpr int kTeams = kThreads / TEAM;
   __shared__ float shared[kThreads / 64];
   __shared__ float meet[kTeams > 1 ? kTeams : 1][TEAM * S::kRun];
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(Backward a) {
   if (r < a.rows) fetch(r);
   for (; r < a.rows; r += step) {
     float x[N], g[N], s1 = 0.0f, s2 = 0.0f;
-    next_x.get(x), next_g.get(g);
+    next_x.get(x, a.d, t), next_g.get(g, a.d, t);
     const float mean = next_mean, rstd = next_rstd;
     if (r + step < a.rows) fetch(r + step);
 #pragma unroll
@@ -345,10 +346,6 @@ __global__ __launch_bounds__(1024) void partials_kernel(const float* partial, in
 }
 
 // ------------------------------------------------------------------------- host
-bool aligned16(const void* p, int64_t stride, size_t esz) {
-  return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(stride * static_cast<int64_t>(esz))) & 15) == 0;
-}
-
 constexpr int64_t kWaveForward = 2048, kWaveBackward = 1024;  // longest rows of a wavefront
 bool is_long(int64_t d) { return d > 8192; }
 
@@ -358,25 +355,25 @@ int64_t groups_of(int64_t rows, int64_t d, int64_t wave_d, int64_t most) {
   return std::min((rows + teams - 1) / teams, most);
 }
 
-template <class T, bool WIDE>
+template <class T, bool WHOLE>
 hipError_t forward(const Forward& a, hipStream_t stream) {
   const dim3 grid(static_cast<uint32_t>(groups_of(a.rows, a.d, kWaveForward, kForwardGroups))), block(kThreads);
-  if (a.d <= 512) return launch(&forward_kernel<T, 64, 8, WIDE>, grid, block, stream, a);
-  if (a.d <= 1024) return launch(&forward_kernel<T, 64, 16, WIDE>, grid, block, stream, a);
-  if (a.d <= 2048) return launch(&forward_kernel<T, 64, 32, WIDE>, grid, block, stream, a);
-  if (a.d <= 4096) return launch(&forward_kernel<T, 256, 16, WIDE>, grid, block, stream, a);
-  if (a.d <= 8192) return launch(&forward_kernel<T, 256, 32, WIDE>, grid, block, stream, a);
+  if (a.d <= 512) return launch(&forward_kernel<T, 64, 8, WHOLE>, grid, block, stream, a);
+  if (a.d <= 1024) return launch(&forward_kernel<T, 64, 16, WHOLE>, grid, block, stream, a);
+  if (a.d <= 2048) return launch(&forward_kernel<T, 64, 32, WHOLE>, grid, block, stream, a);
+  if (a.d <= 4096) return launch(&forward_kernel<T, 256, 16, WHOLE>, grid, block, stream, a);
+  if (a.d <= 8192) return launch(&forward_kernel<T, 256, 32, WHOLE>, grid, block, stream, a);
   return launch(&forward_long_kernel<T>, dim3(static_cast<uint32_t>(std::min<int64_t>(a.rows, 4096))), block, stream, a);
 }
 
-template <class T, bool WIDE>
+template <class T, bool WHOLE>
 hipError_t backward(const Backward& a, int32_t groups, hipStream_t stream) {
   const dim3 grid(static_cast<uint32_t>(groups)), block(kThreads);
-  if (a.d <= 512) return launch(&backward_kernel<T, 64, 8, WIDE>, grid, block, stream, a);
-  if (a.d <= 1024) return launch(&backward_kernel<T, 64, 16, WIDE>, grid, block, stream, a);
-  if (a.d <= 2048) return launch(&backward_kernel<T, 256, 8, WIDE>, grid, block, stream, a);
-  if (a.d <= 4096) return launch(&backward_kernel<T, 256, 16, WIDE>, grid, block, stream, a);
-  if (a.d <= 8192) return launch(&backward_kernel<T, 256, 32, WIDE>, grid, block, stream, a);
+  if (a.d <= 512) return launch(&backward_kernel<T, 64, 8, WHOLE>, grid, block, stream, a);
+  if (a.d <= 1024) return launch(&backward_kernel<T, 64, 16, WHOLE>, grid, block, stream, a);
+  if (a.d <= 2048) return launch(&backward_kernel<T, 256, 8, WHOLE>, grid, block, stream, a);
+  if (a.d <= 4096) return launch(&backward_kernel<T, 256, 16, WHOLE>, grid, block, stream, a);
+  if (a.d <= 8192) return launch(&backward_kernel<T, 256, 32, WHOLE>, grid, block, stream, a);
   hipError_t e = hipSuccess;
   if (a.dx != nullptr)
     e = launch(&backward_long_kernel<T>, dim3(static_cast<uint32_t>(std::min<int64_t>(a.rows, 4096))), block, stream, a);
@@ -408,11 +405,10 @@ int daso_layer_norm(const daso_layer_norm_args* args, hipStream_t stream) {
   if (rc != DASO_OK || s.rows == 0 || s.d == 0) return rc;
   if ((rc = daso::current_device(stream)) != DASO_OK) return rc;
   const daso::Forward a = {s.rows, s.x_stride, s.y_stride, s.x, s.weight, s.bias, s.y, s.mean, s.rstd, static_cast<int32_t>(s.d), s.eps};
-  const size_t e = daso::host::bytes_of(s.type);
-  const bool wide = s.d % 8 == 0 && daso::aligned16(s.x, s.x_stride, e) && daso::aligned16(s.y, s.y_stride, e);
+  const bool whole = s.d % 8 == 0;
   hipError_t err;
-  if (s.type == DASO_TYPE_BF16) err = wide ? daso::forward<uint16_t, true>(a, stream) : daso::forward<uint16_t, false>(a, stream);
-  else err = wide ? daso::forward<float, true>(a, stream) : daso::forward<float, false>(a, stream);
+  if (s.type == DASO_TYPE_BF16) err = whole ? daso::forward<uint16_t, true>(a, stream) : daso::forward<uint16_t, false>(a, stream);
+  else err = whole ? daso::forward<float, true>(a, stream) : daso::forward<float, false>(a, stream);
   return err == hipSuccess ? DASO_OK : DASO_EHIP;
 }
 
@@ -438,13 +434,11 @@ int daso_layer_norm_backward(const daso_layer_norm_backward_args* args, hipStrea
   hipError_t err = hipSuccess;
   if (s.rows > 0) {
     const daso::Backward a = {s.rows, s.dy_stride, s.x_stride, s.dx_stride, s.dy, s.x, s.weight, s.mean, s.rstd, s.dx, partial, d};
-    const size_t e = daso::host::bytes_of(s.type);
-    const bool wide = s.d % 8 == 0 && daso::aligned16(s.x, s.x_stride, e) && daso::aligned16(s.dy, s.dy_stride, e) &&
-                      (s.dx == nullptr || daso::aligned16(s.dx, s.dx_stride, e));
+    const bool whole = s.d % 8 == 0;
     if (s.type == DASO_TYPE_BF16)
-      err = wide ? daso::backward<uint16_t, true>(a, groups, stream) : daso::backward<uint16_t, false>(a, groups, stream);
+      err = whole ? daso::backward<uint16_t, true>(a, groups, stream) : daso::backward<uint16_t, false>(a, groups, stream);
     else
-      err = wide ? daso::backward<float, true>(a, groups, stream) : daso::backward<float, false>(a, groups, stream);
+      err = whole ? daso::backward<float, true>(a, groups, stream) : daso::backward<float, false>(a, groups, stream);
   }
   if (err == hipSuccess && sums)
     err = daso::launch(&daso::partials_kernel, dim3(static_cast<uint32_t>((2 * s.d + 15) / 16)), dim3(1024), stream, (const float*)partial,

@@ -13,6 +13,9 @@ namespace daso {
 typedef float f4v __attribute__((ext_vector_type(4)));
 typedef uint16_t us8 __attribute__((ext_vector_type(8)));
 typedef uint16_t us4 __attribute__((ext_vector_type(4)));
+// The same at any element's place: one load or store all the same, which gfx950 takes at any address.
+typedef f4v f4v_any __attribute__((aligned(4)));
+typedef us8 us8_any __attribute__((aligned(2)));
 
 #if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)
 
@@ -34,26 +37,29 @@ __device__ inline float load1<uint16_t>(const uint16_t* p) { return widen_bf16(*
 __device__ inline void store1(float* p, float v) { *p = v; }
 __device__ inline void store1(uint16_t* p, float v) { *p = to_bf16(v); }
 
-// Eight elements from a 16-byte aligned place.
+// 16 bytes as they are.
+__device__ inline f4v load16(const float* p) { return *(const f4v_any*)p; }
+__device__ inline us8 load16(const uint16_t* p) { return *(const us8_any*)p; }
+// Eight elements.
 __device__ inline void load8(const float* p, float (&v)[8]) {
-  const f4v a = *(const f4v*)p, b = *(const f4v*)(p + 4);
+  const f4v a = *(const f4v_any*)p, b = *(const f4v_any*)(p + 4);
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
 }
 __device__ inline void load8(const uint16_t* p, float (&v)[8]) {
-  const us8 a = *(const us8*)p;
+  const us8 a = *(const us8_any*)p;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = widen_bf16(a[i]);
 }
 __device__ inline void store8(float* p, const float (&v)[8]) {
-  *(f4v*)p = f4v{v[0], v[1], v[2], v[3]};
-  *(f4v*)(p + 4) = f4v{v[4], v[5], v[6], v[7]};
+  *(f4v_any*)p = f4v{v[0], v[1], v[2], v[3]};
+  *(f4v_any*)(p + 4) = f4v{v[4], v[5], v[6], v[7]};
 }
 __device__ inline void store8(uint16_t* p, const float (&v)[8]) {
   us8 a;
 #pragma unroll
   for (int i = 0; i < 8; ++i) a[i] = to_bf16(v[i]);
-  *(us8*)p = a;
+  *(us8_any*)p = a;
 }
 
 // Four, from a place aligned to four elements.
@@ -112,7 +118,7 @@ __device__ inline void planes_tile(const PlanesArgs& p, int64_t batch, int tr, i
   const T* src = (const T*)p.src + batch * p.batch_stride + int64_t(r) * p.stride + c;
   uint16_t hi[16], lo[16];
   float v[16];
-  const bool whole = r < p.rows && c + 16 <= p.cols && (reinterpret_cast<uintptr_t>(src) & 15) == 0;
+  const bool whole = r < p.rows && c + 16 <= p.cols;
   if (whole) {
     float a[8], b[8];
     load8(src, a), load8(src + 8, b);
