@@ -329,6 +329,102 @@ def test_orthogonalize_weak_directions():
             assert off <= schulz_tolerance(want, out == torch.bfloat16, 5), (out, off)
 
 
+@pytest.mark.parametrize("steps", [1, 2, 3])
+@pytest.mark.parametrize("rows,cols", [(130, 200), (200, 130), (72, 700), (700, 72)])
+def test_orthogonalize_few_steps_of_matrices_in_planes(steps, rows, cols):
+    """The first and the last step are one, or neighbours; a tall matrix's last one reads X turned."""
+    announce("orthogonalize few steps", steps, rows, cols)
+    u = torch.randn(2, rows, cols, generator=gen(rows + steps))
+    for out in (torch.float32, torch.bfloat16):
+        got = daso.orthogonalize(u.cuda(), steps=steps, out=torch.full(u.shape, float("nan"), dtype=out, device="cuda"))
+        for i in range(2):
+            want = O.newton_schulz(np64(u[i]), [QUINTIC] * steps)
+            off = np.linalg.norm(np64(got[i]) - want) / np.linalg.norm(want)
+            assert off <= schulz_tolerance(want, out == torch.bfloat16, steps), (i, out, off)
+
+
+@pytest.mark.parametrize("rows,cols", [(330, 610), (610, 330)])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+def test_orthogonalize_many_matrices(rows, cols, out):
+    """Enough of them for the large tiles, which reach past the matrices' sides."""
+    announce("orthogonalize many", rows, cols, out)
+    u = torch.randn(80, rows, cols, generator=gen(rows), dtype=torch.float32) * 1e-2
+    got = daso.orthogonalize(u.cuda(), out=torch.full(u.shape, float("nan"), dtype=out, device="cuda"))
+    assert torch.isfinite(got).all()
+    for i in (0, 41, 79):
+        want = O.newton_schulz(np64(u[i]), [QUINTIC] * 5)
+        off = np.linalg.norm(np64(got[i]) - want) / np.linalg.norm(want)
+        assert off <= schulz_tolerance(want, out == torch.bfloat16, 5), (i, off)
+
+
+def check_loss_on_gpu(n, v, d, dtype, dw_type, seed):
+    """Losses and gradients against the same definition in 64 bits on the GPU, with the bounds of the pieces' test."""
+    h, w, t, s = loss_case(n, v, d, dtype, 0.1, seed)
+    hd, wd, td, sd = h.cuda(), w.cuda(), t.cuda(), s.cuda()
+    loss, lse = daso.linear_cross_entropy(hd, wd, td)
+    dh, dw = daso.linear_cross_entropy_backward(sd, hd, wd, td, lse, dweight=torch.empty(v, d, dtype=dw_type, device="cuda"))
+    z = hd.double() @ wd.double().t()
+    want_lse = torch.logsumexp(z, 1)
+    live = td != -100
+    want_loss = torch.where(live, want_lse - z.gather(1, td.clamp(min=0)[:, None])[:, 0], 0.0)
+    dz = torch.softmax(z, 1)
+    dz.scatter_add_(1, td.clamp(min=0)[:, None], torch.full_like(td, -1)[:, None].double())
+    dz *= torch.where(live, sd.double(), 0.0)[:, None]
+    top = float((hd.double().abs() @ wd.double().abs().t()).max())
+    tol = 2 * d * U * top + 2.0 ** -20 + 16 * U * top
+    assert (lse.double() - want_lse).abs().max() <= tol and (loss.double() - want_loss).abs().max() <= tol
+    want_dh, want_dw = dz @ wd.double(), dz.t() @ hd.double()
+    az = dz.abs() + 1e-12
+    # dz and its partner have 11 bits for a bf16 result, 22 for an fp32 one
+    plane, out = (2.0 ** -11, 2.0 ** -8) if dtype == torch.bfloat16 else (2.0 ** -19, U)
+    bound = (az * (plane + v * U + 4 * tol)) @ wd.double().abs() + want_dh.abs() * out
+    assert ((dh.double() - want_dh).abs() <= bound).all()
+    plane, out = (2.0 ** -11, 2.0 ** -8) if dw_type == torch.bfloat16 else (2.0 ** -19, U)
+    bound = (az * (plane + n * U + 4 * tol)).t() @ hd.double().abs() + want_dw.abs() * out
+    assert ((dw.double() - want_dw).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype,dw_type", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+def test_loss_in_large_tiles_of_odd_sizes(dtype, dw_type):
+    announce("loss in large tiles", dtype, dw_type)
+    check_loss_on_gpu(2003, 7001, 333, dtype, dw_type, 17)
+
+
+@pytest.mark.parametrize("n,v,d", [(2, 9001, 131), (5, 31104, 128), (1, 100, 2047), (3905, 276, 64)])
+def test_loss_of_few_tokens_or_classes(n, v, d):
+    announce("loss of few", n, v, d)
+    check_loss_on_gpu(n, v, d, torch.bfloat16, torch.float32, 23)
+
+
+@pytest.mark.parametrize("d", [7, 9, 257, 1023, 1601, 5001])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_norm_rows_at_any_address(d, dtype):
+    """Rows an odd distance apart that begin at an odd element, and nothing written beside them."""
+    announce("norm at any address", d, dtype)
+    rows = 19
+    x, dy = (wide((torch.randn(rows, d, generator=gen(d + k)) + 0.5).to(dtype), 5, 3) for k in range(2))
+    w, b = torch.randn(d, generator=gen(d + 2)).cuda(), torch.randn(d, generator=gen(d + 3)).cuda()
+    y, mean, rstd = daso.layer_norm(x, w, b)
+    want = daso.layer_norm(x.contiguous(), w, b)
+    assert all(torch.equal(p, q) for p, q in zip((y, mean, rstd), want))
+    flat = torch.full((rows * (d + 5) + 9,), 4.0, dtype=dtype, device="cuda")
+    dx = flat[3:3 + rows * (d + 5)].view(rows, d + 5)[:, :d]
+    daso.layer_norm_backward(dy, x, w, mean, rstd, dx=dx)
+    ref = torch.nn.functional.layer_norm
+    xd = x.double().cpu().requires_grad_()
+    yd = ref(xd, (d,), w.double().cpu(), b.double().cpu(), 1e-5)
+    yd.backward(dy.double().cpu())
+    # 32-bit sums of d terms, and one rounding of the result
+    out = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
+    tol = (d + 64) * U * 8
+    assert ((y.double().cpu() - yd.detach()).abs() <= tol * (1 + yd.detach().abs()) + out * yd.detach().abs()).all()
+    scale = float(xd.grad.abs().max())
+    assert ((dx.double().cpu() - xd.grad).abs() <= tol * (1 + scale) * float(rstd.max()) + out * xd.grad.abs()).all()
+    kept = torch.ones(flat.numel(), dtype=torch.bool, device="cuda")
+    kept[3:3 + rows * (d + 5)].view(rows, d + 5)[:, :d] = False
+    assert (flat[kept] == 4).all()
+
+
 def test_orthogonalize_steps_strides_and_special_values():
     announce("orthogonalize steps")
     u = torch.randn(2, 48, 80, generator=gen(9))
