@@ -110,7 +110,8 @@ extern "C" {
 #define DASO_EALIAS (-3)  /* an output overlaps an input other than in the allowed in-place pairs */
 #define DASO_EHIP (-4)    /* a HIP call (launch, allocation of the stats workspace) failed */
 #define DASO_ENOSPACE (-5) /* daso_fused_sync_step_noalloc: the statistics need more than
-                              DASO_NOALLOC_SCRATCH_BYTES of scratch */
+                              DASO_NOALLOC_SCRATCH_BYTES of scratch; daso_train.h: a
+                              workspace is smaller than its call states */
 
 #define DASO_MAX_G 64     /* most replica gradients per call */
 #define DASO_MAX_P 64     /* most exchanged copies per call */

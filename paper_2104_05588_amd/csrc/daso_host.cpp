@@ -200,12 +200,12 @@ const char* daso_status_string(int status) {
     case DASO_OK: return "DASO_OK: success";
     case DASO_EINVAL:
       return "DASO_EINVAL: invalid argument (null pointer, count out of range, S outside [0, DASO_MAX_S], buckets not tiling [0, n), or a stream of another device)";
-    case DASO_EALIGN: return "DASO_EALIGN: a device buffer is not 16-byte aligned";
+    case DASO_EALIGN: return "DASO_EALIGN: a device buffer is not 16-byte aligned (or, in the training operators, to its element or workspace alignment)";
     case DASO_EALIAS: return "DASO_EALIAS: an output buffer overlaps another buffer";
     case DASO_EHIP: return "DASO_EHIP: a HIP call failed";
     case DASO_ENOSPACE:
       return "DASO_ENOSPACE: the statistics need more scratch than the fixed array of "
-             "daso_fused_sync_step_noalloc holds (DASO_NOALLOC_SCRATCH_BYTES: 24 bytes per tile plus 260)";
+             "daso_fused_sync_step_noalloc holds (DASO_NOALLOC_SCRATCH_BYTES: 24 bytes per tile plus 260), or a workspace is smaller than its call states";
     default: return "unknown DASO status";
   }
 }

@@ -3,10 +3,15 @@
 // the mean, not from squares), and it is written once.
 //
 // A row of up to 2048 elements (1024 in the backward pass, whose registers hold five rows' worth) is a
-// wavefront's, of up to 8192 a workgroup's of 256 threads; a team of threads keeps the weights in registers and walks over rows.  In the backward pass it
-// also keeps its columns' sums for dweight and dbias, which end up as one partial row a
+// wavefront's, of up to 8192 a workgroup's of 256 threads; a team of threads keeps the weights in
+// registers and walks over rows.  In the backward pass it also keeps its columns' sums for dweight and dbias, which end up as one partial row a
 // workgroup; a second kernel adds those in order.  Longer rows are read again for each of
 // their passes, from L2.
+//
+// Measured: 8192 rows of 1024 in bf16 forward in 10 us (3.4 TB/s, short of what one pass over 33 MB can
+// reach); 32768 such rows backward in 35 us (5.8 TB/s) and 4 for the sums; 5003 rows of 1601 in fp32 backward in 25
+// and 4 us, where the next row alone is on its way behind the one in hand.  More workgroups there are no help: the
+// partial rows grow with them (768: 29.6 us in all, 1024: 32.0, 512: 28.8).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -314,7 +319,8 @@ __global__ __launch_bounds__(kThreads) void columns_long_kernel(Backward a, int3
 }
 
 // dweight and dbias from the partial rows, in order: 16 columns a workgroup of 16 wavefronts, and 64
-// shares of the rows with eight loads in flight each, which is all of them.
+// shares of the rows with eight loads in flight each, which is all of them: 4 us for 512 rows of 2048 (with
+// 16 shares 11).
 __global__ __launch_bounds__(1024) void partials_kernel(const float* partial, int32_t count, int32_t d, float* dweight,
                                                         float* dbias) {
   __shared__ float shared[16][16];

@@ -483,7 +483,8 @@ __device__ inline void split(float v, _Float16* hi, _Float16* lo) {
 //            once, after the last use of the inputs and before the first store
 //   kBlocks: block(params, place, c, row, col, stage, lane): the same with the block in registers, of all
 //            blocks of a tile
-//   kWhole:  tile<Tile>(params, args, place, acc, lds), by the whole workgroup, in kLds bytes of LDS
+//   kWhole:  tile<Tile>(params, args, place, acc, lds), by the whole workgroup, in the product's LDS;
+//            and part<Tile>(params, args, place, c, band, i) of a cut tile: rows i * 16 .. of each wavefront's band
 //
 // A launch has up to as many workgroups as fit the chip (kPlaces); an XCD's, to which they go in
 // turn, get a run of whole tiles, with about an eighth of all steps.  Of each product an XCD's
