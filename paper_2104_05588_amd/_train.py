@@ -119,8 +119,9 @@ def _rows(t: torch.Tensor, shape: Tuple[int, int], dtypes, what: str) -> Tuple[i
 def _flat(t: Optional[torch.Tensor], n: int, dtypes, what: str) -> Optional[int]:
     if t is None:
         return None
-    _device_tensor(t, dtypes, what)
-    if t.numel() != n or not t.is_contiguous():
+    if (t.numel() != n or not t.is_contiguous() or not t.is_cuda or t.dtype not in dtypes
+            or t.get_device() != torch.cuda.current_device()):
+        _device_tensor(t, dtypes, what)
         raise ValueError(f"{what} must be contiguous with {n} elements")
     return t.data_ptr()
 
@@ -169,7 +170,8 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
         else:
             y = out
             y_at, y_stride = _rows(y, (rows, d), (x.dtype,), "out")
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind()
+        mean = x.new_empty(rows, dtype=torch.float32)
+        rstd = torch.empty_like(mean)
         a = daso_layer_norm_args(rows, d, _TYPES[x.dtype], eps, x_at, x_stride, weight_at, bias_at, y_at, y_stride,
                                  mean.data_ptr(), rstd.data_ptr())
         L._check(_load().daso_layer_norm(ctypes.byref(a), L._stream_handle(stream)), "daso_layer_norm")
