@@ -36,6 +36,7 @@ using product::f4;
 using product::half4;
 using product::half8;
 
+constexpr float kLog2E = 1.44269504f;
 constexpr float kProbScale = 16384.0f;  // dz / dloss in [-1, 1] as binary16
 
 // Powers of two from the largest finite magnitudes of hidden, weight and dloss, and their reciprocals.
@@ -220,27 +221,30 @@ struct LseOut {
     Tile::block_at(wave, band * 2 + 1, &row0, &col1);
     const int row = at.tm * Tile::kRows + row0 + i * 16 + (lane & 15);
     const f4 c[4] = {c0, c1, c2, c3};
+    const auto column = [&](int k, int e) { return at.tn * Tile::kCols + (k < 2 ? col0 : col1) + (k & 1) * 16 + kq * 4 + e; };
     float z[16], m = -__builtin_inff();
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 16; ++k) z[k] = c[k / 4][k % 4];
+    // few tiles hold a row's target, and fewer reach past the classes
+    if (target >= at.tn * Tile::kCols && target - at.tn * Tile::kCols < Tile::kCols)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int col = at.tn * Tile::kCols + (k < 2 ? col0 : col1) + (k & 1) * 16 + kq * 4 + e;
-        float v = c[k][e] * inv;
-        if (target == col) out.at_target[row] = v;
-        v = col < p.N ? v : -__builtin_inff();
-        z[k * 4 + e] = v;
-        m = fmaxf(m, v);
-      }
+      for (int k = 0; k < 16; ++k)
+        if (target == column(k / 4, k % 4)) out.at_target[row] = z[k] * inv;
+    if ((at.tn + 1) * Tile::kCols > p.N)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) z[k] = column(k / 4, k % 4) < p.N ? z[k] : -__builtin_inff();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) m = fmaxf(m, z[k]);
     m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
     // columns that are all -inf, or none, add nothing; +inf or NaN make the sum NaN
-    const float base = m == -__builtin_inff() ? 0.0f : m;
+    const float unit = inv * kLog2E, base = m == -__builtin_inff() ? 0.0f : m * unit;
     float s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s += __expf(z[e] - base);
+    for (int k = 0; k < 16; ++k) s += __builtin_amdgcn_exp2f(fmaf(z[k], unit, -base));
     s += __shfl_xor(s, 16);
     s += __shfl_xor(s, 32);
+    m *= inv;
     if (kq == 0) *to = make_float2(m, s);
   }
   // A row's parts of the wavefronts side by side.
@@ -358,34 +362,56 @@ struct ProbOut {
     int32_t padded_rows;             // tokens with padding: the planes are contracted over both
     const float *inv_a, *inv_b;
   };
-  __device__ static void block(const Params& out, const product::Place&, const f4 (&acc)[8], int row0, int col0, char* hi, int lane) {
-    if (row0 >= out.padded_rows || col0 >= out.padded) return;
+  struct Inputs {
+    Row rows[4];
+  };
+  __device__ static void fetch(const Params& out, const product::Place&, int row0, int, int lane, Inputs& in) {
+    if (row0 >= out.padded_rows) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) in.rows[i] = out.rows[row0 + i * 16 + (lane & 15)];
+  }
+  template <class F>
+  __device__ static void block(const Params& out, const product::Place&, const f4 (&acc)[8], int row0, int col0, char* hi, int lane,
+                               const Inputs& in, F next) {
+    if (row0 >= out.padded_rows || col0 >= out.padded) {
+      next();
+      return;
+    }
     const int r16 = lane & 15, kq = lane >> 4;
     char* lo = hi + product::kStagePlane;
-    const float inv = out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f;
-    const bool two = out.lo != nullptr;
-    Row rows[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) rows[i] = out.rows[row0 + i * 16 + r16];
+    const float unit = (out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f) * kLog2E;
+    const bool two = out.lo != nullptr, edge = col0 + product::kBlockCols > out.columns;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const Row r = rows[i];
+      const Row r = in.rows[i];
+      const float base = r.lse * kLog2E;
+      const int target = r.target - out.first - col0;
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f(fmaf(acc[i * 2 + k / 4][k % 4], unit, -base));
+      // few blocks hold a row's target, and fewer reach past the classes
+      if (target >= 0 && target < product::kBlockCols)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] -= k / 4 * 16 + kq * 4 + k % 4 == target ? 1.0f : 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = r.target >= 0 ? v[k] * r.g : 0.0f;
+      if (edge)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = col0 + k / 4 * 16 + kq * 4 + k % 4 < out.columns ? v[k] : 0.0f;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int col = col0 + j * 16 + kq * 4;
         half4 h, l;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float v = __expf(acc[i * 2 + j][e] * inv - r.lse) - (out.first + col + e == r.target ? 1.0f : 0.0f);
-          v = r.target >= 0 && col + e < out.columns ? v * r.g : 0.0f;
           _Float16 a, c;
-          product::split(v, &a, &c);
+          product::split(v[j * 4 + e], &a, &c);
           h[e] = a, l[e] = c;
         }
         *(half4*)(hi + product::plane_at(i * 16 + r16, j * 16 + kq * 4)) = h;
         if (two) *(half4*)(lo + product::plane_at(i * 16 + r16, j * 16 + kq * 4)) = l;
       }
     }
+    next();
     product::wait_lds();
     __builtin_amdgcn_wave_barrier();
     const auto straight = [&](const char* plane, _Float16* to) {

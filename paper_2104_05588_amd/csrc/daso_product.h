@@ -481,8 +481,8 @@ __device__ inline void split(float v, _Float16* hi, _Float16* lo) {
 //            block(params, place, row, col, stage, lane, inputs, next), by a wavefront: the staged
 //            block at (row, col) of C, of those that begin inside the result; next is called
 //            once, after the last use of the inputs and before the first store
-//   kBlocks: block(params, place, c, row, col, stage, lane): the same with the block in registers, of all
-//            blocks of a tile
+//   kBlocks: fetch as above, and block(params, place, c, row, col, stage, lane, inputs, next): the same with
+//            the block in registers, of all blocks of a tile
 //   kWhole:  tile<Tile>(params, args, place, acc, lds), by the whole workgroup, in the product's LDS;
 //            and part<Tile>(params, args, place, c, band, i) of a cut tile: rows i * 16 .. of each wavefront's band
 //
@@ -593,11 +593,20 @@ __device__ inline void finish(const typename E::Params& params, const Args& p, c
         has = next, row = next_row, col = next_col;
       }
     } else {
+      // (inputs before the stores of the block before, as above)
+      int row, col;
+      typename E::Inputs in;
+      const auto fetch = [&](int b) {
+        if (b >= Tile::kBlocks) return;
+        Tile::block_at(wave, b, &row, &col);
+        row += at.tm * Tile::kRows, col += at.tn * Tile::kCols;
+        E::fetch(out, at, row, col, lane, in);
+      };
+      fetch(0);
 #pragma unroll
       for (int b = 0; b < Tile::kBlocks; ++b) {
-        int row, col;
-        Tile::block_at(wave, b, &row, &col);
-        E::block(out, at, acc[b], row + at.tm * Tile::kRows, col + at.tn * Tile::kCols, stage, lane);
+        const int of_row = row, of_col = col;
+        E::block(out, at, acc[b], of_row, of_col, stage, lane, in, [&] { fetch(b + 1); });
       }
     }
   }
@@ -735,7 +744,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void product_join_kernel(Launch<E>
     __builtin_amdgcn_wave_barrier();
     E::block(out, at, row, col, stage, lane, in, [] {});
   } else {
-    E::block(out, at, c, row, col, stage, lane);
+    typename E::Inputs in;
+    E::fetch(out, at, row, col, lane, in);
+    E::block(out, at, c, row, col, stage, lane, in, [] {});
   }
 }
 
