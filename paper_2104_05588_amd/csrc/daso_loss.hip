@@ -458,7 +458,6 @@ struct GradOut {
     if (p.turned) {
       // 8 columns of C in a pass, 8 lanes a column, 8 rows of it each
       const int cc = row + (lane & 7) * 8, left = p.cols - cc;
-      const bool wide = ((reinterpret_cast<uintptr_t>(p.out) | (p.ld * (p.bf16 ? 2 : 4))) & 15) == 0 && left >= 8;
       float v[4][8];
 #pragma unroll
       for (int pass = 0; pass < 4; ++pass)
@@ -471,12 +470,11 @@ struct GradOut {
 #pragma unroll
       for (int pass = 0; pass < 4; ++pass) {
         const int rr = col + pass * 8 + (lane >> 3);
-        if (rr < p.rows && left > 0) store_run(p, rr * p.ld + cc, left, wide, v[pass]);
+        if (rr < p.rows && left > 0) store_run(p, rr * p.ld + cc, left, v[pass]);
       }
       return;
     }
     const int r0 = row + product::pass_row(0, lane), cc = col + product::pass_col(lane), left = p.cols - cc;
-    const bool wide = ((reinterpret_cast<uintptr_t>(p.out) | (p.ld * (p.bf16 ? 2 : 4))) & 15) == 0 && left >= 8;
     float v[product::kPasses][8];
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass) {
@@ -491,14 +489,14 @@ struct GradOut {
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass) {
       if (r0 + pass * product::kPassRows >= p.rows || left <= 0) continue;
-      store_run(p, (r0 + pass * product::kPassRows) * p.ld + cc, left, wide, v[pass]);
+      store_run(p, (r0 + pass * product::kPassRows) * p.ld + cc, left, v[pass]);
     }
   }
   // Eight neighbouring values, or the `left` of them that there are.
-  __device__ static void store_run(const Params& p, int64_t to, int left, bool wide, const float (&v)[8]) {
+  __device__ static void store_run(const Params& p, int64_t to, int left, const float (&v)[8]) {
     float* const o32 = (float*)p.out + to;
     uint16_t* const o16 = (uint16_t*)p.out + to;
-    if (wide) {
+    if (left >= 8) {
       if (p.bf16) store8(o16, v);
       else store8(o32, v);
     } else {

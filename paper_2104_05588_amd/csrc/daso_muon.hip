@@ -170,13 +170,10 @@ struct LastOut {
     float left[product::kPasses], right[8];
     Entry entry;
   };
-  // Where a matrix's result lies, and whether eight of its elements may be taken at a time.
-  __device__ static bool place(const Params& p, int batch, const Entry& e, int64_t* out, int64_t* ld) {
+  // Where a matrix's result lies.
+  __device__ static void place(const Params& p, int batch, const Entry& e, int64_t* out, int64_t* ld) {
     *out = p.kind == kStep ? e.start : p.out_batch * batch;
     *ld = p.kind == kStep ? p.cols : p.out_ld;
-    const int64_t esz = p.kind == kBf16 ? 2 : 4;
-    const uintptr_t first = reinterpret_cast<uintptr_t>(p.kind == kStep ? (void*)p.params : p.out);
-    return ((first + *out * esz) & 15) == 0 && ((*ld * esz) & 15) == 0 && (p.wire == nullptr || ((*out | *ld) & 7) == 0);
   }
   __device__ static void fetch(const Params& p, const product::Place& at, int row, int col, int lane, Inputs& in) {
     const int k = product::pass_col(lane), r0 = row + product::pass_row(0, lane), cc = col + k;
@@ -194,7 +191,8 @@ struct LastOut {
     if (p.kind != kStep) return;
     in.entry = p.table[at.batch];
     int64_t out, ld;
-    const bool wide = place(p, at.batch, in.entry, &out, &ld) && cc + 8 <= p.cols;
+    place(p, at.batch, in.entry, &out, &ld);
+    const bool wide = cc + 8 <= p.cols;
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass) {
       if (r0 + pass * product::kPassRows >= p.rows) continue;
@@ -210,7 +208,8 @@ struct LastOut {
                                F next) {
     const int r0 = row + product::pass_row(0, lane), cc = col + product::pass_col(lane);
     int64_t out, ld;
-    const bool wide = place(p, at.batch, in.entry, &out, &ld) && cc + 8 <= p.cols;
+    place(p, at.batch, in.entry, &out, &ld);
+    const bool wide = cc + 8 <= p.cols;
     const float step = p.kind == kStep ? in.entry.step : 0.0f;
     float* const o32 = p.kind == kStep ? p.params : (float*)p.out;
     uint16_t* const o16 = p.kind == kStep ? p.wire : (uint16_t*)p.out;
