@@ -9,10 +9,10 @@
 // twice: keeping them would cost N V 4 bytes written and read, which takes as long as the
 // product at d = 1024 and grows the memory by N V.
 //
-// Bound by the matrix cores: 4096 tokens over 50257 classes of 1024 features forward in 375 to 408 us by machine
-// (1030 to 1120 TFLOP/s; 16 steps a tile leave less of the pipeline's rate than 128 do), 8192 with gradients
+// Bound by the matrix cores: 4096 tokens over 50257 classes of 1024 features forward in 372 to 381 us by machine
+// (1110 to 1130 TFLOP/s; 16 steps a tile leave less of the pipeline's rate than 128 do), 8192 with gradients
 // and an fp32 dweight in 4.0 ms, 4.2 PFLOP counting the logits twice and dweight in two planes.  A few
-// tokens or classes are bound by the chain of eight launches, about 8 us each with what they read.
+// tokens or classes are bound by the chain of eight launches, 3 to 18 us each.
 //
 // Numbers.  bf16 operands are multiplied as they are in the forward product; fp32 ones as two
 // binary16 planes each, scaled by a power of two from the tensor's largest value (22
