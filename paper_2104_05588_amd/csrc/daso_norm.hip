@@ -380,12 +380,13 @@ hipError_t backward(const Backward& a, int32_t groups, hipStream_t stream) {
   if (a.d <= 2048) return launch(&backward_kernel<T, 256, 8, WHOLE>, grid, block, stream, a);
   if (a.d <= 4096) return launch(&backward_kernel<T, 256, 16, WHOLE>, grid, block, stream, a);
   if (a.d <= 8192) return launch(&backward_kernel<T, 256, 32, WHOLE>, grid, block, stream, a);
+  // the columns' sums first: dx may take dy's place
   hipError_t e = hipSuccess;
-  if (a.dx != nullptr)
-    e = launch(&backward_long_kernel<T>, dim3(static_cast<uint32_t>(std::min<int64_t>(a.rows, 4096))), block, stream, a);
-  if (e == hipSuccess && a.partial != nullptr)
+  if (a.partial != nullptr)
     e = launch(&columns_long_kernel<T>, dim3(static_cast<uint32_t>((a.d + kThreads - 1) / kThreads), static_cast<uint32_t>(groups)),
                block, stream, a, groups);
+  if (e == hipSuccess && a.dx != nullptr)
+    e = launch(&backward_long_kernel<T>, dim3(static_cast<uint32_t>(std::min<int64_t>(a.rows, 4096))), block, stream, a);
   return e;
 }
 
