@@ -37,20 +37,21 @@ using product::half4;
 using product::half8;
 
 constexpr float kLog2E = 1.44269504f;
-constexpr float kProbScale = 16384.0f;  // dz / dloss in [-1, 1] as binary16
+constexpr int kProbExponent = 14;  // dz / dloss in [-1, 1], times 2^14, as binary16
+constexpr float kProbScale = 1 << kProbExponent;
 
-// Powers of two from the largest finite magnitudes of hidden, weight and dloss, and their reciprocals.
+// Powers of two from the largest finite magnitudes of hidden, weight and dloss.
 enum Tensor { kHidden, kWeight, kGrad };
 constexpr int kTopParts = 512;  // workgroups that look for one
 struct Scales {
   uint32_t top[3][kTopParts];  // bits of the magnitudes
-  float to[3], inv[3];         // hidden and weight times `to` are below 2^15, dloss times `inv` is at most 1
+  int32_t to[3];               // exponents: hidden and weight times 2^to are below 2^15, dloss times 2^-to is at most 1
 };
 
 // What the backward epilogue needs of a token.
 struct Row {
   float lse;
-  float g;         // dloss * grad_inv * kProbScale
+  float g;         // dloss, scaled, times kProbScale
   int32_t target;  // -1: the whole row is zero
   int32_t pad;
 };
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   if (id == 0 && a.scales != nullptr) {
     for (int t = 0; t < 3; ++t) {
       const int e = scale_exponent(a.scales, t, shared);
-      if (threadIdx.x == 0) a.scales->to[t] = power_of_two(e), a.scales->inv[t] = power_of_two(-e);
+      if (threadIdx.x == 0) a.scales->to[t] = e;
     }
   }
   if (id < a.first[a.count]) {
@@ -200,20 +201,22 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
 
 // ------------------------------------------------------------------------- forward epilogue
 // For each row the maximum and the sum of exponentials of the tile's columns, and the logit of
-// the target where the tile has it.
+// the target where the tile has it.  With SCALED the operands' scaling is taken back first, by its exponent: as a factor
+// it may be zero or infinite where the logits are neither.
+template <bool SCALED>
 struct LseOut {
   static constexpr auto kKind = product::kWhole;
   struct Params {
     float2* parts;  // [tile column][token]
     float* at_target;
     const int64_t* targets;
-    const float *inv_a, *inv_b;  // null, or what takes the operands' scaling back
+    const int32_t *to_a, *to_b;  // SCALED: the exponents of the operands' scales
   };
   // Strip i of a band: 16 rows of it a wavefront, 64 columns of which are in c (two blocks' two
   // columns of 16).
   template <class Tile>
   __device__ static void strip(const Params& out, const product::Args& p, const product::Place& at, const f4& c0, const f4& c1,
-                               const f4& c2, const f4& c3, int band, int i, int32_t target, float inv, int wave, int lane,
+                               const f4& c2, const f4& c3, int band, int i, int32_t target, int shift, int wave, int lane,
                                float2* to) {
     const int kq = lane >> 4;
     int row0, col0, col1;
@@ -224,12 +227,12 @@ struct LseOut {
     const auto column = [&](int k, int e) { return at.tn * Tile::kCols + (k < 2 ? col0 : col1) + (k & 1) * 16 + kq * 4 + e; };
     float z[16], m = -__builtin_inff();
 #pragma unroll
-    for (int k = 0; k < 16; ++k) z[k] = c[k / 4][k % 4];
+    for (int k = 0; k < 16; ++k) z[k] = SCALED ? __builtin_ldexpf(c[k / 4][k % 4], shift) : c[k / 4][k % 4];
     // few tiles hold a row's target, and fewer reach past the classes
     if (target >= at.tn * Tile::kCols && target - at.tn * Tile::kCols < Tile::kCols)
 #pragma unroll
       for (int k = 0; k < 16; ++k)
-        if (target == column(k / 4, k % 4)) out.at_target[row] = z[k] * inv;
+        if (target == column(k / 4, k % 4)) out.at_target[row] = z[k];
     if ((at.tn + 1) * Tile::kCols > p.N)
 #pragma unroll
       for (int k = 0; k < 16; ++k) z[k] = column(k / 4, k % 4) < p.N ? z[k] : -__builtin_inff();
@@ -238,13 +241,12 @@ struct LseOut {
     m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
     // columns that are all -inf, or none, add nothing; +inf or NaN make the sum NaN
-    const float unit = inv * kLog2E, base = m == -__builtin_inff() ? 0.0f : m * unit;
+    const float base = m == -__builtin_inff() ? 0.0f : m * kLog2E;
     float s = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += __builtin_amdgcn_exp2f(fmaf(z[k], unit, -base));
+    for (int k = 0; k < 16; ++k) s += __builtin_amdgcn_exp2f(fmaf(z[k], kLog2E, -base));
     s += __shfl_xor(s, 16);
     s += __shfl_xor(s, 32);
-    m *= inv;
     if (kq == 0) *to = make_float2(m, s);
   }
   // A row's parts of the wavefronts side by side.
@@ -259,7 +261,7 @@ struct LseOut {
     for (int w = 0; w < kAcross; ++w) s += from[w].y * __expf(from[w].x - base);
     out.parts[int64_t(at.tn) * p.M + row] = make_float2(m, s);
   }
-  __device__ static float scale(const Params& out) { return out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f; }
+  __device__ static int scale(const Params& out) { return SCALED ? -(*out.to_a + *out.to_b) : 0; }
   // A row's target as a column of the product, or none.
   __device__ static int32_t target_of(const Params& out, const product::Args& p, int row) {
     const int64_t t = out.targets[min(row, p.M - 1)];
@@ -273,7 +275,7 @@ struct LseOut {
     constexpr int kBands = Tile::kBlocks / 2;      // runs of 64 rows a wavefront holds
     const int lane = product::thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     float2* shared = (float2*)lds;  // [row][kAcross]
-    const float inv = scale(out);
+    const int shift = scale(out);
     int32_t target[kBands][4];
     int row0, col0;
 #pragma unroll
@@ -287,7 +289,7 @@ struct LseOut {
       for (int i = 0; i < 4; ++i) {
         Tile::block_at(wave, band * 2, &row0, &col0);
         strip<Tile>(out, p, at, acc[band * 2][i * 2], acc[band * 2][i * 2 + 1], acc[band * 2 + 1][i * 2], acc[band * 2 + 1][i * 2 + 1],
-                    band, i, target[band][i], inv, wave, lane, shared + (row0 + i * 16 + (lane & 15)) * kAcross + wave % kAcross);
+                    band, i, target[band][i], shift, wave, lane, shared + (row0 + i * 16 + (lane & 15)) * kAcross + wave % kAcross);
       }
     __syncthreads();
     for (int in = threadIdx.x; in < Tile::kRows; in += Tile::kThreads)
@@ -352,6 +354,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* parts, int32_t 
 
 // ------------------------------------------------------------------------- backward epilogues
 // dz of a piece's columns as planes; columns beyond the vocabulary are zero.
+template <bool SCALED>
 struct ProbOut {
   static constexpr auto kKind = product::kBlocks;
   struct Params {
@@ -360,7 +363,7 @@ struct ProbOut {
     int64_t ld;
     int32_t first, columns, padded;  // the piece: its first class, its classes, its columns with padding
     int32_t padded_rows;             // tokens with padding: the planes are contracted over both
-    const float *inv_a, *inv_b;
+    const int32_t *to_a, *to_b;      // SCALED: the exponents of the operands' scales
   };
   struct Inputs {
     Row rows[4];
@@ -379,7 +382,7 @@ struct ProbOut {
     }
     const int r16 = lane & 15, kq = lane >> 4;
     char* lo = hi + product::kStagePlane;
-    const float unit = (out.inv_a != nullptr ? *out.inv_a * *out.inv_b : 1.0f) * kLog2E;
+    const int shift = SCALED ? -(*out.to_a + *out.to_b) : 0;
     const bool two = out.lo != nullptr, edge = col0 + product::kBlockCols > out.columns;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -388,7 +391,10 @@ struct ProbOut {
       const int target = r.target - out.first - col0;
       float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f(fmaf(acc[i * 2 + k / 4][k % 4], unit, -base));
+      for (int k = 0; k < 8; ++k) {
+        const float z = SCALED ? __builtin_ldexpf(acc[i * 2 + k / 4][k % 4], shift) : acc[i * 2 + k / 4][k % 4];
+        v[k] = __builtin_amdgcn_exp2f(fmaf(z, kLog2E, -base));
+      }
       // few blocks hold a row's target, and fewer reach past the classes
       if (target >= 0 && target < product::kBlockCols)
 #pragma unroll
@@ -426,12 +432,12 @@ struct ProbOut {
   }
 };
 
-// A gradient: (C * grad * inv / kProbScale) [+ sum], as the sum so far or as the result; or, where
+// A gradient: C with the scales of dz and its partner taken back [+ sum], as the sum so far or as the result; or, where
 // `turned`, C^T of that.
 struct GradOut {
   static constexpr auto kKind = product::kStaged;
   struct Params {
-    const float *grad, *inv;
+    const int32_t *to_grad, *to;  // the exponents of dloss and of the partner's scale
     const float* before;  // the sum of the pieces so far, or null
     int64_t before_ld;
     void* out;
@@ -442,11 +448,11 @@ struct GradOut {
   };
   struct Inputs {
     float before[product::kPasses][8];
-    float factor, inv;
+    int shift;
   };
   __device__ static void fetch(const Params& p, const product::Place&, int row, int col, int lane, Inputs& in) {
     const int r0 = row + product::pass_row(0, lane), cc = col + product::pass_col(lane);
-    in.factor = *p.grad * (1.0f / kProbScale), in.inv = *p.inv;
+    in.shift = *p.to_grad - *p.to - kProbExponent;
     if (p.before == nullptr) return;
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass)  // padded to whole vectors
@@ -464,7 +470,8 @@ struct GradOut {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int r = (lane & 7) * 8 + i, c = pass * 8 + (lane >> 3);
-          v[pass][i] = *(const float*)(stage + r * 128 + (((c >> 2) ^ ((r >> 1) & 7)) * 16) + (c & 3) * 4) * in.inv * in.factor;
+          v[pass][i] = *(const float*)(stage + r * 128 + (((c >> 2) ^ ((r >> 1) & 7)) * 16) + (c & 3) * 4);
+          v[pass][i] = __builtin_ldexpf(v[pass][i], in.shift);
         }
       next();
 #pragma unroll
@@ -481,7 +488,7 @@ struct GradOut {
       product::pass_values(stage, pass, lane, v[pass]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        v[pass][i] = v[pass][i] * in.inv * in.factor;
+        v[pass][i] = __builtin_ldexpf(v[pass][i], in.shift);
         if (p.before != nullptr) v[pass][i] += in.before[pass][i];
       }
     }
@@ -670,6 +677,8 @@ hipError_t prepare(const daso_loss_args& s, const Plan& q, bool backward, Operan
   return e;
 }
 
+// F32: the operands are fp32, in two planes each, and scaled.
+template <bool F32>
 hipError_t forward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
   char* ws = static_cast<char*>(s.workspace);
   const product::Sums sums = {reinterpret_cast<float*>(ws + q.sums), q.sums_bytes};
@@ -677,23 +686,23 @@ hipError_t forward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
   Operands o;
   hipError_t e = prepare(s, q, false, &o, stream);
   if (e != hipSuccess) return e;
-  product::Launch<LseOut> all = {};
+  product::Launch<LseOut<F32>> all = {};
   all.count = 1;
   logits(all.args[0], q, o, s.tokens, 0, s.vocab);
-  LseOut::Params& out = all.out[0];
+  auto& out = all.out[0];
   out.parts = reinterpret_cast<float2*>(ws + q.parts);
   out.at_target = reinterpret_cast<float*>(ws + q.at_target);
   out.targets = s.targets;
-  out.inv_a = q.f32 ? &sc->inv[kHidden] : nullptr, out.inv_b = q.f32 ? &sc->inv[kWeight] : nullptr;
+  out.to_a = &sc->to[kHidden], out.to_b = &sc->to[kWeight];
   const int64_t across = product::large_tiles(all) ? 256 : 128;
-  if (q.f32) e = product::launch_products<false, false>(all, sums, stream);
-  else e = product::launch_products<true, false>(all, sums, stream);
+  e = product::launch_products<!F32, false>(all, sums, stream);
   if (e != hipSuccess) return e;
   return launch(&join_kernel, dim3(static_cast<uint32_t>((s.tokens + 15) / 16)), dim3(256), stream, (const float2*)out.parts,
                 static_cast<int32_t>((s.vocab + across - 1) / across), s.tokens, s.vocab, s.targets, s.ignore_index,
                 (const float*)out.at_target, s.loss, s.lse);
 }
 
+template <bool F32>
 hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
   char* ws = static_cast<char*>(s.workspace);
   const product::Sums sums = {reinterpret_cast<float*>(ws + q.sums), q.sums_bytes};
@@ -707,32 +716,32 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
   for (int64_t k = 0; k < q.pieces && e == hipSuccess; ++k) {
     const int64_t first = k * q.piece, classes = std::min(q.piece, s.vocab - first);
     const int64_t width = std::max<int64_t>(128, up(classes, 64));
-    product::Launch<ProbOut> prob = {};
+    product::Launch<ProbOut<F32>> prob = {};
     prob.count = 1;
     logits(prob.args[0], q, o, s.tokens, first, classes);
-    ProbOut::Params& out = prob.out[0];
+    auto& out = prob.out[0];
     out.rows = rows;
     // dz in two planes where a product in 22 bits reads it
     out.hi = at(q.p[0]), out.lo = q.p[1] != 0 ? at(q.p[1]) : nullptr;
     out.ld = width;
     out.first = static_cast<int32_t>(first), out.columns = static_cast<int32_t>(classes), out.padded = static_cast<int32_t>(width);
     out.padded_rows = static_cast<int32_t>(q.n_p);
-    out.inv_a = q.f32 ? &sc->inv[kHidden] : nullptr, out.inv_b = q.f32 ? &sc->inv[kWeight] : nullptr;
-    e = q.f32 ? product::launch_products<false, false>(prob, sums, stream) : product::launch_products<true, false>(prob, sums, stream);
+    out.to_a = &sc->to[kHidden], out.to_b = &sc->to[kWeight];
+    e = product::launch_products<!F32, false>(prob, sums, stream);
     if (e != hipSuccess) break;
     // dhidden = dz weight and dweight^T = hidden^T dz, both with the right operand read turned
     product::Launch<GradOut> grads = {};
     if (dh) {
       product::Args& a = grads.args[grads.count];
       const _Float16 *w0 = at(q.wp[0]) + first * q.d_p, *w1 = at(q.wp[1]) + first * q.d_p;
-      a.segments = q.f32 ? 3 : 1;
+      a.segments = F32 ? 3 : 1;
       a.a[0] = at(q.p[0]), a.b[0] = w0;
       a.a[1] = at(q.p[0]), a.b[1] = w1;
       a.a[2] = at(q.p[1]), a.b[2] = w0;
       a.lda = width, a.ldb = q.d_p, a.steps = static_cast<int32_t>(width / 64);
       a.M = static_cast<int32_t>(s.tokens), a.N = static_cast<int32_t>(q.d_p), a.batch = 1;
       GradOut::Params& g = grads.out[grads.count++];
-      g.grad = &sc->to[kGrad], g.inv = &sc->inv[kWeight];
+      g.to_grad = &sc->to[kGrad], g.to = &sc->to[kWeight];
       float* sum = reinterpret_cast<float*>(ws + q.sum);
       if (k > 0) g.before = sum, g.before_ld = q.d_p;
       g.rows = a.M;
@@ -742,14 +751,14 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
     if (dw) {
       product::Args& a = grads.args[grads.count];
       // dz in one plane or two; hidden in one (exact) where it is bf16
-      a.segments = q.f32 ? 3 : dw32 ? 2 : 1;
+      a.segments = F32 ? 3 : dw32 ? 2 : 1;
       a.a[0] = at(q.ht[0]), a.b[0] = at(q.p[0]);
       a.a[1] = at(q.ht[0]), a.b[1] = at(q.p[1]);
       a.a[2] = at(q.ht[1]), a.b[2] = at(q.p[0]);
       a.lda = q.n_p, a.ldb = width, a.steps = static_cast<int32_t>(q.n_p / 64);
       a.M = static_cast<int32_t>(s.d), a.N = static_cast<int32_t>(width), a.batch = 1;
       GradOut::Params& g = grads.out[grads.count++];
-      g.grad = &sc->to[kGrad], g.inv = &sc->inv[kHidden];
+      g.to_grad = &sc->to[kGrad], g.to = &sc->to[kHidden];
       g.out = static_cast<char*>(s.dweight) + first * s.dweight_stride * static_cast<int64_t>(host::bytes_of(s.dweight_type));
       g.ld = s.dweight_stride, g.bf16 = !dw32;
       g.rows = static_cast<int32_t>(classes), g.cols = a.M, g.turned = 1;
@@ -779,7 +788,8 @@ int daso_linear_cross_entropy(const daso_loss_args* args, hipStream_t stream) {
   const daso::Plan q = daso::plan_of(*args, false);
   if ((rc = daso::host::check_workspace(args->workspace, args->workspace_bytes, q.bytes)) != DASO_OK) return rc;
   if ((rc = daso::current_device(stream)) != DASO_OK) return rc;
-  return daso::forward(*args, q, stream) == hipSuccess ? DASO_OK : DASO_EHIP;
+  const hipError_t e = q.f32 ? daso::forward<true>(*args, q, stream) : daso::forward<false>(*args, q, stream);
+  return e == hipSuccess ? DASO_OK : DASO_EHIP;
 }
 
 int daso_linear_cross_entropy_backward(const daso_loss_args* args, hipStream_t stream) {
@@ -798,7 +808,7 @@ int daso_linear_cross_entropy_backward(const daso_loss_args* args, hipStream_t s
             ? daso::launch(&daso::zero_rows_kernel<float>, grid, block, stream, (float*)s.dweight, s.dweight_stride, s.vocab, s.d)
             : daso::launch(&daso::zero_rows_kernel<uint16_t>, grid, block, stream, (uint16_t*)s.dweight, s.dweight_stride, s.vocab, s.d);
   } else {
-    e = daso::backward(s, q, stream);
+    e = q.f32 ? daso::backward<true>(s, q, stream) : daso::backward<false>(s, q, stream);
   }
   return e == hipSuccess ? DASO_OK : DASO_EHIP;
 }
