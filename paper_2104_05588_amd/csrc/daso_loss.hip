@@ -37,6 +37,9 @@ using product::half4;
 using product::half8;
 
 constexpr float kLog2E = 1.44269504f;
+// exp(z - m) is 2^(z log2 e - m log2 e) in one multiply-add, whose second product is rounded: of m = 2^10 it is off by up to
+// 2^-14, of 2^32 by 2^8, and the power by its exponential.  From here on m is subtracted first.
+constexpr float kLargeLogit = 1 << 10;
 constexpr int kProbExponent = 14;  // dz / dloss in [-1, 1], times 2^14, as binary16
 constexpr float kProbScale = 1 << kProbExponent;
 
@@ -241,8 +244,12 @@ struct LseOut {
     m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
     // columns that are all -inf, or none, add nothing; +inf or NaN make the sum NaN
-    const float base = m == -__builtin_inff() ? 0.0f : m * kLog2E;
-    float s = 0.0f;
+    float base = m == -__builtin_inff() ? 0.0f : m * kLog2E, s = 0.0f;
+    if (__builtin_fabsf(base) >= kLargeLogit) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) z[k] -= m;
+      base = 0.0f;
+    }
 #pragma unroll
     for (int k = 0; k < 16; ++k) s += __builtin_amdgcn_exp2f(fmaf(z[k], kLog2E, -base));
     s += __shfl_xor(s, 16);
@@ -387,14 +394,19 @@ struct ProbOut {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const Row r = in.rows[i];
-      const float base = r.lse * kLog2E;
+      float base = r.lse * kLog2E;
       const int target = r.target - out.first - col0;
       float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float z = SCALED ? __builtin_ldexpf(acc[i * 2 + k / 4][k % 4], shift) : acc[i * 2 + k / 4][k % 4];
-        v[k] = __builtin_amdgcn_exp2f(fmaf(z, kLog2E, -base));
+      for (int k = 0; k < 8; ++k) v[k] = SCALED ? __builtin_ldexpf(acc[i * 2 + k / 4][k % 4], shift) : acc[i * 2 + k / 4][k % 4];
+      if (__builtin_fabsf(base) >= kLargeLogit) {
+        // (a logit that is summed in another order than the forward pass's may come out above the log-sum-exp)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = v[k] > r.lse ? 0.0f : v[k] - r.lse;
+        base = 0.0f;
       }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f(fmaf(v[k], kLog2E, -base));
       // few blocks hold a row's target, and fewer reach past the classes
       if (target >= 0 && target < product::kBlockCols)
 #pragma unroll

@@ -1,12 +1,13 @@
-"""Calls of the training operators at the edges of what they take: in place at every length, operands of any size.
-Tolerances as derived in test_gpu_train."""
+"""Calls of the training operators at the edges of what they take: in place at every length, operands of any size,
+whatever lies in ignored places.  Tolerances as derived in test_gpu_train."""
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
 import paper_2104_05588_amd as daso  # noqa: E402
-from tests.test_gpu_train import announce, check_loss, gen, loss_case  # noqa: E402
+from oracle import train_oracle as O  # noqa: E402
+from tests.test_gpu_train import U, announce, check_loss, close, gen, loss_case, np64  # noqa: E402
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(), reason="no GPU")]
 
@@ -45,3 +46,35 @@ def test_loss_of_huge_operands_that_do_not_meet():
     h[:, 48:], w[:, :48] = 0, 0
     h, w = h * 1e25, w * 1e25
     check_loss(h, w, t, s * 1e-20, h.cuda(), w.cuda())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("size", [1e3, 1e5, 1e6, 1e9])
+def test_loss_of_huge_logits(dtype, size):
+    """Logits up to 1e18: of each token the largest one decides, and nothing overflows."""
+    announce("loss of huge logits", dtype, size)
+    n, v, d = 130, 300, 96
+    h, w, t, s = loss_case(n, v, d, dtype, 0.1, 47)
+    h, w = (h.double() * size).to(dtype), (w.double() * size).to(dtype)
+    hd, wd, td = h.cuda(), w.cuda(), t.cuda()
+    loss, lse = daso.linear_cross_entropy(hd, wd, td)
+    h64, w64, s64 = np64(h), np64(w), np.where(t.numpy() == -100, 0, np64(s))
+    want_loss, want_lse = O.linear_cross_entropy(h64, w64, t.numpy())
+    mag = (np.abs(h64) @ np.abs(w64).T).max(axis=1)
+    tol = 2 * (d * U + 2.0 ** -20) * mag + 8 * U * (np.abs(want_lse) + mag)
+    close(lse, want_lse, tol, "lse")
+    close(loss, want_loss, tol, "loss")
+    # p may be anything where two logits are nearer to each other than they are off; else it is zero or one
+    dh, dw = daso.linear_cross_entropy_backward(s.cuda(), hd, wd, td, lse, dweight=torch.empty(v, d, device="cuda"))
+    a = np.abs(s64)[:, None]
+    assert torch.isfinite(dh).all() and torch.isfinite(dw).all()
+    assert (np.abs(np64(dh)) <= (a * 2.01) * np.abs(w64).sum(axis=0)).all()
+    z = h64 @ w64.T
+    two = np.sort(z, axis=1)[:, -2:]
+    sure = two[:, 1] - two[:, 0] > 2 * tol + 100
+    assert sure.sum() > n // 4
+    want_dh, _, _ = O.linear_cross_entropy_backward(s64, h64, w64, t.numpy())
+    # where one class is sure its p is off by what the logit and the log-sum-exp are, of which 1e5 is all of it; the others' are zero
+    off = np.abs(np64(dh) - want_dh)
+    plane = np.abs(want_dh) * 2.0 ** -8 + a * np.abs(w64).max() * (2.0 ** -10 + v * 2.0 ** -37)
+    assert (off <= a * np.abs(w64[z.argmax(axis=1)]) * 1.01 + plane)[sure].all()
