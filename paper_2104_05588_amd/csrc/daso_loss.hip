@@ -15,9 +15,9 @@
 // tokens or classes are bound by the chain of eight launches, 3 to 18 us each.
 //
 // Numbers.  bf16 operands are multiplied as they are in the forward product; fp32 ones as two
-// binary16 planes each, scaled by a power of two from the tensor's largest value (22
-// bits).  In the backward products dz is binary16, of values in [-1, 1] times 2^14, which keeps 3 bits
-// more than bf16 would, and hidden and weight are turned to binary16 by the same scaling
+// binary16 planes each (22 bits), hidden scaled by a power of two from each row's largest value, weight by one from the
+// tensor's.  In the backward products dz is binary16, of values in [-1, 1] times 2^14, which keeps 3 bits
+// more than bf16 would, and hidden and weight are turned to binary16 by a scale each
 // (exact for a bf16 value within 2^-32 of the largest), so that a bf16 result is off by 2e-4 before it is
 // rounded; fp32 results take dz as two planes.
 #include <hip/hip_runtime.h>
@@ -41,120 +41,150 @@ constexpr float kLog2E = 1.44269504f;
 // 2^-14, of 2^32 by 2^8, and the power by its exponential.  From here on m is subtracted first.
 constexpr float kLargeLogit = 1 << 10;
 constexpr int kProbExponent = 14;  // dz / dloss in [-1, 1], times 2^14, as binary16
-constexpr float kProbScale = 1 << kProbExponent;
 
-// Powers of two from the largest finite magnitudes of hidden, weight and dloss.
+// Exponents of scales, from the largest finite magnitudes of hidden, weight and dloss.
 enum Tensor { kHidden, kWeight, kGrad };
-constexpr int kTopParts = 512;  // workgroups that look for one
+constexpr int kTopParts = 512;     // workgroups that look for one
+constexpr int kNone = -(1 << 20);  // the exponent of zero
 struct Scales {
-  uint32_t top[3][kTopParts];  // bits of the magnitudes
-  int32_t to[3];               // exponents: hidden and weight times 2^to are below 2^15, dloss times 2^-to is at most 1
+  int32_t top[3][kTopParts];  // exponents of the magnitudes
+  int32_t to[3];              // hidden and weight times 2^to are below 2^15, dloss times 2^-to is at most 1
 };
 
 // What the backward epilogue needs of a token.
 struct Row {
   float lse;
-  float g;         // dloss, scaled, times kProbScale
+  float g;         // dloss, scaled, times 2^kProbExponent
   int32_t target;  // -1: the whole row is zero
-  int32_t pad;
+  int32_t to;      // fp32 operands: the exponent of its scale in the logits
 };
 
-__device__ inline float power_of_two(int e) { return __builtin_bit_cast(float, uint32_t(min(max(e, -126), 127) + 127) << 23); }
+// floor(log2) of a magnitude (of a subnormal one the least normal's).
+__device__ inline int exponent_of(float magnitude) {
+  const uint32_t bits = __builtin_bit_cast(uint32_t, magnitude);
+  return bits == 0 ? kNone : static_cast<int>(max(bits >> 23, 1u)) - 127;
+}
+// The exponent that brings what has `top` for its largest value's into binary16, below 2^15.
+__device__ inline int to_half(int top) { return top == kNone ? 0 : 14 - top; }
 
 struct TopArgs {
-  struct {
-    const void* src;
-    int64_t stride, rows, cols;
-    int32_t type;
-  } of[3];
+  const void *hidden, *weight;
+  int64_t hidden_stride, weight_stride, tokens, vocab, d;
+  const float* dloss;  // null: not looked at
+  int32_t* row_top;    // of each token's hidden
   Scales* out;
 };
 
+__device__ inline void take_finite(float v, float& m) {
+  v = __builtin_fabsf(v);
+  m = fmaxf(m, v < __builtin_inff() ? v : 0.0f);
+}
+
+// The largest magnitude of a run of elements, of which a thread takes eight in four places at a time.
 template <class T>
-__device__ inline float top_of(const T* src, int64_t stride, int64_t rows, int64_t cols) {
+__device__ inline float top_of_run(const T* src, int64_t n) {
   float m = 0.0f;
-  auto take = [&](float v) {
-    v = __builtin_fabsf(v);
-    m = fmaxf(m, v < __builtin_inff() ? v : 0.0f);
-  };
-  if (stride == cols) {  // one run of elements, of which a thread takes eight in four places at a time
-    const int64_t n = rows * cols, whole = n / 8 * 8, id = blockIdx.x * 256 + threadIdx.x, step = gridDim.x * int64_t(2048);
-    for (int64_t i = id * 8; i < whole; i += 4 * step) {
-      float v[4][8] = {};
+  const int64_t whole = n / 8 * 8, id = blockIdx.x * 256 + threadIdx.x, step = gridDim.x * int64_t(2048);
+  for (int64_t i = id * 8; i < whole; i += 4 * step) {
+    float v[4][8] = {};
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (i + k * step < whole) load8(src + i + k * step, v[k]);
+    for (int k = 0; k < 4; ++k)
+      if (i + k * step < whole) load8(src + i + k * step, v[k]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) take(v[k][j]);
-    }
-    if (whole + id < n) take(load1(src + whole + id));
-    return wave_max(m);
+      for (int j = 0; j < 8; ++j) take_finite(v[k][j], m);
   }
+  if (whole + id < n) take_finite(load1(src + whole + id), m);
+  return wave_max(m);
+}
+
+// Calls f(row, largest magnitude), in every lane, for a wavefront's rows: four at a time for loads in flight, or, where
+// there are no more rows than wavefronts, four places of one (a classifier's 256 rows of 2048: 2 us less).
+template <class T, class F>
+__device__ inline void tops_of_rows(const T* src, int64_t stride, int64_t rows, int64_t cols, F f) {
   const int64_t wave = (blockIdx.x * 256 + threadIdx.x) >> 6, waves = gridDim.x * 4;
   const int lane = threadIdx.x & 63;
   const int64_t whole = cols / 8 * 8;
-  // four rows at a time, for loads in flight
+  const bool few = rows <= waves;
+  const int64_t next = few ? 0 : waves, along = few ? 512 : 0, step = few ? 2048 : 512;
   for (int64_t r = wave; r < rows; r += 4 * waves) {
-    for (int64_t c = lane * 8; c < whole; c += 512) {
+    float m[4] = {};
+    for (int64_t c = lane * 8; c < whole; c += step) {
       float v[4][8] = {};
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (r + k * waves < rows) load8(src + (r + k * waves) * stride + c, v[k]);
+        if (r + k * next < rows && c + k * along < whole) load8(src + (r + k * next) * stride + c + k * along, v[k]);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) take(v[k][i]);
+        for (int i = 0; i < 8; ++i) take_finite(v[k][i], m[k]);
     }
     if (whole + lane < cols) {
       float v[4] = {};
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (r + k * waves < rows) v[k] = load1(src + (r + k * waves) * stride + whole + lane);
+        if (r + k * next < rows) v[k] = load1(src + (r + k * next) * stride + whole + lane);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) take(v[k]);
+      for (int k = 0; k < 4; ++k) take_finite(v[k], m[k]);
     }
+    if (few) {
+      f(r, wave_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))));
+      continue;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (r + k * waves < rows) f(r + k * waves, wave_max(m[k]));
   }
-  return wave_max(m);
 }
 
 // Workgroup (x, y): part x of tensor y.
+template <class T>
 __global__ __launch_bounds__(256) void tops_kernel(TopArgs a) {
-  __shared__ float shared[4];
-  const auto& s = a.of[blockIdx.y];
-  const float m = s.type == DASO_TYPE_BF16 ? top_of((const uint16_t*)s.src, s.stride, s.rows, s.cols)
-                                           : top_of((const float*)s.src, s.stride, s.rows, s.cols);
-  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = m;
+  __shared__ int32_t shared[4];
+  int top = kNone;
+  if (blockIdx.y == kHidden) {
+    tops_of_rows((const T*)a.hidden, a.hidden_stride, a.tokens, a.d, [&](int64_t row, float m) {
+      const int e = exponent_of(m);
+      if ((threadIdx.x & 63) == 0) a.row_top[row] = e;
+      top = max(top, e);
+    });
+  } else if (blockIdx.y == kGrad) {
+    if (a.dloss != nullptr) top = exponent_of(top_of_run(a.dloss, a.tokens));
+  } else if (a.weight_stride == a.d) {
+    top = exponent_of(top_of_run((const T*)a.weight, a.vocab * a.d));
+  } else {
+    tops_of_rows((const T*)a.weight, a.weight_stride, a.vocab, a.d, [&](int64_t, float m) { top = max(top, exponent_of(m)); });
+  }
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = top;
   __syncthreads();
-  if (threadIdx.x == 0)
-    a.out->top[blockIdx.y][blockIdx.x] = __builtin_bit_cast(uint32_t, fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3])));
+  if (threadIdx.x == 0) a.out->top[blockIdx.y][blockIdx.x] = max(max(shared[0], shared[1]), max(shared[2], shared[3]));
 }
 
 // The exponent of a tensor's scale, by a workgroup of 256.
-__device__ inline int scale_exponent(const Scales* s, int tensor, uint32_t* shared) {
-  uint32_t m = max(s->top[tensor][threadIdx.x], s->top[tensor][threadIdx.x + 256]);
+__device__ inline int scale_exponent(const Scales* s, int tensor, int32_t* shared) {
+  int m = max(s->top[tensor][threadIdx.x], s->top[tensor][threadIdx.x + 256]);
 #pragma unroll
-  for (int k = 32; k > 0; k >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), k)));
+  for (int k = 32; k > 0; k >>= 1) m = max(m, __shfl_xor(m, k));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = m;
   __syncthreads();
   m = max(max(shared[0], shared[1]), max(shared[2], shared[3]));
-  const int e = m == 0 ? 0 : static_cast<int>(max(m >> 23, 1u)) - 127;
-  return min(max(tensor == kGrad ? e + 1 : 14 - e, -126), 126);
+  return tensor != kGrad ? to_half(m) : m == kNone ? 0 : m + 1;
 }
 static_assert(kTopParts == 512, "two parts a thread");
 
 // What comes before the products of a pass, in one launch: planes of hidden and weight, and the
 // backward pass's rows.
 constexpr int kMaxPlanes = 4;
+enum ScaleBy { kRaw, kByRow = 1, kByTensor = 2 };  // kByTensor + the tensor
 struct PrepareArgs {
   int32_t count;
   int64_t first[kMaxPlanes + 2];  // workgroups of each job: the planes, then the rows
   PlanesArgs planes[kMaxPlanes];
-  int32_t tensor[kMaxPlanes];
-  int32_t raw[kMaxPlanes];
+  int32_t by[kMaxPlanes];         // how a job's values are scaled
   Scales* scales;                 // null: none are needed
+  const int32_t* row_top;
   Row* rows;
   int64_t padded, tokens, vocab;
   const float *lse, *dloss;
@@ -165,7 +195,7 @@ struct PrepareArgs {
 template <class T>
 __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   __shared__ uint16_t lds[2][64][66];
-  __shared__ uint32_t shared[4];
+  __shared__ int32_t shared[4];
   const int64_t id = blockIdx.x + int64_t(blockIdx.y) * gridDim.x;
   if (id >= a.first[a.count + 1]) return;
   if (id == 0 && a.scales != nullptr) {
@@ -180,11 +210,16 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
     const PlanesArgs& p = a.planes[k];
     const int64_t t = id - a.first[k], across = p.cols_p / 64;
     const int tr = static_cast<int>(t / across), tc = static_cast<int>(t % across);
-    if (a.raw[k]) planes_tile<T, true>(p, 0, tr, tc, 1.0f, lds);
-    else planes_tile<T, false>(p, 0, tr, tc, power_of_two(scale_exponent(a.scales, a.tensor[k], shared)), lds);
+    if (a.by[k] == kRaw) {
+      planes_tile<T, true>(p, 0, tr, tc, [](float v) { return v; }, lds);
+      return;
+    }
+    const int row = min(tr * 64 + static_cast<int>(threadIdx.x >> 2), p.rows - 1);  // this thread's
+    const int to = a.by[k] == kByRow ? to_half(a.row_top[row]) : scale_exponent(a.scales, a.by[k] - kByTensor, shared);
+    planes_tile<T, false>(p, 0, tr, tc, [to](float v) { return __builtin_ldexpf(v, to); }, lds);
     return;
   }
-  const float inv = power_of_two(-scale_exponent(a.scales, kGrad, shared));
+  const int to_grad = scale_exponent(a.scales, kGrad, shared);
   const int64_t i = (id - a.first[a.count]) * 256 + threadIdx.x;
   if (i >= a.padded) return;
   Row r = {0.0f, 0.0f, -1, 0};
@@ -192,7 +227,8 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
     const int64_t t = a.targets[i];
     if (t >= 0 && t < a.vocab && t != a.ignore) {
       r.lse = a.lse[i];
-      r.g = a.dloss[i] * inv * kProbScale;
+      r.g = __builtin_ldexpf(a.dloss[i], kProbExponent - to_grad);
+      r.to = to_half(a.row_top[i]);
       r.target = static_cast<int32_t>(t);
     } else if (t != a.ignore) {
       r.g = __builtin_nanf("");
@@ -213,7 +249,7 @@ struct LseOut {
     float2* parts;  // [tile column][token]
     float* at_target;
     const int64_t* targets;
-    const int32_t *to_a, *to_b;  // SCALED: the exponents of the operands' scales
+    const int32_t *row_top, *to_b;  // SCALED: of the left operand's rows, and the exponent of the right one's scale
   };
   // Strip i of a band: 16 rows of it a wavefront, 64 columns of which are in c (two blocks' two
   // columns of 16).
@@ -268,7 +304,10 @@ struct LseOut {
     for (int w = 0; w < kAcross; ++w) s += from[w].y * __expf(from[w].x - base);
     out.parts[int64_t(at.tn) * p.M + row] = make_float2(m, s);
   }
-  __device__ static int scale(const Params& out) { return SCALED ? -(*out.to_a + *out.to_b) : 0; }
+  // What takes the scales of a row's logits back.
+  __device__ static int shift_of(const Params& out, const product::Args& p, int row) {
+    return SCALED ? -(to_half(out.row_top[min(row, p.M - 1)]) + *out.to_b) : 0;
+  }
   // A row's target as a column of the product, or none.
   __device__ static int32_t target_of(const Params& out, const product::Args& p, int row) {
     const int64_t t = out.targets[min(row, p.M - 1)];
@@ -282,13 +321,13 @@ struct LseOut {
     constexpr int kBands = Tile::kBlocks / 2;      // runs of 64 rows a wavefront holds
     const int lane = product::thread_here() & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     float2* shared = (float2*)lds;  // [row][kAcross]
-    const int shift = scale(out);
-    int32_t target[kBands][4];
+    int32_t target[kBands][4], shift[kBands][4];
     int row0, col0;
 #pragma unroll
     for (int k = 0; k < kBands * 4; ++k) {
       Tile::block_at(wave, k / 4 * 2, &row0, &col0);
-      target[k / 4][k % 4] = target_of(out, p, at.tm * Tile::kRows + row0 + k % 4 * 16 + (lane & 15));
+      const int row = at.tm * Tile::kRows + row0 + k % 4 * 16 + (lane & 15);
+      target[k / 4][k % 4] = target_of(out, p, row), shift[k / 4][k % 4] = shift_of(out, p, row);
     }
 #pragma unroll
     for (int band = 0; band < kBands; ++band)
@@ -296,7 +335,7 @@ struct LseOut {
       for (int i = 0; i < 4; ++i) {
         Tile::block_at(wave, band * 2, &row0, &col0);
         strip<Tile>(out, p, at, acc[band * 2][i * 2], acc[band * 2][i * 2 + 1], acc[band * 2 + 1][i * 2], acc[band * 2 + 1][i * 2 + 1],
-                    band, i, target[band][i], shift, wave, lane, shared + (row0 + i * 16 + (lane & 15)) * kAcross + wave % kAcross);
+                    band, i, target[band][i], shift[band][i], wave, lane, shared + (row0 + i * 16 + (lane & 15)) * kAcross + wave % kAcross);
       }
     __syncthreads();
     for (int in = threadIdx.x; in < Tile::kRows; in += Tile::kThreads)
@@ -310,8 +349,8 @@ struct LseOut {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int row0, col0;
     Tile::block_at(wave, band * 2, &row0, &col0);
-    const int32_t target = target_of(out, p, at.tm * Tile::kRows + row0 + i * 16 + (lane & 15));
-    strip<Tile>(out, p, at, c[0], c[1], c[2], c[3], band, i, target, scale(out), wave, lane,
+    const int row = at.tm * Tile::kRows + row0 + i * 16 + (lane & 15);
+    strip<Tile>(out, p, at, c[0], c[1], c[2], c[3], band, i, target_of(out, p, row), shift_of(out, p, row), wave, lane,
                 shared + (wave / kAcross * 16 + (lane & 15)) * kAcross + wave % kAcross);
     __syncthreads();
     if (threadIdx.x >= 32) return;
@@ -370,7 +409,7 @@ struct ProbOut {
     int64_t ld;
     int32_t first, columns, padded;  // the piece: its first class, its classes, its columns with padding
     int32_t padded_rows;             // tokens with padding: the planes are contracted over both
-    const int32_t *to_a, *to_b;      // SCALED: the exponents of the operands' scales
+    const int32_t* to_b;             // SCALED: the exponent of the right operand's scale
   };
   struct Inputs {
     Row rows[4];
@@ -389,7 +428,7 @@ struct ProbOut {
     }
     const int r16 = lane & 15, kq = lane >> 4;
     char* lo = hi + product::kStagePlane;
-    const int shift = SCALED ? -(*out.to_a + *out.to_b) : 0;
+    const int to_b = SCALED ? *out.to_b : 0;
     const bool two = out.lo != nullptr, edge = col0 + product::kBlockCols > out.columns;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -398,7 +437,7 @@ struct ProbOut {
       const int target = r.target - out.first - col0;
       float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = SCALED ? __builtin_ldexpf(acc[i * 2 + k / 4][k % 4], shift) : acc[i * 2 + k / 4][k % 4];
+      for (int k = 0; k < 8; ++k) v[k] = SCALED ? __builtin_ldexpf(acc[i * 2 + k / 4][k % 4], -(r.to + to_b)) : acc[i * 2 + k / 4][k % 4];
       if (__builtin_fabsf(base) >= kLargeLogit) {
         // (a logit that is summed in another order than the forward pass's may come out above the log-sum-exp)
 #pragma unroll
@@ -549,7 +588,7 @@ struct Plan {
   int64_t n_p, d_p, v_p;          // padded tokens, features, classes
   int64_t piece, pieces;          // classes of a piece (but the last), pieces
   bool f32, copy_h, copy_w;       // operands of the logits that are copied
-  size_t scales, sums, sums_bytes, parts, at_target, rows, h[2], w[2], ht[2], wp[2], p[2], sum;
+  size_t scales, row_top, sums, sums_bytes, parts, at_target, rows, h[2], w[2], ht[2], wp[2], p[2], sum;
   size_t bytes;
 };
 
@@ -578,6 +617,7 @@ Plan plan_of(const daso_loss_args& s, bool backward) {
   };
   const int planes = q.f32 ? 2 : 1;
   q.scales = take(sizeof(Scales));
+  q.row_top = take(q.f32 || backward ? 4 * s.tokens : 0);
   for (int i = 0; i < planes; ++i) {
     // with a copy or without: what a call needs is then known from its sizes alone
     q.h[i] = take(2 * q.n_p * q.d_p);
@@ -623,14 +663,14 @@ void logits(product::Args& a, const Plan& q, const Operands& o, int64_t tokens, 
   a.M = static_cast<int32_t>(tokens), a.N = static_cast<int32_t>(classes), a.batch = 1;
 }
 
-void add_planes(PrepareArgs& a, int32_t tensor, bool raw, const void* src, int64_t stride, int64_t rows, int64_t cols,
+void add_planes(PrepareArgs& a, int32_t by, const void* src, int64_t stride, int64_t rows, int64_t cols,
                 int64_t rows_p, int64_t cols_p, char* d0, char* d1, char* t0, char* t1) {
   PlanesArgs& p = a.planes[a.count];
   p.src = src, p.stride = stride;
   p.rows = static_cast<int32_t>(rows), p.cols = static_cast<int32_t>(cols);
   p.rows_p = static_cast<int32_t>(rows_p), p.cols_p = static_cast<int32_t>(cols_p);
   p.d[0] = (uint16_t*)d0, p.d[1] = (uint16_t*)d1, p.t[0] = (uint16_t*)t0, p.t[1] = (uint16_t*)t1;
-  a.tensor[a.count] = tensor, a.raw[a.count] = raw ? 1 : 0;
+  a.by[a.count] = by;
   a.first[a.count + 1] = a.first[a.count] + (rows_p / 64) * (cols_p / 64);
   ++a.count;
 }
@@ -641,31 +681,29 @@ hipError_t prepare(const daso_loss_args& s, const Plan& q, bool backward, Operan
   Scales* sc = reinterpret_cast<Scales*>(ws + q.scales);
   hipError_t e = hipSuccess;
   const bool scaled = q.f32 || backward;
+  int32_t* row_top = reinterpret_cast<int32_t*>(ws + q.row_top);
   if (scaled) {
-    TopArgs t = {};
-    t.of[kHidden] = {s.hidden, s.hidden_stride, s.tokens, s.d, s.type};
-    t.of[kWeight] = {s.weight, s.weight_stride, s.vocab, s.d, s.type};
-      t.of[kGrad] = {s.dloss, 1, backward ? s.tokens : 0, 1, DASO_TYPE_F32};
-    t.out = sc;
-    e = launch(&tops_kernel, dim3(kTopParts, 3), dim3(256), stream, t);
+    const TopArgs t = {s.hidden, s.weight, s.hidden_stride, s.weight_stride, s.tokens, s.vocab, s.d, backward ? s.dloss : nullptr, row_top, sc};
+    e = s.type == DASO_TYPE_BF16 ? launch(&tops_kernel<uint16_t>, dim3(kTopParts, 3), dim3(256), stream, t)
+                                 : launch(&tops_kernel<float>, dim3(kTopParts, 3), dim3(256), stream, t);
   }
   PrepareArgs a = {};
-  const auto place = [ws](size_t at, bool wanted) { return wanted ? ws + at : nullptr; };
   const bool ht = backward && s.dweight != nullptr, wp = backward && s.dhidden != nullptr;
-  const auto hidden = [&](bool raw, char* d0, char* d1, char* t0, char* t1) {
-    add_planes(a, kHidden, raw, s.hidden, s.hidden_stride, s.tokens, s.d, q.n_p, q.d_p, d0, d1, t0, t1);
+  const auto hidden = [&](int32_t by, char* d0, char* d1, char* t0, char* t1) {
+    add_planes(a, by, s.hidden, s.hidden_stride, s.tokens, s.d, q.n_p, q.d_p, d0, d1, t0, t1);
   };
-  const auto weight = [&](bool raw, char* d0, char* d1, char* t0, char* t1) {
-    add_planes(a, kWeight, raw, s.weight, s.weight_stride, s.vocab, s.d, q.v_p, q.d_p, d0, d1, t0, t1);
+  const auto weight = [&](int32_t by, char* d0, char* d1) {
+    add_planes(a, by, s.weight, s.weight_stride, s.vocab, s.d, q.v_p, q.d_p, d0, d1, nullptr, nullptr);
   };
   if (q.f32) {
-    weight(false, ws + q.w[0], ws + q.w[1], nullptr, nullptr);
-    hidden(false, ws + q.h[0], ws + q.h[1], place(q.ht[0], ht), place(q.ht[1], ht));
+    weight(kByTensor + kWeight, ws + q.w[0], ws + q.w[1]);
+    hidden(kByRow, ws + q.h[0], ws + q.h[1], nullptr, nullptr);
+    if (ht) hidden(kByTensor + kHidden, nullptr, nullptr, ws + q.ht[0], ws + q.ht[1]);
   } else {
-    if (q.copy_w) weight(true, ws + q.w[0], nullptr, nullptr, nullptr);
-    if (q.copy_h) hidden(true, ws + q.h[0], nullptr, nullptr, nullptr);
-    if (wp) weight(false, ws + q.wp[0], nullptr, nullptr, nullptr);
-    if (ht) hidden(false, nullptr, nullptr, ws + q.ht[0], nullptr);
+    if (q.copy_w) weight(kRaw, ws + q.w[0], nullptr);
+    if (q.copy_h) hidden(kRaw, ws + q.h[0], nullptr, nullptr, nullptr);
+    if (wp) weight(kByTensor + kWeight, ws + q.wp[0], nullptr);
+    if (ht) hidden(kByTensor + kHidden, nullptr, nullptr, ws + q.ht[0], nullptr);
   }
   a.first[a.count + 1] = a.first[a.count];
   if (backward) {
@@ -675,6 +713,7 @@ hipError_t prepare(const daso_loss_args& s, const Plan& q, bool backward, Operan
     a.lse = s.lse, a.dloss = s.dloss, a.targets = s.targets, a.ignore = s.ignore_index;
   }
   a.scales = scaled ? sc : nullptr;
+  a.row_top = row_top;
   const int64_t groups = a.first[a.count + 1], row = int64_t(1) << 20;
   if (e == hipSuccess && groups > 0) {
     const dim3 grid(static_cast<uint32_t>(std::min(groups, row)), static_cast<uint32_t>((groups + row - 1) / row));
@@ -705,7 +744,7 @@ hipError_t forward(const daso_loss_args& s, const Plan& q, hipStream_t stream) {
   out.parts = reinterpret_cast<float2*>(ws + q.parts);
   out.at_target = reinterpret_cast<float*>(ws + q.at_target);
   out.targets = s.targets;
-  out.to_a = &sc->to[kHidden], out.to_b = &sc->to[kWeight];
+  out.row_top = reinterpret_cast<const int32_t*>(ws + q.row_top), out.to_b = &sc->to[kWeight];
   const int64_t across = product::large_tiles(all) ? 256 : 128;
   e = product::launch_products<!F32, false>(all, sums, stream);
   if (e != hipSuccess) return e;
@@ -738,7 +777,7 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
     out.ld = width;
     out.first = static_cast<int32_t>(first), out.columns = static_cast<int32_t>(classes), out.padded = static_cast<int32_t>(width);
     out.padded_rows = static_cast<int32_t>(q.n_p);
-    out.to_a = &sc->to[kHidden], out.to_b = &sc->to[kWeight];
+    out.to_b = &sc->to[kWeight];
     e = product::launch_products<!F32, false>(prob, sums, stream);
     if (e != hipSuccess) break;
     // dhidden = dz weight and dweight^T = hidden^T dz, both with the right operand read turned

@@ -382,7 +382,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(LayOut a) {
   const double* s = a.sums + (a.first_matrix[k] + batch) * host::kSumParts;
   const double sum = group_sum(static_cast<int>(threadIdx.x) < a.parts ? s[threadIdx.x] : 0.0, shared);
   const float scale = static_cast<float>(kScale / (sqrt(sum) + a.eps));
-  planes_tile<T, false>(p, batch, static_cast<int>((t % per) / across), static_cast<int>(t % across), scale, lds);
+  planes_tile<T, false>(p, batch, static_cast<int>((t % per) / across), static_cast<int>(t % across), [scale](float v) { return scale * v; }, lds);
 }
 
 // ------------------------------------------------------------------------- small matrices

@@ -109,10 +109,10 @@ struct PlanesArgs {
   uint16_t *d[2], *t[2];  // hi, lo
 };
 
-// One 64 x 64 tile by 256 threads.  RAW: the source's 16-bit patterns themselves (bf16),
-// else scale * value as binary16 hi and lo.
-template <class T, bool RAW>
-__device__ inline void planes_tile(const PlanesArgs& p, int64_t batch, int tr, int tc, float scale, uint16_t (*lds)[64][66]) {
+// One 64 x 64 tile by 256 threads, four neighbouring ones a row of the source.  RAW: the source's 16-bit patterns
+// themselves (bf16), else scaled(value) as binary16 hi and lo.
+template <class T, bool RAW, class F>
+__device__ inline void planes_tile(const PlanesArgs& p, int64_t batch, int tr, int tc, F scaled, uint16_t (*lds)[64][66]) {
   const int row = threadIdx.x >> 2, col = (threadIdx.x & 3) * 16;
   const int r = tr * 64 + row, c = tc * 64 + col;
   const T* src = (const T*)p.src + batch * p.batch_stride + int64_t(r) * p.stride + c;
@@ -135,7 +135,7 @@ __device__ inline void planes_tile(const PlanesArgs& p, int64_t batch, int tr, i
       lo[i] = 0;
     } else {
       _Float16 h, l;
-      product::split(scale * v[i], &h, &l);
+      product::split(scaled(v[i]), &h, &l);
       hi[i] = __builtin_bit_cast(uint16_t, h), lo[i] = __builtin_bit_cast(uint16_t, l);
     }
   }

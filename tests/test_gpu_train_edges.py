@@ -78,3 +78,30 @@ def test_loss_of_huge_logits(dtype, size):
     off = np.abs(np64(dh) - want_dh)
     plane = np.abs(want_dh) * 2.0 ** -8 + a * np.abs(w64).max() * (2.0 ** -10 + v * 2.0 ** -37)
     assert (off <= a * np.abs(w64[z.argmax(axis=1)]) * 1.01 + plane)[sure].all()
+
+
+@pytest.mark.parametrize("big", [1e6, 1e12, 1e18])
+def test_loss_of_tokens_of_any_size(big):
+    """fp32 rows of hidden from tiny to huge side by side: each token's loss and dhidden are its own."""
+    announce("hidden over binades", big)
+    n, v, d = 130, 300, 96
+    h, w, t, s = loss_case(n, v, d, torch.float32, 0.1, 43)
+    size = torch.ones(n)
+    size[::5], size[1::5] = big, 1.0 / big
+    h = h * size[:, None]
+    hd, wd, td = h.cuda(), w.cuda(), t.cuda()
+    loss, lse = daso.linear_cross_entropy(hd, wd, td)
+    dh, _ = daso.linear_cross_entropy_backward(s.cuda(), hd, wd, td, lse)
+    h64, w64, s64 = np64(h), np64(w), np.where(t.numpy() == -100, 0, np64(s))
+    want_loss, want_lse = O.linear_cross_entropy(h64, w64, t.numpy())
+    mag = (np.abs(h64) @ np.abs(w64).T).max(axis=1)
+    ze = (d * U + 2.0 ** -20) * mag
+    tol = 2 * ze + 2.0 ** -20 + 8 * U * (np.abs(want_lse) + mag)
+    close(lse, want_lse, tol, "lse")
+    close(loss, want_loss, tol, "loss")
+    want_dh, _, dz = O.linear_cross_entropy_backward(s64, h64, w64, t.numpy())
+    # (of a huge token p is one or zero where the logits lie further apart than they are off, and anything between them else)
+    a = np.abs(s64)[:, None]
+    p = np.abs(dz) + (np.arange(v)[None] == t.numpy()[:, None]) * a
+    off = np.where((size > 1).numpy()[:, None], a, p * np.minimum(2 * (ze + tol), 1)[:, None]) + 2.0 ** -19 * np.abs(dz) + 2.0 ** -37 * a
+    close(dh, want_dh, off @ np.abs(w64) + np.abs(want_dh) * U, "dhidden")
