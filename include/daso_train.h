@@ -88,7 +88,11 @@ int daso_layer_norm_backward(const daso_layer_norm_backward_args* args, hipStrea
  *     lse_i = log sum_v exp(z_v),  loss_i = lse_i - z_target
  * and loss_i = 0 where the target is ignore_index.  The logits z are summed in 32 bits, in
  * tiles that are reduced while they are in registers; they are never stored.  A target that is
- * neither a class nor ignore_index makes its loss NaN (and the gradients that it reaches). */
+ * neither a class nor ignore_index makes its loss NaN (and the gradients that it reaches).
+ *
+ * Range: fp32 operands are taken in 22 bits, but not below 2^-39 of the largest magnitude: of the token's row of hidden
+ * in the logits, of all of weight, and for dweight of the largest dloss_i * hidden_i.  bf16 ones are taken as they are in
+ * the logits, and in the gradients' products down to 2^-31 of the same magnitudes (with fewer bits to 2^-39). */
 typedef struct daso_loss_args {
   int64_t tokens, vocab, d;   /* vocab and d >= 1; tokens and strides of operands at most 4 * DASO_MAX_SIDE */
   int32_t type;               /* of hidden, weight and dhidden */
@@ -117,7 +121,9 @@ int daso_linear_cross_entropy(const daso_loss_args* args, hipStream_t stream);
  *     dhidden = dz weight,  dweight = dz^T hidden
  * taken over pieces of the vocabulary, whose logits are computed again.  dz is rounded to 11
  * bits for the products whose result is bf16 and held as a sum of two such parts (22 bits)
- * for those whose result is fp32.  With tokens == 0 dweight is zero. */
+ * for those whose result is fp32, and to 2^-38 of its token's dloss_i, whatever the others' are.
+ * Nothing of an ignored token, or of one whose dloss is zero, counts in the products: it may hold any numbers, and an
+ * ignored one NaN and infinities.  With tokens == 0 dweight is zero. */
 int daso_linear_cross_entropy_backward(const daso_loss_args* args, hipStream_t stream);
 
 /* Newton-Schulz orthogonalisation of a batch of matrices U (rows x cols):

@@ -16,10 +16,11 @@
 //
 // Numbers.  bf16 operands are multiplied as they are in the forward product; fp32 ones as two
 // binary16 planes each (22 bits), hidden scaled by a power of two from each row's largest value, weight by one from the
-// tensor's.  In the backward products dz is binary16, of values in [-1, 1] times 2^14, which keeps 3 bits
-// more than bf16 would, and hidden and weight are turned to binary16 by a scale each
-// (exact for a bf16 value within 2^-32 of the largest), so that a bf16 result is off by 2e-4 before it is
-// rounded; fp32 results take dz as two planes.
+// tensor's.  In the backward products dz is binary16, a token's values in [-1, 1] times 2^14 and the power of
+// two of its dloss, which keeps 3 bits more than bf16 would whatever the other tokens' dloss are.  For dhidden
+// that power comes back by rows in the epilogue; for dweight it is put into hidden's rows, where those of tokens without a
+// gradient are zeros.  They and weight are turned to binary16 by a scale each (exact for a bf16 value within 2^-31 of the
+// largest), so that a bf16 result is off by 2e-4 before it is rounded; fp32 results take dz as two planes.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -40,23 +41,24 @@ constexpr float kLog2E = 1.44269504f;
 // exp(z - m) is 2^(z log2 e - m log2 e) in one multiply-add, whose second product is rounded: of m = 2^10 it is off by up to
 // 2^-14, of 2^32 by 2^8, and the power by its exponential.  From here on m is subtracted first.
 constexpr float kLargeLogit = 1 << 10;
-constexpr int kProbExponent = 14;  // dz / dloss in [-1, 1], times 2^14, as binary16
+constexpr int kProbExponent = 14;  // dz is in [-1, 1] times its token's power of two; as binary16, times 2^14
 
-// Exponents of scales, from the largest finite magnitudes of hidden, weight and dloss.
-enum Tensor { kHidden, kWeight, kGrad };
-constexpr int kTopParts = 512;     // workgroups that look for one
+// Exponents of scales: weight times 2^to is below 2^15, and hidden, each token's with its dloss's power of two, likewise.
+enum Tensor { kHidden, kWeight };
+constexpr int kTopParts = 512;     // workgroups that look for the largest values of one
 constexpr int kNone = -(1 << 20);  // the exponent of zero
 struct Scales {
-  int32_t top[3][kTopParts];  // exponents of the magnitudes
-  int32_t to[3];              // hidden and weight times 2^to are below 2^15, dloss times 2^-to is at most 1
+  int32_t top[2][kTopParts];  // exponents of the largest finite magnitudes
+  int32_t to[2];
 };
 
-// What the backward epilogue needs of a token.
+// What the backward epilogues need of a token.
 struct Row {
   float lse;
-  float g;         // dloss, scaled, times 2^kProbExponent
+  float g;         // dloss times 2^(kProbExponent - by)
   int32_t target;  // -1: the whole row is zero
-  int32_t to;      // fp32 operands: the exponent of its scale in the logits
+  int16_t to;      // fp32 operands: the exponent of its scale in the logits
+  int16_t by;      // dloss times 2^-by is in [-1, 1]
 };
 
 // floor(log2) of a magnitude (of a subnormal one the least normal's).
@@ -67,10 +69,24 @@ __device__ inline int exponent_of(float magnitude) {
 // The exponent that brings what has `top` for its largest value's into binary16, below 2^15.
 __device__ inline int to_half(int top) { return top == kNone ? 0 : 14 - top; }
 
+// What a token's part in the gradients goes by.
+struct Token {
+  float dloss;
+  int64_t target;
+  // The power of two that its dloss is taken by; kNone: nothing of the token reaches the gradients, whatever it holds.
+  __device__ int by(int64_t ignore) const {
+    if (target == ignore || dloss == 0.0f) return kNone;
+    const float m = __builtin_fabsf(dloss);
+    return m < __builtin_inff() ? exponent_of(m) + 1 : 0;
+  }
+};
+
 struct TopArgs {
   const void *hidden, *weight;
   int64_t hidden_stride, weight_stride, tokens, vocab, d;
-  const float* dloss;  // null: not looked at
+  const float* dloss;  // null: only the rows' own are wanted of hidden
+  const int64_t* targets;
+  int64_t ignore;
   int32_t* row_top;    // of each token's hidden
   Scales* out;
 };
@@ -99,10 +115,10 @@ __device__ inline float top_of_run(const T* src, int64_t n) {
   return wave_max(m);
 }
 
-// Calls f(row, largest magnitude), in every lane, for a wavefront's rows: four at a time for loads in flight, or, where
+// Calls f(row, largest magnitude, get(row)), in every lane, for a wavefront's rows, get before they are read: four at a time for loads in flight, or, where
 // there are no more rows than wavefronts, four places of one (a classifier's 256 rows of 2048: 2 us less).
-template <class T, class F>
-__device__ inline void tops_of_rows(const T* src, int64_t stride, int64_t rows, int64_t cols, F f) {
+template <class T, class G, class F>
+__device__ inline void tops_of_rows(const T* src, int64_t stride, int64_t rows, int64_t cols, G get, F f) {
   const int64_t wave = (blockIdx.x * 256 + threadIdx.x) >> 6, waves = gridDim.x * 4;
   const int lane = threadIdx.x & 63;
   const int64_t whole = cols / 8 * 8;
@@ -110,6 +126,9 @@ __device__ inline void tops_of_rows(const T* src, int64_t stride, int64_t rows, 
   const int64_t next = few ? 0 : waves, along = few ? 512 : 0, step = few ? 2048 : 512;
   for (int64_t r = wave; r < rows; r += 4 * waves) {
     float m[4] = {};
+    decltype(get(r)) with[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) with[k] = get(min(r + k * next, rows - 1));
     for (int64_t c = lane * 8; c < whole; c += step) {
       float v[4][8] = {};
 #pragma unroll
@@ -129,12 +148,12 @@ __device__ inline void tops_of_rows(const T* src, int64_t stride, int64_t rows, 
       for (int k = 0; k < 4; ++k) take_finite(v[k], m[k]);
     }
     if (few) {
-      f(r, wave_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))));
+      f(r, wave_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))), with[0]);
       continue;
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (r + k * waves < rows) f(r + k * waves, wave_max(m[k]));
+      if (r + k * waves < rows) f(r + k * waves, wave_max(m[k]), with[k]);
   }
 }
 
@@ -144,17 +163,17 @@ __global__ __launch_bounds__(256) void tops_kernel(TopArgs a) {
   __shared__ int32_t shared[4];
   int top = kNone;
   if (blockIdx.y == kHidden) {
-    tops_of_rows((const T*)a.hidden, a.hidden_stride, a.tokens, a.d, [&](int64_t row, float m) {
-      const int e = exponent_of(m);
+    const auto token = [&](int64_t row) { return a.dloss != nullptr ? Token{a.dloss[row], a.targets[row]} : Token{0.0f, 0}; };
+    tops_of_rows((const T*)a.hidden, a.hidden_stride, a.tokens, a.d, token, [&](int64_t row, float m, const Token& t) {
+      const int e = exponent_of(m), by = t.by(a.ignore);
       if ((threadIdx.x & 63) == 0) a.row_top[row] = e;
-      top = max(top, e);
+      if (e != kNone && by != kNone) top = max(top, e + by);
     });
-  } else if (blockIdx.y == kGrad) {
-    if (a.dloss != nullptr) top = exponent_of(top_of_run(a.dloss, a.tokens));
   } else if (a.weight_stride == a.d) {
     top = exponent_of(top_of_run((const T*)a.weight, a.vocab * a.d));
   } else {
-    tops_of_rows((const T*)a.weight, a.weight_stride, a.vocab, a.d, [&](int64_t, float m) { top = max(top, exponent_of(m)); });
+    tops_of_rows((const T*)a.weight, a.weight_stride, a.vocab, a.d, [](int64_t) { return 0; },
+                 [&](int64_t, float m, int) { top = max(top, exponent_of(m)); });
   }
   if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = top;
   __syncthreads();
@@ -170,14 +189,15 @@ __device__ inline int scale_exponent(const Scales* s, int tensor, int32_t* share
   if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = m;
   __syncthreads();
   m = max(max(shared[0], shared[1]), max(shared[2], shared[3]));
-  return tensor != kGrad ? to_half(m) : m == kNone ? 0 : m + 1;
+  return to_half(m);
 }
 static_assert(kTopParts == 512, "two parts a thread");
 
 // What comes before the products of a pass, in one launch: planes of hidden and weight, and the
 // backward pass's rows.
 constexpr int kMaxPlanes = 4;
-enum ScaleBy { kRaw, kByRow = 1, kByTensor = 2 };  // kByTensor + the tensor
+// Not at all; rows of hidden for the logits; weight; rows of hidden for dweight, each with its dloss's power of two.
+enum ScaleBy { kRaw, kByRow, kByWeight, kByGrad };
 struct PrepareArgs {
   int32_t count;
   int64_t first[kMaxPlanes + 2];  // workgroups of each job: the planes, then the rows
@@ -199,7 +219,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   const int64_t id = blockIdx.x + int64_t(blockIdx.y) * gridDim.x;
   if (id >= a.first[a.count + 1]) return;
   if (id == 0 && a.scales != nullptr) {
-    for (int t = 0; t < 3; ++t) {
+    for (int t = 0; t < 2; ++t) {
       const int e = scale_exponent(a.scales, t, shared);
       if (threadIdx.x == 0) a.scales->to[t] = e;
     }
@@ -215,20 +235,24 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
       return;
     }
     const int row = min(tr * 64 + static_cast<int>(threadIdx.x >> 2), p.rows - 1);  // this thread's
-    const int to = a.by[k] == kByRow ? to_half(a.row_top[row]) : scale_exponent(a.scales, a.by[k] - kByTensor, shared);
-    planes_tile<T, false>(p, 0, tr, tc, [to](float v) { return __builtin_ldexpf(v, to); }, lds);
+    const bool grad = a.by[k] == kByGrad;
+    const Token token = grad ? Token{a.dloss[row], a.targets[row]} : Token{0.0f, 0};
+    const int to_all = a.by[k] == kByRow ? to_half(a.row_top[row]) : scale_exponent(a.scales, grad ? kHidden : kWeight, shared);
+    const int by = grad ? token.by(a.ignore) : 0, to = to_all + by;
+    planes_tile<T, false>(p, 0, tr, tc, [to, by](float v) { return by == kNone ? 0.0f : __builtin_ldexpf(v, to); }, lds);
     return;
   }
-  const int to_grad = scale_exponent(a.scales, kGrad, shared);
   const int64_t i = (id - a.first[a.count]) * 256 + threadIdx.x;
   if (i >= a.padded) return;
-  Row r = {0.0f, 0.0f, -1, 0};
+  Row r = {0.0f, 0.0f, -1, 0, 0};
   if (i < a.tokens) {
     const int64_t t = a.targets[i];
     if (t >= 0 && t < a.vocab && t != a.ignore) {
       r.lse = a.lse[i];
-      r.g = __builtin_ldexpf(a.dloss[i], kProbExponent - to_grad);
-      r.to = to_half(a.row_top[i]);
+      const int by = Token{a.dloss[i], t}.by(a.ignore);
+      r.by = static_cast<int16_t>(by == kNone ? 0 : by);
+      r.g = __builtin_ldexpf(a.dloss[i], kProbExponent - r.by);
+      r.to = static_cast<int16_t>(to_half(a.row_top[i]));
       r.target = static_cast<int32_t>(t);
     } else if (t != a.ignore) {
       r.g = __builtin_nanf("");
@@ -488,7 +512,8 @@ struct ProbOut {
 struct GradOut {
   static constexpr auto kKind = product::kStaged;
   struct Params {
-    const int32_t *to_grad, *to;  // the exponents of dloss and of the partner's scale
+    const Row* tokens;   // of dhidden's rows: the powers of two of their dloss; null: they are in the partner
+    const int32_t* to;   // the exponent of the partner's scale
     const float* before;  // the sum of the pieces so far, or null
     int64_t before_ld;
     void* out;
@@ -499,11 +524,14 @@ struct GradOut {
   };
   struct Inputs {
     float before[product::kPasses][8];
-    int shift;
+    int shift[product::kPasses];  // what takes the scales back, by rows
   };
   __device__ static void fetch(const Params& p, const product::Place&, int row, int col, int lane, Inputs& in) {
     const int r0 = row + product::pass_row(0, lane), cc = col + product::pass_col(lane);
-    in.shift = *p.to_grad - *p.to - kProbExponent;
+    const int to = *p.to + kProbExponent;
+#pragma unroll
+    for (int pass = 0; pass < product::kPasses; ++pass)
+      in.shift[pass] = (p.tokens != nullptr ? p.tokens[r0 + pass * product::kPassRows].by : 0) - to;
     if (p.before == nullptr) return;
 #pragma unroll
     for (int pass = 0; pass < product::kPasses; ++pass)  // padded to whole vectors
@@ -522,7 +550,7 @@ struct GradOut {
         for (int i = 0; i < 8; ++i) {
           const int r = (lane & 7) * 8 + i, c = pass * 8 + (lane >> 3);
           v[pass][i] = *(const float*)(stage + r * 128 + (((c >> 2) ^ ((r >> 1) & 7)) * 16) + (c & 3) * 4);
-          v[pass][i] = __builtin_ldexpf(v[pass][i], in.shift);
+          v[pass][i] = __builtin_ldexpf(v[pass][i], in.shift[0]);
         }
       next();
 #pragma unroll
@@ -539,7 +567,7 @@ struct GradOut {
       product::pass_values(stage, pass, lane, v[pass]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        v[pass][i] = __builtin_ldexpf(v[pass][i], in.shift);
+        v[pass][i] = __builtin_ldexpf(v[pass][i], in.shift[pass]);
         if (p.before != nullptr) v[pass][i] += in.before[pass][i];
       }
     }
@@ -683,9 +711,9 @@ hipError_t prepare(const daso_loss_args& s, const Plan& q, bool backward, Operan
   const bool scaled = q.f32 || backward;
   int32_t* row_top = reinterpret_cast<int32_t*>(ws + q.row_top);
   if (scaled) {
-    const TopArgs t = {s.hidden, s.weight, s.hidden_stride, s.weight_stride, s.tokens, s.vocab, s.d, backward ? s.dloss : nullptr, row_top, sc};
-    e = s.type == DASO_TYPE_BF16 ? launch(&tops_kernel<uint16_t>, dim3(kTopParts, 3), dim3(256), stream, t)
-                                 : launch(&tops_kernel<float>, dim3(kTopParts, 3), dim3(256), stream, t);
+    const TopArgs t = {s.hidden, s.weight, s.hidden_stride, s.weight_stride, s.tokens, s.vocab, s.d, backward ? s.dloss : nullptr, s.targets, s.ignore_index, row_top, sc};
+    e = s.type == DASO_TYPE_BF16 ? launch(&tops_kernel<uint16_t>, dim3(kTopParts, 2), dim3(256), stream, t)
+                                 : launch(&tops_kernel<float>, dim3(kTopParts, 2), dim3(256), stream, t);
   }
   PrepareArgs a = {};
   const bool ht = backward && s.dweight != nullptr, wp = backward && s.dhidden != nullptr;
@@ -696,14 +724,14 @@ hipError_t prepare(const daso_loss_args& s, const Plan& q, bool backward, Operan
     add_planes(a, by, s.weight, s.weight_stride, s.vocab, s.d, q.v_p, q.d_p, d0, d1, nullptr, nullptr);
   };
   if (q.f32) {
-    weight(kByTensor + kWeight, ws + q.w[0], ws + q.w[1]);
+    weight(kByWeight, ws + q.w[0], ws + q.w[1]);
     hidden(kByRow, ws + q.h[0], ws + q.h[1], nullptr, nullptr);
-    if (ht) hidden(kByTensor + kHidden, nullptr, nullptr, ws + q.ht[0], ws + q.ht[1]);
+    if (ht) hidden(kByGrad, nullptr, nullptr, ws + q.ht[0], ws + q.ht[1]);
   } else {
     if (q.copy_w) weight(kRaw, ws + q.w[0], nullptr);
     if (q.copy_h) hidden(kRaw, ws + q.h[0], nullptr, nullptr, nullptr);
-    if (wp) weight(kByTensor + kWeight, ws + q.wp[0], nullptr);
-    if (ht) hidden(kByTensor + kHidden, nullptr, nullptr, ws + q.ht[0], nullptr);
+    if (wp) weight(kByWeight, ws + q.wp[0], nullptr);
+    if (ht) hidden(kByGrad, nullptr, nullptr, ws + q.ht[0], nullptr);
   }
   a.first[a.count + 1] = a.first[a.count];
   if (backward) {
@@ -792,7 +820,7 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
       a.lda = width, a.ldb = q.d_p, a.steps = static_cast<int32_t>(width / 64);
       a.M = static_cast<int32_t>(s.tokens), a.N = static_cast<int32_t>(q.d_p), a.batch = 1;
       GradOut::Params& g = grads.out[grads.count++];
-      g.to_grad = &sc->to[kGrad], g.to = &sc->to[kWeight];
+      g.tokens = rows, g.to = &sc->to[kWeight];
       float* sum = reinterpret_cast<float*>(ws + q.sum);
       if (k > 0) g.before = sum, g.before_ld = q.d_p;
       g.rows = a.M;
@@ -809,7 +837,7 @@ hipError_t backward(const daso_loss_args& s, const Plan& q, hipStream_t stream) 
       a.lda = q.n_p, a.ldb = width, a.steps = static_cast<int32_t>(q.n_p / 64);
       a.M = static_cast<int32_t>(s.d), a.N = static_cast<int32_t>(width), a.batch = 1;
       GradOut::Params& g = grads.out[grads.count++];
-      g.to_grad = &sc->to[kGrad], g.to = &sc->to[kHidden];
+      g.to = &sc->to[kHidden];
       g.out = static_cast<char*>(s.dweight) + first * s.dweight_stride * static_cast<int64_t>(host::bytes_of(s.dweight_type));
       g.ld = s.dweight_stride, g.bf16 = !dw32;
       g.rows = static_cast<int32_t>(classes), g.cols = a.M, g.turned = 1;

@@ -80,6 +80,60 @@ def test_loss_of_huge_logits(dtype, size):
     assert (off <= a * np.abs(w64[z.argmax(axis=1)]) * 1.01 + plane)[sure].all()
 
 
+@pytest.mark.parametrize("dtype,grad", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("h_junk,s_junk", [(1e20, 1e9), (1.0, 3e38), (1e30, 0.0), (1e-30, 1e-30)])
+@pytest.mark.parametrize("n,v,d", [(150, 300, 96), (70, 129, 65)])
+def test_what_lies_in_ignored_rows_changes_nothing(dtype, grad, h_junk, s_junk, n, v, d):
+    """hidden and dloss of ignored tokens may hold any value: the same bits for all others."""
+    announce("ignored rows", dtype, grad, h_junk, s_junk, n, v, d)
+    h, w, t, s = loss_case(n, v, d, dtype, 0.3, n + v)
+    s *= 1e-4
+    gone = t == -100
+    h[gone], s[gone] = 0, 0
+    loss, lse, dh, dw = check_loss(h, w, t, s, h.cuda(), w.cuda(), grad)
+    h2, s2 = h.clone(), s.clone()
+    h2[gone] = (torch.randn(int(gone.sum()), d, generator=gen(1)) * h_junk).to(dtype)
+    s2[gone] = s_junk
+    td, wd = t.cuda(), w.cuda()
+    loss2, lse2 = daso.linear_cross_entropy(h2.cuda(), wd, td)
+    dh2, dw2 = daso.linear_cross_entropy_backward(s2.cuda(), h2.cuda(), wd, td, lse2, dweight=torch.empty(v, d, dtype=grad, device="cuda"))
+    live = ~gone.cuda()
+    assert torch.equal(lse2[live], lse[live]) and torch.equal(loss2, loss)
+    _, want = O.linear_cross_entropy(np64(h2), np64(w), t.numpy())
+    mag = (np.abs(np64(h2)) @ np.abs(np64(w)).T).max(axis=1)
+    close(lse2, want, (d * U + 2.0 ** -20) * 2 * mag + 2.0 ** -19 + 8 * U * np.abs(want), "lse")
+    assert torch.equal(dh2, dh) and not dh2[~live].any() and torch.equal(dw2, dw)
+
+
+@pytest.mark.parametrize("dtype,grad", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("low,high", [(-60, 0), (-100, -40), (0, 60)])
+def test_gradients_of_tokens_of_any_weight(dtype, grad, low, high):
+    """dloss over many binades: each token's dhidden has its own bits, and dweight those of its largest terms."""
+    announce("dloss over binades", dtype, grad, low, high)
+    n, v, d = 130, 300, 96
+    h, w, t, _ = loss_case(n, v, d, dtype, 0.1, 41)
+    s = torch.exp2(torch.linspace(low, high, n, dtype=torch.float64)).float() * (torch.rand(n, generator=gen(2)) + 1)
+    s[::3] *= -1
+    hd, wd, td, sd = h.cuda(), w.cuda(), t.cuda(), s.cuda()
+    _, lse = daso.linear_cross_entropy(hd, wd, td)
+    dh, dw = daso.linear_cross_entropy_backward(sd, hd, wd, td, lse, dweight=torch.empty(v, d, dtype=grad, device="cuda"))
+    h64, w64, s64 = np64(h), np64(w), np.where(t.numpy() == -100, 0, np64(s))
+    want_dh, want_dw, dz = O.linear_cross_entropy_backward(s64, h64, w64, t.numpy())
+    # p is off by its logit's and the log-sum-exp's error, 2^-14 with room; dz by its planes, or by 2^-38 of its token's dloss
+    a, bf16 = np.abs(s64)[:, None], dtype == torch.bfloat16
+    p = np.abs(dz) + (np.arange(v)[None] == t.numpy()[:, None]) * a
+    ze = (d * U + 2.0 ** -20) * (np.abs(h64) @ np.abs(w64).T).max(axis=1) + 2.0 ** -16
+    off = (2.0 ** -11 if bf16 else 2.0 ** -20) * np.abs(dz) + p * 2 * ze[:, None] + 2.0 ** -37 * a
+    close(dh, want_dh, off @ np.abs(w64) + v * U * (np.abs(dz) @ np.abs(w64)) + np.abs(want_dh) * (2.0 ** -8 if bf16 else U), "dhidden")
+    # a term of dweight is also off by 2^-37 of the largest dloss_i * hidden_i
+    narrow = grad == torch.bfloat16
+    off = (2.0 ** -11 if narrow else 2.0 ** -19) * np.abs(dz) + p * 2 * ze[:, None] + 2.0 ** -37 * a
+    most = (a * np.abs(h64).max(axis=1, keepdims=True)).max()
+    share = (np.abs(dz) / np.maximum(a, 1e-300)).T.sum(axis=1, keepdims=True)
+    tol = off.T @ np.abs(h64) + n * U * (np.abs(dz).T @ np.abs(h64)) + 2.0 ** -37 * most * share
+    close(dw, want_dw, tol + np.abs(want_dw) * (2.0 ** -8 if narrow else U), "dweight")
+
+
 @pytest.mark.parametrize("big", [1e6, 1e12, 1e18])
 def test_loss_of_tokens_of_any_size(big):
     """fp32 rows of hidden from tiny to huge side by side: each token's loss and dhidden are its own."""
@@ -105,3 +159,20 @@ def test_loss_of_tokens_of_any_size(big):
     p = np.abs(dz) + (np.arange(v)[None] == t.numpy()[:, None]) * a
     off = np.where((size > 1).numpy()[:, None], a, p * np.minimum(2 * (ze + tol), 1)[:, None]) + 2.0 ** -19 * np.abs(dz) + 2.0 ** -37 * a
     close(dh, want_dh, off @ np.abs(w64) + np.abs(want_dh) * U, "dhidden")
+
+
+@pytest.mark.parametrize("dtype,grad", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), -float("inf")])
+def test_ignored_rows_without_numbers(dtype, grad, junk):
+    """NaN and infinities in hidden and dloss of ignored tokens reach no gradient."""
+    announce("ignored rows without numbers", dtype, grad, junk)
+    h, w, t, s = loss_case(150, 300, 96, dtype, 0.3, 51)
+    gone = t == -100
+    h[gone], s[gone] = 0, 0
+    _, _, dh, dw = check_loss(h, w, t, s, h.cuda(), w.cuda(), grad)
+    h[gone, 5:9], s[gone] = junk, junk
+    loss, lse = daso.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    assert torch.isfinite(loss).all()
+    dh2, dw2 = daso.linear_cross_entropy_backward(s.cuda(), h.cuda(), w.cuda(), t.cuda(), lse,
+                                                  dweight=torch.empty(300, 96, dtype=grad, device="cuda"))
+    assert torch.equal(dh2, dh) and torch.equal(dw2, dw)
