@@ -320,7 +320,9 @@ class MuonStep:
     here, so that each call costs one C call.  grads are g fp32 flat buffers, params and
     momentum fp32 (updated in place), matrices the (start, rows, cols) that are stepped; wire
     receives their bf16 form.  The tensors must stay alive (and keep their storage)
-    while the object is used, and calls on it must not overlap."""
+    while the object is used, and so must the object while a graph that a call was captured into is replayed;
+    calls on it must not overlap.  They may run on any stream: the first on a stream waits there for what the stream of
+    construction has queued (not in a capture, before which that work has to be done)."""
 
     def __init__(self, grads: Sequence[torch.Tensor], params: torch.Tensor, momentum: torch.Tensor,
                  matrices: Sequence[Tuple[int, int, int]], lr: float, mu: float = 0.95, weight_decay: float = 0.0,
@@ -350,13 +352,28 @@ class MuonStep:
         self.args = a
         self._byref = ctypes.byref(a)
         self._device = torch.cuda.current_device()
+        self._made_on = L._stream_handle(stream).value
+        self._streams = {self._made_on}  # on which the workspace is in order
         self._fn = _load().daso_muon_step
 
     def __call__(self, stream=None) -> None:
         if torch.cuda.current_device() != self._device:
             raise ValueError(f"prepared on cuda:{self._device}, called with cuda:{torch.cuda.current_device()} "
                              "current")
-        L._check(self._fn(self._byref, L._stream_handle(stream)), "daso_muon_step")
+        handle = L._stream_handle(stream)
+        if handle.value not in self._streams and self._workspace is not None:
+            self._bring_workspace(torch.cuda.current_stream() if stream is None else stream)
+        L._check(self._fn(self._byref, handle), "daso_muon_step")
+
+    def _bring_workspace(self, to: torch.cuda.Stream) -> None:
+        """The workspace is of the stream of construction: memory that the work queued there may still use, and that
+        goes back to it when the object does.  `to` waits for the one, and the allocator for `to` before the other."""
+        self._workspace.record_stream(to)
+        with torch.cuda.stream(to):
+            if torch.cuda.is_current_stream_capturing():
+                return
+        to.wait_stream(torch.cuda.ExternalStream(self._made_on) if self._made_on else torch.cuda.default_stream())
+        self._streams.add(to.cuda_stream or None)
 
 
 def muon_step(grads, params, momentum, matrices, lr, mu=0.95, weight_decay=0.0, nesterov=True, steps=5,

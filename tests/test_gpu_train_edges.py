@@ -176,3 +176,47 @@ def test_ignored_rows_without_numbers(dtype, grad, junk):
     dh2, dw2 = daso.linear_cross_entropy_backward(s.cuda(), h.cuda(), w.cuda(), t.cuda(), lse,
                                                   dweight=torch.empty(300, 96, dtype=grad, device="cuda"))
     assert torch.equal(dh2, dh) and torch.equal(dw2, dw)
+
+
+# ------------------------------------------------------------------------- the step on other streams
+def test_muon_step_on_streams_it_was_not_made_on():
+    """The same bits, with the workspace's memory in use on the stream of construction before and after."""
+    announce("muon step on other streams")
+    mats, n = [(0, 192, 256), (49152, 256, 192)], 98304
+    r = gen(61)
+    grads, p0, m0 = [torch.randn(n, generator=r).cuda() for _ in range(4)], torch.randn(n, generator=r).cuda(), torch.randn(n, generator=r).cuda()
+    want_p, want_m = p0.clone(), m0.clone()
+    daso.muon_step(grads, want_p, want_m, mats, 0.1, 0.9)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        p, m = p0.clone(), m0.clone()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        size = daso.MuonStep(grads, p, m, mats, 0.1, 0.9).args.workspace_bytes
+        for _ in range(20):
+            torch.empty(size, dtype=torch.uint8, device="cuda").fill_(255)  # (memory that the step is given next)
+        step = daso.MuonStep(grads, p, m, mats, 0.1, 0.9)
+        step(side)
+        del step
+        for _ in range(20):
+            torch.empty(size, dtype=torch.uint8, device="cuda").fill_(255)
+        side.synchronize()
+        assert torch.equal(p, want_p) and torch.equal(m, want_m)
+
+
+def test_muon_step_captured_on_another_stream():
+    announce("muon step captured")
+    mats, n = [(0, 192, 256), (49152, 256, 192)], 98304
+    r = gen(62)
+    grads, p0, m0 = [torch.randn(n, generator=r).cuda() for _ in range(2)], torch.randn(n, generator=r).cuda(), torch.randn(n, generator=r).cuda()
+    p, m, want_p, want_m = p0.clone(), m0.clone(), p0.clone(), m0.clone()
+    step, eager = daso.MuonStep(grads, p, m, mats, 0.1, 0.9), daso.MuonStep(grads, want_p, want_m, mats, 0.1, 0.9)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        graph.replay()
+        eager()
+        torch.cuda.synchronize()
+        assert torch.equal(p, want_p) and torch.equal(m, want_m), k

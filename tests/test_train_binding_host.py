@@ -1,0 +1,97 @@
+"""The training operators' binding without a GPU: what it asks of streams and the allocator, with stand-ins for both."""
+import contextlib
+import ctypes
+
+import pytest
+import torch
+
+from paper_2104_05588_amd import _lib as L
+from paper_2104_05588_amd import _train as T
+
+
+class FakeStream:
+    def __init__(self, handle, device_index=0):
+        self.cuda_stream, self.device_index, self.device = handle, device_index, torch.device("cuda", device_index)
+        self.capturing, self.waits = False, []
+
+    def wait_stream(self, other):
+        self.waits.append(other.cuda_stream)
+
+
+class FakeWorkspace:
+    def __init__(self):
+        self.recorded = []
+
+    def record_stream(self, stream):
+        self.recorded.append(stream.cuda_stream)
+
+
+@pytest.fixture
+def cuda(monkeypatch):
+    """torch.cuda with a current stream and device 0, and no GPU."""
+    state = {"stream": FakeStream(0)}
+
+    @contextlib.contextmanager
+    def on(stream):
+        before, state["stream"] = state["stream"], stream
+        yield
+        state["stream"] = before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: state["stream"])
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda: FakeStream(0))
+    monkeypatch.setattr(torch.cuda, "ExternalStream", FakeStream)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: state["stream"].capturing)
+    monkeypatch.setattr(L, "_current_raw_stream", lambda device: state["stream"].cuda_stream)
+    return state
+
+
+def prepared(made_on):
+    """A MuonStep made on a stream of that handle, whose C call notes the stream that it gets."""
+    step, calls = T.MuonStep.__new__(T.MuonStep), []
+    step._workspace, step._device, step._byref = FakeWorkspace(), 0, None
+    step._made_on = ctypes.c_void_p(made_on).value
+    step._streams = {step._made_on}
+
+    def fn(args, handle):
+        calls.append(handle.value or 0)
+        return L.DASO_OK
+
+    step._fn = fn
+    return step, calls
+
+
+@pytest.mark.parametrize("made_on", [0, 0x1000])
+def test_muon_step_on_another_stream_waits_and_is_recorded(cuda, made_on):
+    step, calls = prepared(made_on)
+    own, other = FakeStream(made_on), FakeStream(0x2000)
+    step(own)
+    assert calls == [made_on] and step._workspace.recorded == []
+    step(other), step(other)
+    assert calls == [made_on, 0x2000, 0x2000]
+    assert other.waits == [made_on] and step._workspace.recorded == [0x2000]  # before the first call, and for good
+    third = FakeStream(0x3000)
+    with torch.cuda.stream(third):
+        step()
+    assert calls[-1] == 0x3000 and third.waits == [made_on] and step._workspace.recorded == [0x2000, 0x3000]
+    step(own)
+    assert len(step._workspace.recorded) == 2
+
+
+def test_muon_step_captured_on_another_stream_waits_for_nothing_outside(cuda):
+    step, calls = prepared(0)
+    side = FakeStream(0x2000)
+    side.capturing = True
+    step(side)
+    assert calls == [0x2000] and side.waits == [] and step._workspace.recorded == [0x2000]
+    side.capturing = False
+    step(side)
+    assert side.waits == [0]
+
+
+def test_muon_step_that_is_made_on_the_default_stream_may_be_called_there_by_name(cuda):
+    step, _ = prepared(0x1000)
+    named = FakeStream(0)
+    step(named), step(named)
+    assert named.waits == [0x1000] and step._workspace.recorded == [0]
