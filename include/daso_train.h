@@ -41,7 +41,8 @@ extern "C" {
 /* Layer norm of each row x of d elements:
  *     mean = sum x / d,  rstd = 1 / sqrt(sum (x - mean)^2 / d + eps),
  *     y = (x - mean) * rstd * weight + bias
- * in 32 bits, rounded once to the type of y.  rows == 0 or d == 0 is a no-op. */
+ * in 32 bits, rounded once to the type of y.  rows == 0 or d == 0 is a no-op: mean and rstd,
+ * which rows of no elements do not have, are not written. */
 typedef struct daso_layer_norm_args {
   int64_t rows, d;      /* d <= DASO_MAX_NORM_D */
   int32_t type;         /* of x and y */

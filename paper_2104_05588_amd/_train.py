@@ -172,6 +172,9 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
             y_at, y_stride = _rows(y, (rows, d), (x.dtype,), "out")
         mean = x.new_empty(rows, dtype=torch.float32)
         rstd = torch.empty_like(mean)
+        if d == 0:  # the call is a no-op; a row of no elements has the statistics 0 / 0
+            mean.fill_(math.nan)
+            rstd.fill_(math.nan)
         a = daso_layer_norm_args(rows, d, _TYPES[x.dtype], eps, x_at, x_stride, weight_at, bias_at, y_at, y_stride,
                                  mean.data_ptr(), rstd.data_ptr())
         L._check(_load().daso_layer_norm(ctypes.byref(a), L._stream_handle(stream)), "daso_layer_norm")

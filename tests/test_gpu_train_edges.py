@@ -178,6 +178,19 @@ def test_ignored_rows_without_numbers(dtype, grad, junk):
     assert torch.equal(dh2, dh) and torch.equal(dw2, dw)
 
 
+# ------------------------------------------------------------------------- layer norm of nothing
+@pytest.mark.parametrize("rows", [0, 1, 700])
+def test_layer_norm_of_empty_rows(rows):
+    """A row of no elements has no mean: 0 / 0."""
+    announce("layer norm of empty rows", rows)
+    torch.full((4096,), 5.0, device="cuda")  # (what the allocator hands out next has been written)
+    y, mean, rstd = daso.layer_norm(torch.empty(rows, 0, device="cuda"))
+    assert y.shape == (rows, 0) and mean.shape == rstd.shape == (rows,)
+    assert torch.isnan(mean).all() and torch.isnan(rstd).all()
+    dx, dw, db = daso.layer_norm_backward(y, y, None, mean, rstd)
+    assert dx.shape == (rows, 0) and dw.numel() == 0 and db.numel() == 0
+
+
 # ------------------------------------------------------------------------- the step on other streams
 def test_muon_step_on_streams_it_was_not_made_on():
     """The same bits, with the workspace's memory in use on the stream of construction before and after."""
