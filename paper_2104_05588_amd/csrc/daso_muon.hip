@@ -357,6 +357,19 @@ __global__ __launch_bounds__(256) void squares_kernel(const T* src, int64_t batc
   if (threadIdx.x == 0) sums[blockIdx.y * host::kSumParts + blockIdx.x] = sum;
 }
 
+// What brings a matrix to kScale / (|u| + eps) of itself, in two steps: for the smallest and the largest norms that is no
+// normal fp32 number.
+struct Normal {
+  float factor;
+  int exponent;
+  __device__ Normal(double squares, float eps) {
+    const double scale = kScale / (sqrt(squares) + eps);
+    exponent = scale > 0.0 && scale < 1e300 ? ilogb(scale) : 0;
+    factor = static_cast<float>(ldexp(scale, -exponent));
+  }
+  __device__ float operator()(float v) const { return __builtin_ldexpf(v, exponent) * factor; }
+};
+
 struct LayOut {
   int32_t groups;
   int32_t parts;  // sums of a matrix
@@ -381,8 +394,8 @@ __global__ __launch_bounds__(256) void normalise_kernel(LayOut a) {
   __shared__ double shared[4];
   const double* s = a.sums + (a.first_matrix[k] + batch) * host::kSumParts;
   const double sum = group_sum(static_cast<int>(threadIdx.x) < a.parts ? s[threadIdx.x] : 0.0, shared);
-  const float scale = static_cast<float>(kScale / (sqrt(sum) + a.eps));
-  planes_tile<T, false>(p, batch, static_cast<int>((t % per) / across), static_cast<int>(t % across), [scale](float v) { return scale * v; }, lds);
+  const Normal scaled(sum, a.eps);
+  planes_tile<T, false>(p, batch, static_cast<int>((t % per) / across), static_cast<int>(t % across), scaled, lds);
 }
 
 // ------------------------------------------------------------------------- small matrices
@@ -467,11 +480,13 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_kernel(SmallArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) square += static_cast<double>(x[i][j][e]) * x[i][j][e];
   }
-  const float scale = static_cast<float>(kScale / (sqrt(group_sum(square, sums)) + a.eps));
+  const Normal scaled(group_sum(square, sums), a.eps);
 #pragma unroll
   for (int i = 0; i < kSmallGroups; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[i][j] *= scale;
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i][j][e] = scaled(x[i][j][e]);
   // columns between n and the last step's end are read as zeros
   for (int k = threadIdx.x; k < kSmallM * 8; k += kSmallThreads) {
     const int row = k >> 3, at = (n_steps * 64 - 64 + (k & 7) * 8) * 2;

@@ -191,6 +191,20 @@ def test_layer_norm_of_empty_rows(rows):
     assert dx.shape == (rows, 0) and dw.numel() == 0 and db.numel() == 0
 
 
+# ------------------------------------------------------------------------- Newton-Schulz
+@pytest.mark.parametrize("rows,cols", [(24, 40), (130, 200)])
+@pytest.mark.parametrize("size", [3e-38, 1e-36])
+def test_orthogonalize_of_tiny_matrices(rows, cols, size):
+    """With eps = 0 the scale of a matrix does not matter, down to the smallest normal numbers."""
+    announce("orthogonalize tiny", rows, cols, size)
+    u = torch.randint(1, 4, (rows, cols), generator=gen(3)).float() * torch.sign(torch.randn(rows, cols, generator=gen(4)))
+    got = daso.orthogonalize((u * size).cuda(), eps=0.0)
+    want = O.newton_schulz(np64(u * size), [(3.4445, -4.7750, 2.0315)] * 5, 0.0)
+    # as the tolerance of test_gpu_train for fp32: 4 roundings of 2^-21 a step, and what the weak directions add
+    tol = 4 * 5 * 2.0 ** -21 + 2.0 ** -22 * 3.5 ** 5 / np.linalg.norm(want) + U
+    assert np.linalg.norm(np64(got) - want) <= tol * np.linalg.norm(want)
+
+
 # ------------------------------------------------------------------------- the step on other streams
 def test_muon_step_on_streams_it_was_not_made_on():
     """The same bits, with the workspace's memory in use on the stream of construction before and after."""
