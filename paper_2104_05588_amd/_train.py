@@ -127,8 +127,13 @@ def _flat(t: Optional[torch.Tensor], n: int, dtypes, what: str) -> Optional[int]
 
 
 def _on(stream: Optional[torch.cuda.Stream]):
-    """What is allocated for a call belongs to the stream that the call runs on."""
-    return _HERE if stream is None else torch.cuda.stream(stream)
+    """What is allocated for a call belongs to the stream that the call runs on, which is one of the current device:
+    torch.cuda.stream would make another one current, under tensors of this one."""
+    if stream is None:
+        return _HERE
+    if stream.device_index != torch.cuda.current_device():
+        raise ValueError(f"the stream is of cuda:{stream.device_index}, not of the current device cuda:{torch.cuda.current_device()}")
+    return torch.cuda.stream(stream)
 
 
 _HERE = contextlib.nullcontext()
@@ -371,10 +376,11 @@ class MuonStep:
     def _bring_workspace(self, to: torch.cuda.Stream) -> None:
         """The workspace is of the stream of construction: memory that the work queued there may still use, and that
         goes back to it when the object does.  `to` waits for the one, and the allocator for `to` before the other."""
+        with _on(to):
+            capturing = torch.cuda.is_current_stream_capturing()
         self._workspace.record_stream(to)
-        with torch.cuda.stream(to):
-            if torch.cuda.is_current_stream_capturing():
-                return
+        if capturing:
+            return
         to.wait_stream(torch.cuda.ExternalStream(self._made_on) if self._made_on else torch.cuda.default_stream())
         self._streams.add(to.cuda_stream or None)
 

@@ -95,3 +95,52 @@ def test_muon_step_that_is_made_on_the_default_stream_may_be_called_there_by_nam
     named = FakeStream(0)
     step(named), step(named)
     assert named.waits == [0x1000] and step._workspace.recorded == [0]
+
+
+class FakeTensor:
+    """A tensor that passes the checks of a call on device 0."""
+
+    def __init__(self, *shape, dtype=torch.float32):
+        self.shape, self.dtype, self.is_cuda, self.device = torch.Size(shape), dtype, True, torch.device("cuda", 0)
+
+    def get_device(self):
+        return 0
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def is_contiguous(self):
+        return True
+
+    def stride(self):
+        return (self.shape[-1], 1)[-self.dim():]
+
+    def data_ptr(self):
+        return 0x10000000
+
+    def new_empty(self, *args, **kwargs):
+        raise AssertionError("allocates before the stream is refused")
+
+
+def test_a_stream_of_another_device_is_refused(cuda, monkeypatch):
+    """Before anything is allocated, and before the device of the stream would become the current one."""
+    def no_allocation(*args, **kwargs):
+        raise AssertionError("allocates before the stream is refused")
+
+    monkeypatch.setattr(torch, "empty", no_allocation)
+    other = FakeStream(0x2000, device_index=1)
+    x, v, t = FakeTensor(4, 8), FakeTensor(4), FakeTensor(4, dtype=torch.int64)
+    w, flat = FakeTensor(5, 8), FakeTensor(64)
+    for call in (lambda: T.layer_norm(x, stream=other), lambda: T.layer_norm_backward(x, x, None, v, v, stream=other),
+                 lambda: T.linear_cross_entropy(x, w, t, stream=other),
+                 lambda: T.linear_cross_entropy_backward(v, x, w, t, v, stream=other), lambda: T.orthogonalize(x, stream=other),
+                 lambda: T.muon_step([flat], flat, flat, [(0, 4, 4)], 0.1, stream=other)):
+        with pytest.raises(ValueError, match="the stream is of cuda:1"):
+            call()
+    step, calls = prepared(0)
+    with pytest.raises(ValueError, match="the stream is of cuda:1"):
+        step(other)
+    assert calls == [] and step._workspace.recorded == []
