@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <map>
 #include <utility>
 
@@ -61,17 +62,23 @@ bool stride_ok(int64_t stride, int64_t row, int64_t rows) {
 
 bool finite_not_negative(float v) { return v >= 0.0f && std::isfinite(v); }
 
-// Outputs against inputs and each other; `in_place` is the one input that outputs[0] may be.
-int check_alias(const std::vector<Block>& outputs, const std::vector<Block>& inputs, int in_place) {
-  for (size_t o = 0; o < outputs.size(); ++o) {
-    for (size_t i = 0; i < inputs.size(); ++i) {
-      if (o == 0 && static_cast<int>(i) == in_place && same(outputs[o], inputs[i])) continue;
-      if (overlap(outputs[o], inputs[i])) return DASO_EALIAS;
+// Outputs against inputs and each other; `in_place` is the one input that outputs[0] may be.  (Lists of the call's own: an
+// entry point that only checks its arguments and launches allocates nothing that could throw.)
+template <class Inputs>
+int check_alias(std::initializer_list<Block> outputs, const Inputs& inputs, int in_place) {
+  for (const Block* o = outputs.begin(); o != outputs.end(); ++o) {
+    int i = 0;
+    for (const Block& in : inputs) {
+      const bool allowed = i++ == in_place && o == outputs.begin() && same(*o, in);
+      if (!allowed && overlap(*o, in)) return DASO_EALIAS;
     }
-    for (size_t k = 0; k < o; ++k)
-      if (overlap(outputs[o], outputs[k])) return DASO_EALIAS;
+    for (const Block* k = outputs.begin(); k != o; ++k)
+      if (overlap(*o, *k)) return DASO_EALIAS;
   }
   return DASO_OK;
+}
+int check_alias(std::initializer_list<Block> outputs, std::initializer_list<Block> inputs, int in_place) {
+  return check_alias<std::initializer_list<Block>>(outputs, inputs, in_place);
 }
 
 int64_t padded(int64_t k) { return std::max<int64_t>(128, (k + 63) / 64 * 64); }

@@ -1,0 +1,171 @@
+// Exercises the host-only code of the training operators (argument checks, rounds and workspace offsets of the
+// Newton-Schulz steps) under AddressSanitizer and UndefinedBehaviorSanitizer, and without memory.  Built with the host
+// compiler alone; fake device addresses are never dereferenced.  Exit status 0 when every expectation holds.
+#include <algorithm>
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <new>
+#include <random>
+#include <vector>
+
+#include "daso_train.h"
+#include "daso_train_host.h"
+
+static int failures = 0;
+#define EXPECT(cond)                                                     \
+  do {                                                                   \
+    if (!(cond)) {                                                       \
+      std::fprintf(stderr, "%s:%d: expectation failed: %s\n", __FILE__,  \
+                   __LINE__, #cond);                                     \
+      ++failures;                                                        \
+    }                                                                    \
+  } while (0)
+
+static bool no_memory = false;
+void* operator new(size_t n) {
+  void* p = no_memory ? nullptr : std::malloc(n ? n : 1);
+  if (p == nullptr) throw std::bad_alloc();
+  return p;
+}
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete(void* p, size_t) noexcept { std::free(p); }
+
+using namespace daso::host;
+typedef std::mt19937_64 Rng;
+
+template <class T>
+static T* at(uint64_t address) { return reinterpret_cast<T*>(address); }
+static int64_t one_of(Rng& rng, std::initializer_list<int64_t> of) { return of.begin()[rng() % of.size()]; }
+// A small address now and then null, odd or inside another buffer's; strides and sizes at the ends of their ranges too.
+static uint64_t address(Rng& rng) { return rng() % 12 == 0 ? 0 : 0x10000000 + (rng() % 24) * 0x8000 + (rng() % 8 == 0 ? rng() % 64 : 0); }
+static int64_t size_of(Rng& rng) { return one_of(rng, {-1, 0, 1, 2, 7, 64, 65, 1000, 65536, 65537, 1 << 20, (1 << 20) + 1, int64_t(1) << 40, INT64_MAX}); }
+
+static daso_layer_norm_args layer_norm(Rng& rng) {
+  return {size_of(rng), size_of(rng), int32_t(rng() % 3), 1e-5f, at<void>(address(rng)), size_of(rng), at<float>(address(rng)),
+          at<float>(address(rng)), at<void>(address(rng)), size_of(rng), at<float>(address(rng)), at<float>(address(rng))};
+}
+static daso_layer_norm_backward_args layer_norm_backward(Rng& rng) {
+  return {size_of(rng), size_of(rng), int32_t(rng() % 3), 0, at<void>(address(rng)), size_of(rng), at<void>(address(rng)), size_of(rng),
+          at<float>(address(rng)), at<float>(address(rng)), at<float>(address(rng)), at<void>(address(rng)), size_of(rng),
+          at<float>(address(rng)), at<float>(address(rng)), at<void>(address(rng)), rng()};
+}
+static daso_loss_args loss(Rng& rng) {
+  return {size_of(rng), size_of(rng), size_of(rng), int32_t(rng() % 3), int32_t(rng() % 3), at<void>(address(rng)), size_of(rng),
+          at<void>(address(rng)), size_of(rng), at<int64_t>(address(rng)), -100, at<float>(address(rng)), at<float>(address(rng)),
+          at<float>(address(rng)), at<void>(address(rng)), size_of(rng), at<void>(address(rng)), size_of(rng), at<void>(address(rng)), rng()};
+}
+static float coefficients[3 * DASO_MAX_SCHULZ_STEPS] = {3.4445f, -4.775f, 2.0315f};
+static daso_orthogonalize_args orthogonalize(Rng& rng) {
+  return {size_of(rng), size_of(rng), size_of(rng), int32_t(rng() % 3), int32_t(rng() % 3), at<void>(address(rng)), size_of(rng),
+          size_of(rng), at<void>(address(rng)), size_of(rng), size_of(rng), int32_t(rng() % 18), 0.0f, coefficients, at<void>(address(rng)), rng()};
+}
+
+static bool status(int rc) { return rc == DASO_OK || rc == DASO_EINVAL || rc == DASO_EALIGN || rc == DASO_EALIAS; }
+
+// Every call ends in a status: no overflow, no read of what a null pointer names, and, without memory, no exception.
+static void check_calls(Rng& rng, int trials) {
+  int taken = 0;
+  for (int t = 0; t < trials; ++t) {
+    int rc[5];
+    const auto norm = layer_norm(rng);
+    const auto back = layer_norm_backward(rng);
+    const auto ce = loss(rng);
+    const auto ns = orthogonalize(rng);
+    no_memory = true;
+    try {
+      rc[0] = check_layer_norm(norm), rc[1] = check_layer_norm_backward(back), rc[2] = check_loss(ce, false), rc[3] = check_loss(ce, true);
+      rc[4] = check_orthogonalize(ns);
+    } catch (const std::bad_alloc&) {
+      no_memory = false;
+      EXPECT(!"a check of arguments allocates");
+      return;
+    }
+    no_memory = false;
+    for (int k : rc) {
+      EXPECT(status(k));
+      taken += k == DASO_OK;
+    }
+  }
+  EXPECT(taken > trials / 100);
+}
+
+// The pairs that may be one buffer, and a stride that makes them two that overlap.
+static void alias_checks() {
+  daso_layer_norm_args a = {10, 64, DASO_TYPE_F32, 1e-5f, at<void>(0x10000), 64, nullptr, nullptr, at<void>(0x10000), 64, nullptr, nullptr};
+  EXPECT(check_layer_norm(a) == DASO_OK);
+  a.y_stride = 65;
+  EXPECT(check_layer_norm(a) == DASO_EALIAS);
+  a.y_stride = 64, a.mean = at<float>(0x10000 + 4 * 64);
+  EXPECT(check_layer_norm(a) == DASO_EALIAS);
+  daso_layer_norm_backward_args b = {10, 64, DASO_TYPE_F32, 0, at<void>(0x10000), 64, at<void>(0x20000), 64, nullptr, at<float>(0x30000),
+                                     at<float>(0x31000), at<void>(0x10000), 64, at<float>(0x40000), at<float>(0x41000), nullptr, 0};
+  EXPECT(check_layer_norm_backward(b) == DASO_OK);
+  b.dx = at<void>(0x20000);  // x is read by the sums too
+  EXPECT(check_layer_norm_backward(b) == DASO_EALIAS);
+  b.dx = nullptr, b.dbias = b.dweight;
+  EXPECT(check_layer_norm_backward(b) == DASO_EALIAS);
+  float c[3] = {1, 1, 1};
+  daso_orthogonalize_args o = {2, 8, 8, DASO_TYPE_F32, DASO_TYPE_F32, at<void>(0x10000), 64, 8, at<void>(0x10000), 64, 8, 1, 0.0f, c, nullptr, 0};
+  EXPECT(check_orthogonalize(o) == DASO_OK);
+  o.out_type = DASO_TYPE_BF16;
+  EXPECT(check_orthogonalize(o) == DASO_EALIAS);
+}
+
+// Each matrix once, matrices of one shape together, and no two regions of a round's workspace overlap.
+static void round_checks(Rng& rng, int trials) {
+  struct Region {
+    size_t from, bytes;
+  };
+  for (int t = 0; t < trials; ++t) {
+    const bool source = rng() % 2, full = rng() % 2;
+    std::vector<Shape> shapes;
+    const int kinds = 1 + int(rng() % 12);
+    for (int k = 0; k < kinds; ++k) {
+      const int64_t top = one_of(rng, {1, 64, 640, 5000, 1 << 16});
+      const Shape s = {1 + int64_t(rng() % top), 1 + int64_t(rng() % std::min<int64_t>(top, (int64_t(1) << 28) / top))};
+      for (int i = int(rng() % 200); i >= 0; --i) shapes.push_back(s);
+    }
+    std::shuffle(shapes.begin(), shapes.end(), rng);
+    std::vector<int> seen(shapes.size(), 0);
+    for (const SchulzRound& r : plan_rounds(shapes, source, full)) {
+      EXPECT(!r.groups.empty() && r.groups.size() <= size_t(kRoundGroups) && r.matrices.size() <= size_t(kRoundMatrices));
+      std::vector<Region> taken = {{0, kRoundTables}};
+      size_t first = 0;
+      for (const SchulzGroup& g : r.groups) {
+        EXPECT(g.count > 0 && size_t(g.first) == first);
+        first += size_t(g.count);
+        for (int32_t i = 0; i < g.count && first <= r.matrices.size(); ++i) {
+          const int32_t m = r.matrices[size_t(g.first + i)];
+          ++seen[size_t(m)];
+          EXPECT(shapes[size_t(m)].rows == g.rows && shapes[size_t(m)].cols == g.cols);
+        }
+        EXPECT(g.tall == (g.rows > g.cols) && g.m >= std::min(g.rows, g.cols) && g.n >= std::max(g.rows, g.cols) && g.m % 64 == 0 && g.n % 64 == 0 && g.m >= 128);
+        const size_t k = size_t(g.count), square = size_t(2 * g.m * g.m) * k, planes = size_t(2 * g.m * g.n) * k;
+        if (source) taken.push_back({g.source, size_t(4 * g.rows * g.cols) * k});
+        if (g.small) continue;
+        for (int p = 0; p < 2; ++p) {
+          taken.insert(taken.end(), {{g.x[0][p], planes}, {g.x[1][p], planes}, {g.gram[p], square}, {g.poly[p], square}, {g.rest[p], size_t(4 * g.m) * k}});
+          if (g.tall) taken.push_back({g.xt[p], planes});
+        }
+      }
+      EXPECT(first == r.matrices.size());
+      taken.push_back({r.sums, r.sums_bytes});
+      std::sort(taken.begin(), taken.end(), [](const Region& a, const Region& b) { return a.from < b.from || (a.from == b.from && a.bytes < b.bytes); });
+      for (size_t i = 0; i < taken.size(); ++i) {
+        EXPECT(taken[i].from % 256 == 0 && taken[i].from + taken[i].bytes <= r.bytes);
+        if (i > 0) EXPECT(taken[i - 1].from + taken[i - 1].bytes <= taken[i].from);
+      }
+    }
+    EXPECT(std::all_of(seen.begin(), seen.end(), [](int n) { return n == 1; }));
+  }
+}
+
+int main() {
+  Rng rng(20);
+  check_calls(rng, 200000);
+  alias_checks();
+  round_checks(rng, 400);
+  if (failures == 0) std::printf("train host checks ok\n");
+  return failures == 0 ? 0 : 1;
+}
