@@ -32,10 +32,9 @@ constexpr int kBlockRows = 64, kBlockCols = 32;  // what an epilogue is handed a
 constexpr int kStagePlane = kBlockRows * kBlockCols * 2 + (kBlockRows / 8) * 16;
 constexpr int kWaveStage = 2 * kStagePlane;
 static_assert(kWaveStage >= kBlockRows * kBlockCols * 4, "a staged block fits");
-constexpr int64_t kMaxLd = int64_t(1) << 22;  // row offsets within a tile stay in 32 bits
 constexpr int kMaxProblems = 8;               // products of one launch
 
-// Operands: rows of `ld` elements, 16-byte aligned, ld a multiple of 8, of which the first
+// Operands: rows of `ld` elements, 16-byte aligned, ld a multiple of 8 and at most host::kMaxLd, of which the first
 // steps * 64 are contracted (zeros beyond the true length).  Rows from M (N) on are not
 // read: a tile that reaches past them reads the last row again, and its epilogue leaves
 // what comes of it.  A turned B has steps * 64 rows, which are contracted, of N values; N is a multiple of 8.
@@ -822,7 +821,7 @@ int deal(Launch<E>& all, const Sums& sums, int* cut) {
     p.tiles_m = (p.M + kSide - 1) / kSide;
     p.tiles_n = (p.N + kSide - 1) / kSide;
     first[k + 1] = first[k] + tile_count(p);
-    if (tile_count(p) > INT32_MAX / 2) return -1;
+    if (tile_count(p) > INT32_MAX / 2 || p.lda > host::kMaxLd || p.ldb > host::kMaxLd) return -1;
     units += tile_count(p) * steps_of(p);
   }
   *cut = 0;

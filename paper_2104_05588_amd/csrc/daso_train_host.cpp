@@ -129,7 +129,7 @@ int check_layer_norm_backward(const daso_layer_norm_backward_args& s) {
 
 // ------------------------------------------------------------------------- the loss
 int check_loss_sizes(const daso_loss_args& s) {
-  if (s.tokens < 0 || s.tokens > 4 * DASO_MAX_SIDE || s.vocab < 1 || s.vocab > DASO_MAX_SIDE || s.d < 1 || s.d > DASO_MAX_SIDE)
+  if (s.tokens < 0 || s.tokens > kMaxLd || s.vocab < 1 || s.vocab > DASO_MAX_SIDE || s.d < 1 || s.d > DASO_MAX_SIDE)
     return DASO_EINVAL;
   if (!known(s.type) || !known(s.dweight_type)) return DASO_EINVAL;
   return DASO_OK;
@@ -148,7 +148,7 @@ int check_loss(const daso_loss_args& s, bool backward) {
   }
   if (s.tokens == 0) return DASO_OK;
   if (!stride_ok(s.hidden_stride, s.d, s.tokens) || !stride_ok(s.weight_stride, s.d, s.vocab)) return DASO_EINVAL;
-  if (s.hidden_stride > DASO_MAX_SIDE * 4 || s.weight_stride > DASO_MAX_SIDE * 4) return DASO_EINVAL;
+  if (s.hidden_stride > kMaxLd || s.weight_stride > kMaxLd) return DASO_EINVAL;
   if ((rc = first({need(h), need(w), need(t), need(lse)})) != DASO_OK) return rc;
   if (!backward) {
     const Block loss = flat(s.loss, s.tokens, 4);

@@ -27,6 +27,10 @@ int check_orthogonalize_sizes(const daso_orthogonalize_args& s);
 int check_muon_sizes(const daso_muon_args& s);
 int check_workspace(const void* p, size_t bytes, size_t need);
 
+// The longest rows of a product's operands, in elements: the offsets of a tile's 256 rows stay in 32 bits.
+constexpr int64_t kMaxLd = 4 * DASO_MAX_SIDE;
+static_assert(255 * 2 * kMaxLd + 128 <= UINT32_MAX, "the last byte of a tile's last row");
+
 // ------------------------------------------------------------------ sums of cut tiles
 // Steps of a part of a tile, at the least, and the most parts of an XCD's pool, a workgroup
 // (daso_product.h).

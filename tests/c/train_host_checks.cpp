@@ -112,6 +112,20 @@ static void alias_checks() {
   EXPECT(check_orthogonalize(o) == DASO_EALIAS);
 }
 
+// A product's operands may have rows of kMaxLd elements: the loss's as they lie in memory, and hidden turned, of all tokens.
+static void row_checks() {
+  daso_loss_args a = {2, 3, 64, DASO_TYPE_BF16, DASO_TYPE_BF16, at<void>(0x100000000), kMaxLd, at<void>(0x200000000), kMaxLd,
+                      at<int64_t>(0x300000000), -100, at<float>(0x400000000), at<float>(0x500000000), at<float>(0x600000000),
+                      at<void>(0x700000000), 64, at<void>(0x800000000), 64, nullptr, 0};
+  EXPECT(check_loss(a, false) == DASO_OK && check_loss(a, true) == DASO_OK);
+  for (int64_t daso_loss_args::*field : {&daso_loss_args::hidden_stride, &daso_loss_args::weight_stride, &daso_loss_args::tokens}) {
+    const int64_t was = a.*field;
+    a.*field = kMaxLd + 1;
+    EXPECT(check_loss(a, false) == DASO_EINVAL && check_loss(a, true) == DASO_EINVAL);
+    a.*field = was;
+  }
+}
+
 // Each matrix once, matrices of one shape together, and no two regions of a round's workspace overlap.
 static void round_checks(Rng& rng, int trials) {
   struct Region {
@@ -165,6 +179,7 @@ int main() {
   Rng rng(20);
   check_calls(rng, 200000);
   alias_checks();
+  row_checks();
   round_checks(rng, 400);
   if (failures == 0) std::printf("train host checks ok\n");
   return failures == 0 ? 0 : 1;
