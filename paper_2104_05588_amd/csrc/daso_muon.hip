@@ -854,21 +854,17 @@ size_t most_bytes(const std::vector<SchulzRound>& rounds) {
   return most;
 }
 
-std::vector<host::Shape> shapes_of(const daso_orthogonalize_args& s) {
-  if (s.rows == 0 || s.cols == 0) return {};
-  return std::vector<host::Shape>(static_cast<size_t>(s.batch), host::Shape{s.rows, s.cols});
-}
 std::vector<host::Shape> shapes_of(const daso_muon_args& s) {
   std::vector<host::Shape> v;
   for (int32_t i = 0; i < s.nmatrices; ++i) v.push_back({s.matrices[i].rows, s.matrices[i].cols});
   return v;
 }
 
+// The matrices from `at` on.
 template <class T>
-hipError_t orthogonalize_round(const daso_orthogonalize_args& s, const SchulzRound& r, hipStream_t stream) {
+hipError_t orthogonalize_round(const daso_orthogonalize_args& s, const SchulzRound& r, int64_t at, hipStream_t stream) {
   char* ws = static_cast<char*>(s.workspace);
   const SchulzGroup& g = r.groups[0];  // one shape
-  const int64_t at = r.matrices[0];
   const T* src = static_cast<const T*>(s.src) + at * s.src_batch_stride;
   const int64_t rows = s.rows;
   const int32_t parts = static_cast<int32_t>(std::min<int64_t>(parts_of(rows * s.cols), rows));
@@ -938,8 +934,10 @@ int daso_orthogonalize_workspace(const daso_orthogonalize_args* args, size_t* by
   if (args == nullptr || bytes == nullptr) return DASO_EINVAL;
   const int rc = daso::host::check_orthogonalize_sizes(*args);
   if (rc != DASO_OK) return rc;
+  *bytes = 0;
+  if (args->batch == 0 || args->rows == 0 || args->cols == 0) return DASO_OK;
   try {
-    *bytes = daso::most_bytes(daso::host::plan_rounds(daso::shapes_of(*args), false, args->out_type == DASO_TYPE_F32));
+    *bytes = daso::host::plan_batch(args->batch, {args->rows, args->cols}, args->out_type == DASO_TYPE_F32).full.bytes;
   } catch (const std::bad_alloc&) {
     return DASO_EHIP;
   }
@@ -952,12 +950,13 @@ int daso_orthogonalize(const daso_orthogonalize_args* args, hipStream_t stream) 
   int rc = daso::host::check_orthogonalize(s);
   if (rc != DASO_OK || s.batch == 0 || s.rows == 0 || s.cols == 0) return rc;
   try {
-    const std::vector<SchulzRound> rounds = daso::host::plan_rounds(daso::shapes_of(s), false, s.out_type == DASO_TYPE_F32);
-    if ((rc = daso::host::check_workspace(s.workspace, s.workspace_bytes, daso::most_bytes(rounds))) != DASO_OK) return rc;
+    const daso::host::SchulzBatch b = daso::host::plan_batch(s.batch, {s.rows, s.cols}, s.out_type == DASO_TYPE_F32);
+    if ((rc = daso::host::check_workspace(s.workspace, s.workspace_bytes, b.full.bytes)) != DASO_OK) return rc;
     if ((rc = daso::current_device(stream)) != DASO_OK) return rc;
-    for (const SchulzRound& r : rounds) {
-      const hipError_t e = s.type == DASO_TYPE_F32 ? daso::orthogonalize_round<float>(s, r, stream)
-                                                   : daso::orthogonalize_round<uint16_t>(s, r, stream);
+    for (int64_t k = 0; k < b.rounds; ++k) {
+      const SchulzRound& r = k + 1 < b.rounds ? b.full : b.last;
+      const hipError_t e = s.type == DASO_TYPE_F32 ? daso::orthogonalize_round<float>(s, r, k * b.each, stream)
+                                                   : daso::orthogonalize_round<uint16_t>(s, r, k * b.each, stream);
       if (e != hipSuccess) return DASO_EHIP;
     }
   } catch (const std::bad_alloc&) {

@@ -301,5 +301,17 @@ std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with
   return rounds;
 }
 
+SchulzBatch plan_batch(int64_t batch, const Shape& shape, bool full) {
+  const auto round_of = [&](int64_t matrices) {
+    return plan_rounds(std::vector<Shape>(static_cast<size_t>(matrices), shape), false, full)[0];
+  };
+  SchulzBatch b = {};
+  b.full = round_of(std::min<int64_t>(batch, kRoundMatrices));
+  b.each = static_cast<int64_t>(b.full.matrices.size());
+  b.rounds = (batch + b.each - 1) / b.each;
+  b.last = batch % b.each != 0 ? round_of(batch % b.each) : b.full;
+  return b;
+}
+
 }  // namespace host
 }  // namespace daso

@@ -80,6 +80,14 @@ struct Shape {
 // Rounds over the given matrices, in order of first appearance of their shapes.  full: products in 22 bits.
 std::vector<SchulzRound> plan_rounds(const std::vector<Shape>& shapes, bool with_source, bool full);
 
+// Rounds over a batch of matrices of one shape, however many: all of them like `full` but, where there is one, the last.
+struct SchulzBatch {
+  SchulzRound full, last;
+  int64_t each;    // matrices of a full round
+  int64_t rounds;  // with the last
+};
+SchulzBatch plan_batch(int64_t batch, const Shape& shape, bool full);
+
 // The matrices that one workgroup takes (daso_muon.hip): what they need of its LDS, and whether they fit.
 constexpr int kSmallM = 64, kSmallGroups = 5;                        // m, and groups of 128 columns of n, at most
 constexpr int kGramStride = kSmallM * 2 + 16;                        // bytes a row of the gram matrix

@@ -175,12 +175,35 @@ static void round_checks(Rng& rng, int trials) {
   }
 }
 
+// A batch of one shape: the rounds of plan_rounds, and as little memory for any number of matrices.
+static void batch_checks(Rng& rng, int trials) {
+  for (int t = 0; t < trials; ++t) {
+    const int64_t top = one_of(rng, {1, 64, 640, 5000, 20000});
+    const Shape s = {1 + int64_t(rng() % top), 1 + int64_t(rng() % top)};
+    const bool full = rng() % 2;
+    const int64_t batch = 1 + int64_t(rng() % 500);
+    const std::vector<SchulzRound> rounds = plan_rounds(std::vector<Shape>(size_t(batch), s), false, full);
+    const SchulzBatch b = plan_batch(batch, s, full);
+    EXPECT(b.rounds == int64_t(rounds.size()));
+    size_t most = 0;
+    for (size_t k = 0; k < rounds.size(); ++k) {
+      const SchulzRound& r = k + 1 < rounds.size() ? b.full : b.last;
+      EXPECT(rounds[k].matrices[0] == int64_t(k) * b.each && r.groups.size() == 1 && r.groups[0].count == rounds[k].groups[0].count && r.bytes == rounds[k].bytes);
+      most = std::max(most, r.bytes);
+    }
+    EXPECT(most == b.full.bytes);
+  }
+  const SchulzBatch many = plan_batch(INT32_MAX, {1, 1}, true);
+  EXPECT(many.each == kRoundMatrices && many.rounds == (int64_t(INT32_MAX) + kRoundMatrices - 1) / kRoundMatrices);
+}
+
 int main() {
   Rng rng(20);
   check_calls(rng, 200000);
   alias_checks();
   row_checks();
   round_checks(rng, 400);
+  batch_checks(rng, 2000);
   if (failures == 0) std::printf("train host checks ok\n");
   return failures == 0 ? 0 : 1;
 }

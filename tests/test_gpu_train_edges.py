@@ -247,3 +247,19 @@ def test_muon_step_captured_on_another_stream():
         eager()
         torch.cuda.synchronize()
         assert torch.equal(p, want_p) and torch.equal(m, want_m), k
+
+
+@pytest.mark.parametrize("rows,cols", [(24, 40), (72, 100), (100, 72)])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+def test_orthogonalize_in_several_rounds(rows, cols, out):
+    """More matrices than are taken at a time, the last round with fewer; and in place."""
+    announce("orthogonalize in rounds", rows, cols, out)
+    u = torch.randn(300, rows, cols, generator=gen(71)).cuda()
+    got = daso.orthogonalize(u, out=torch.full(u.shape, float("nan"), dtype=out, device="cuda"))
+    for i in (0, 127, 128, 255, 256, 299):
+        want = O.newton_schulz(np64(u[i]), [(3.4445, -4.7750, 2.0315)] * 5)
+        plane = 2.0 ** -11 if out == torch.bfloat16 else 2.0 ** -21  # (the tolerance of test_gpu_train)
+        tol = 4 * 5 * plane + 2.0 ** -22 * 3.5 ** 5 / np.linalg.norm(want) + (2.0 ** -8 if out == torch.bfloat16 else U)
+        assert np.linalg.norm(np64(got[i]) - want) <= tol * np.linalg.norm(want), i
+    if out == torch.float32:
+        assert torch.equal(daso.orthogonalize(u, out=u), got)

@@ -1,12 +1,17 @@
 """The training operators' binding without a GPU: what it asks of streams and the allocator, with stand-ins for both."""
 import contextlib
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
 
 from paper_2104_05588_amd import _lib as L
 from paper_2104_05588_amd import _train as T
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 class FakeStream:
@@ -144,3 +149,23 @@ def test_a_stream_of_another_device_is_refused(cuda, monkeypatch):
     with pytest.raises(ValueError, match="the stream is of cuda:1"):
         step(other)
     assert calls == [] and step._workspace.recorded == []
+
+
+def test_the_plan_of_a_large_batch_takes_no_memory_by_its_size():
+    """daso_orthogonalize_workspace of 2^31 - 1 matrices within 2 GiB of address space more than the library itself."""
+    program = """
+import ctypes, resource, sys
+from paper_2104_05588_amd import _train as T
+lib = T._load()
+pages = int(open("/proc/self/statm").read().split()[0])
+limit = pages * resource.getpagesize() + (2 << 30)
+resource.setrlimit(resource.RLIMIT_AS, (limit, limit))
+a = T.daso_orthogonalize_args(batch=2 ** 31 - 1, rows=1, cols=1, type=0, out_type=0)
+n = ctypes.c_size_t(0)
+rc = lib.daso_orthogonalize_workspace(ctypes.byref(a), ctypes.byref(n))
+print("status", rc, n.value)
+"""
+    res = subprocess.run([sys.executable, "-c", program], capture_output=True, text=True, timeout=120, cwd=ROOT)
+    status = [line.split() for line in res.stdout.splitlines() if line.startswith("status")]
+    assert res.returncode == 0 and status, res.stderr[-2000:]
+    assert int(status[0][1]) == L.DASO_OK and 0 < int(status[0][2]) < 1 << 20
