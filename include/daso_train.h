@@ -14,7 +14,8 @@
  * Further:
  *  - Types: DASO_TYPE_F32 or DASO_TYPE_BF16 where an argument says so.  Rows may lie
  *    `stride` elements apart (stride >= the row's length).  Pointers need the alignment of
- *    their element; 16-byte aligned rows are the fast case.
+ *    their element; 16-byte aligned rows are the fast case.  Two buffers may be columns of one wider buffer (rows the
+ *    same distance apart, one's beside the other's); else they count as overlapping where their spans do.
  *  - Workspaces are the caller's too: the *_workspace functions (host only) state the
  *    bytes, the pointer is aligned to 256, and a smaller one is refused with
  *    DASO_ENOSPACE.  A workspace holds nothing between calls; calls that may run at the

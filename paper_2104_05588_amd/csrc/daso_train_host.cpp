@@ -34,9 +34,17 @@ uintptr_t end(const Block& b) {
   if (b.outer == 0 || b.rows == 0 || b.row == 0) return begin(b);
   return begin(b) + static_cast<uintptr_t>((b.outer - 1) * b.outer_stride + (b.rows - 1) * b.stride + b.row) * b.esz;
 }
-// By their spans: rows of one buffer that lie between another's count as an overlap.
+// Rows the same distance apart, of which one buffer's lie beside the other's: columns of one wider buffer.
+bool beside(const Block& a, const Block& b) {
+  if (a.outer > 1 || b.outer > 1 || a.rows <= 1 || b.rows <= 1) return false;
+  const uintptr_t apart = static_cast<uintptr_t>(a.stride) * a.esz;
+  if (apart != static_cast<uintptr_t>(b.stride) * b.esz || apart == 0) return false;
+  const uintptr_t behind = begin(b) >= begin(a) ? (begin(b) - begin(a)) % apart : (apart - (begin(a) - begin(b)) % apart) % apart;
+  return behind >= static_cast<uintptr_t>(a.row) * a.esz && behind + static_cast<uintptr_t>(b.row) * b.esz <= apart;
+}
+// By their spans, but for such rows.
 bool overlap(const Block& a, const Block& b) {
-  return a.p != nullptr && b.p != nullptr && begin(a) < end(b) && begin(b) < end(a);
+  return a.p != nullptr && b.p != nullptr && begin(a) < end(b) && begin(b) < end(a) && !beside(a, b);
 }
 bool same(const Block& a, const Block& b) {
   return a.p == b.p && a.esz == b.esz && (a.rows <= 1 || a.stride == b.stride) &&

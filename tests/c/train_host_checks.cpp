@@ -112,6 +112,36 @@ static void alias_checks() {
   EXPECT(check_orthogonalize(o) == DASO_EALIAS);
 }
 
+// Two row blocks of one buffer are told apart element by element where their strides agree, and never taken as apart where
+// they are not.
+static void beside_checks(Rng& rng, int trials) {
+  int apart = 0;
+  for (int t = 0; t < trials; ++t) {
+    const int64_t rows = 1 + int64_t(rng() % 5), d = 1 + int64_t(rng() % 6), xs = d + int64_t(rng() % 9), ys = rng() % 3 ? xs : d + int64_t(rng() % 9);
+    const int64_t from = int64_t(rng() % 40);
+    daso_layer_norm_args a = {rows, d, DASO_TYPE_F32, 1e-5f, at<void>(0x10000), xs, nullptr, nullptr, at<void>(0x10000 + 4 * from), ys, nullptr, nullptr};
+    if (rng() % 2) {
+      const void* x = a.x;
+      a.x = a.y, a.y = const_cast<void*>(x);
+      std::swap(a.x_stride, a.y_stride);
+    }
+    std::vector<char> used(400, 0);
+    const auto element = [](const void* p, int64_t i) { return (reinterpret_cast<uintptr_t>(p) - 0x10000) / 4 + size_t(i); };
+    bool meet = false;
+    for (int64_t r = 0; r < rows; ++r)
+      for (int64_t c = 0; c < d; ++c) used[element(a.x, r * a.x_stride + c)] = 1;
+    for (int64_t r = 0; r < rows; ++r)
+      for (int64_t c = 0; c < d; ++c) meet |= used[element(a.y, r * a.y_stride + c)] != 0;
+    const bool same = a.x == a.y && (rows == 1 || a.x_stride == a.y_stride);
+    const int rc = check_layer_norm(a);
+    EXPECT(rc == DASO_OK || rc == DASO_EALIAS);
+    if (meet && !same) EXPECT(rc == DASO_EALIAS);
+    if (same || (!meet && a.x_stride == a.y_stride && rows > 1)) EXPECT(rc == DASO_OK);
+    apart += rc == DASO_OK;
+  }
+  EXPECT(apart > trials / 10);
+}
+
 // A product's operands may have rows of kMaxLd elements: the loss's as they lie in memory, and hidden turned, of all tokens.
 static void row_checks() {
   daso_loss_args a = {2, 3, 64, DASO_TYPE_BF16, DASO_TYPE_BF16, at<void>(0x100000000), kMaxLd, at<void>(0x200000000), kMaxLd,
@@ -202,6 +232,7 @@ int main() {
   check_calls(rng, 200000);
   alias_checks();
   row_checks();
+  beside_checks(rng, 100000);
   round_checks(rng, 400);
   batch_checks(rng, 2000);
   if (failures == 0) std::printf("train host checks ok\n");

@@ -263,3 +263,34 @@ def test_orthogonalize_in_several_rounds(rows, cols, out):
         assert np.linalg.norm(np64(got[i]) - want) <= tol * np.linalg.norm(want), i
     if out == torch.float32:
         assert torch.equal(daso.orthogonalize(u, out=u), got)
+
+
+# ------------------------------------------------------------------------- columns of one buffer
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 129, 9000])
+def test_operands_that_are_columns_of_one_buffer(dtype, d):
+    """Outputs beside the inputs of their rows: the bits of separate buffers, and nothing written between."""
+    announce("columns of one buffer", dtype, d)
+    n, v = 70, 90
+    store = torch.full((n, 3 * d + 10), 3.0, dtype=dtype, device="cuda")
+    x, y, z = store[:, 1:d + 1], store[:, d + 2:2 * d + 2], store[:, 2 * d + 7:3 * d + 7]
+    x.copy_(torch.randn(n, d, generator=gen(d)))
+    kept = store.clone()
+    want, mean, rstd = daso.layer_norm(x.contiguous())
+    got, mean2, rstd2 = daso.layer_norm(x, out=y)
+    assert got is y and torch.equal(y, want) and torch.equal(mean, mean2) and torch.equal(rstd, rstd2)
+    want = daso.layer_norm_backward(y.contiguous(), x.contiguous(), None, mean, rstd)
+    got = daso.layer_norm_backward(y, x, None, mean, rstd, dx=z)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    z.copy_(kept[:, 2 * d + 7:3 * d + 7]), y.copy_(kept[:, d + 2:2 * d + 2])
+    assert torch.equal(store, kept)
+    w = (torch.randn(v, d, generator=gen(d + 1)) * 0.05).to(dtype).cuda()
+    t, s = torch.randint(0, v, (n,), generator=gen(3)).cuda(), torch.rand(n, generator=gen(4)).cuda()
+    want_loss, want_lse = daso.linear_cross_entropy(x.contiguous(), w, t)
+    loss, lse = daso.linear_cross_entropy(x, w, t)
+    assert torch.equal(loss, want_loss) and torch.equal(lse, want_lse)
+    want, want_dw = daso.linear_cross_entropy_backward(s, x.contiguous(), w, t, lse)
+    got, dw = daso.linear_cross_entropy_backward(s, x, w, t, lse, dhidden=y)
+    assert torch.equal(y, want) and torch.equal(dw, want_dw)
+    y.copy_(kept[:, d + 2:2 * d + 2])
+    assert torch.equal(store, kept)
