@@ -115,8 +115,9 @@ __device__ inline float top_of_run(const T* src, int64_t n) {
   return wave_max(m);
 }
 
-// Calls f(row, largest magnitude, get(row)), in every lane, for a wavefront's rows, get before they are read: four at a time for loads in flight, or, where
-// there are no more rows than wavefronts, four places of one (a classifier's 256 rows of 2048: 2 us less).
+// Calls f(row, largest magnitude, get(row)), in every lane, for a wavefront's rows, get before they are read: four rows at a
+// time for loads in flight, or, where there are no more rows than wavefronts, four places of one (a classifier's 256 rows of
+// 2048: 1.5 us less).
 template <class T, class G, class F>
 __device__ inline void tops_of_rows(const T* src, int64_t stride, int64_t rows, int64_t cols, G get, F f) {
   const int64_t wave = (blockIdx.x * 256 + threadIdx.x) >> 6, waves = gridDim.x * 4;

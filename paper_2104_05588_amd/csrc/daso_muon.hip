@@ -357,17 +357,15 @@ __global__ __launch_bounds__(256) void squares_kernel(const T* src, int64_t batc
   if (threadIdx.x == 0) sums[blockIdx.y * host::kSumParts + blockIdx.x] = sum;
 }
 
-// What brings a matrix to kScale / (|u| + eps) of itself, in two steps: for the smallest and the largest norms that is no
-// normal fp32 number.
+// What brings a matrix to kScale / (|u| + eps) of itself: the factor `then`, and before it `first`, which is 1 but where the
+// norm is so small, or so large, that the factor would be no normal fp32 number.
 struct Normal {
-  float factor;
-  int exponent;
+  float first, then;
   __device__ Normal(double squares, float eps) {
     const double scale = kScale / (sqrt(squares) + eps);
-    exponent = scale > 0.0 && scale < 1e300 ? ilogb(scale) : 0;
-    factor = static_cast<float>(ldexp(scale, -exponent));
+    first = scale > 0x1p100 && scale < 0x1p1000 ? 0x1p100f : scale < 0x1p-100 ? 0x1p-100f : 1.0f;
+    then = static_cast<float>(scale / first);
   }
-  __device__ float operator()(float v) const { return __builtin_ldexpf(v, exponent) * factor; }
 };
 
 struct LayOut {
@@ -395,7 +393,8 @@ __global__ __launch_bounds__(256) void normalise_kernel(LayOut a) {
   const double* s = a.sums + (a.first_matrix[k] + batch) * host::kSumParts;
   const double sum = group_sum(static_cast<int>(threadIdx.x) < a.parts ? s[threadIdx.x] : 0.0, shared);
   const Normal scaled(sum, a.eps);
-  planes_tile<T, false>(p, batch, static_cast<int>((t % per) / across), static_cast<int>(t % across), scaled, lds);
+  planes_tile<T, false>(p, batch, static_cast<int>((t % per) / across), static_cast<int>(t % across),
+                        [scaled](float v) { return v * scaled.first * scaled.then; }, lds);
 }
 
 // ------------------------------------------------------------------------- small matrices
@@ -481,12 +480,15 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_kernel(SmallArgs a) {
       for (int e = 0; e < 4; ++e) square += static_cast<double>(x[i][j][e]) * x[i][j][e];
   }
   const Normal scaled(group_sum(square, sums), a.eps);
+  if (scaled.first != 1.0f)
+#pragma unroll
+    for (int i = 0; i < kSmallGroups; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i][j] *= scaled.first;
 #pragma unroll
   for (int i = 0; i < kSmallGroups; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][j][e] = scaled(x[i][j][e]);
+    for (int j = 0; j < 4; ++j) x[i][j] *= scaled.then;
   // columns between n and the last step's end are read as zeros
   for (int k = threadIdx.x; k < kSmallM * 8; k += kSmallThreads) {
     const int row = k >> 3, at = (n_steps * 64 - 64 + (k & 7) * 8) * 2;
