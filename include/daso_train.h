@@ -89,7 +89,8 @@ int daso_layer_norm_backward(const daso_layer_norm_backward_args* args, hipStrea
  * the classes v,
  *     lse_i = log sum_v exp(z_v),  loss_i = lse_i - z_target
  * and loss_i = 0 where the target is ignore_index.  The logits z are summed in 32 bits, in
- * tiles that are reduced while they are in registers; they are never stored.  A target that is
+ * tiles that are reduced while they are in registers; only parts of the sums of a call of few tiles go through the
+ * workspace.  A target that is
  * neither a class nor ignore_index makes its loss NaN (and the gradients that it reaches).
  *
  * Range: fp32 operands are taken in 22 bits, but not below 2^-39 of the largest magnitude: of the token's row of hidden

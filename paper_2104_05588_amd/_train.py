@@ -3,7 +3,10 @@ layer norm, the cross entropy of an output projection, and orthogonalised update
 
 As in _lib: tensors are checked and their addresses and the current HIP stream cross the C ABI;
 every step of the computation runs in the library's kernels.  Outputs that are not
-given, and workspaces, come from torch's allocator, on the stream that the call runs on."""
+given, and workspaces, come from torch's allocator, on the stream that the call runs on.
+
+Nothing here is recorded by autograd: results of tensors that require a gradient have no history, and the gradients are what the
+*_backward functions return."""
 from __future__ import annotations
 
 import contextlib

@@ -9,10 +9,11 @@
 // twice: keeping them would cost N V 4 bytes written and read, which takes as long as the
 // product at d = 1024 and grows the memory by N V.
 //
-// Bound by the matrix cores: 4096 tokens over 50257 classes of 1024 features forward in 372 to 381 us by machine
-// (1110 to 1130 TFLOP/s; 16 steps a tile leave less of the pipeline's rate than 128 do), 8192 with gradients
+// Bound by the matrix cores: 4096 tokens over 50257 classes of 1024 features forward in 364 to 395 us by machine
+// (1070 to 1160 TFLOP/s; 16 steps a tile leave less of the pipeline's rate than 128 do), 8192 with gradients
 // and an fp32 dweight in 4.0 ms, 4.2 PFLOP counting the logits twice and dweight in two planes.  A few
-// tokens or classes are bound by the chain of eight launches, 3 to 18 us each.
+// tokens or classes are bound by the chain of eight launches, 3 to 18 us each.  Where a launch has few tiles, they are cut, and
+// the parts' sums of logits lie in the workspace until the second kernel has added them.
 //
 // Numbers.  bf16 operands are multiplied as they are in the forward product; fp32 ones as two
 // binary16 planes each (22 bits), hidden scaled by a power of two from each row's largest value, weight by one from the
