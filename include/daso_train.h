@@ -125,8 +125,8 @@ int daso_linear_cross_entropy(const daso_loss_args* args, hipStream_t stream);
  * taken over pieces of the vocabulary, whose logits are computed again.  dz is rounded to 11
  * bits for the products whose result is bf16 and held as a sum of two such parts (22 bits)
  * for those whose result is fp32, and to 2^-38 of its token's dloss_i, whatever the others' are.
- * Nothing of an ignored token, or of one whose dloss is zero, counts in the products: it may hold any numbers, and an
- * ignored one NaN and infinities.  With tokens == 0 dweight is zero. */
+ * Nothing of an ignored token, or of one whose dloss is zero, counts in them, whatever it holds: its dz is zero.  With
+ * tokens == 0 dweight is zero. */
 int daso_linear_cross_entropy_backward(const daso_loss_args* args, hipStream_t stream);
 
 /* Newton-Schulz orthogonalisation of a batch of matrices U (rows x cols):

@@ -249,13 +249,16 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   Row r = {0.0f, 0.0f, -1, 0, 0};
   if (i < a.tokens) {
     const int64_t t = a.targets[i];
-    if (t >= 0 && t < a.vocab && t != a.ignore) {
-      r.lse = a.lse[i];
-      const int by = Token{a.dloss[i], t}.by(a.ignore);
-      r.by = static_cast<int16_t>(by == kNone ? 0 : by);
-      r.g = __builtin_ldexpf(a.dloss[i], kProbExponent - r.by);
-      r.to = static_cast<int16_t>(to_half(a.row_top[i]));
-      r.target = static_cast<int32_t>(t);
+    const Token token = {a.dloss[i], t};
+    const int by = token.by(a.ignore);
+    if (t >= 0 && t < a.vocab) {
+      if (by != kNone) {
+        r.lse = a.lse[i];
+        r.g = __builtin_ldexpf(token.dloss, kProbExponent - by);
+        r.target = static_cast<int32_t>(t);
+        r.to = static_cast<int16_t>(to_half(a.row_top[i]));
+        r.by = static_cast<int16_t>(by);
+      }
     } else if (t != a.ignore) {
       r.g = __builtin_nanf("");
       r.target = 0;

@@ -178,6 +178,24 @@ def test_ignored_rows_without_numbers(dtype, grad, junk):
     assert torch.equal(dh2, dh) and torch.equal(dw2, dw)
 
 
+@pytest.mark.parametrize("dtype,grad", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), 1e38, 1.0])
+def test_tokens_without_weight(dtype, grad, junk):
+    """A token whose dloss is zero counts in no gradient, whatever it holds, as with a loss that is masked by weights."""
+    announce("tokens without weight", dtype, grad, junk)
+    h, w, t, s = loss_case(150, 300, 96, dtype, 0.0, 53)
+    gone = torch.rand(150, generator=gen(54)) < 0.3
+    h[gone], s[gone] = 0, 0
+    s[~gone] += 0.1
+    _, _, dh, dw = check_loss(h, w, t, s, h.cuda(), w.cuda(), grad)
+    h[gone, 5:9] = junk
+    s[gone] *= -1  # (and the other zero)
+    _, lse = daso.linear_cross_entropy(h.cuda(), w.cuda(), t.cuda())
+    dh2, dw2 = daso.linear_cross_entropy_backward(s.cuda(), h.cuda(), w.cuda(), t.cuda(), lse,
+                                                  dweight=torch.empty(300, 96, dtype=grad, device="cuda"))
+    assert torch.equal(dh2, dh) and torch.equal(dw2, dw)
+
+
 # ------------------------------------------------------------------------- layer norm of nothing
 @pytest.mark.parametrize("rows", [0, 1, 700])
 def test_layer_norm_of_empty_rows(rows):
