@@ -23,7 +23,8 @@ CAPI_CLUSTER_SRC = os.path.join(ROOT, "tests", "c", "daso_cluster_capi.c")
 CAPI_CLUSTER = os.path.join(PKG, "daso_cluster_capi")
 
 SOURCES = ["daso_kernels.hip", "daso_api.hip", "daso_host.cpp", "daso_schedule.cpp",
-           "daso_train_host.cpp", "daso_norm.hip", "daso_loss.hip", "daso_muon.hip"]
+           "daso_train_host.cpp", "daso_norm.hip", "daso_loss.hip", "daso_muon.hip",
+           "daso_block_host.cpp", "daso_rotary.hip", "daso_attention.hip", "daso_clip.hip"]
 # The bench's bandwidth-ceiling probes (the step's access pattern without its
 # arithmetic): a library of their own, outside the C ABI.
 PROBE_SOURCE = "daso_ceiling.hip"

@@ -1,0 +1,332 @@
+// What the attention kernels are made of: where a workgroup's rows lie, tiles of rows in LDS, and
+// the two kinds of products with them.
+//
+// All products are made with the tile's rows as the left operand and 32 rows of the wavefront's own as the right one,
+// which are its columns: C[i][j], j = lane % 32, of which a lane holds i = 8 (r / 4) + 4 (lane / 32) + r % 4 for
+// r = 0..15.  So what a softmax reduces over lies in one lane and the one 32 above it, and values of C are at once in place as
+// the right operand of a product that contracts over i: the order of the contraction is free, so the left operand
+// is read in the order in which the lanes hold them.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "daso_block_host.h"
+#include "daso_planes.h"
+#include "daso_product.h"
+
+namespace daso {
+namespace attention {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef u4 u4_any __attribute__((aligned(2)));
+using product::bhalf8;
+using product::half4;
+using product::half8;
+
+struct Rows {
+  void* p;
+  int64_t token, head;  // strides in elements
+};
+
+struct Attention {
+  int64_t tokens;
+  const int64_t* offsets;  // or null: one sequence of all tokens
+  int32_t sequences, heads, kv_heads, share;  // share: query heads of a key head
+  int32_t dim, causal, zero_q, zero_k, zero_v;  // zeros behind the last sequence
+  int32_t tiles;  // of a head, at most
+  float scale, scale2;  // scale2 = scale * log2 e
+  Rows q, k, v, out, dout, dq, dk, dv;
+  float *lse, *delta;  // heads x tokens
+};
+
+// The tile of a workgroup: rows `row`.. of the sequence of `len` tokens from `start` on.
+struct Place {
+  int64_t start;
+  int32_t len, row, head;
+};
+
+__device__ inline int64_t read_lane(int64_t v, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(v), lane);
+  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), lane);
+  return static_cast<int64_t>(uint64_t(hi) << 32 | lo);
+}
+
+// Workgroups of neighbouring numbers go to the eight XCDs in turn.  Where the heads can be dealt to them evenly each XCD
+// takes whole heads one after the other, whose keys then stay in its L2; else the heads' tiles are dealt in turn.
+// Of a causal sequence the tiles that are the most work come first.
+// first_most: the first tiles of a sequence are the most work (keys), else the last ones (queries).
+// kRest: a tile of the rows behind the last sequence.
+enum Found { kNone, kSequence, kRest };
+template <int ROWS>
+__device__ inline Found place_of(const Attention& a, int heads, bool first_most, Place* at) {
+  const int id = blockIdx.x;
+  int index;
+  if (heads % 8 == 0) {
+    const int in = id >> 3, each = heads >> 3;
+    at->head = (id & 7) * each + in / a.tiles;
+    index = in % a.tiles;
+  } else {
+    at->head = id % heads;
+    index = id / heads;
+  }
+  int tile, tiles;
+  if (a.offsets == nullptr) {
+    at->start = 0, at->len = static_cast<int32_t>(a.tokens);
+    tile = index, tiles = (at->len + ROWS - 1) / ROWS;
+    if (tile >= tiles) return kNone;
+  } else {
+    const int lane = threadIdx.x & 63;
+    int before = 0, base = 0;
+    for (;;) {
+      int64_t from = 0, to = 0;
+      if (base + lane < a.sequences) from = a.offsets[base + lane], to = a.offsets[base + lane + 1];
+      if (!(from >= 0 && to >= from && to <= a.tokens)) to = from = 0;
+      const int mine = (static_cast<int>(to - from) + ROWS - 1) / ROWS;
+      int upto = mine;
+#pragma unroll
+      for (int s = 1; s < 64; s <<= 1) {
+        const int v = __shfl_up(upto, s);
+        if (lane >= s) upto += v;
+      }
+      const uint64_t found = __ballot(before + upto > index);
+      if (found != 0) {
+        const int l = __builtin_ctzll(found);
+        at->start = read_lane(from, l), at->len = static_cast<int32_t>(read_lane(to, l) - at->start);
+        tiles = __builtin_amdgcn_readlane(mine, l);
+        tile = index - before - (__builtin_amdgcn_readlane(upto, l) - tiles);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
+      base += 64;
+      if (base >= a.sequences) {
+        at->start = a.offsets[a.sequences], at->row = (index - before) * ROWS;
+        if (at->start < 0 || at->start > a.tokens) return kNone;
+        at->len = static_cast<int32_t>(a.tokens - at->start);
+        return at->row < at->len ? kRest : kNone;
+      }
+    }
+  }
+  at->row = (a.causal && !first_most ? tiles - 1 - tile : tile) * ROWS;
+  return kSequence;
+}
+
+__device__ inline float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ inline float other_half(float v) { return __shfl_xor(v, 32); }
+
+__device__ inline bool special(uint16_t, uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+__device__ inline bool special(float, uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
+
+// What differs by type.  A part is 16 bytes of a row, a lane's share of a contraction over elements: half h of
+// the lanes has elements 16 c + 8 h.. of a bf16 row in part c, which is one instruction, and elements h * D / 2 + 4 c.. of an
+// fp32 row, which is four.
+template <class T, int D>
+struct Kind;
+
+template <int D>
+struct Kind<uint16_t, D> {
+  static constexpr int kParts = D / 16;
+  static constexpr int kPitch = D <= 64 ? 128 : 256;  // bytes from row to row in LDS
+  // 16-byte piece c of row r lies in place c ^ mixed(r): 16 lanes that read one piece of 16 rows then touch all 64 banks
+  // once, and so do 16 that read four neighbouring pieces of four rows.
+  __device__ static int mixed(int r) { return kPitch == 128 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3); }
+  __device__ static int piece_at(int row, int piece) { return row * kPitch + ((piece ^ mixed(row)) << 4); }
+  __device__ static int part_at(int row, int c, int h) { return piece_at(row, 2 * c + h); }
+  __device__ static int part_element(int c, int h) { return 16 * c + 8 * h; }
+  __device__ static f16v multiply(u4 a, u4 b, f16v c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bhalf8, a), __builtin_bit_cast(bhalf8, b), c, 0, 0, 0);
+  }
+  __device__ static float dot(u4 a, u4 b) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sum = fmaf(__builtin_bit_cast(float, a[i] << 16), __builtin_bit_cast(float, b[i] << 16), sum);
+      sum = fmaf(__builtin_bit_cast(float, a[i] & 0xffff0000u), __builtin_bit_cast(float, b[i] & 0xffff0000u), sum);
+    }
+    return sum;
+  }
+  // Values of C as a right operand: of each half of the 32 rows, rounded to nearest even.
+  struct Right {
+    bhalf8 of[2];
+    __device__ explicit Right(const f16v& v) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) of[j][i] = static_cast<__bf16>(v[8 * j + i]);
+    }
+  };
+  // Columns 32 b.. of rows 16 j.. as a left operand: two transposed reads of four rows each.
+  __device__ static bhalf8 turned(const char* tile, int row, int b, int j) {
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int r = row + 16 * j + 4 * h + ((lane & 15) >> 2), piece = 4 * b + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    const int in = (lane & 1) * 8;
+    const half4 x = product::read_turned(tile + piece_at(r, piece) + in), y = product::read_turned(tile + piece_at(r + 8, piece) + in);
+    return __builtin_bit_cast(bhalf8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  // acc += (columns 32 b.. of 32 rows)^T right
+  __device__ static void gather(const char* tile, int row, int b, const Right& right, f16v& acc) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(tile, row, b, j), right.of[j], acc, 0, 0, 0);
+  }
+  // The same where rows may hold what is no number, which counts only in columns where `seen` is not zero.
+  __device__ static void gather_seen(const char* tile, int row, int b, const Right& right, const Right& seen, f16v& acc) {
+    f16v count = {};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const u4 words = __builtin_bit_cast(u4, turned(tile, row, b, j));
+      u4 clean, odd;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w = words[i], lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0;
+        clean[i] = w & ~(lo | hi);
+        odd[i] = 0x3f803f80u & (lo | hi);  // ones
+      }
+      acc = multiply(clean, __builtin_bit_cast(u4, right.of[j]), acc);
+      count = multiply(odd, __builtin_bit_cast(u4, seen.of[j]), count);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = count[r] > 0.0f ? __builtin_nanf("") : acc[r];
+  }
+  // Four neighbouring elements of a row.
+  __device__ static void put(uint16_t* p, float a, float b, float c, float d) {
+    typedef us4 us4_any __attribute__((aligned(2)));
+    *(us4_any*)p = us4{to_bf16(a), to_bf16(b), to_bf16(c), to_bf16(d)};
+  }
+};
+
+template <int D>
+struct Kind<float, D> {
+  static constexpr int kParts = D / 8;
+  static constexpr int kPitch = D * 4 + 16;
+  __device__ static int piece_at(int row, int piece) { return row * kPitch + piece * 16; }
+  __device__ static int part_at(int row, int c, int h) { return row * kPitch + h * (D * 2) + c * 16; }
+  __device__ static int part_element(int c, int h) { return h * (D / 2) + 4 * c; }
+  __device__ static f16v multiply(u4 a, u4 b, f16v c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = a[i], y = b[i];
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y), c, 0, 0, 0);
+    }
+    return c;
+  }
+  __device__ static float dot(u4 a, u4 b) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = a[i], y = b[i];
+      sum = fmaf(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y), sum);
+    }
+    return sum;
+  }
+  struct Right {
+    f16v of;
+    __device__ explicit Right(const f16v& v) : of(v) {}
+  };
+  __device__ static float turned(const char* tile, int row, int b, int r) {
+    const int lane = threadIdx.x & 63;
+    return *(const float*)(tile + (row + 8 * (r / 4) + 4 * (lane >> 5) + r % 4) * kPitch + (32 * b + (lane & 31)) * 4);
+  }
+  __device__ static void gather(const char* tile, int row, int b, const Right& right, f16v& acc) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(turned(tile, row, b, r), right.of[r], acc, 0, 0, 0);
+  }
+  __device__ static void gather_seen(const char* tile, int row, int b, const Right& right, const Right& seen, f16v& acc) {
+    f16v count = {};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float v = turned(tile, row, b, r);
+      const bool odd = special(0.0f, __builtin_bit_cast(uint32_t, v));
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(odd ? 0.0f : v, right.of[r], acc, 0, 0, 0);
+      count = __builtin_amdgcn_mfma_f32_32x32x2f32(odd ? 1.0f : 0.0f, seen.of[r], count, 0, 0, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = count[r] > 0.0f ? __builtin_nanf("") : acc[r];
+  }
+  __device__ static void put(float* p, float a, float b, float c, float d) { *(f4v_any*)p = f4v{a, b, c, d}; }
+};
+
+// ROWS rows of a head on their way to LDS: loaded while the tile before is worked on, written after it.  Rows from `len`
+// on and elements from `dim` on are zeros.
+template <class T, int D, int ROWS, int THREADS>
+struct Stage {
+  using K = Kind<T, D>;
+  static constexpr int kPieces = D * sizeof(T) / 16;  // a row
+  static constexpr int kEach = ROWS * kPieces / THREADS;
+  static constexpr int kBytes = ROWS * K::kPitch;
+  static_assert(ROWS * kPieces % THREADS == 0, "every thread has as many pieces");
+  u4 v[kEach];
+  // p: row 0 of the sequence
+  __device__ void load(const T* p, int64_t stride, int row, int len, int dim) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int id = threadIdx.x + i * THREADS, r = row + id / kPieces, c = id % kPieces * int(16 / sizeof(T));
+      v[i] = r < len && c < dim ? *(const u4_any*)(p + r * stride + c) : u4{0, 0, 0, 0};
+    }
+  }
+  __device__ void store(char* lds) const {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int id = threadIdx.x + i * THREADS;
+      *(u4*)(lds + K::piece_at(id / kPieces, id % kPieces)) = v[i];
+    }
+  }
+  __device__ bool any_special() const {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t w = v[i][k];
+        any |= special(T(0), w);
+      }
+    return any;
+  }
+};
+
+// A lane's parts of one row, from memory: row `r` of the sequence, or zeros.
+template <class T, int D>
+__device__ inline void own_row(const T* p, int64_t stride, int r, bool there, int dim, u4 (&parts)[Kind<T, D>::kParts]) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int c = 0; c < Kind<T, D>::kParts; ++c) {
+    const int e = Kind<T, D>::part_element(c, h);
+    parts[c] = there && e < dim ? *(const u4_any*)(p + r * stride + e) : u4{0, 0, 0, 0};
+  }
+}
+
+// C of 32 rows of a tile and the wavefront's columns.
+template <class T, int D>
+__device__ inline f16v scores(const char* tile, int row, const u4 (&own)[Kind<T, D>::kParts], f16v c) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < Kind<T, D>::kParts; ++i)
+    c = Kind<T, D>::multiply(*(const u4*)(tile + Kind<T, D>::part_at(row + (lane & 31), i, lane >> 5)), own[i], c);
+  return c;
+}
+
+// The row (of 32) that value r of C belongs to in this lane.
+__device__ inline int row_in(int r) { return 8 * (r / 4) + 4 * ((threadIdx.x & 63) >> 5) + r % 4; }
+
+// Sums over columns 32 b.. of a row: the lane's elements, times `factor`, rounded once.
+template <class T, int D>
+__device__ inline void put_row(T* row, const f16v (&acc)[D / 32], float factor, int dim) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      if (32 * b + 8 * g < dim)
+        Kind<T, D>::put(row + 32 * b + 8 * g + 4 * h, acc[b][4 * g] * factor, acc[b][4 * g + 1] * factor, acc[b][4 * g + 2] * factor,
+                        acc[b][4 * g + 3] * factor);
+}
+
+// Zeros in the tile's rows.
+template <int ROWS, class T>
+__device__ inline void zero_rows(T* p, int64_t stride, const Place& at, int dim) {
+  for (int i = threadIdx.x; i < ROWS * dim; i += blockDim.x)
+    if (at.row + i / dim < at.len) p[(at.row + i / dim) * stride + i % dim] = T(0);
+}
+
+}  // namespace attention
+}  // namespace daso
