@@ -10,11 +10,17 @@ straight into its flat gradient buffer.  Then the node averages its replicas and
 on the embedding, the output projection and the norms, MuonStep on the hidden matrices.  Every few batches the nodes exchange
 `wire`, and a batch later global_merge takes the copies in.
 
+    python -m workloads.language_model --heads 4 --kv-heads 2 --clip 1
+
+gives each block causal attention in front of its two products (head_norm_rotary and packed_attention, each row of a batch
+a sequence), and clips the replicas' mean gradient before the step (clip_gradients).
+
 The tokens are drawn from a Markov chain whose entropy is the least loss that a model can reach."""
 from __future__ import annotations
 
 import argparse
-from typing import Dict, List, Tuple
+import math
+from typing import Dict, List, Optional, Tuple
 
 import torch
 
@@ -26,18 +32,25 @@ ALIGN = 64  # elements: every tensor of the flat buffers starts on 128 bytes of 
 class Layout:
     """Where the model's tensors lie in a flat buffer: first what SGD steps, then the hidden matrices."""
 
-    def __init__(self, vocab: int, d: int, blocks: int):
+    def __init__(self, vocab: int, d: int, blocks: int, heads: int = 0, kv_heads: int = 0):
         self.vocab, self.d, self.blocks = vocab, d, blocks
+        self.heads, self.kv_heads = heads, kv_heads or heads
+        self.dim = d // heads if heads else 0  # of a head
         shapes = [("embedding", (vocab, d)), ("output", (vocab, d)), ("norm.weight", (d,)), ("norm.bias", (d,))]
         for b in range(blocks):
             shapes += [(f"{b}.norm.weight", (d,)), (f"{b}.norm.bias", (d,))]
+            if heads:
+                shapes += [(f"{b}.seen.norm.weight", (d,)), (f"{b}.seen.norm.bias", (d,)), (f"{b}.q.norm.weight", (self.dim,)),
+                           (f"{b}.k.norm.weight", (self.dim,))]
         hidden = []
         for b in range(blocks):
+            if heads:
+                hidden += [(f"{b}.qkv", ((heads + 2 * self.kv_heads) * self.dim, d)), (f"{b}.join", (d, heads * self.dim))]
             hidden += [(f"{b}.up", (4 * d, d)), (f"{b}.down", (d, 4 * d))]
         self.spans: Dict[str, Tuple[int, Tuple[int, ...]]] = {}
         at = 0
         for name, shape in shapes + hidden:
-            if name == "0.up":
+            if hidden and name == hidden[0][0]:
                 self.rest = at  # elements before the hidden matrices
             self.spans[name] = (at, shape)
             size = shape[0] * (shape[1] if len(shape) > 1 else 1)
@@ -64,16 +77,57 @@ class Layout:
         return flat.to(device)
 
 
+class Sequences:
+    """Where a replica's tokens lie in their sequences: what its attention needs of a batch."""
+
+    def __init__(self, lay: Layout, rows: int, length: int, device="cuda"):
+        self.offsets = torch.arange(rows + 1, device=device) * length
+        self.positions = torch.arange(length, device=device).repeat(rows)
+        self.frequencies = daso.rotary_frequencies(lay.dim, device=device)
+
+
+def _parts(lay: Layout, qkv: torch.Tensor):
+    """The heads of queries, keys and values in the rows of their joint projection."""
+    return qkv.view(-1, lay.heads + 2 * lay.kv_heads, lay.dim).split((lay.heads, lay.kv_heads, lay.kv_heads), 1)
+
+
+def _attend(lay: Layout, b: int, w, f, x: torch.Tensor, at: Sequences):
+    """x with what its tokens see, and what the way back needs."""
+    y, mean, rstd = daso.layer_norm(x, f(f"{b}.seen.norm.weight"), f(f"{b}.seen.norm.bias"))
+    q, k, v = _parts(lay, y @ w(f"{b}.qkv").t())
+    tq, tk = daso.head_norm_rotary(q, k, at.positions, at.frequencies, f(f"{b}.q.norm.weight"), f(f"{b}.k.norm.weight"))
+    out, lse = daso.packed_attention(tq, tk, v, at.offsets)
+    return x + out.flatten(1) @ w(f"{b}.join").t(), (x, y, mean, rstd, q, k, v, tq, tk, out, lse)
+
+
+def _attend_backward(lay: Layout, b: int, w, f, g, dx: torch.Tensor, kept: tuple, at: Sequences) -> torch.Tensor:
+    x, y, mean, rstd, q, k, v, tq, tk, out, lse = kept
+    g(f"{b}.join").copy_(dx.t() @ out.flatten(1))
+    dqkv = torch.empty(len(x), (lay.heads + 2 * lay.kv_heads) * lay.dim, dtype=x.dtype, device=x.device)
+    dq, dk, dv = _parts(lay, dqkv)
+    daso.packed_attention_backward((dx @ w(f"{b}.join")).view_as(out), tq, tk, v, out, lse, at.offsets, dq=dq, dk=dk, dv=dv)
+    daso.head_norm_rotary_backward(dq, dk, q, k, at.positions, at.frequencies, f(f"{b}.q.norm.weight"), f(f"{b}.k.norm.weight"),
+                                   dq=dq, dk=dk, dq_weight=g(f"{b}.q.norm.weight"), dk_weight=g(f"{b}.k.norm.weight"))
+    g(f"{b}.qkv").copy_(dqkv.t() @ y)
+    dn, _, _ = daso.layer_norm_backward(dqkv @ w(f"{b}.qkv"), x, f(f"{b}.seen.norm.weight"), mean, rstd,
+                                        dweight=g(f"{b}.seen.norm.weight"), dbias=g(f"{b}.seen.norm.bias"))
+    return dx + dn
+
+
 def gradients(lay: Layout, params: torch.Tensor, wire: torch.Tensor, tokens: torch.Tensor, targets: torch.Tensor,
-              grad: torch.Tensor) -> torch.Tensor:
-    """One replica's pass: the tokens' losses, and their mean's gradient into `grad` (all of it but the padding)."""
+              grad: torch.Tensor, at: Optional[Sequences] = None) -> torch.Tensor:
+    """One replica's pass: the tokens' losses, and their mean's gradient into `grad` (all of it but the padding).  A model with
+    heads needs `at`."""
     w, f, g = (lambda k: lay.view(wire, k)), (lambda k: lay.view(params, k)), (lambda k: lay.view(grad, k))
     x = w("embedding")[tokens]
     kept: List[tuple] = []
     for b in range(lay.blocks):
+        seen = None
+        if lay.heads:
+            x, seen = _attend(lay, b, w, f, x, at)
         y, mean, rstd = daso.layer_norm(x, f(f"{b}.norm.weight"), f(f"{b}.norm.bias"))
         a = torch.relu(y @ w(f"{b}.up").t())
-        kept.append((x, y, mean, rstd, a))
+        kept.append((x, y, mean, rstd, a, seen))
         x = x + a @ w(f"{b}.down").t()
     h, mean, rstd = daso.layer_norm(x, f("norm.weight"), f("norm.bias"))
     loss, lse = daso.linear_cross_entropy(h, w("output"), targets)
@@ -83,38 +137,44 @@ def gradients(lay: Layout, params: torch.Tensor, wire: torch.Tensor, tokens: tor
     dh, _ = daso.linear_cross_entropy_backward(dloss, h, w("output"), targets, lse, dweight=g("output"))
     dx, _, _ = daso.layer_norm_backward(dh, x, f("norm.weight"), mean, rstd, dweight=g("norm.weight"), dbias=g("norm.bias"))
     for b in reversed(range(lay.blocks)):
-        x, y, mean, rstd, a = kept[b]
+        x, y, mean, rstd, a, seen = kept[b]
         g(f"{b}.down").copy_(dx.t() @ a)
         da = (dx @ w(f"{b}.down")) * (a > 0)
         g(f"{b}.up").copy_(da.t() @ y)
         dn, _, _ = daso.layer_norm_backward(da @ w(f"{b}.up"), x, f(f"{b}.norm.weight"), mean, rstd,
                                             dweight=g(f"{b}.norm.weight"), dbias=g(f"{b}.norm.bias"))
         dx = dx + dn
+        if lay.heads:
+            dx = _attend_backward(lay, b, w, f, g, dx, seen, at)
     g("embedding").zero_().index_add_(0, tokens, dx.float())
     return loss
 
 
 class Node:
-    """A node's buffers, and its step over g replica gradients."""
+    """A node's buffers, and its step over g replica gradients, whose mean's norm is at most `clip` unless that is 0."""
 
-    def __init__(self, lay: Layout, seed: int, g: int = 2, lr: float = 1.0, hidden_lr: float = 0.02):
-        self.lay = lay
+    def __init__(self, lay: Layout, seed: int, g: int = 2, lr: float = 1.0, hidden_lr: float = 0.02, clip: float = 0.0):
+        self.lay, self.clip = lay, clip
         self.params = lay.init(seed, "cuda")
         self.momentum = torch.zeros(lay.n, device="cuda")
         self.wire = torch.empty(lay.n, dtype=torch.bfloat16, device="cuda")
         self.grads = [torch.zeros(lay.n, device="cuda") for _ in range(g)]
         daso.pack_bf16(self.params, self.wire)
         k = lay.rest
-        self._rest = daso.FusedStep([t[:k] for t in self.grads], self.params[:k], self.momentum[:k], [], [(0, k, 0)], lr=lr,
+        self._tensors = sorted((start, math.prod(shape)) for start, shape in lay.spans.values())
+        stepped = self.grads[:1] if clip else self.grads  # clipping leaves the mean in the first replica's buffer
+        self._rest = daso.FusedStep([t[:k] for t in stepped], self.params[:k], self.momentum[:k], [], [(0, k, 0)], lr=lr,
                                     mu=0.9, wire=self.wire[:k])
-        self._hidden = daso.MuonStep(self.grads, self.params, self.momentum, lay.matrices, lr=hidden_lr, wire=self.wire)
+        self._hidden = daso.MuonStep(stepped, self.params, self.momentum, lay.matrices, lr=hidden_lr, wire=self.wire)
 
-    def step(self, tokens: List[torch.Tensor], targets: List[torch.Tensor]) -> torch.Tensor:
+    def step(self, tokens: List[torch.Tensor], targets: List[torch.Tensor], at: Optional[Sequences] = None) -> torch.Tensor:
         """One batch, a part of it for each replica; the replicas' mean losses."""
         means = []
         for grad, x, t in zip(self.grads, tokens, targets):
-            loss = gradients(self.lay, self.params, self.wire, x, t, grad)
+            loss = gradients(self.lay, self.params, self.wire, x, t, grad, at)
             means.append(loss.sum() / (t != -100).sum().clamp(min=1))
+        if self.clip:
+            daso.clip_gradients(self.grads, self.clip, self._tensors)
         self._rest()
         self._hidden()
         return torch.stack(means)
@@ -146,18 +206,20 @@ class Chain:
 
 
 def train(steps: int = 60, nodes: int = 2, g: int = 2, vocab: int = 1000, d: int = 256, blocks: int = 2, rows: int = 16,
-          length: int = 64, every: int = 4, S: int = 1, seed: int = 0, tell=None) -> Tuple[List[float], float, List[Node]]:
+          length: int = 64, every: int = 4, S: int = 1, seed: int = 0, heads: int = 0, kv_heads: int = 0, clip: float = 0.0,
+          tell=None) -> Tuple[List[float], float, List[Node]]:
     """The mean loss of each batch, the chain's entropy and the nodes, which after the last batch hold one state."""
-    lay, chain = Layout(vocab, d, blocks), Chain(vocab, seed)
+    lay, chain = Layout(vocab, d, blocks, heads, kv_heads), Chain(vocab, seed)
+    at = Sequences(lay, rows, length) if heads else None
     gen = torch.Generator("cuda").manual_seed(seed + 1)
-    cluster = [Node(lay, seed, g) for _ in range(nodes)]
+    cluster = [Node(lay, seed, g, clip=clip) for _ in range(nodes)]
     sent: Dict[int, List[torch.Tensor]] = {}
     losses: List[float] = []
     for t in range(steps):
         means = []
         for node in cluster:
             parts = [chain.sample(rows, length, gen) for _ in range(g)]
-            means.append(node.step([p[:, :-1].reshape(-1) for p in parts], [p[:, 1:].reshape(-1) for p in parts]))
+            means.append(node.step([p[:, :-1].reshape(-1) for p in parts], [p[:, 1:].reshape(-1) for p in parts], at))
         if t - S in sent:
             copies = sent.pop(t - S)
             for node in cluster:
@@ -181,13 +243,16 @@ def main() -> None:
     ap.add_argument("--vocab", type=int, default=1000)
     ap.add_argument("--features", type=int, default=256)
     ap.add_argument("--blocks", type=int, default=2)
+    ap.add_argument("--heads", type=int, default=0, help="attention heads (0: no attention)")
+    ap.add_argument("--kv-heads", type=int, default=0, help="heads of keys and values (0: as many)")
+    ap.add_argument("--clip", type=float, default=0.0, help="largest norm of the averaged gradient (0: any)")
     a = ap.parse_args()
 
     def tell(t, loss):
         if t % 10 == 9 or t == 0:
             print(f"batch {t + 1:4d}  loss {loss:.4f}", flush=True)
 
-    losses, entropy, _ = train(a.steps, a.nodes, a.replicas, a.vocab, a.features, a.blocks, tell=tell)
+    losses, entropy, _ = train(a.steps, a.nodes, a.replicas, a.vocab, a.features, a.blocks, heads=a.heads, kv_heads=a.kv_heads, clip=a.clip, tell=tell)
     print(f"loss {losses[0]:.4f} to {losses[-1]:.4f}; the chain's entropy is {entropy:.4f}")
 
 
