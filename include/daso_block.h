@@ -78,7 +78,7 @@ int daso_head_norm_rotary_backward(const daso_rotary_args* args, hipStream_t str
  * each token i and head h, over the tokens j of i's sequence (with DASO_ATTENTION_CAUSAL those up to i),
  * with the key head h * kv_heads / heads:
  *     z_j = scale * q_i . k_j,  lse = log sum exp z_j,  out = sum exp(z_j - lse) v_j
- * Nothing of a token that i does not see counts, whatever it holds.  Sums and statistics are in 32 bits; with
+ * Token strides are at most 2 * DASO_MAX_SIDE.  Nothing of a token that i does not see counts, whatever it holds.  Sums and statistics are in 32 bits; with
  * bf16 operands exp(z - max) is rounded to bf16 for its product with v.  offsets ascend from 0; a pair
  * that does not, or that passes `tokens`, is taken as an empty sequence.  The rows of tokens in no
  * sequence are not written but where a flag asks for zeros.  An infinite or NaN v_j may give NaN where the formula gives an infinity. */

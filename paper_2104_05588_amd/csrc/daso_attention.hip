@@ -17,6 +17,15 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 constexpr int kThreads = 256, kWaves = 4, kOwn = kWaves * 32;  // rows of a workgroup
+constexpr float kGrowth = 10.0f;
+constexpr int kPairs = 512;  // units that make pairs worth while: two workgroups a CU
+// Wavefronts a SIMD that the registers are dealt for.
+template <class T, int D>
+constexpr int kForwardPerSimd = sizeof(T) == 2 && D <= 64 ? 3 : sizeof(T) == 2 || D < 128 ? 2 : 1;
+template <class T, int D>
+constexpr int kQueryPerSimd = sizeof(T) == 2 ? (D <= 32 ? 3 : D <= 96 ? 2 : 1) : D <= 64 ? 2 : 1;
+template <class T, int D>
+constexpr int kKeyPerSimd = sizeof(T) == 2 ? (D <= 64 ? 2 : 1) : D <= 32 ? 2 : 1;
 template <class T>
 constexpr int kTile = sizeof(T) == 2 ? 64 : 32;  // rows of a tile in LDS
 
@@ -26,126 +35,137 @@ __device__ inline const T* head_of(const Rows& r, int64_t start, int head) {
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads) void forward_kernel(Attention a) {
+__device__ inline void forward_tile(const Attention& a, const Place& at, char (&lds)[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes]) {
   using K = Kind<T, D>;
   constexpr int kKeys = kTile<T>, kSubs = kKeys / 32;
   using S = Stage<T, D, kKeys, kThreads>;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][S::kBytes];
-  __shared__ int odd;  // a tile that not all rows see holds values that are no numbers
-  Place at;
-  const Found found = place_of<kOwn>(a, a.heads, false, &at);
-  if (found == kNone) return;
-  if (found == kRest) {
-    if (!a.zero_q) return;
-    zero_rows<kOwn>((T*)head_of<T>(a.out, at.start, at.head), a.out.token, at, a.dim);
-    zero_rows<kOwn>(a.lse + at.head * a.tokens + at.start, 1, at, 1);
-    return;
-  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
   const T *k = head_of<T>(a.k, at.start, at.head / a.share), *v = head_of<T>(a.v, at.start, at.head / a.share);
   u4 q[K::kParts];
-  own_row<T, D>(head_of<T>(a.q, at.start, at.head), a.q.token, mine, mine < at.len, a.dim, q);
+  own_row<kOwn, T, D>(head_of<T>(a.q, at.start, at.head), a.q.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, q);
   const int last = a.causal ? min(mine, at.len - 1) : at.len - 1;  // key that the lane's query sees
   const int keys = a.causal ? min(at.len, at.row + kOwn) : at.len;
-  const int wave_keys = a.causal ? min(at.len, first + 32) : at.len;
-  const int all_see = a.causal ? min(at.len, first + 1) : at.len;  // keys below are seen by the whole wavefront
-  const int checked = a.causal ? at.row : at.len;  // keys from here on are not seen by all of the workgroup
+  const int whole = (a.causal ? min(at.len, at.row + 1) : at.len) / kKeys * kKeys;  // keys below are seen by all queries
   f16v acc[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; ++b) acc[b] = (f16v)0.0f;
-  float top = -INFINITY, sum = 0.0f;  // of z log2 e; the lane's keys' share of the sum
-  if (threadIdx.x == 0) odd = 0;
-  S ks, vs;
-  const auto fetch = [&](int key) { ks.load(k, a.k.token, key, at.len, a.dim), vs.load(v, a.v.token, key, at.len, a.dim); };
-  const auto keep = [&](int key, int buffer) {
-    ks.store(lds[buffer][0]), vs.store(lds[buffer][1]);
-    if (key + kKeys > checked && vs.any_special()) odd = 1;
-  };
-  fetch(0);
-  __syncthreads();
-  keep(0, 0);
-  __syncthreads();
-  for (int key = 0, buffer = 0; key < keys; key += kKeys, buffer ^= 1) {
-    const bool more = key + kKeys < keys;
-    if (more) fetch(key + kKeys);
-    if (key < wave_keys) {
-      f16v z[kSubs];
+  // The exponents' base, of z log2 e, and the lane's keys' share of the sum.  The base follows the maximum only where that
+  // has grown by more than 2^kGrowth, which the sums have room for.
+  float top = -INFINITY, base = 0.0f, sum = 0.0f;
+  S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
+  const auto fetch = [&](int key) { ks.load(key, at.len), vs.load(key, at.len); };
+  const auto keep = [&](int buffer) { ks.store(lds[buffer][0]), vs.store(lds[buffer][1]); };
+  // The base for the scores of 32 keys, and their powers in place of them.
+  const auto raise = [&](const f16v& z) {
+    float most = z[0];
 #pragma unroll
-      for (int s = 0; s < kSubs; ++s) z[s] = scores<T, D>(lds[buffer][0], s * 32, q, (f16v)0.0f);
-      if (key + kKeys > all_see)
-#pragma unroll
-        for (int s = 0; s < kSubs; ++s)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) z[s][r] = key + s * 32 + row_in(r) <= last ? z[s][r] : -INFINITY;
-      float most = z[0][0];
-#pragma unroll
-      for (int s = 0; s < kSubs; ++s)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) most = fmaxf(most, z[s][r]);
-      most = fmaxf(top, fmaxf(most, other_half(most)) * a.scale2);
-      const float base = most == -INFINITY ? 0.0f : most;  // where nothing counts yet
-      const float alpha = exp2_fast(top - base);
-      top = most;
+    for (int r = 1; r < 16; ++r) most = fmaxf(most, z[r]);
+    most = halves_max(most) * a.scale2;
+    const bool grown = most > top + kGrowth;  // (a row of its own: nothing that other rows hold changes its bits)
+    if (__any(grown)) {
+      const float alpha = grown ? exp2_fast(top - most) : 1.0f;
+      top = grown ? most : top, base = grown ? most : base;
       sum *= alpha;
 #pragma unroll
       for (int b = 0; b < D / 32; ++b) acc[b] *= alpha;
-#pragma unroll
-      for (int s = 0; s < kSubs; ++s) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          z[s][r] = exp2_fast(fmaf(z[s][r], a.scale2, -base));
-          sum += z[s][r];
-        }
-        const typename K::Right p(z[s]);
-        if (odd != 0 && key + kKeys > all_see) {
-          f16v see;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) see[r] = key + s * 32 + row_in(r) <= last ? 1.0f : 0.0f;
-          const typename K::Right seen(see);
-#pragma unroll
-          for (int b = 0; b < D / 32; ++b) K::gather_seen(lds[buffer][1], s * 32, b, p, seen, acc[b]);
-        } else {
-#pragma unroll
-          for (int b = 0; b < D / 32; ++b) K::gather(lds[buffer][1], s * 32, b, p, acc[b]);
-        }
-      }
     }
-    if (more) keep(key + kKeys, buffer ^ 1);
+  };
+  const auto soften = [&](f16v& z) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -base));
+    sum += sum_of(z);
+  };
+  const auto step = [&](int buffer) {
+    f16v z = scores<T, D>(lds[buffer][0], 0, q, (f16v)0.0f);
+#pragma unroll
+    for (int s = 0; s < kSubs; ++s) {
+      raise(z);
+      f16v next;
+      if (s + 1 < kSubs) next = scores<T, D>(lds[buffer][0], (s + 1) * 32, q, (f16v)0.0f);
+      soften(z);
+      const typename K::Right p(z);
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b) K::gather(lds[buffer][1], s * 32, b, p, acc[b]);
+      z = next;
+    }
+  };
+  // The same for keys of which each query sees its own.
+  const auto step_part = [&](int key, int buffer) {
+#pragma unroll 1
+    for (int s = 0; s < kSubs; ++s) {
+      if (a.causal && key + s * 32 >= first + 32) break;
+      f16v z = scores<T, D>(lds[buffer][0], s * 32, q, (f16v)0.0f);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z[r] = key + s * 32 + row_in(r) <= last ? z[r] : -INFINITY;
+      raise(z);
+      soften(z);
+      const typename K::Right p(z);
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b)
+        K::template gather_part<1>(lds[buffer][1], s * 32, b, p, last - key, acc[b]);
+    }
+  };
+  fetch(0);
+  __syncthreads();
+  keep(0);
+  __syncthreads();
+  int key = 0, buffer = 0;
+  for (; key < whole; key += kKeys, buffer ^= 1) {
+    const bool more = key + kKeys < keys;
+    if (more) fetch(key + kKeys);
+    step(buffer);
+    if (more) keep(buffer ^ 1);
     __syncthreads();
   }
-  sum += other_half(sum);
+  for (; key < keys; key += kKeys, buffer ^= 1) {
+    const bool more = key + kKeys < keys;
+    if (more) fetch(key + kKeys);
+    step_part(key, buffer);
+    if (more) keep(buffer ^ 1);
+    __syncthreads();
+  }
+  sum = halves_sum(sum);
   if (mine >= at.len) return;
   put_row<T, D>((T*)head_of<T>(a.out, at.start, at.head) + mine * a.out.token, acc, 1.0f / sum, a.dim);
-  if (lane < 32) a.lse[at.head * a.tokens + at.start + mine] = (top + log2f(sum)) * kLn2;
+  if (lane < 32) a.lse[at.head * a.tokens + at.start + mine] = (base + log2f(sum)) * kLn2;
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads) void query_kernel(Attention a) {
+__global__ __launch_bounds__(kThreads, (kForwardPerSimd<T, D>)) void forward_kernel(Attention a) {
+  __shared__ __attribute__((aligned(16))) char lds[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes];
+  Place at;
+  const Found found = place_of<kOwn>(a, a.heads, &at);
+  if (found == kNone) return;
+  for (int t = 0; t < 2 && at.turn<kOwn>(a, t, true); ++t) {
+    if (found == kSequence) {
+      forward_tile<T, D>(a, at, lds);
+      __syncthreads();
+      continue;
+    }
+    if (!a.zero_q) return;
+    zero_rows<kOwn>((T*)head_of<T>(a.out, at.start, at.head), a.out.token, at, a.dim);
+    zero_rows<kOwn>(a.lse + at.head * a.tokens + at.start, 1, at, 1);
+  }
+}
+
+template <class T, int D>
+__device__ inline void query_tile(const Attention& a, const Place& at, char (&lds)[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes]) {
   using K = Kind<T, D>;
   constexpr int kKeys = kTile<T>, kSubs = kKeys / 32;
   using S = Stage<T, D, kKeys, kThreads>;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][S::kBytes];
-  __shared__ int odd;
-  Place at;
-  const Found found = place_of<kOwn>(a, a.heads, false, &at);
-  if (found == kNone) return;
-  if (found == kRest) {
-    if (a.zero_q) zero_rows<kOwn>((T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, at, a.dim);
-    return;
-  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
   const bool there = mine < at.len;
   const T *k = head_of<T>(a.k, at.start, at.head / a.share), *v = head_of<T>(a.v, at.start, at.head / a.share);
   u4 q[K::kParts], g[K::kParts];
-  own_row<T, D>(head_of<T>(a.q, at.start, at.head), a.q.token, mine, there, a.dim, q);
-  own_row<T, D>(head_of<T>(a.dout, at.start, at.head), a.dout.token, mine, there, a.dim, g);
+  own_row<kOwn, T, D>(head_of<T>(a.q, at.start, at.head), a.q.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, q);
+  own_row<kOwn, T, D>(head_of<T>(a.dout, at.start, at.head), a.dout.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, g);
   float delta = 0.0f;
   {
     u4 o[K::kParts];
-    own_row<T, D>(head_of<T>(a.out, at.start, at.head), a.out.token, mine, there, a.dim, o);
+    own_row<kOwn, T, D>(head_of<T>(a.out, at.start, at.head), a.out.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, o);
 #pragma unroll
     for (int c = 0; c < K::kParts; ++c) delta += K::dot(g[c], o[c]);
-    delta += other_half(delta);
+    delta = halves_sum(delta);
   }
   const int64_t stat = at.head * a.tokens + at.start + mine;
   const float lse2 = there ? a.lse[stat] * kLog2e : INFINITY;
@@ -154,20 +174,15 @@ __global__ __launch_bounds__(kThreads) void query_kernel(Attention a) {
   const int keys = a.causal ? min(at.len, at.row + kOwn) : at.len;
   const int wave_keys = a.causal ? min(at.len, first + 32) : at.len;
   const int all_see = a.causal ? min(at.len, first + 1) : at.len;
-  const int checked = a.causal ? at.row : at.len;
   f16v acc[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; ++b) acc[b] = (f16v)0.0f;
-  if (threadIdx.x == 0) odd = 0;
-  S ks, vs;
-  const auto fetch = [&](int key) { ks.load(k, a.k.token, key, at.len, a.dim), vs.load(v, a.v.token, key, at.len, a.dim); };
-  const auto keep = [&](int key, int buffer) {
-    ks.store(lds[buffer][0]), vs.store(lds[buffer][1]);
-    if (key + kKeys > checked && ks.any_special()) odd = 1;
-  };
+  S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
+  const auto fetch = [&](int key) { ks.load(key, at.len), vs.load(key, at.len); };
+  const auto keep = [&](int buffer) { ks.store(lds[buffer][0]), vs.store(lds[buffer][1]); };
   fetch(0);
   __syncthreads();
-  keep(0, 0);
+  keep(0);
   __syncthreads();
   for (int key = 0, buffer = 0; key < keys; key += kKeys, buffer ^= 1) {
     const bool more = key + kKeys < keys;
@@ -184,60 +199,62 @@ __global__ __launch_bounds__(kThreads) void query_kernel(Attention a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) z[r] = key + s * 32 + row_in(r) <= last ? z[r] : 0.0f;
         const typename K::Right ds(z);
-        if (odd != 0 && part) {
-          f16v see;
+        if (part) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) see[r] = key + s * 32 + row_in(r) <= last ? 1.0f : 0.0f;
-          const typename K::Right seen(see);
-#pragma unroll
-          for (int b = 0; b < D / 32; ++b) K::gather_seen(lds[buffer][0], s * 32, b, ds, seen, acc[b]);
+          for (int b = 0; b < D / 32; ++b)
+            K::template gather_part<1>(lds[buffer][0], s * 32, b, ds, last - key, acc[b]);
         } else {
 #pragma unroll
           for (int b = 0; b < D / 32; ++b) K::gather(lds[buffer][0], s * 32, b, ds, acc[b]);
         }
       }
     }
-    if (more) keep(key + kKeys, buffer ^ 1);
+    if (more) keep(buffer ^ 1);
     __syncthreads();
   }
   if (there) put_row<T, D>((T*)head_of<T>(a.dq, at.start, at.head) + mine * a.dq.token, acc, a.scale, a.dim);
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads) void key_kernel(Attention a) {
+__global__ __launch_bounds__(kThreads, (kQueryPerSimd<T, D>)) void query_kernel(Attention a) {
+  __shared__ __attribute__((aligned(16))) char lds[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes];
+  Place at;
+  const Found found = place_of<kOwn>(a, a.heads, &at);
+  if (found == kNone) return;
+  for (int t = 0; t < 2 && at.turn<kOwn>(a, t, true); ++t) {
+    if (found == kSequence) {
+      query_tile<T, D>(a, at, lds);
+      __syncthreads();
+      continue;
+    }
+    if (a.zero_q) zero_rows<kOwn>((T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, at, a.dim);
+  }
+}
+
+template <class T, int D>
+__device__ inline void key_tile(const Attention& a, const Place& at, char (&lds)[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes],
+                                float (&stats)[2][2][kTile<T>]) {
   using K = Kind<T, D>;
   constexpr int kQueries = kTile<T>, kSubs = kQueries / 32;
   using S = Stage<T, D, kQueries, kThreads>;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][S::kBytes];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][kQueries];
-  __shared__ int odd;
-  Place at;
-  const Found found = place_of<kOwn>(a, a.kv_heads, true, &at);
-  if (found == kNone) return;
-  if (found == kRest) {
-    if (a.zero_k) zero_rows<kOwn>((T*)head_of<T>(a.dk, at.start, at.head), a.dk.token, at, a.dim);
-    if (a.zero_v) zero_rows<kOwn>((T*)head_of<T>(a.dv, at.start, at.head), a.dv.token, at, a.dim);
-    return;
-  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
   const bool there = mine < at.len;
   u4 k[K::kParts], v[K::kParts];
-  own_row<T, D>(head_of<T>(a.k, at.start, at.head), a.k.token, mine, there, a.dim, k);
-  own_row<T, D>(head_of<T>(a.v, at.start, at.head), a.v.token, mine, there, a.dim, v);
+  own_row<kOwn, T, D>(head_of<T>(a.k, at.start, at.head), a.k.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, k);
+  own_row<kOwn, T, D>(head_of<T>(a.v, at.start, at.head), a.v.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, v);
   f16v dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; ++b) dk[b] = dv[b] = (f16v)0.0f;
-  if (threadIdx.x == 0) odd = 0;
   // the queries that see a key of the workgroup, head by head
   const int from = a.causal ? at.row / kQueries * kQueries : 0;
   const int tiles = (at.len - from + kQueries - 1) / kQueries, steps = tiles * a.share;
   const int whole = a.causal ? first + 31 : 0;  // queries from here on see all keys of the wavefront
-  S qs, gs;
+  S qs((const T*)nullptr, a.q.token, a.dim), gs((const T*)nullptr, a.dout.token, a.dim);
   float stat = 0.0f;
   const auto fetch = [&](int step) {
     const int head = at.head * a.share + step / tiles, row = from + step % tiles * kQueries;
-    qs.load(head_of<T>(a.q, at.start, head), a.q.token, row, at.len, a.dim);
-    gs.load(head_of<T>(a.dout, at.start, head), a.dout.token, row, at.len, a.dim);
+    qs.p = head_of<T>(a.q, at.start, head), gs.p = head_of<T>(a.dout, at.start, head);
+    qs.load(row, at.len), gs.load(row, at.len);
     if (threadIdx.x < 2 * kQueries) {
       const int r = row + threadIdx.x % kQueries;
       const int64_t i = head * a.tokens + at.start + r;
@@ -245,14 +262,13 @@ __global__ __launch_bounds__(kThreads) void key_kernel(Attention a) {
       else stat = r < at.len ? -a.delta[i] : 0.0f;
     }
   };
-  const auto keep = [&](int step, int buffer) {
+  const auto keep = [&](int buffer) {
     qs.store(lds[buffer][0]), gs.store(lds[buffer][1]);
     if (threadIdx.x < 2 * kQueries) stats[buffer][threadIdx.x / kQueries][threadIdx.x % kQueries] = stat;
-    if (a.causal && from + step % tiles * kQueries < at.row + kOwn && (qs.any_special() || gs.any_special())) odd = 1;
   };
   fetch(0);
   __syncthreads();
-  keep(0, 0);
+  keep(0);
   __syncthreads();
   for (int step = 0, buffer = 0; step < steps; ++step, buffer ^= 1) {
     const bool more = step + 1 < steps;
@@ -285,15 +301,12 @@ __global__ __launch_bounds__(kThreads) void key_kernel(Attention a) {
             z[r] = sees ? z[r] : 0.0f, dp[r] = sees ? dp[r] : 0.0f;
           }
         const typename K::Right p(z), ds(dp);
-        if (odd != 0 && part) {
-          f16v see;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) see[r] = row + s * 32 + row_in(r) >= mine ? 1.0f : 0.0f;  // (rows that are not there are zeros)
-          const typename K::Right seen(see);
+        if (part) {
+          const int limit = row - mine;  // (rows that are not there are zeros)
 #pragma unroll
           for (int b = 0; b < D / 32; ++b) {
-            K::gather_seen(lds[buffer][1], s * 32, b, p, seen, dv[b]);
-            K::gather_seen(lds[buffer][0], s * 32, b, ds, seen, dk[b]);
+            K::template gather_part<-1>(lds[buffer][1], s * 32, b, p, limit, dv[b]);
+            K::template gather_part<-1>(lds[buffer][0], s * 32, b, ds, limit, dk[b]);
           }
         } else {
 #pragma unroll
@@ -304,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void key_kernel(Attention a) {
         }
       }
     }
-    if (more) keep(step + 1, buffer ^ 1);
+    if (more) keep(buffer ^ 1);
     __syncthreads();
   }
   if (!there) return;
@@ -312,13 +325,40 @@ __global__ __launch_bounds__(kThreads) void key_kernel(Attention a) {
   put_row<T, D>((T*)head_of<T>(a.dv, at.start, at.head) + mine * a.dv.token, dv, 1.0f, a.dim);
 }
 
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, (kKeyPerSimd<T, D>)) void key_kernel(Attention a) {
+  __shared__ __attribute__((aligned(16))) char lds[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes];
+  __shared__ __attribute__((aligned(16))) float stats[2][2][kTile<T>];
+  Place at;
+  const Found found = place_of<kOwn>(a, a.kv_heads, &at);
+  if (found == kNone) return;
+  for (int t = 0; t < 2 && at.turn<kOwn>(a, t, false); ++t) {
+    if (found == kSequence) {
+      key_tile<T, D>(a, at, lds, stats);
+      __syncthreads();
+      continue;
+    }
+    if (a.zero_k) zero_rows<kOwn>((T*)head_of<T>(a.dk, at.start, at.head), a.dk.token, at, a.dim);
+    if (a.zero_v) zero_rows<kOwn>((T*)head_of<T>(a.dv, at.start, at.head), a.dv.token, at, a.dim);
+  }
+}
+
 // ------------------------------------------------------------------------- host
+// The units of a head, at most, and whether they are pairs of tiles.
+Attention dealt(Attention a, int heads) {
+  const int64_t tiles = (a.tokens + kOwn - 1) / kOwn;
+  a.pairs = a.causal && tiles * heads / 2 >= kPairs;
+  const int rows = a.pairs ? 2 * kOwn : kOwn;
+  a.units = static_cast<int32_t>(a.offsets != nullptr ? a.tokens / rows + a.sequences + 1 : (a.tokens + rows - 1) / rows);
+  return a;
+}
 template <class T, int D>
 hipError_t queue(const Attention& a, bool backward, hipStream_t stream) {
-  const dim3 block(kThreads), queries(static_cast<uint32_t>(a.tiles * a.heads)), keys(static_cast<uint32_t>(a.tiles * a.kv_heads));
-  if (!backward) return launch(&forward_kernel<T, D>, queries, block, stream, a);
-  const hipError_t err = launch(&query_kernel<T, D>, queries, block, stream, a);
-  return err == hipSuccess ? launch(&key_kernel<T, D>, keys, block, stream, a) : err;
+  const Attention q = dealt(a, a.heads), k = dealt(a, a.kv_heads);
+  const dim3 block(kThreads), queries(static_cast<uint32_t>(q.units * q.heads)), keys(static_cast<uint32_t>(k.units * k.kv_heads));
+  if (!backward) return launch(&forward_kernel<T, D>, queries, block, stream, q);
+  const hipError_t err = launch(&query_kernel<T, D>, queries, block, stream, q);
+  return err == hipSuccess ? launch(&key_kernel<T, D>, keys, block, stream, k) : err;
 }
 template <class T>
 hipError_t queue(const Attention& a, bool backward, hipStream_t stream) {
@@ -331,13 +371,13 @@ hipError_t queue(const Attention& a, bool backward, hipStream_t stream) {
 size_t backward_bytes(const daso_attention_args& s) { return static_cast<size_t>(s.tokens) * size_t(s.heads) * sizeof(float); }
 
 int run(const daso_attention_args& s, bool backward, hipStream_t stream) {
-  const auto rows = [](const daso_heads& h) { return Rows{h.data, h.token_stride, h.head_stride}; };
+  // (of a single token the distance to the next may be anything)
+  const auto rows = [&s](const daso_heads& h) { return Rows{h.data, s.tokens > 1 ? h.token_stride : s.dim, h.head_stride}; };
   Attention a;
   a.tokens = s.tokens, a.offsets = s.offsets, a.sequences = s.sequences, a.heads = s.heads, a.kv_heads = s.kv_heads;
   a.share = s.heads / s.kv_heads, a.dim = s.dim, a.causal = (s.flags & DASO_ATTENTION_CAUSAL) != 0;
   a.zero_q = (s.flags & DASO_ATTENTION_ZERO_Q) != 0, a.zero_k = (s.flags & DASO_ATTENTION_ZERO_K) != 0;
   a.zero_v = (s.flags & DASO_ATTENTION_ZERO_V) != 0;
-  a.tiles = static_cast<int32_t>(s.offsets != nullptr ? s.tokens / kOwn + s.sequences + 1 : (s.tokens + kOwn - 1) / kOwn);
   a.scale = s.scale, a.scale2 = s.scale * kLog2e;
   a.q = rows(s.q), a.k = rows(s.k), a.v = rows(s.v), a.out = rows(s.out), a.dout = rows(s.dout);
   a.dq = rows(s.dq), a.dk = rows(s.dk), a.dv = rows(s.dv), a.lse = s.lse, a.delta = static_cast<float*>(s.workspace);

@@ -35,16 +35,34 @@ struct Attention {
   const int64_t* offsets;  // or null: one sequence of all tokens
   int32_t sequences, heads, kv_heads, share;  // share: query heads of a key head
   int32_t dim, causal, zero_q, zero_k, zero_v;  // zeros behind the last sequence
-  int32_t tiles;  // of a head, at most
+  int32_t units, pairs;  // units: of a head, at most
   float scale, scale2;  // scale2 = scale * log2 e
   Rows q, k, v, out, dout, dq, dk, dv;
   float *lse, *delta;  // heads x tokens
 };
 
-// The tile of a workgroup: rows `row`.. of the sequence of `len` tokens from `start` on.
+// What a workgroup works on: a unit of the sequence of `len` tokens from `start` on, which is a tile of rows or, with
+// Attention::pairs, the unit-th tile from either end (which together are as much work as any other two such tiles).
 struct Place {
   int64_t start;
-  int32_t len, row, head;
+  int32_t len, head;
+  int32_t unit, tiles;  // tiles: of the sequence
+  int32_t row;          // of the tile in hand
+  // Takes up tile 0 or 1 of the unit; false where there is none.
+  template <int ROWS>
+  __device__ bool turn(const Attention& a, int t, bool last_first) {
+    int tile = unit;
+    if (a.pairs) {
+      if (t == 1 && tiles - 1 - unit == unit) return false;
+      if ((t == 0) == last_first) tile = tiles - 1 - unit;
+    } else if (t == 1) {
+      return false;
+    } else if (a.causal && last_first) {
+      tile = tiles - 1 - unit;
+    }
+    row = tile * ROWS;
+    return true;
+  }
 };
 
 __device__ inline int64_t read_lane(int64_t v, int lane) {
@@ -54,69 +72,101 @@ __device__ inline int64_t read_lane(int64_t v, int lane) {
 }
 
 // Workgroups of neighbouring numbers go to the eight XCDs in turn.  Where the heads can be dealt to them evenly each XCD
-// takes whole heads one after the other, whose keys then stay in its L2; else the heads' tiles are dealt in turn.
-// Of a causal sequence the tiles that are the most work come first.
-// first_most: the first tiles of a sequence are the most work (keys), else the last ones (queries).
-// kRest: a tile of the rows behind the last sequence.
+// takes whole heads one after the other, whose keys then stay in its L2; else the heads' units are dealt in turn.
+// kRest: a unit of the rows behind the last sequence.
 enum Found { kNone, kSequence, kRest };
 template <int ROWS>
-__device__ inline Found place_of(const Attention& a, int heads, bool first_most, Place* at) {
+__device__ inline Found place_of(const Attention& a, int heads, Place* at) {
   const int id = blockIdx.x;
   int index;
   if (heads % 8 == 0) {
     const int in = id >> 3, each = heads >> 3;
-    at->head = (id & 7) * each + in / a.tiles;
-    index = in % a.tiles;
+    at->head = (id & 7) * each + in / a.units;
+    index = in % a.units;
   } else {
     at->head = id % heads;
     index = id / heads;
   }
-  int tile, tiles;
+  const auto units_of = [&](int tiles) { return a.pairs ? (tiles + 1) >> 1 : tiles; };
   if (a.offsets == nullptr) {
     at->start = 0, at->len = static_cast<int32_t>(a.tokens);
-    tile = index, tiles = (at->len + ROWS - 1) / ROWS;
-    if (tile >= tiles) return kNone;
-  } else {
-    const int lane = threadIdx.x & 63;
-    int before = 0, base = 0;
-    for (;;) {
-      int64_t from = 0, to = 0;
-      if (base + lane < a.sequences) from = a.offsets[base + lane], to = a.offsets[base + lane + 1];
-      if (!(from >= 0 && to >= from && to <= a.tokens)) to = from = 0;
-      const int mine = (static_cast<int>(to - from) + ROWS - 1) / ROWS;
-      int upto = mine;
-#pragma unroll
-      for (int s = 1; s < 64; s <<= 1) {
-        const int v = __shfl_up(upto, s);
-        if (lane >= s) upto += v;
-      }
-      const uint64_t found = __ballot(before + upto > index);
-      if (found != 0) {
-        const int l = __builtin_ctzll(found);
-        at->start = read_lane(from, l), at->len = static_cast<int32_t>(read_lane(to, l) - at->start);
-        tiles = __builtin_amdgcn_readlane(mine, l);
-        tile = index - before - (__builtin_amdgcn_readlane(upto, l) - tiles);
-        break;
-      }
-      before += __builtin_amdgcn_readlane(upto, 63);
-      base += 64;
-      if (base >= a.sequences) {
-        at->start = a.offsets[a.sequences], at->row = (index - before) * ROWS;
-        if (at->start < 0 || at->start > a.tokens) return kNone;
-        at->len = static_cast<int32_t>(a.tokens - at->start);
-        return at->row < at->len ? kRest : kNone;
-      }
-    }
+    at->unit = index, at->tiles = (at->len + ROWS - 1) / ROWS;
+    return index < units_of(at->tiles) ? kSequence : kNone;
   }
-  at->row = (a.causal && !first_most ? tiles - 1 - tile : tile) * ROWS;
-  return kSequence;
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int base = 0; base < a.sequences; base += 64) {
+    int64_t from = 0, to = 0;
+    if (base + lane < a.sequences) from = a.offsets[base + lane], to = a.offsets[base + lane + 1];
+    if (!(from >= 0 && to >= from && to <= a.tokens)) to = from = 0;
+    const int mine = units_of((static_cast<int>(to - from) + ROWS - 1) / ROWS);
+    int upto = mine;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int v = __shfl_up(upto, s);
+      if (lane >= s) upto += v;
+    }
+    const uint64_t found = __ballot(before + upto > index);
+    if (found != 0) {
+      const int l = __builtin_ctzll(found);
+      at->start = read_lane(from, l), at->len = static_cast<int32_t>(read_lane(to, l) - at->start);
+      at->tiles = (at->len + ROWS - 1) / ROWS;
+      at->unit = index - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
+      return kSequence;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  at->start = a.offsets[a.sequences];
+  if (at->start < 0 || at->start > a.tokens) return kNone;
+  at->len = static_cast<int32_t>(a.tokens - at->start);
+  at->unit = index - before, at->tiles = (at->len + ROWS - 1) / ROWS;
+  return at->unit < units_of(at->tiles) ? kRest : kNone;
 }
 
 __device__ inline float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
-__device__ inline float other_half(float v) { return __shfl_xor(v, 32); }
+// The value in this lane and in the one 32 away, in the same order in both.
+struct Halves {
+  float lower, upper;
+  __device__ explicit Halves(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    lower = __builtin_bit_cast(float, static_cast<uint32_t>(both[0])), upper = __builtin_bit_cast(float, static_cast<uint32_t>(both[1]));
+  }
+};
+__device__ inline float halves_sum(float v) {
+  const Halves h(v);
+  return h.lower + h.upper;
+}
+__device__ inline float halves_max(float v) {
+  const Halves h(v);
+  return fmaxf(h.lower, h.upper);
+}
 
 __device__ inline bool special(uint16_t, uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 __device__ inline bool special(float, uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
+
+// A tree, so that no add waits for more than three others.
+__device__ inline float sum_of(const f16v& v) {
+  float s[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = (v[i] + v[4 + i]) + (v[8 + i] + v[12 + i]);
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// The row (of 32) that value r of C belongs to in this lane.
+__device__ inline int row_in(int r) { return 8 * (r / 4) + 4 * ((threadIdx.x & 63) >> 5) + r % 4; }
+
+// NaN in values of C whose column sees what is no number in the contraction: `least` is, in lane i % 32, the signed place
+// of row i's first such value (of the half of the contraction that the lane holds), `limit` the last one that the lane's column sees.
+__device__ inline void spoil(int least, int limit, f16v& acc) {
+  least = min(least, __shfl_xor(least, 32));
+  const bool upper = (threadIdx.x & 32) != 0;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int lo = __builtin_amdgcn_readlane(least, 8 * (r / 4) + r % 4), hi = __builtin_amdgcn_readlane(least, 8 * (r / 4) + 4 + r % 4);
+    acc[r] = (upper ? hi : lo) <= limit ? __builtin_nanf("") : acc[r];
+  }
+}
 
 // What differs by type.  A part is 16 bytes of a row, a lane's share of a contraction over elements: half h of
 // the lanes has elements 16 c + 8 h.. of a bf16 row in part c, which is one instruction, and elements h * D / 2 + 4 c.. of an
@@ -169,24 +219,37 @@ struct Kind<uint16_t, D> {
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(tile, row, b, j), right.of[j], acc, 0, 0, 0);
   }
-  // The same where rows may hold what is no number, which counts only in columns where `seen` is not zero.
-  __device__ static void gather_seen(const char* tile, int row, int b, const Right& right, const Right& seen, f16v& acc) {
-    f16v count = {};
+  // The same where a column sees row i only if SIGN * i <= limit: what is no number in a row counts only in columns that see it.
+  template <int SIGN>
+  __device__ static void gather_part(const char* tile, int row, int b, const Right& right, int limit, f16v& acc) {
+    bhalf8 left[2];
+    bool any = false;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const u4 words = __builtin_bit_cast(u4, turned(tile, row, b, j));
-      u4 clean, odd;
+      left[j] = turned(tile, row, b, j);
+      const u4 words = __builtin_bit_cast(u4, left[j]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t w = words[i], lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0;
-        clean[i] = w & ~(lo | hi);
-        odd[i] = 0x3f803f80u & (lo | hi);  // ones
+      for (int i = 0; i < 4; ++i) any |= special(uint16_t(0), words[i]);
+    }
+    int least = INT32_MAX;  // SIGN * row of the element's first such value
+    const bool odd = __any(any);
+    if (__builtin_expect(odd, 0)) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        u4 words = __builtin_bit_cast(u4, left[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = row + 16 * j + row_in(4 * (i / 2) + i % 2 * 2);
+          const uint32_t w = words[i];
+          if ((w & 0x7f80u) == 0x7f80u) words[i] &= 0xffff0000u, least = min(least, SIGN * r);
+          if ((w & 0x7f800000u) == 0x7f800000u) words[i] &= 0xffffu, least = min(least, SIGN * (r + 1));
+        }
+        left[j] = __builtin_bit_cast(bhalf8, words);
       }
-      acc = multiply(clean, __builtin_bit_cast(u4, right.of[j]), acc);
-      count = multiply(odd, __builtin_bit_cast(u4, seen.of[j]), count);
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = count[r] > 0.0f ? __builtin_nanf("") : acc[r];
+    for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(left[j], right.of[j], acc, 0, 0, 0);
+    if (__builtin_expect(odd, 0)) spoil(least, limit, acc);
   }
   // Four neighbouring elements of a row.
   __device__ static void put(uint16_t* p, float a, float b, float c, float d) {
@@ -231,20 +294,30 @@ struct Kind<float, D> {
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(turned(tile, row, b, r), right.of[r], acc, 0, 0, 0);
   }
-  __device__ static void gather_seen(const char* tile, int row, int b, const Right& right, const Right& seen, f16v& acc) {
-    f16v count = {};
+  template <int SIGN>
+  __device__ static void gather_part(const char* tile, int row, int b, const Right& right, int limit, f16v& acc) {
+    int least = INT32_MAX;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float v = turned(tile, row, b, r);
       const bool odd = special(0.0f, __builtin_bit_cast(uint32_t, v));
+      least = min(least, odd ? SIGN * (row + row_in(r)) : INT32_MAX);
       acc = __builtin_amdgcn_mfma_f32_32x32x2f32(odd ? 0.0f : v, right.of[r], acc, 0, 0, 0);
-      count = __builtin_amdgcn_mfma_f32_32x32x2f32(odd ? 1.0f : 0.0f, seen.of[r], count, 0, 0, 0);
     }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = count[r] > 0.0f ? __builtin_nanf("") : acc[r];
+    if (__builtin_expect(__any(least != INT32_MAX), 0)) spoil(least, limit, acc);
   }
   __device__ static void put(float* p, float a, float b, float c, float d) { *(f4v_any*)p = f4v{a, b, c, d}; }
 };
+
+// Rows `row`.. of a sequence of `len`, at most ROWS: p is its row 0.  Reads beyond them, and at kNowhere, give zeros.
+constexpr uint32_t kNowhere = 0x80000000u;
+template <int ROWS, class T>
+__device__ inline __amdgpu_buffer_rsrc_t window(const T* p, int64_t stride, int row, int len, int dim) {
+  const int rows = max(min(len - row, ROWS), 0);
+  const int bytes = rows == 0 ? 0 : ((rows - 1) * static_cast<int>(stride) + dim) * static_cast<int>(sizeof(T));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + row * stride), 0, bytes, 0x00027000);
+}
+__device__ inline u4 read16(__amdgpu_buffer_rsrc_t from, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, 0); }
 
 // ROWS rows of a head on their way to LDS: loaded while the tile before is worked on, written after it.  Rows from `len`
 // on and elements from `dim` on are zeros.
@@ -255,14 +328,22 @@ struct Stage {
   static constexpr int kEach = ROWS * kPieces / THREADS;
   static constexpr int kBytes = ROWS * K::kPitch;
   static_assert(ROWS * kPieces % THREADS == 0, "every thread has as many pieces");
+  const T* p;  // row 0 of the sequence
+  int64_t stride;
+  int dim;
+  uint32_t from[kEach];
   u4 v[kEach];
-  // p: row 0 of the sequence
-  __device__ void load(const T* p, int64_t stride, int row, int len, int dim) {
+  __device__ Stage(const T* p, int64_t stride, int dim) : p(p), stride(stride), dim(dim) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int id = threadIdx.x + i * THREADS, r = row + id / kPieces, c = id % kPieces * int(16 / sizeof(T));
-      v[i] = r < len && c < dim ? *(const u4_any*)(p + r * stride + c) : u4{0, 0, 0, 0};
+      const int id = threadIdx.x + i * THREADS, r = id / kPieces, c = id % kPieces * int(16 / sizeof(T));
+      from[i] = c < dim ? (r * static_cast<uint32_t>(stride) + c) * uint32_t(sizeof(T)) : kNowhere;
     }
+  }
+  __device__ void load(int row, int len) {
+    const __amdgpu_buffer_rsrc_t w = window<ROWS>(p, stride, row, len, dim);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) v[i] = read16(w, from[i]);
   }
   __device__ void store(char* lds) const {
 #pragma unroll
@@ -271,27 +352,17 @@ struct Stage {
       *(u4*)(lds + K::piece_at(id / kPieces, id % kPieces)) = v[i];
     }
   }
-  __device__ bool any_special() const {
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t w = v[i][k];
-        any |= special(T(0), w);
-      }
-    return any;
-  }
 };
 
-// A lane's parts of one row, from memory: row `r` of the sequence, or zeros.
-template <class T, int D>
-__device__ inline void own_row(const T* p, int64_t stride, int r, bool there, int dim, u4 (&parts)[Kind<T, D>::kParts]) {
+// A lane's parts of one of the ROWS rows of a workgroup: row + own of the sequence, or zeros.
+template <int ROWS, class T, int D>
+__device__ inline void own_row(const T* p, int64_t stride, int row, int own, int len, int dim, u4 (&parts)[Kind<T, D>::kParts]) {
   const int h = (threadIdx.x & 63) >> 5;
+  const __amdgpu_buffer_rsrc_t w = window<ROWS>(p, stride, row, len, dim);
 #pragma unroll
   for (int c = 0; c < Kind<T, D>::kParts; ++c) {
     const int e = Kind<T, D>::part_element(c, h);
-    parts[c] = there && e < dim ? *(const u4_any*)(p + r * stride + e) : u4{0, 0, 0, 0};
+    parts[c] = read16(w, e < dim ? (own * static_cast<uint32_t>(stride) + e) * uint32_t(sizeof(T)) : kNowhere);
   }
 }
 
@@ -304,9 +375,6 @@ __device__ inline f16v scores(const char* tile, int row, const u4 (&own)[Kind<T,
     c = Kind<T, D>::multiply(*(const u4*)(tile + Kind<T, D>::part_at(row + (lane & 31), i, lane >> 5)), own[i], c);
   return c;
 }
-
-// The row (of 32) that value r of C belongs to in this lane.
-__device__ inline int row_in(int r) { return 8 * (r / 4) + 4 * ((threadIdx.x & 63) >> 5) + r % 4; }
 
 // Sums over columns 32 b.. of a row: the lane's elements, times `factor`, rounded once.
 template <class T, int D>

@@ -115,7 +115,9 @@ int check_attention(const daso_attention_args& s, bool backward) {
   if (s.offsets == nullptr && s.sequences != 1) return DASO_EINVAL;
   const size_t e = bytes_of(s.type);
   Rows q, k, v, out, dout, dq, dk, dv;
-  const auto heads = [&](const daso_heads& h, int32_t count, Rows* to) { return rows_of_heads(h, s.tokens, count, s.dim, e, to); };
+  const auto heads = [&](const daso_heads& h, int32_t count, Rows* to) {
+    return (s.tokens <= 1 || h.token_stride <= kMaxTokenStride) && rows_of_heads(h, s.tokens, count, s.dim, e, to);
+  };
   if (!heads(s.q, s.heads, &q) || !heads(s.k, s.kv_heads, &k) || !heads(s.v, s.kv_heads, &v) || !heads(s.out, s.heads, &out))
     return DASO_EINVAL;
   const Rows at = line(s.offsets, int64_t(s.sequences) + 1, 8), lse = line(s.lse, s.tokens * s.heads, 4);

@@ -11,6 +11,11 @@
 namespace daso {
 namespace host {
 
+// The largest distance of two tokens' rows in an attention, in elements: the byte offsets of a workgroup's 128 rows stay
+// below 2^31.
+constexpr int64_t kMaxTokenStride = 2 * DASO_MAX_SIDE;
+static_assert(127 * kMaxTokenStride * 4 + DASO_MAX_HEAD_DIM * 4 < (int64_t(1) << 31), "offsets of 31 bits");
+
 int check_rotary_sizes(const daso_rotary_args& s);
 int check_rotary(const daso_rotary_args& s, bool backward);
 int check_attention_sizes(const daso_attention_args& s);

@@ -109,7 +109,7 @@ def test_attention_rejects(lib):
             (dict(tokens=1 << 24, heads=16, kv_heads=16), EINVAL), (dict(offsets=None), EINVAL), (dict(offsets=A + 20 * MB + 4), EALIGN),
             (dict(q=rows(None, 256, 64)), EINVAL), (dict(v=rows(None, 128, 64)), EINVAL), (dict(out=rows(None, 256, 64)), EINVAL),
             (dict(lse=None), EINVAL), (dict(lse=A + 21 * MB + 2), EALIGN), (dict(k=rows(A + MB + 1, 128, 64)), EALIGN),
-            (dict(k=rows(A + MB, 127, 64)), EINVAL), (dict(v=rows(A, 0, 64)), EINVAL), (dict(v=rows(A, 128, 0)), EINVAL),
+            (dict(k=rows(A + MB, 127, 64)), EINVAL), (dict(v=rows(A, 0, 64)), EINVAL), (dict(v=rows(A, 128, 0)), EINVAL), (dict(v=rows(A, (2 << 20) + 8, 64)), EINVAL),
             (dict(tokens=0, q=rows(None, 0, 0)), OK), (dict(sequences=0, offsets=None), OK)]
     both += [(dict(v=rows(A, s, 64)), EINVAL) for s in NEVER] + [(dict(out=rows(A + 3 * MB, 256, s)), EINVAL) for s in NEVER]
     forward = [(dict(out=rows(A, 256, 64)), EALIAS), (dict(out=rows(A + MB + 128, 256, 64)), EALIAS), (dict(lse=A + 3 * MB), EALIAS),

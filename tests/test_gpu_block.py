@@ -511,9 +511,9 @@ def test_calls_on_two_streams_at_once():
 
 
 def test_heads_in_a_far_part_of_a_long_buffer():
-    """Rows whose distance in elements passes 32 bits."""
+    """Rows whose distance from the first passes 32 bits, in elements and in bytes."""
     announce("far rows")
-    n, dim, apart = 130, 64, (1 << 25) + 8
+    n, dim, apart = 2100, 64, 2 << 20
     store = torch.empty(n * apart, dtype=BF16, device="cuda")
     far = [store[i * 128:].as_strided((n, 2, dim), (apart, dim, 1)) for i in range(3)]
     q, k, v, dout = attention_case(n, 2, 2, dim, BF16, 31)
