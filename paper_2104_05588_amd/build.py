@@ -24,7 +24,8 @@ CAPI_CLUSTER = os.path.join(PKG, "daso_cluster_capi")
 
 SOURCES = ["daso_kernels.hip", "daso_api.hip", "daso_host.cpp", "daso_schedule.cpp",
            "daso_train_host.cpp", "daso_norm.hip", "daso_loss.hip", "daso_muon.hip",
-           "daso_block_host.cpp", "daso_rotary.hip", "daso_attention.hip", "daso_clip.hip"]
+           "daso_block_host.cpp", "daso_rotary.hip", "daso_attention.hip",
+           "daso_attention_keys.hip", "daso_clip.hip"]
 # The bench's bandwidth-ceiling probes (the step's access pattern without its
 # arithmetic): a library of their own, outside the C ABI.
 PROBE_SOURCE = "daso_ceiling.hip"
@@ -41,6 +42,9 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument",
 ]
+# What a source is compiled with besides.  The attention's scores go from the matrix cores to vector instructions: their
+# sums are to lie in vector registers, also in kernels that need more registers than these.
+MORE_FLAGS = {"daso_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def hipcc() -> str:
@@ -69,7 +73,7 @@ def build(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory() as objs:
         def compiled(source: str) -> str:
             obj = os.path.join(objs, source + ".o")
-            _run([hipcc(), *compile_flags, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", obj], verbose)
+            _run([hipcc(), *compile_flags, *MORE_FLAGS.get(source, []), "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", obj], verbose)
             return obj
 
         # one source at a time is a minute, of which the step's kernels are the most

@@ -1,4 +1,4 @@
-// Attention over packed sequences, forward and backward (daso_block.h).
+// Attention over packed sequences, forward and the backward pass by queries (daso_block.h).
 //
 // Forward: a wavefront has 32 queries and walks over the keys it sees, with the running maximum and sum of the softmax.
 // Backward: two passes that each compute the scores again, so that no sum is added up across workgroups: one
@@ -14,26 +14,12 @@ namespace daso {
 namespace attention {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-constexpr int kThreads = 256, kWaves = 4, kOwn = kWaves * 32;  // rows of a workgroup
 constexpr float kGrowth = 10.0f;
-constexpr int kPairs = 512;  // units that make pairs worth while: two workgroups a CU
 // Wavefronts a SIMD that the registers are dealt for.
 template <class T, int D>
 constexpr int kForwardPerSimd = sizeof(T) == 2 && D <= 64 ? 3 : sizeof(T) == 2 || D < 128 ? 2 : 1;
 template <class T, int D>
-constexpr int kQueryPerSimd = sizeof(T) == 2 ? (D <= 32 ? 3 : D <= 96 ? 2 : 1) : D <= 64 ? 2 : 1;
-template <class T, int D>
-constexpr int kKeyPerSimd = sizeof(T) == 2 ? (D <= 64 ? 2 : 1) : D <= 32 ? 2 : 1;
-template <class T>
-constexpr int kTile = sizeof(T) == 2 ? 64 : 32;  // rows of a tile in LDS
-
-template <class T>
-__device__ inline const T* head_of(const Rows& r, int64_t start, int head) {
-  return (const T*)r.p + start * r.token + head * r.head;
-}
-
+constexpr int kQueryPerSimd = sizeof(T) == 2 ? (D <= 32 ? 3 : 2) : D <= 64 ? 2 : 1;
 template <class T, int D>
 __device__ inline void forward_tile(const Attention& a, const Place& at, char (&lds)[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes]) {
   using K = Kind<T, D>;
@@ -53,8 +39,8 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
   // has grown by more than 2^kGrowth, which the sums have room for.
   float top = -INFINITY, base = 0.0f, sum = 0.0f;
   S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
-  const auto fetch = [&](int key) { ks.load(key, at.len), vs.load(key, at.len); };
-  const auto keep = [&](int buffer) { ks.store(lds[buffer][0]), vs.store(lds[buffer][1]); };
+  // The next tile comes in two halves, its keys during the first half of this one and its values during the second.
+  const auto turn = [&](int key, int buffer) { ks.store(lds[buffer ^ 1][0]), vs.load(key + kKeys, at.len); };
   // The base for the scores of 32 keys, and their powers in place of them.
   const auto raise = [&](const f16v& z) {
     float most = z[0];
@@ -75,7 +61,7 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
     for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -base));
     sum += sum_of(z);
   };
-  const auto step = [&](int buffer) {
+  const auto step = [&](int key, int buffer) {
     f16v z = scores<T, D>(lds[buffer][0], 0, q, (f16v)0.0f);
 #pragma unroll
     for (int s = 0; s < kSubs; ++s) {
@@ -86,6 +72,7 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
       const typename K::Right p(z);
 #pragma unroll
       for (int b = 0; b < D / 32; ++b) K::gather(lds[buffer][1], s * 32, b, p, acc[b]);
+      if (s == (kSubs - 1) / 2) turn(key, buffer);
       z = next;
     }
   };
@@ -93,35 +80,38 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
   const auto step_part = [&](int key, int buffer) {
 #pragma unroll 1
     for (int s = 0; s < kSubs; ++s) {
-      if (a.causal && key + s * 32 >= first + 32) break;
+      const int from = key + s * 32;
+      if (from >= keys || (a.causal && from >= first + 32)) break;
       f16v z = scores<T, D>(lds[buffer][0], s * 32, q, (f16v)0.0f);
+      const bool part = from + 31 > (a.causal ? min(first, at.len - 1) : at.len - 1);
+      if (part)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) z[r] = key + s * 32 + row_in(r) <= last ? z[r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) z[r] = from + row_in(r) <= last ? z[r] : -INFINITY;
       raise(z);
       soften(z);
       const typename K::Right p(z);
 #pragma unroll
-      for (int b = 0; b < D / 32; ++b)
-        K::template gather_part<1>(lds[buffer][1], s * 32, b, p, last - key, acc[b]);
+      for (int b = 0; b < D / 32; ++b) {
+        if (part) K::template gather_part<1>(lds[buffer][1], s * 32, b, p, last - key, acc[b]);
+        else K::gather(lds[buffer][1], s * 32, b, p, acc[b]);
+      }
     }
   };
-  fetch(0);
-  __syncthreads();
-  keep(0);
+  ks.load(0, at.len), vs.load(0, at.len);
+  ks.store(lds[0][0]), vs.store(lds[0][1]);
   __syncthreads();
   int key = 0, buffer = 0;
   for (; key < whole; key += kKeys, buffer ^= 1) {
-    const bool more = key + kKeys < keys;
-    if (more) fetch(key + kKeys);
-    step(buffer);
-    if (more) keep(buffer ^ 1);
+    ks.load(key + kKeys, at.len);
+    step(key, buffer);
+    vs.store(lds[buffer ^ 1][1]);
     __syncthreads();
   }
   for (; key < keys; key += kKeys, buffer ^= 1) {
-    const bool more = key + kKeys < keys;
-    if (more) fetch(key + kKeys);
+    ks.load(key + kKeys, at.len);
     step_part(key, buffer);
-    if (more) keep(buffer ^ 1);
+    turn(key, buffer);
+    vs.store(lds[buffer ^ 1][1]);
     __syncthreads();
   }
   sum = halves_sum(sum);
@@ -131,21 +121,14 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, (kForwardPerSimd<T, D>)) void forward_kernel(Attention a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kForwardPerSimd<T, D>, kForwardPerSimd<T, D>))) void forward_kernel(Attention a) {
   __shared__ __attribute__((aligned(16))) char lds[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes];
   Place at;
-  const Found found = place_of<kOwn>(a, a.heads, &at);
-  if (found == kNone) return;
-  for (int t = 0; t < 2 && at.turn<kOwn>(a, t, true); ++t) {
-    if (found == kSequence) {
-      forward_tile<T, D>(a, at, lds);
-      __syncthreads();
-      continue;
-    }
-    if (!a.zero_q) return;
-    zero_rows<kOwn>((T*)head_of<T>(a.out, at.start, at.head), a.out.token, at, a.dim);
-    zero_rows<kOwn>(a.lse + at.head * a.tokens + at.start, 1, at, 1);
-  }
+  const Found found = place_of<kOwn, true>(a, a.heads, &at);
+  if (found == kSequence) return forward_tile<T, D>(a, at, lds);
+  if (found == kNone || !a.zero_q) return;
+  zero_rows<kOwn>((T*)head_of<T>(a.out, at.start, at.head), a.out.token, at, a.dim);
+  zero_rows<kOwn>(a.lse + at.head * a.tokens + at.start, 1, at, 1);
 }
 
 template <class T, int D>
@@ -172,193 +155,94 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
   if (there && lane < 32) a.delta[stat] = delta;
   const int last = a.causal ? min(mine, at.len - 1) : at.len - 1;
   const int keys = a.causal ? min(at.len, at.row + kOwn) : at.len;
-  const int wave_keys = a.causal ? min(at.len, first + 32) : at.len;
-  const int all_see = a.causal ? min(at.len, first + 1) : at.len;
+  const int whole = sizeof(T) == 2 ? (a.causal ? min(at.len, at.row + 1) : at.len) / kKeys * kKeys : 0;  // as in the forward pass
   f16v acc[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; ++b) acc[b] = (f16v)0.0f;
   S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
-  const auto fetch = [&](int key) { ks.load(key, at.len), vs.load(key, at.len); };
-  const auto keep = [&](int buffer) { ks.store(lds[buffer][0]), vs.store(lds[buffer][1]); };
-  fetch(0);
-  __syncthreads();
-  keep(0);
-  __syncthreads();
-  for (int key = 0, buffer = 0; key < keys; key += kKeys, buffer ^= 1) {
-    const bool more = key + kKeys < keys;
-    if (more) fetch(key + kKeys);
-    if (key < wave_keys) {
+  // The next tile in halves, as in the forward pass, where registers are short: 8192 x 16 x 128 in 730 us against 870 in one piece
+  // with one wavefront a SIMD.  Else in one, which has longer to come: 8192 x 16 x 64 in 419 us against 530.
+  constexpr bool kHalves = D > 96;
+  const auto fetch = [&](int key) {
+    ks.load(key, at.len);
+    if constexpr (!kHalves) vs.load(key, at.len);
+  };
+  const auto turn = [&](int key, int buffer) {
+    if constexpr (kHalves) ks.store(lds[buffer ^ 1][0]), vs.load(key + kKeys, at.len);
+  };
+  const auto keep = [&](int buffer) {
+    if constexpr (!kHalves) ks.store(lds[buffer][0]);
+    vs.store(lds[buffer][1]);
+  };
+  const auto step = [&](int key, int buffer) {
 #pragma unroll
-      for (int s = 0; s < kSubs; ++s) {
-        f16v z = scores<T, D>(lds[buffer][0], s * 32, q, (f16v)0.0f);
-        const f16v dp = scores<T, D>(lds[buffer][1], s * 32, g, (f16v)(-delta));
+    for (int s = 0; s < kSubs; ++s) {
+      f16v z = scores<T, D>(lds[buffer][0], s * 32, q, (f16v)0.0f);
+      const f16v dp = scores<T, D>(lds[buffer][1], s * 32, g, (f16v)(-delta));
 #pragma unroll
-        for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -lse2)) * dp[r];
-        const bool part = key + kKeys > all_see;
-        if (part)
+      for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -lse2)) * dp[r];
+      const typename K::Right ds(z);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) z[r] = key + s * 32 + row_in(r) <= last ? z[r] : 0.0f;
-        const typename K::Right ds(z);
-        if (part) {
+      for (int b = 0; b < D / 32; ++b) K::gather(lds[buffer][0], s * 32, b, ds, acc[b]);
+      if (s == (kSubs - 1) / 2) turn(key, buffer);
+    }
+  };
+  const auto step_part = [&](int key, int buffer) {
+#pragma unroll 1
+    for (int s = 0; s < kSubs; ++s) {
+      const int from = key + s * 32;
+      if (from >= keys || (a.causal && from >= first + 32)) break;
+      f16v z = scores<T, D>(lds[buffer][0], s * 32, q, (f16v)0.0f);
+      const f16v dp = scores<T, D>(lds[buffer][1], s * 32, g, (f16v)(-delta));
 #pragma unroll
-          for (int b = 0; b < D / 32; ++b)
-            K::template gather_part<1>(lds[buffer][0], s * 32, b, ds, last - key, acc[b]);
-        } else {
+      for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -lse2)) * dp[r];
+      const bool part = from + 31 > (a.causal ? min(first, at.len - 1) : at.len - 1);
+      if (part)
 #pragma unroll
-          for (int b = 0; b < D / 32; ++b) K::gather(lds[buffer][0], s * 32, b, ds, acc[b]);
-        }
+        for (int r = 0; r < 16; ++r) z[r] = from + row_in(r) <= last ? z[r] : 0.0f;
+      const typename K::Right ds(z);
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b) {
+        if (part) K::template gather_part<1>(lds[buffer][0], s * 32, b, ds, last - key, acc[b]);
+        else K::gather(lds[buffer][0], s * 32, b, ds, acc[b]);
       }
     }
-    if (more) keep(buffer ^ 1);
+  };
+  ks.load(0, at.len), vs.load(0, at.len);
+  ks.store(lds[0][0]), vs.store(lds[0][1]);
+  __syncthreads();
+  int key = 0, buffer = 0;
+  for (; key < whole; key += kKeys, buffer ^= 1) {
+    fetch(key + kKeys);
+    step(key, buffer);
+    keep(buffer ^ 1);
+    __syncthreads();
+  }
+  for (; key < keys; key += kKeys, buffer ^= 1) {
+    fetch(key + kKeys);
+    step_part(key, buffer);
+    turn(key, buffer);
+    keep(buffer ^ 1);
     __syncthreads();
   }
   if (there) put_row<T, D>((T*)head_of<T>(a.dq, at.start, at.head) + mine * a.dq.token, acc, a.scale, a.dim);
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, (kQueryPerSimd<T, D>)) void query_kernel(Attention a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kQueryPerSimd<T, D>, kQueryPerSimd<T, D>))) void query_kernel(Attention a) {
   __shared__ __attribute__((aligned(16))) char lds[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes];
   Place at;
-  const Found found = place_of<kOwn>(a, a.heads, &at);
-  if (found == kNone) return;
-  for (int t = 0; t < 2 && at.turn<kOwn>(a, t, true); ++t) {
-    if (found == kSequence) {
-      query_tile<T, D>(a, at, lds);
-      __syncthreads();
-      continue;
-    }
-    if (a.zero_q) zero_rows<kOwn>((T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, at, a.dim);
-  }
-}
-
-template <class T, int D>
-__device__ inline void key_tile(const Attention& a, const Place& at, char (&lds)[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes],
-                                float (&stats)[2][2][kTile<T>]) {
-  using K = Kind<T, D>;
-  constexpr int kQueries = kTile<T>, kSubs = kQueries / 32;
-  using S = Stage<T, D, kQueries, kThreads>;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
-  const bool there = mine < at.len;
-  u4 k[K::kParts], v[K::kParts];
-  own_row<kOwn, T, D>(head_of<T>(a.k, at.start, at.head), a.k.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, k);
-  own_row<kOwn, T, D>(head_of<T>(a.v, at.start, at.head), a.v.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, v);
-  f16v dk[D / 32], dv[D / 32];
-#pragma unroll
-  for (int b = 0; b < D / 32; ++b) dk[b] = dv[b] = (f16v)0.0f;
-  // the queries that see a key of the workgroup, head by head
-  const int from = a.causal ? at.row / kQueries * kQueries : 0;
-  const int tiles = (at.len - from + kQueries - 1) / kQueries, steps = tiles * a.share;
-  const int whole = a.causal ? first + 31 : 0;  // queries from here on see all keys of the wavefront
-  S qs((const T*)nullptr, a.q.token, a.dim), gs((const T*)nullptr, a.dout.token, a.dim);
-  float stat = 0.0f;
-  const auto fetch = [&](int step) {
-    const int head = at.head * a.share + step / tiles, row = from + step % tiles * kQueries;
-    qs.p = head_of<T>(a.q, at.start, head), gs.p = head_of<T>(a.dout, at.start, head);
-    qs.load(row, at.len), gs.load(row, at.len);
-    if (threadIdx.x < 2 * kQueries) {
-      const int r = row + threadIdx.x % kQueries;
-      const int64_t i = head * a.tokens + at.start + r;
-      if (threadIdx.x < kQueries) stat = r < at.len ? -a.lse[i] * kLog2e : -INFINITY;  // exp of rows that are not there is 0
-      else stat = r < at.len ? -a.delta[i] : 0.0f;
-    }
-  };
-  const auto keep = [&](int buffer) {
-    qs.store(lds[buffer][0]), gs.store(lds[buffer][1]);
-    if (threadIdx.x < 2 * kQueries) stats[buffer][threadIdx.x / kQueries][threadIdx.x % kQueries] = stat;
-  };
-  fetch(0);
-  __syncthreads();
-  keep(0);
-  __syncthreads();
-  for (int step = 0, buffer = 0; step < steps; ++step, buffer ^= 1) {
-    const bool more = step + 1 < steps;
-    if (more) fetch(step + 1);
-    const int row = from + step % tiles * kQueries;
-    if (!a.causal || row + kQueries > first) {
-#pragma unroll
-      for (int s = 0; s < kSubs; ++s) {
-        f16v lse, z, dp;
-        const int h = lane >> 5;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f4v x = *(const f4v*)&stats[buffer][0][s * 32 + 8 * g + 4 * h], y = *(const f4v*)&stats[buffer][1][s * 32 + 8 * g + 4 * h];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) lse[4 * g + i] = x[i], dp[4 * g + i] = y[i];
-        }
-        z = scores<T, D>(lds[buffer][0], s * 32, k, (f16v)0.0f);
-        dp = scores<T, D>(lds[buffer][1], s * 32, v, dp);
-        const bool part = row < whole || row + kQueries > at.len;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          z[r] = exp2_fast(fmaf(z[r], a.scale2, lse[r]));
-          dp[r] *= z[r];
-        }
-        if (part)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int i = row + s * 32 + row_in(r);
-            const bool sees = i < at.len && (!a.causal || i >= mine);
-            z[r] = sees ? z[r] : 0.0f, dp[r] = sees ? dp[r] : 0.0f;
-          }
-        const typename K::Right p(z), ds(dp);
-        if (part) {
-          const int limit = row - mine;  // (rows that are not there are zeros)
-#pragma unroll
-          for (int b = 0; b < D / 32; ++b) {
-            K::template gather_part<-1>(lds[buffer][1], s * 32, b, p, limit, dv[b]);
-            K::template gather_part<-1>(lds[buffer][0], s * 32, b, ds, limit, dk[b]);
-          }
-        } else {
-#pragma unroll
-          for (int b = 0; b < D / 32; ++b) {
-            K::gather(lds[buffer][1], s * 32, b, p, dv[b]);
-            K::gather(lds[buffer][0], s * 32, b, ds, dk[b]);
-          }
-        }
-      }
-    }
-    if (more) keep(buffer ^ 1);
-    __syncthreads();
-  }
-  if (!there) return;
-  put_row<T, D>((T*)head_of<T>(a.dk, at.start, at.head) + mine * a.dk.token, dk, a.scale, a.dim);
-  put_row<T, D>((T*)head_of<T>(a.dv, at.start, at.head) + mine * a.dv.token, dv, 1.0f, a.dim);
-}
-
-template <class T, int D>
-__global__ __launch_bounds__(kThreads, (kKeyPerSimd<T, D>)) void key_kernel(Attention a) {
-  __shared__ __attribute__((aligned(16))) char lds[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][kTile<T>];
-  Place at;
-  const Found found = place_of<kOwn>(a, a.kv_heads, &at);
-  if (found == kNone) return;
-  for (int t = 0; t < 2 && at.turn<kOwn>(a, t, false); ++t) {
-    if (found == kSequence) {
-      key_tile<T, D>(a, at, lds, stats);
-      __syncthreads();
-      continue;
-    }
-    if (a.zero_k) zero_rows<kOwn>((T*)head_of<T>(a.dk, at.start, at.head), a.dk.token, at, a.dim);
-    if (a.zero_v) zero_rows<kOwn>((T*)head_of<T>(a.dv, at.start, at.head), a.dv.token, at, a.dim);
-  }
+  const Found found = place_of<kOwn, true>(a, a.heads, &at);
+  if (found == kSequence) return query_tile<T, D>(a, at, lds);
+  if (found == kNone || !a.zero_q) return;
+  zero_rows<kOwn>((T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, at, a.dim);
 }
 
 // ------------------------------------------------------------------------- host
-// The units of a head, at most, and whether they are pairs of tiles.
-Attention dealt(Attention a, int heads) {
-  const int64_t tiles = (a.tokens + kOwn - 1) / kOwn;
-  a.pairs = a.causal && tiles * heads / 2 >= kPairs;
-  const int rows = a.pairs ? 2 * kOwn : kOwn;
-  a.units = static_cast<int32_t>(a.offsets != nullptr ? a.tokens / rows + a.sequences + 1 : (a.tokens + rows - 1) / rows);
-  return a;
-}
 template <class T, int D>
 hipError_t queue(const Attention& a, bool backward, hipStream_t stream) {
-  const Attention q = dealt(a, a.heads), k = dealt(a, a.kv_heads);
-  const dim3 block(kThreads), queries(static_cast<uint32_t>(q.units * q.heads)), keys(static_cast<uint32_t>(k.units * k.kv_heads));
-  if (!backward) return launch(&forward_kernel<T, D>, queries, block, stream, q);
-  const hipError_t err = launch(&query_kernel<T, D>, queries, block, stream, q);
-  return err == hipSuccess ? launch(&key_kernel<T, D>, keys, block, stream, k) : err;
+  const dim3 block(kThreads), queries(static_cast<uint32_t>(a.tiles * a.heads));
+  return backward ? launch(&query_kernel<T, D>, queries, block, stream, a) : launch(&forward_kernel<T, D>, queries, block, stream, a);
 }
 template <class T>
 hipError_t queue(const Attention& a, bool backward, hipStream_t stream) {
@@ -368,7 +252,14 @@ hipError_t queue(const Attention& a, bool backward, hipStream_t stream) {
   return queue<T, 128>(a, backward, stream);
 }
 
-size_t backward_bytes(const daso_attention_args& s) { return static_cast<size_t>(s.tokens) * size_t(s.heads) * sizeof(float); }
+// Of the workspace: delta, and the parts' sums of dk and dv.  (As many tiles as there may be: whether offsets are given does not
+// count.)
+size_t delta_bytes(const daso_attention_args& s) { return (size_t(s.tokens) * size_t(s.heads) * sizeof(float) + 255) / 256 * 256; }
+int32_t key_parts(const daso_attention_args& s) { return parts_of(s.tokens / kOwn + s.sequences + 1, s.kv_heads, s.heads / s.kv_heads); }
+size_t backward_bytes(const daso_attention_args& s) {
+  const size_t parts = size_t(key_parts(s));
+  return delta_bytes(s) + (parts > 1 ? parts * 2 * size_t(s.tokens) * size_t(s.kv_heads) * size_t(s.dim) * sizeof(float) : 0);
+}
 
 int run(const daso_attention_args& s, bool backward, hipStream_t stream) {
   // (of a single token the distance to the next may be anything)
@@ -378,10 +269,14 @@ int run(const daso_attention_args& s, bool backward, hipStream_t stream) {
   a.share = s.heads / s.kv_heads, a.dim = s.dim, a.causal = (s.flags & DASO_ATTENTION_CAUSAL) != 0;
   a.zero_q = (s.flags & DASO_ATTENTION_ZERO_Q) != 0, a.zero_k = (s.flags & DASO_ATTENTION_ZERO_K) != 0;
   a.zero_v = (s.flags & DASO_ATTENTION_ZERO_V) != 0;
+  a.tiles = tiles_of<kOwn>(a);
   a.scale = s.scale, a.scale2 = s.scale * kLog2e;
   a.q = rows(s.q), a.k = rows(s.k), a.v = rows(s.v), a.out = rows(s.out), a.dout = rows(s.dout);
   a.dq = rows(s.dq), a.dk = rows(s.dk), a.dv = rows(s.dv), a.lse = s.lse, a.delta = static_cast<float*>(s.workspace);
-  const hipError_t err = s.type == DASO_TYPE_BF16 ? queue<uint16_t>(a, backward, stream) : queue<float>(a, backward, stream);
+  a.parts = key_parts(s), a.partial = reinterpret_cast<float*>(static_cast<char*>(s.workspace) + (backward ? delta_bytes(s) : 0));
+  a.sorted = a.tiles * a.heads <= kFewTiles;
+  hipError_t err = s.type == DASO_TYPE_BF16 ? queue<uint16_t>(a, backward, stream) : queue<float>(a, backward, stream);
+  if (backward && err == hipSuccess) err = queue_keys(a, s.type, stream);
   return err == hipSuccess ? DASO_OK : DASO_EHIP;
 }
 

@@ -21,6 +21,12 @@ namespace attention {
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef u4 u4_any __attribute__((aligned(2)));
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+constexpr int kThreads = 256, kWaves = 4, kOwn = kWaves * 32;  // rows of a workgroup
+template <class T>
+constexpr int kTile = sizeof(T) == 2 ? 64 : 32;  // rows of a tile in LDS
+constexpr int kFewTiles = 2048;  // Attention::sorted: up to eight a CU
 using product::bhalf8;
 using product::half4;
 using product::half8;
@@ -35,34 +41,20 @@ struct Attention {
   const int64_t* offsets;  // or null: one sequence of all tokens
   int32_t sequences, heads, kv_heads, share;  // share: query heads of a key head
   int32_t dim, causal, zero_q, zero_k, zero_v;  // zeros behind the last sequence
-  int32_t units, pairs;  // units: of a head, at most
+  int32_t tiles, sorted;  // tiles: of a head, at most
   float scale, scale2;  // scale2 = scale * log2 e
   Rows q, k, v, out, dout, dq, dk, dv;
   float *lse, *delta;  // heads x tokens
+  // Parts that the query heads of a key head are taken in by the pass by keys, where its tiles are few: their sums of dk and
+  // dv, [part][dk, dv][token][key head][dim], are added by a kernel of their own.
+  int32_t parts;
+  float* partial;
 };
 
-// What a workgroup works on: a unit of the sequence of `len` tokens from `start` on, which is a tile of rows or, with
-// Attention::pairs, the unit-th tile from either end (which together are as much work as any other two such tiles).
+// What a workgroup works on: rows `row`.. of the sequence of `len` tokens from `start` on.
 struct Place {
   int64_t start;
-  int32_t len, head;
-  int32_t unit, tiles;  // tiles: of the sequence
-  int32_t row;          // of the tile in hand
-  // Takes up tile 0 or 1 of the unit; false where there is none.
-  template <int ROWS>
-  __device__ bool turn(const Attention& a, int t, bool last_first) {
-    int tile = unit;
-    if (a.pairs) {
-      if (t == 1 && tiles - 1 - unit == unit) return false;
-      if ((t == 0) == last_first) tile = tiles - 1 - unit;
-    } else if (t == 1) {
-      return false;
-    } else if (a.causal && last_first) {
-      tile = tiles - 1 - unit;
-    }
-    row = tile * ROWS;
-    return true;
-  }
+  int32_t len, row, head;
 };
 
 __device__ inline int64_t read_lane(int64_t v, int lane) {
@@ -71,27 +63,34 @@ __device__ inline int64_t read_lane(int64_t v, int lane) {
   return static_cast<int64_t>(uint64_t(hi) << 32 | lo);
 }
 
-// Workgroups of neighbouring numbers go to the eight XCDs in turn.  Where the heads can be dealt to them evenly each XCD
-// takes whole heads one after the other, whose keys then stay in its L2; else the heads' units are dealt in turn.
-// kRest: a unit of the rows behind the last sequence.
+constexpr int kSorted = 32;  // sequences, at most, whose tiles are taken in the order of their work
+
+// Workgroups of neighbouring numbers go to the eight XCDs in turn.  Where the heads can be dealt to them evenly an XCD takes
+// heads of its own, one after the other, so that their keys stay in its L2.  A causal sequence's tiles that are the most
+// work come first: the last ones (QUERIES) or the first ones (keys).  With Attention::sorted, for launches of few tiles a CU, all
+// tiles of the heads and of up to kSorted sequences come in the order of their work: 8 x 1024 tokens of 16 heads of 64 forward in
+// 38 us against 45, where 32 x 1024 tokens, whose keys do not fit the L2s together, would take 167 against 141.
+// kRest: a tile of the rows behind the last sequence.
 enum Found { kNone, kSequence, kRest };
-template <int ROWS>
+template <int ROWS, bool QUERIES>
 __device__ inline Found place_of(const Attention& a, int heads, Place* at) {
   const int id = blockIdx.x;
   int index;
   if (heads % 8 == 0) {
     const int in = id >> 3, each = heads >> 3;
-    at->head = (id & 7) * each + in / a.units;
-    index = in % a.units;
+    const int by = a.sorted ? each : a.tiles, rest = in % by;
+    at->head = (id & 7) * each + (a.sorted ? rest : in / by);
+    index = a.sorted ? in / by : rest;
   } else {
     at->head = id % heads;
     index = id / heads;
   }
-  const auto units_of = [&](int tiles) { return a.pairs ? (tiles + 1) >> 1 : tiles; };
+  const bool last_first = QUERIES && a.causal;
   if (a.offsets == nullptr) {
     at->start = 0, at->len = static_cast<int32_t>(a.tokens);
-    at->unit = index, at->tiles = (at->len + ROWS - 1) / ROWS;
-    return index < units_of(at->tiles) ? kSequence : kNone;
+    const int tiles = (at->len + ROWS - 1) / ROWS;
+    at->row = (last_first ? tiles - 1 - index : index) * ROWS;
+    return index < tiles ? kSequence : kNone;
   }
   const int lane = threadIdx.x & 63;
   int before = 0;
@@ -99,7 +98,38 @@ __device__ inline Found place_of(const Attention& a, int heads, Place* at) {
     int64_t from = 0, to = 0;
     if (base + lane < a.sequences) from = a.offsets[base + lane], to = a.offsets[base + lane + 1];
     if (!(from >= 0 && to >= from && to <= a.tokens)) to = from = 0;
-    const int mine = units_of((static_cast<int>(to - from) + ROWS - 1) / ROWS);
+    const int mine = (static_cast<int>(to - from) + ROWS - 1) / ROWS;
+    if (a.causal && a.sorted && a.sequences <= kSorted) {
+      // A tile's work is its place from the light end of its sequence, 1, 2, ..  more[j]: the tiles of more work than lane +
+      // 64 j.  The index-th tile is of the least work w that no more than index tiles exceed.
+      int more[4] = {0, 0, 0, 0}, all = 0;
+      bool small = true;
+      for (int s = 0; s < a.sequences; ++s) {
+        const int n = __builtin_amdgcn_readlane(mine, s);
+        small &= n < 256, all += n;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) more[j] += max(n - lane - 64 * j, 0);
+      }
+      if (small && index < all) {
+        int w = 0, above = 0;
+        bool found = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint64_t few = __ballot(more[j] <= index);
+          if (!found && few != 0) {
+            const int l = __builtin_ctzll(few);
+            w = 64 * j + l, above = __builtin_amdgcn_readlane(more[j], l), found = true;
+          }
+        }
+        // the (index - above)-th of the sequences that have such a tile
+        const uint64_t have = __ballot(mine >= w);
+        const int rank = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(have >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(have), 0));
+        const int l = __builtin_ctzll(__ballot(mine >= w && rank == index - above));
+        at->start = read_lane(from, l), at->len = static_cast<int32_t>(read_lane(to, l) - at->start);
+        at->row = (QUERIES ? w - 1 : __builtin_amdgcn_readlane(mine, l) - w) * ROWS;
+        return kSequence;
+      }
+    }
     int upto = mine;
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
@@ -108,10 +138,10 @@ __device__ inline Found place_of(const Attention& a, int heads, Place* at) {
     }
     const uint64_t found = __ballot(before + upto > index);
     if (found != 0) {
-      const int l = __builtin_ctzll(found);
+      const int l = __builtin_ctzll(found), tiles = __builtin_amdgcn_readlane(mine, l);
       at->start = read_lane(from, l), at->len = static_cast<int32_t>(read_lane(to, l) - at->start);
-      at->tiles = (at->len + ROWS - 1) / ROWS;
-      at->unit = index - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
+      const int tile = index - before - (__builtin_amdgcn_readlane(upto, l) - tiles);
+      at->row = (last_first ? tiles - 1 - tile : tile) * ROWS;
       return kSequence;
     }
     before += __builtin_amdgcn_readlane(upto, 63);
@@ -119,8 +149,8 @@ __device__ inline Found place_of(const Attention& a, int heads, Place* at) {
   at->start = a.offsets[a.sequences];
   if (at->start < 0 || at->start > a.tokens) return kNone;
   at->len = static_cast<int32_t>(a.tokens - at->start);
-  at->unit = index - before, at->tiles = (at->len + ROWS - 1) / ROWS;
-  return at->unit < units_of(at->tiles) ? kRest : kNone;
+  at->row = (index - before) * ROWS;
+  return at->row < at->len ? kRest : kNone;
 }
 
 __device__ inline float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -219,6 +249,18 @@ struct Kind<uint16_t, D> {
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(tile, row, b, j), right.of[j], acc, 0, 0, 0);
   }
+  // Columns 32 b.. of 32 rows, read ahead.
+  struct Left {
+    bhalf8 of[2];
+    __device__ void read(const char* tile, int row, int b) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) of[j] = turned(tile, row, b, j);
+    }
+  };
+  __device__ static void gather(const Left& left, const Right& right, f16v& acc) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(left.of[j], right.of[j], acc, 0, 0, 0);
+  }
   // The same where a column sees row i only if SIGN * i <= limit: what is no number in a row counts only in columns that see it.
   template <int SIGN>
   __device__ static void gather_part(const char* tile, int row, int b, const Right& right, int limit, f16v& acc) {
@@ -250,11 +292,6 @@ struct Kind<uint16_t, D> {
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(left[j], right.of[j], acc, 0, 0, 0);
     if (__builtin_expect(odd, 0)) spoil(least, limit, acc);
-  }
-  // Four neighbouring elements of a row.
-  __device__ static void put(uint16_t* p, float a, float b, float c, float d) {
-    typedef us4 us4_any __attribute__((aligned(2)));
-    *(us4_any*)p = us4{to_bf16(a), to_bf16(b), to_bf16(c), to_bf16(d)};
   }
 };
 
@@ -306,7 +343,6 @@ struct Kind<float, D> {
     }
     if (__builtin_expect(__any(least != INT32_MAX), 0)) spoil(least, limit, acc);
   }
-  __device__ static void put(float* p, float a, float b, float c, float d) { *(f4v_any*)p = f4v{a, b, c, d}; }
 };
 
 // Rows `row`.. of a sequence of `len`, at most ROWS: p is its row 0.  Reads beyond them, and at kNowhere, give zeros.
@@ -325,9 +361,8 @@ template <class T, int D, int ROWS, int THREADS>
 struct Stage {
   using K = Kind<T, D>;
   static constexpr int kPieces = D * sizeof(T) / 16;  // a row
-  static constexpr int kEach = ROWS * kPieces / THREADS;
+  static constexpr int kAll = ROWS * kPieces, kEach = (kAll + THREADS - 1) / THREADS;
   static constexpr int kBytes = ROWS * K::kPitch;
-  static_assert(ROWS * kPieces % THREADS == 0, "every thread has as many pieces");
   const T* p;  // row 0 of the sequence
   int64_t stride;
   int dim;
@@ -337,7 +372,7 @@ struct Stage {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int id = threadIdx.x + i * THREADS, r = id / kPieces, c = id % kPieces * int(16 / sizeof(T));
-      from[i] = c < dim ? (r * static_cast<uint32_t>(stride) + c) * uint32_t(sizeof(T)) : kNowhere;
+      from[i] = c < dim && id < kAll ? (r * static_cast<uint32_t>(stride) + c) * uint32_t(sizeof(T)) : kNowhere;
     }
   }
   __device__ void load(int row, int len) {
@@ -349,7 +384,7 @@ struct Stage {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int id = threadIdx.x + i * THREADS;
-      *(u4*)(lds + K::piece_at(id / kPieces, id % kPieces)) = v[i];
+      if (kAll % THREADS == 0 || id < kAll) *(u4*)(lds + K::piece_at(id / kPieces, id % kPieces)) = v[i];
     }
   }
 };
@@ -366,6 +401,20 @@ __device__ inline void own_row(const T* p, int64_t stride, int row, int own, int
   }
 }
 
+// Nothing is moved across by the compiler.
+__device__ inline void pin() { __builtin_amdgcn_sched_barrier(0); }
+
+// A lane's parts of 32 rows of a tile.
+template <class T, int D>
+struct Parts {
+  u4 of[Kind<T, D>::kParts];
+  __device__ void read(const char* tile, int row) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < Kind<T, D>::kParts; ++i) of[i] = *(const u4*)(tile + Kind<T, D>::part_at(row + (lane & 31), i, lane >> 5));
+  }
+};
+
 // C of 32 rows of a tile and the wavefront's columns.
 template <class T, int D>
 __device__ inline f16v scores(const char* tile, int row, const u4 (&own)[Kind<T, D>::kParts], f16v c) {
@@ -376,6 +425,13 @@ __device__ inline f16v scores(const char* tile, int row, const u4 (&own)[Kind<T,
   return c;
 }
 
+// Four neighbouring elements of a row.
+__device__ inline void put4(uint16_t* p, float a, float b, float c, float d) {
+  typedef us4 us4_any __attribute__((aligned(2)));
+  *(us4_any*)p = us4{to_bf16(a), to_bf16(b), to_bf16(c), to_bf16(d)};
+}
+__device__ inline void put4(float* p, float a, float b, float c, float d) { *(f4v_any*)p = f4v{a, b, c, d}; }
+
 // Sums over columns 32 b.. of a row: the lane's elements, times `factor`, rounded once.
 template <class T, int D>
 __device__ inline void put_row(T* row, const f16v (&acc)[D / 32], float factor, int dim) {
@@ -385,8 +441,8 @@ __device__ inline void put_row(T* row, const f16v (&acc)[D / 32], float factor, 
 #pragma unroll
     for (int g = 0; g < 4; ++g)
       if (32 * b + 8 * g < dim)
-        Kind<T, D>::put(row + 32 * b + 8 * g + 4 * h, acc[b][4 * g] * factor, acc[b][4 * g + 1] * factor, acc[b][4 * g + 2] * factor,
-                        acc[b][4 * g + 3] * factor);
+        put4(row + 32 * b + 8 * g + 4 * h, acc[b][4 * g] * factor, acc[b][4 * g + 1] * factor, acc[b][4 * g + 2] * factor,
+             acc[b][4 * g + 3] * factor);
 }
 
 // Zeros in the tile's rows.
@@ -395,6 +451,26 @@ __device__ inline void zero_rows(T* p, int64_t stride, const Place& at, int dim)
   for (int i = threadIdx.x; i < ROWS * dim; i += blockDim.x)
     if (at.row + i / dim < at.len) p[(at.row + i / dim) * stride + i % dim] = T(0);
 }
+
+template <class T>
+__device__ inline const T* head_of(const Rows& r, int64_t start, int head) {
+  return (const T*)r.p + start * r.token + head * r.head;
+}
+
+// Tiles of a head, at most.
+template <int ROWS>
+inline int32_t tiles_of(const Attention& a) {
+  return static_cast<int32_t>(a.offsets != nullptr ? a.tokens / ROWS + a.sequences + 1 : (a.tokens + ROWS - 1) / ROWS);
+}
+
+// The backward pass by keys (daso_attention_keys.hip), after the one by queries; and into how many parts it goes.
+constexpr int kKeyTiles = 512;  // workgroups that make parts needless: two a CU
+inline int32_t parts_of(int64_t tiles, int32_t kv_heads, int32_t share) {
+  int32_t parts = 1;
+  while (parts < share && (share % parts != 0 || tiles * kv_heads * parts < kKeyTiles)) ++parts;
+  return parts;
+}
+hipError_t queue_keys(const Attention& a, int32_t type, hipStream_t stream);
 
 }  // namespace attention
 }  // namespace daso

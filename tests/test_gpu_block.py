@@ -265,6 +265,26 @@ def test_what_a_token_does_not_see_changes_nothing(dtype, dim, n, bad):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [100, 130])
+def test_what_all_tokens_see_reaches_all(dtype, n):
+    """Not causal: a value that is no number reaches each token of its sequence, in the last part of a tile too."""
+    announce("seen by all", dtype, n)
+    for which, token in ((2, n - 1), (3, n - 1), (1, 3), (0, n - 2)):
+        t = attention_case(n, 2, 2, 64, dtype, 13)
+        t[which][token, 1, 5] = float("nan")
+        out, lse, (dq, dk, dv) = both_ways(*t, causal=False, dtype=dtype)
+        assert torch.isfinite(out[:, 0]).all() and torch.isfinite(dk[:, 0]).all() and torch.isfinite(dv[:, 0]).all()
+        if which == 2:
+            assert out[:, 1, 5].isnan().all() and torch.isfinite(out[:, 1, 6]).all() and dq[:, 1].isnan().all()
+        elif which == 3:
+            assert dv[:, 1, 5].isnan().all() and torch.isfinite(dv[:, 1, 6]).all() and dk[:, 1].isnan().all()
+        elif which == 1:
+            assert lse[1].isnan().all() and dv[:, 1].isnan().all()
+        else:
+            assert dk[:, 1].isnan().all() and dv[:, 1].isnan().all() and out[token, 1].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("size", [1e-3, 30.0, 1e4])
 def test_attention_of_small_and_huge_scores(dtype, size):
     """From weights that are all alike to one that decides: nothing overflows, and p is as exact as its score is."""
