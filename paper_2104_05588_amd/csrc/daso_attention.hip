@@ -27,8 +27,14 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
   using S = Stage<T, D, kKeys, kThreads>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
   const T *k = head_of<T>(a.k, at.start, at.head / a.share), *v = head_of<T>(a.v, at.start, at.head / a.share);
+  char* const room = lds[0][0];
+  S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
   u4 q[K::kParts];
-  own_row<kOwn, T, D>(head_of<T>(a.q, at.start, at.head), a.q.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, q);
+  {
+    const Own<T, D> mine(head_of<T>(a.q, at.start, at.head), a.q.token, at.row, at.len, a.dim);
+    ks.load(0, at.len), vs.load(0, at.len);
+    mine.read(room, q);
+  }
   const int last = a.causal ? min(mine, at.len - 1) : at.len - 1;  // key that the lane's query sees
   const int keys = a.causal ? min(at.len, at.row + kOwn) : at.len;
   const int whole = (a.causal ? min(at.len, at.row + 1) : at.len) / kKeys * kKeys;  // keys below are seen by all queries
@@ -38,7 +44,6 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
   // The exponents' base, of z log2 e, and the lane's keys' share of the sum.  The base follows the maximum only where that
   // has grown by more than 2^kGrowth, which the sums have room for.
   float top = -INFINITY, base = 0.0f, sum = 0.0f;
-  S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
   // The next tile comes in two halves, its keys during the first half of this one and its values during the second.
   const auto turn = [&](int key, int buffer) { ks.store(lds[buffer ^ 1][0]), vs.load(key + kKeys, at.len); };
   // The base for the scores of 32 keys, and their powers in place of them.
@@ -97,7 +102,6 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
       }
     }
   };
-  ks.load(0, at.len), vs.load(0, at.len);
   ks.store(lds[0][0]), vs.store(lds[0][1]);
   __syncthreads();
   int key = 0, buffer = 0;
@@ -115,9 +119,8 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
     __syncthreads();
   }
   sum = halves_sum(sum);
-  if (mine >= at.len) return;
-  put_row<T, D>((T*)head_of<T>(a.out, at.start, at.head) + mine * a.out.token, acc, 1.0f / sum, a.dim);
-  if (lane < 32) a.lse[at.head * a.tokens + at.start + mine] = (base + log2f(sum)) * kLn2;
+  put_rows<T, D>(room, (T*)head_of<T>(a.out, at.start, at.head), a.out.token, first, at.len, a.dim, acc, 1.0f / sum);
+  if (lane < 32 && mine < at.len) a.lse[at.head * a.tokens + at.start + mine] = (base + log2f(sum)) * kLn2;
 }
 
 template <class T, int D>
@@ -127,8 +130,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kForwa
   const Found found = place_of<kOwn, true>(a, a.heads, &at);
   if (found == kSequence) return forward_tile<T, D>(a, at, lds);
   if (found == kNone || !a.zero_q) return;
-  zero_rows<kOwn>((T*)head_of<T>(a.out, at.start, at.head), a.out.token, at, a.dim);
-  zero_rows<kOwn>(a.lse + at.head * a.tokens + at.start, 1, at, 1);
+  zero_rows((T*)head_of<T>(a.out, at.start, at.head), a.out.token, at, a.dim);
+  zero_rows(a.lse + at.head * a.tokens + at.start, 1, at, 1);
 }
 
 template <class T, int D>
@@ -139,16 +142,29 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
   const bool there = mine < at.len;
   const T *k = head_of<T>(a.k, at.start, at.head / a.share), *v = head_of<T>(a.v, at.start, at.head / a.share);
+  char* const room = lds[0][0];
+  S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
   u4 q[K::kParts], g[K::kParts];
-  own_row<kOwn, T, D>(head_of<T>(a.q, at.start, at.head), a.q.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, q);
-  own_row<kOwn, T, D>(head_of<T>(a.dout, at.start, at.head), a.dout.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, g);
   float delta = 0.0f;
   {
-    u4 o[K::kParts];
-    own_row<kOwn, T, D>(head_of<T>(a.out, at.start, at.head), a.out.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, o);
+    const auto own = [&](const Rows& rows) { return Own<T, D>(head_of<T>(rows, at.start, at.head), rows.token, at.row, at.len, a.dim); };
+    const auto sum = [&] {
 #pragma unroll
-    for (int c = 0; c < K::kParts; ++c) delta += K::dot(g[c], o[c]);
-    delta = halves_sum(delta);
+      for (int c = 0; c < K::kParts; ++c) delta += K::dot(g[c], q[c]);
+      delta = halves_sum(delta);
+    };
+    if constexpr (D > 96) {  // (where registers are short one after the other)
+      own(a.out).read(room, q), own(a.dout).read(room, g);
+      sum();
+      own(a.q).read(room, q);
+      ks.load(0, at.len), vs.load(0, at.len);
+    } else {
+      const Own<T, D> o = own(a.out), dout = own(a.dout), mine = own(a.q);
+      o.read(room, q), dout.read(room, g);
+      sum();
+      ks.load(0, at.len), vs.load(0, at.len);
+      mine.read(room, q);
+    }
   }
   const int64_t stat = at.head * a.tokens + at.start + mine;
   const float lse2 = there ? a.lse[stat] * kLog2e : INFINITY;
@@ -159,7 +175,6 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
   f16v acc[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; ++b) acc[b] = (f16v)0.0f;
-  S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
   // The next tile in halves, as in the forward pass, where registers are short: 8192 x 16 x 128 in 730 us against 870 in one piece
   // with one wavefront a SIMD.  Else in one, which has longer to come: 8192 x 16 x 64 in 419 us against 530.
   constexpr bool kHalves = D > 96;
@@ -208,7 +223,6 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
       }
     }
   };
-  ks.load(0, at.len), vs.load(0, at.len);
   ks.store(lds[0][0]), vs.store(lds[0][1]);
   __syncthreads();
   int key = 0, buffer = 0;
@@ -225,7 +239,7 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
     keep(buffer ^ 1);
     __syncthreads();
   }
-  if (there) put_row<T, D>((T*)head_of<T>(a.dq, at.start, at.head) + mine * a.dq.token, acc, a.scale, a.dim);
+  put_rows<T, D>(room, (T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, first, at.len, a.dim, acc, a.scale);
 }
 
 template <class T, int D>
@@ -235,14 +249,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kQuery
   const Found found = place_of<kOwn, true>(a, a.heads, &at);
   if (found == kSequence) return query_tile<T, D>(a, at, lds);
   if (found == kNone || !a.zero_q) return;
-  zero_rows<kOwn>((T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, at, a.dim);
+  zero_rows((T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, at, a.dim);
 }
 
 // ------------------------------------------------------------------------- host
 template <class T, int D>
 hipError_t queue(const Attention& a, bool backward, hipStream_t stream) {
-  const dim3 block(kThreads), queries(static_cast<uint32_t>(a.tiles * a.heads));
-  return backward ? launch(&query_kernel<T, D>, queries, block, stream, a) : launch(&forward_kernel<T, D>, queries, block, stream, a);
+  const dim3 block(kThreads), grid(static_cast<uint32_t>(a.tiles * a.heads));
+  return backward ? launch(&query_kernel<T, D>, grid, block, stream, a) : launch(&forward_kernel<T, D>, grid, block, stream, a);
 }
 template <class T>
 hipError_t queue(const Attention& a, bool backward, hipStream_t stream) {
@@ -269,12 +283,11 @@ int run(const daso_attention_args& s, bool backward, hipStream_t stream) {
   a.share = s.heads / s.kv_heads, a.dim = s.dim, a.causal = (s.flags & DASO_ATTENTION_CAUSAL) != 0;
   a.zero_q = (s.flags & DASO_ATTENTION_ZERO_Q) != 0, a.zero_k = (s.flags & DASO_ATTENTION_ZERO_K) != 0;
   a.zero_v = (s.flags & DASO_ATTENTION_ZERO_V) != 0;
-  a.tiles = tiles_of<kOwn>(a);
   a.scale = s.scale, a.scale2 = s.scale * kLog2e;
   a.q = rows(s.q), a.k = rows(s.k), a.v = rows(s.v), a.out = rows(s.out), a.dout = rows(s.dout);
   a.dq = rows(s.dq), a.dk = rows(s.dk), a.dv = rows(s.dv), a.lse = s.lse, a.delta = static_cast<float*>(s.workspace);
   a.parts = key_parts(s), a.partial = reinterpret_cast<float*>(static_cast<char*>(s.workspace) + (backward ? delta_bytes(s) : 0));
-  a.sorted = a.tiles * a.heads <= kFewTiles;
+  a.tiles = tiles_of<kOwn>(a), a.sorted = a.tiles * a.heads <= kFewTiles;
   hipError_t err = s.type == DASO_TYPE_BF16 ? queue<uint16_t>(a, backward, stream) : queue<float>(a, backward, stream);
   if (backward && err == hipSuccess) err = queue_keys(a, s.type, stream);
   return err == hipSuccess ? DASO_OK : DASO_EHIP;

@@ -23,11 +23,15 @@ __device__ inline void key_tile(const Attention& a, const Place& at,
   constexpr bool kAlone = sizeof(T) == 2 && kKeyPerSimd<T, D> == 1;
   using S = Stage<T, D, kQueries, kThreads>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
-  const bool there = mine < at.len;
   const int kv = at.head / a.parts, part = at.head % a.parts, each = a.share / a.parts;
+  char* const room = lds[0][0];
   u4 k[K::kParts], v[K::kParts];
-  own_row<kOwn, T, D>(head_of<T>(a.k, at.start, kv), a.k.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, k);
-  own_row<kOwn, T, D>(head_of<T>(a.v, at.start, kv), a.v.token, at.row, wave * 32 + (lane & 31), at.len, a.dim, v);
+  {
+    const Own<T, D> keys(head_of<T>(a.k, at.start, kv), a.k.token, at.row, at.len, a.dim);
+    const Own<T, D> values(head_of<T>(a.v, at.start, kv), a.v.token, at.row, at.len, a.dim);
+    keys.read(room, k);
+    values.read(room, v);
+  }
   f16v dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; ++b) dk[b] = dv[b] = (f16v)0.0f;
@@ -122,16 +126,16 @@ __device__ inline void key_tile(const Attention& a, const Place& at,
     head = next_head, row = next_row, buffer ^= 1;
     __syncthreads();
   }
-  if (!there) return;
   if (a.parts > 1) {
-    const int64_t plane = a.tokens * a.kv_heads * a.dim;
-    float* to = a.partial + 2 * part * plane + ((at.start + mine) * a.kv_heads + kv) * a.dim;
-    put_row<float, D>(to, dk, a.scale, a.dim);
-    put_row<float, D>(to + plane, dv, 1.0f, a.dim);
+    const int64_t plane = a.tokens * a.kv_heads * a.dim, apart = int64_t(a.kv_heads) * a.dim;
+    float* to = a.partial + 2 * part * plane + at.start * apart + kv * a.dim;
+    if (mine >= at.len) return;
+    put_own<D>(to + mine * apart, dk, a.scale, a.dim);
+    put_own<D>(to + plane + mine * apart, dv, 1.0f, a.dim);
     return;
   }
-  put_row<T, D>((T*)head_of<T>(a.dk, at.start, kv) + mine * a.dk.token, dk, a.scale, a.dim);
-  put_row<T, D>((T*)head_of<T>(a.dv, at.start, kv) + mine * a.dv.token, dv, 1.0f, a.dim);
+  put_rows<T, D>(room, (T*)head_of<T>(a.dk, at.start, kv), a.dk.token, first, at.len, a.dim, dk, a.scale);
+  put_rows<T, D>(room, (T*)head_of<T>(a.dv, at.start, kv), a.dv.token, first, at.len, a.dim, dv, 1.0f);
 }
 
 template <class T, int D>
@@ -143,8 +147,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kKeyPe
   if (found == kSequence) return key_tile<T, D>(a, at, lds, stats);
   if (found == kNone || at.head % a.parts != 0) return;
   at.head /= a.parts;
-  if (a.zero_k) zero_rows<kOwn>((T*)head_of<T>(a.dk, at.start, at.head), a.dk.token, at, a.dim);
-  if (a.zero_v) zero_rows<kOwn>((T*)head_of<T>(a.dv, at.start, at.head), a.dv.token, at, a.dim);
+  if (a.zero_k) zero_rows((T*)head_of<T>(a.dk, at.start, at.head), a.dk.token, at, a.dim);
+  if (a.zero_v) zero_rows((T*)head_of<T>(a.dv, at.start, at.head), a.dv.token, at, a.dim);
 }
 
 // dk and dv of 32 rows from the parts, in order.

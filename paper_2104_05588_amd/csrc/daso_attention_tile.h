@@ -26,7 +26,6 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kThreads = 256, kWaves = 4, kOwn = kWaves * 32;  // rows of a workgroup
 template <class T>
 constexpr int kTile = sizeof(T) == 2 ? 64 : 32;  // rows of a tile in LDS
-constexpr int kFewTiles = 2048;  // Attention::sorted: up to eight a CU
 using product::bhalf8;
 using product::half4;
 using product::half8;
@@ -65,11 +64,14 @@ __device__ inline int64_t read_lane(int64_t v, int lane) {
 
 constexpr int kSorted = 32;  // sequences, at most, whose tiles are taken in the order of their work
 
-// Workgroups of neighbouring numbers go to the eight XCDs in turn.  Where the heads can be dealt to them evenly an XCD takes
-// heads of its own, one after the other, so that their keys stay in its L2.  A causal sequence's tiles that are the most
-// work come first: the last ones (QUERIES) or the first ones (keys).  With Attention::sorted, for launches of few tiles a CU, all
-// tiles of the heads and of up to kSorted sequences come in the order of their work: 8 x 1024 tokens of 16 heads of 64 forward in
-// 38 us against 45, where 32 x 1024 tokens, whose keys do not fit the L2s together, would take 167 against 141.
+// Workgroups of neighbouring numbers go to the eight XCDs in turn, and in an XCD to its parts.  Where the heads can be dealt to
+// them evenly an XCD takes heads of its own, so that their keys stay in its L2.
+//
+// In causal sequences a tile's work is its place from the light end, which is the first tile of queries and the last one of
+// keys.  With Attention::sorted, for launches of few tiles a CU, all tiles of the heads and of up to kSorted sequences come in the
+// order of their work, the most first.  Else, whose keys would not fit the L2s together, head by head and sequence
+// by sequence, from another tile on in each, so that no part of an XCD is dealt the heavy ones alone: 32 x 1024 tokens of 16 heads of
+// 64 forward in 154 us, 182 where each sequence begins with its heaviest tile.
 // kRest: a tile of the rows behind the last sequence.
 enum Found { kNone, kSequence, kRest };
 template <int ROWS, bool QUERIES>
@@ -140,7 +142,7 @@ __device__ inline Found place_of(const Attention& a, int heads, Place* at) {
     if (found != 0) {
       const int l = __builtin_ctzll(found), tiles = __builtin_amdgcn_readlane(mine, l);
       at->start = read_lane(from, l), at->len = static_cast<int32_t>(read_lane(to, l) - at->start);
-      const int tile = index - before - (__builtin_amdgcn_readlane(upto, l) - tiles);
+      const int tile = (index - before - (__builtin_amdgcn_readlane(upto, l) - tiles) + base + l) % tiles;
       at->row = (last_first ? tiles - 1 - tile : tile) * ROWS;
       return kSequence;
     }
@@ -360,45 +362,77 @@ __device__ inline u4 read16(__amdgpu_buffer_rsrc_t from, uint32_t at) { return _
 template <class T, int D, int ROWS, int THREADS>
 struct Stage {
   using K = Kind<T, D>;
-  static constexpr int kPieces = D * sizeof(T) / 16;  // a row
-  static constexpr int kAll = ROWS * kPieces, kEach = (kAll + THREADS - 1) / THREADS;
+  // Pieces of 16 bytes a row, and threads across it.  A thread's pieces are whole rows apart: it has one place, and a window of its
+  // own (in scalar registers) for each piece.
+  static constexpr int kPieces = D * sizeof(T) / 16, kAcross = kPieces == 12 ? 16 : kPieces == 24 ? 32 : kPieces;
+  static constexpr int kRows = THREADS / kAcross, kEach = ROWS / kRows;
   static constexpr int kBytes = ROWS * K::kPitch;
+  static_assert(THREADS % kAcross == 0 && ROWS % kRows == 0, "every thread has as many pieces");
   const T* p;  // row 0 of the sequence
   int64_t stride;
   int dim;
-  uint32_t from[kEach];
+  uint32_t from;
   u4 v[kEach];
   __device__ Stage(const T* p, int64_t stride, int dim) : p(p), stride(stride), dim(dim) {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int id = threadIdx.x + i * THREADS, r = id / kPieces, c = id % kPieces * int(16 / sizeof(T));
-      from[i] = c < dim && id < kAll ? (r * static_cast<uint32_t>(stride) + c) * uint32_t(sizeof(T)) : kNowhere;
-    }
+    const int r = threadIdx.x / kAcross, c = threadIdx.x % kAcross * int(16 / sizeof(T));
+    from = c < dim ? (r * static_cast<uint32_t>(stride) + c) * uint32_t(sizeof(T)) : kNowhere;
   }
   __device__ void load(int row, int len) {
-    const __amdgpu_buffer_rsrc_t w = window<ROWS>(p, stride, row, len, dim);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) v[i] = read16(w, from[i]);
+    for (int i = 0; i < kEach; ++i) v[i] = read16(window<kRows>(p, stride, row + i * kRows, len, dim), from);
   }
   __device__ void store(char* lds) const {
+    const int r = threadIdx.x / kAcross, c = threadIdx.x % kAcross;
+    if (kPieces != kAcross && c >= kPieces) return;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int id = threadIdx.x + i * THREADS;
-      if (kAll % THREADS == 0 || id < kAll) *(u4*)(lds + K::piece_at(id / kPieces, id % kPieces)) = v[i];
-    }
+    for (int i = 0; i < kEach; ++i) *(u4*)(lds + K::piece_at(r + i * kRows, c)) = v[i];
   }
 };
 
-// A lane's parts of one of the ROWS rows of a workgroup: row + own of the sequence, or zeros.
-template <int ROWS, class T, int D>
-__device__ inline void own_row(const T* p, int64_t stride, int row, int own, int len, int dim, u4 (&parts)[Kind<T, D>::kParts]) {
-  const int h = (threadIdx.x & 63) >> 5;
-  const __amdgpu_buffer_rsrc_t w = window<ROWS>(p, stride, row, len, dim);
+// A workgroup's kOwn rows come and go through LDS, by whole lines: a lane's own 16 bytes of 32 rows at a time would ask
+// for each line four times or more.  `lds` has room for kOwn rows.
+template <class T, int D>
+struct Own {
+  using K = Kind<T, D>;
+  Stage<T, D, kOwn, kThreads> rows;
+  __device__ Own(const T* p, int64_t stride, int row, int len, int dim) : rows(p, stride, dim) { rows.load(row, len); }
+  // The lane's parts of its row.  All wavefronts take part; nobody uses `lds` before or after without a meeting.
+  __device__ void read(char* lds, u4 (&parts)[K::kParts]) const {
+    rows.store(lds);
+    __syncthreads();
+    const int own = (threadIdx.x >> 6) * 32 + (threadIdx.x & 31), h = (threadIdx.x & 63) >> 5;
 #pragma unroll
-  for (int c = 0; c < Kind<T, D>::kParts; ++c) {
-    const int e = Kind<T, D>::part_element(c, h);
-    parts[c] = read16(w, e < dim ? (own * static_cast<uint32_t>(stride) + e) * uint32_t(sizeof(T)) : kNowhere);
+    for (int c = 0; c < K::kParts; ++c) parts[c] = *(const u4*)(lds + K::part_at(own, c, h));
+    __syncthreads();
   }
+};
+
+// Four neighbouring elements of a row in LDS.
+__device__ inline void keep4(uint16_t* p, float a, float b, float c, float d) { *(us4*)p = us4{to_bf16(a), to_bf16(b), to_bf16(c), to_bf16(d)}; }
+__device__ inline void keep4(float* p, float a, float b, float c, float d) { *(f4v*)p = f4v{a, b, c, d}; }
+
+// A wavefront's 32 rows of sums, times `factor`, rounded once: p is row 0 of the sequence, `first` the wavefront's first row.
+template <class T, int D>
+__device__ inline void put_rows(char* lds, T* p, int64_t stride, int first, int len, int dim, const f16v (&acc)[D / 32], float factor) {
+  using K = Kind<T, D>;
+  constexpr int kPieces = D * sizeof(T) / 16, kEach = 16 / sizeof(T);
+  const int lane = threadIdx.x & 63, h = lane >> 5, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int e = 32 * b + 8 * g + 4 * h;
+      keep4((T*)(lds + K::piece_at(wave * 32 + (lane & 31), e / kEach)) + e % kEach, acc[b][4 * g] * factor, acc[b][4 * g + 1] * factor,
+            acc[b][4 * g + 2] * factor, acc[b][4 * g + 3] * factor);
+    }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int i = 0; i < 32 * kPieces / 64; ++i) {
+    const int id = lane + i * 64, r = id / kPieces, c = id % kPieces;
+    const u4 v = *(const u4*)(lds + K::piece_at(wave * 32 + r, c));
+    if (first + r < len && c * kEach < dim) *(u4_any*)(p + (first + r) * stride + c * kEach) = v;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // Nothing is moved across by the compiler.
@@ -432,9 +466,9 @@ __device__ inline void put4(uint16_t* p, float a, float b, float c, float d) {
 }
 __device__ inline void put4(float* p, float a, float b, float c, float d) { *(f4v_any*)p = f4v{a, b, c, d}; }
 
-// Sums over columns 32 b.. of a row: the lane's elements, times `factor`, rounded once.
-template <class T, int D>
-__device__ inline void put_row(T* row, const f16v (&acc)[D / 32], float factor, int dim) {
+// A lane's sums of its own row, in 32 bits and by itself.
+template <int D>
+__device__ inline void put_own(float* row, const f16v (&acc)[D / 32], float factor, int dim) {
   const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
@@ -446,9 +480,9 @@ __device__ inline void put_row(T* row, const f16v (&acc)[D / 32], float factor, 
 }
 
 // Zeros in the tile's rows.
-template <int ROWS, class T>
+template <class T>
 __device__ inline void zero_rows(T* p, int64_t stride, const Place& at, int dim) {
-  for (int i = threadIdx.x; i < ROWS * dim; i += blockDim.x)
+  for (int i = threadIdx.x; i < kOwn * dim; i += kThreads)
     if (at.row + i / dim < at.len) p[(at.row + i / dim) * stride + i % dim] = T(0);
 }
 
@@ -462,6 +496,7 @@ template <int ROWS>
 inline int32_t tiles_of(const Attention& a) {
   return static_cast<int32_t>(a.offsets != nullptr ? a.tokens / ROWS + a.sequences + 1 : (a.tokens + ROWS - 1) / ROWS);
 }
+constexpr int32_t kFewTiles = 2048;  // Attention::sorted: up to eight a CU
 
 // The backward pass by keys (daso_attention_keys.hip), after the one by queries; and into how many parts it goes.
 constexpr int kKeyTiles = 512;  // workgroups that make parts needless: two a CU
