@@ -122,7 +122,7 @@ typedef struct daso_span {
  * factor is taken in 64 bits and rounded once; a NaN norm makes it NaN.  Elements outside the
  * tensors are neither counted nor written. */
 typedef struct daso_clip_args {
-  int64_t n;                   /* elements of every buffer, <= DASO_MAX_N */
+  int64_t n;                   /* elements of every buffer; n / 1024 + 2 * ntensors < 2^24 */
   int32_t g;                   /* 1..DASO_MAX_G */
   int32_t ntensors;            /* 0: the whole buffer is one */
   const float* const* grads;   /* host array of g device pointers, aligned to 16 */

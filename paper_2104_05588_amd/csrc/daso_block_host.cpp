@@ -139,7 +139,7 @@ int check_clip_sizes(const daso_clip_args& s) {
     if (span.start < at || span.start > s.n || span.n < 0 || span.n > s.n - span.start) return DASO_EINVAL;
     at = span.start + span.n;
   }
-  return DASO_OK;
+  return s.n / kPiece + 2 * int64_t(s.ntensors) < kMostPieces ? DASO_OK : DASO_EINVAL;
 }
 
 int check_clip(const daso_clip_args& s) {
@@ -161,17 +161,14 @@ int check_clip(const daso_clip_args& s) {
   return check_rows({out, norm, each}, {}, 0);
 }
 
-ClipPlan plan_clip(const daso_clip_args& s) {
-  int64_t n = s.ntensors > 0 ? 0 : s.n;
-  for (int32_t t = 0; t < s.ntensors; ++t) n += s.tensors[t].n;
-  ClipPlan p;
-  p.chunk = std::max(kClipLeastChunk, (chunks_of(n, kClipChunks) + 1023) / 1024 * 1024);
-  p.chunks = s.ntensors > 0 ? 0 : chunks_of(s.n, p.chunk);
-  for (int32_t t = 0; t < s.ntensors; ++t) p.chunks += chunks_of(s.tensors[t].n, p.chunk);
-  return p;
+int64_t pieces_of(const daso_clip_args& s) {
+  if (s.ntensors == 0) return pieces_of(daso_span{0, s.n});
+  int64_t pieces = 0;
+  for (int32_t t = 0; t < s.ntensors; ++t) pieces += pieces_of(s.tensors[t]);
+  return pieces;
 }
 
-int32_t fill_table(const daso_clip_args& s, int64_t chunk, int32_t tensor, ClipTable* table) {
+int32_t fill_table(const daso_clip_args& s, int32_t tensor, bool merged, ClipTable* table) {
   const daso_span whole = {0, s.n};
   const daso_span* spans = s.ntensors > 0 ? s.tensors : &whole;
   const int32_t count = s.ntensors > 0 ? s.ntensors : 1;
@@ -179,17 +176,23 @@ int32_t fill_table(const daso_clip_args& s, int64_t chunk, int32_t tensor, ClipT
   t.tensor = tensor, t.runs = 0;
   t.bound[0] = spans[tensor].start, t.first[0] = 0;
   int32_t taken = 0;
-  const auto run = [&t](int64_t end, int64_t chunks, int32_t number) {
+  const auto run = [&t](int64_t end, int64_t pieces, int32_t number) {
     t.number[t.runs] = static_cast<int16_t>(number);
-    t.bound[t.runs + 1] = end, t.first[t.runs + 1] = t.first[t.runs] + static_cast<int32_t>(chunks);
+    t.bound[t.runs + 1] = end, t.first[t.runs + 1] = t.first[t.runs] + static_cast<int32_t>(pieces);
     ++t.runs;
   };
   for (; tensor + taken < count; ++taken) {
     const daso_span& span = spans[tensor + taken];
     const bool gap = span.start != t.bound[t.runs];
+    if (merged && !gap && taken > 0) {
+      const daso_span grown = {t.bound[t.runs - 1], span.start + span.n - t.bound[t.runs - 1]};
+      t.bound[t.runs] = span.start + span.n;
+      t.first[t.runs] = t.first[t.runs - 1] + static_cast<int32_t>(pieces_of(grown));
+      continue;
+    }
     if (t.runs + (gap ? 2 : 1) > kClipRuns) break;
     if (gap) run(span.start, 0, -1);
-    run(span.start + span.n, chunks_of(span.n, chunk), taken);
+    run(span.start + span.n, pieces_of(span), taken);
   }
   return taken;
 }

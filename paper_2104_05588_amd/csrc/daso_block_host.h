@@ -23,28 +23,27 @@ int check_attention(const daso_attention_args& s, bool backward);
 int check_clip_sizes(const daso_clip_args& s);
 int check_clip(const daso_clip_args& s);
 
-// How the tensors of a clipping are cut: chunks of one tensor each, a partial sum of squares a chunk.
-struct ClipPlan {
-  int64_t chunk;   // elements
-  int64_t chunks;  // of all tensors
-};
-constexpr int64_t kClipChunks = 2048;      // and one more a tensor, at most
-constexpr int64_t kClipLeastChunk = 4096;  // elements
-ClipPlan plan_clip(const daso_clip_args& s);
-inline int64_t chunks_of(int64_t n, int64_t chunk) { return n / chunk + (n % chunk != 0); }
+// How the tensors of a clipping are cut: pieces of 1024 elements, counted from the buffer's start, of one tensor each: a workgroup
+// and a partial sum of squares a piece.
+constexpr int64_t kPiece = 1024;
+constexpr int64_t kMostPieces = int64_t(1) << 24;
+constexpr int64_t kJoined = 4096;  // pieces from which on their sums are added by kernels of their own
+inline int64_t pieces_of(const daso_span& t) { return t.n == 0 ? 0 : (t.start + t.n - 1) / kPiece - t.start / kPiece + 1; }
+int64_t pieces_of(const daso_clip_args& s);
 
 // What of a clipping one launch takes: runs of elements between neighbouring boundaries, of which those that are a tensor
-// have chunks and gaps between tensors none.
+// have pieces and gaps between tensors none.
 constexpr int kClipRuns = 208;
 struct ClipTable {
   int64_t bound[kClipRuns + 1];  // run i: bound[i] <= element < bound[i + 1]
-  int32_t first[kClipRuns + 1];  // its first chunk, counted from the launch's first
+  int32_t first[kClipRuns + 1];  // its first piece, counted from the launch's first
   int16_t number[kClipRuns];     // its tensor, counted from the launch's first, or -1
   int32_t tensor;                // number of the first tensor
   int32_t runs;
 };
-// Fills the table with the tensors from `tensor` on that fit; returns how many.
-int32_t fill_table(const daso_clip_args& s, int64_t chunk, int32_t tensor, ClipTable* table);
+// Fills the table with the tensors from `tensor` on that fit; returns how many.  merged: tensors next to each other are one run,
+// whose pieces are not those of the tensors apart.
+int32_t fill_table(const daso_clip_args& s, int32_t tensor, bool merged, ClipTable* table);
 
 }  // namespace host
 }  // namespace daso
