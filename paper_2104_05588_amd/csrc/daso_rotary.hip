@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kForwardGroups = 2048;  // most workgroups of a forward pass
-constexpr int kPartialGroups = 512;   // of a backward one
+constexpr int kPartialGroups = 1024;  // of a backward one: four a CU
 constexpr int kShareTokens = 4096;    // with fewer tokens several wavefronts take a token's heads
 
 struct Rows {
@@ -104,6 +104,11 @@ struct Raw {
     if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
     else return __builtin_bit_cast(float, i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
   }
+  // two elements, rounded to nearest even by the hardware's conversion (written out it is five instructions an element)
+  __device__ static uint32_t two(float a, float b) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, b2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+  }
   // the pairs' elements
   __device__ void get(float (&a)[8], float (&b)[8]) const {
 #pragma unroll
@@ -124,8 +129,7 @@ struct Raw {
       for (int r = 0; r < 4; ++r) {
         if (!at.is[r]) continue;
         if constexpr (sizeof(T) == 2) {
-          typedef us4 us4_any __attribute__((aligned(2)));
-          *(us4_any*)(row + at.at[r]) = us4{to_bf16(v[4 * r]), to_bf16(v[4 * r + 1]), to_bf16(v[4 * r + 2]), to_bf16(v[4 * r + 3])};
+          *(pair_word_any*)(row + at.at[r]) = pair_word{two(v[4 * r], v[4 * r + 1]), two(v[4 * r + 2], v[4 * r + 3])};
         } else {
           *(f4v_any*)(row + at.at[r]) = f4v{v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]};
         }
@@ -134,38 +138,59 @@ struct Raw {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         if (!at.is[r]) continue;
-        float e[8];
+        if constexpr (sizeof(T) == 2) {
+          *(word_any*)(row + at.at[r]) = word{two(v[8 * r], v[8 * r + 1]), two(v[8 * r + 2], v[8 * r + 3]), two(v[8 * r + 4], v[8 * r + 5]),
+                                              two(v[8 * r + 6], v[8 * r + 7])};
+        } else {
+          float e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = v[8 * r + i];
-        store8(row + at.at[r], e);
+          for (int i = 0; i < 8; ++i) e[i] = v[8 * r + i];
+          store8(row + at.at[r], e);
+        }
       }
     }
   }
 };
 
-// fp32 weights of a lane's pairs, which lie as the row does.
-template <Order ORDER>
-__device__ inline void weights(const float* w, const Place<ORDER>& at, float (&a)[8], float (&b)[8]) {
-  if (w == nullptr) {
+// What a lane in a head needs of a vector, 16 floats, lies together in LDS; 80 bytes from lane to lane, so that the reads of a
+// head's lanes take all banks evenly.
+constexpr int kLaneFloats = 20;
+__device__ inline void read_pairs(const float* p, float (&a)[8], float (&b)[8]) {
+  const f4v v[4] = {*(const f4v*)p, *(const f4v*)(p + 4), *(const f4v*)(p + 8), *(const f4v*)(p + 12)};
 #pragma unroll
-    for (int p = 0; p < 8; ++p) a[p] = b[p] = 1.0f;
-    return;
+  for (int i = 0; i < 8; ++i) a[i] = v[i / 4][i % 4], b[i] = v[2 + i / 4][i % 4];
+}
+// The weights of queries and keys (ones where there are none), by the first lanes of the workgroup.
+template <int LANES, Order ORDER>
+__device__ inline void keep_weights(const Rotary& a, float (*lds)[LANES * kLaneFloats]) {
+  if (threadIdx.x < 2 * LANES) {
+    const int of = threadIdx.x / LANES, in = threadIdx.x % LANES;
+    const Place<ORDER> at(a, in * 8);
+    float x[8], y[8];
+#pragma unroll
+    for (int p = 0; p < 8; ++p) x[p] = y[p] = 1.0f;
+    if (a.weight[of] != nullptr) {
+      Raw<float, ORDER> raw;
+      raw.load(a.weight[of], at, true);
+      raw.get(x, y);
+    }
+#pragma unroll
+    for (int p = 0; p < 8; ++p) lds[of][in * kLaneFloats + p] = x[p], lds[of][in * kLaneFloats + 8 + p] = y[p];
   }
-  Raw<float, ORDER> raw;
-  raw.load(w, at, true);
-  raw.get(a, b);
+  __syncthreads();
 }
 
 // cos and sin of the token's angle, pair by pair, in the wavefront's part of LDS; pairs that are not turned have 1 and 0.
-__device__ inline void angles(const Rotary& a, int64_t token, double turns, float2* table, int lane) {
-  float2 cs = {1.0f, 0.0f};
+__device__ inline void angles(const Rotary& a, int64_t token, double turns, float* table, int lane) {
+  float cosine = 1.0f, sine = 0.0f;
   if (lane < a.turned) {
     // whole turns are taken off in 64 bits; twice what is left is in [-1, 1]
     const double at = static_cast<double>(a.positions[token]) * turns;
-    sincospif(2.0f * static_cast<float>(at - rint(at)), &cs.y, &cs.x);
+    sincospif(2.0f * static_cast<float>(at - rint(at)), &sine, &cosine);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  table[lane] = cs;
+  float* const to = table + lane / 8 * kLaneFloats + lane % 8;
+  to[0] = cosine, to[8] = sine;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 __device__ inline double turns_of(const Rotary& a, int lane) {
@@ -203,11 +228,11 @@ struct Walk {
 
 template <class T, int LANES, Order ORDER>
 __global__ __launch_bounds__(kThreads) void forward_kernel(Rotary a) {
-  __shared__ float2 tables[kWaves][64];
+  __shared__ __attribute__((aligned(16))) float tables[kWaves][8 * kLaneFloats];
+  __shared__ __attribute__((aligned(16))) float weights[2][LANES * kLaneFloats];
   const int lane = threadIdx.x & 63, in = lane % LANES, slot = lane / LANES;
-  float2* const table = tables[threadIdx.x >> 6];
+  float* const table = tables[threadIdx.x >> 6];
   const Place<ORDER> at(a, in * 8);
-  const double turns = turns_of(a, lane);
   Walk<LANES> w(a);
   Raw<T, ORDER> raw;
   const auto load = [&] {
@@ -216,14 +241,13 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(Rotary a) {
     raw.load(row, at, h < a.all);
   };
   if (w.there()) load();
-  float qa[8], qb[8], ka[8], kb[8];
-  weights(a.weight[0], at, qa, qb);
-  weights(a.weight[1], at, ka, kb);
+  const double turns = turns_of(a, lane);
+  keep_weights<LANES, ORDER>(a, weights);
   int64_t known = -1;
   while (w.there()) {
     const int64_t token = w.token(a);
     const int h = w.pass * Walk<LANES>::kHeads + slot, of = h >= a.heads;
-    float x[8], y[8], sum = 0.0f;
+    float x[8], y[8], cosine[8], sine[8], wa[8], wb[8], sum = 0.0f;
     raw.get(x, y);
     w.next(a);
     if (w.there()) load();
@@ -232,46 +256,51 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(Rotary a) {
 #pragma unroll
     for (int p = 0; p < 8; ++p) sum = fmaf(x[p], x[p], fmaf(y[p], y[p], sum));
     const float rstd = 1.0f / sqrtf(fmaf(head_sum<LANES>(sum), a.inv, a.eps));
+    read_pairs(table + in * kLaneFloats, cosine, sine);
+    read_pairs(weights[of] + in * kLaneFloats, wa, wb);
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
-      const float2 cs = table[in * 8 + p];
-      const float u = x[p] * rstd * (of ? ka[p] : qa[p]), v = y[p] * rstd * (of ? kb[p] : qb[p]);
-      x[p] = fmaf(u, cs.x, -(v * cs.y));
-      y[p] = fmaf(v, cs.x, u * cs.y);
+      const float u = x[p] * rstd * wa[p], v = y[p] * rstd * wb[p];
+      x[p] = fmaf(u, cosine[p], -(v * sine[p]));
+      y[p] = fmaf(v, cosine[p], u * sine[p]);
     }
     if (h < a.all)
       Raw<T, ORDER>::store((T*)a.to[of].p + token * a.to[of].token + (h - (of ? a.heads : 0)) * a.to[of].head, at, x, y);
   }
 }
 
+// Registers for four wavefronts a SIMD, three where rows are wider or in runs of four: 16384 tokens of 40 heads of 128 in 114 us,
+// with the weights in registers and two wavefronts 120, with three 130.
+template <class T, Order ORDER>
+constexpr int kPerSimd = sizeof(T) == 2 && ORDER != kFours ? 4 : 3;
 template <class T, int LANES, Order ORDER>
-__global__ __launch_bounds__(kThreads) void backward_kernel(Rotary a) {
-  __shared__ float2 tables[kWaves][64];
+__global__ __launch_bounds__(kThreads, (kPerSimd<T, ORDER>)) void backward_kernel(Rotary a) {
+  __shared__ __attribute__((aligned(16))) float tables[kWaves][8 * kLaneFloats];
+  __shared__ __attribute__((aligned(16))) float weights[2][LANES * kLaneFloats];
   __shared__ float sums[kWaves][2][LANES * 16];
+  constexpr int kHeads = Walk<LANES>::kHeads;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = lane % LANES, slot = lane / LANES;
-  float2* const table = tables[wave];
+  float* const table = tables[wave];
   const Place<ORDER> at(a, in * 8);
-  const double turns = turns_of(a, lane);
   Walk<LANES> w(a);
   Raw<T, ORDER> raw, grad;
   const auto load = [&] {
-    const int h = w.pass * Walk<LANES>::kHeads + slot, of = h >= a.heads, in_of = h - (of ? a.heads : 0);
+    const int h = w.pass * kHeads + slot, of = h >= a.heads, in_of = h - (of ? a.heads : 0);
     const int64_t token = w.token(a);
     raw.load((const T*)a.x[of].p + token * a.x[of].token + in_of * a.x[of].head, at, h < a.all);
     grad.load((const T*)a.dy[of].p + token * a.dy[of].token + in_of * a.dy[of].head, at, h < a.all);
   };
   if (w.there()) load();
-  float qa[8], qb[8], ka[8], kb[8];
-  weights(a.weight[0], at, qa, qb);
-  weights(a.weight[1], at, ka, kb);
+  const double turns = turns_of(a, lane);
+  keep_weights<LANES, ORDER>(a, weights);
   float da[2][8], db[2][8];
 #pragma unroll
   for (int p = 0; p < 8; ++p) da[0][p] = da[1][p] = db[0][p] = db[1][p] = 0.0f;
   int64_t known = -1;
   while (w.there()) {
     const int64_t token = w.token(a);
-    const int h = w.pass * Walk<LANES>::kHeads + slot, of = h >= a.heads;
-    float x[8], y[8], u[8], v[8], sum = 0.0f, dot = 0.0f;
+    const int first = w.pass * kHeads, h = first + slot, of = h >= a.heads;
+    float x[8], y[8], u[8], v[8], s[8], t[8], wa[8], wb[8], sum = 0.0f, dot = 0.0f;
     raw.get(x, y), grad.get(u, v);
     w.next(a);
     if (w.there()) load();
@@ -280,15 +309,30 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(Rotary a) {
 #pragma unroll
     for (int p = 0; p < 8; ++p) sum = fmaf(x[p], x[p], fmaf(y[p], y[p], sum));
     const float rstd = 1.0f / sqrtf(fmaf(head_sum<LANES>(sum), a.inv, a.eps));
+    read_pairs(table + in * kLaneFloats, wa, wb);
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {  // turned back
+      s[p] = fmaf(u[p], wa[p], v[p] * wb[p]), t[p] = fmaf(v[p], wa[p], -(u[p] * wb[p]));
+      x[p] *= rstd, y[p] *= rstd;
+    }
+    if (first + kHeads <= a.heads) {  // queries alone
+#pragma unroll
+      for (int p = 0; p < 8; ++p) da[0][p] = fmaf(s[p], x[p], da[0][p]), db[0][p] = fmaf(t[p], y[p], db[0][p]);
+    } else if (first >= a.heads) {  // keys alone
+#pragma unroll
+      for (int p = 0; p < 8; ++p) da[1][p] = fmaf(s[p], x[p], da[1][p]), db[1][p] = fmaf(t[p], y[p], db[1][p]);
+    } else {
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        const float m = s[p] * x[p], n = t[p] * y[p];
+        da[0][p] += of ? 0.0f : m, da[1][p] += of ? m : 0.0f;
+        db[0][p] += of ? 0.0f : n, db[1][p] += of ? n : 0.0f;
+      }
+    }
+    read_pairs(weights[of] + in * kLaneFloats, wa, wb);
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
-      const float2 cs = table[in * 8 + p];
-      const float s = fmaf(u[p], cs.x, v[p] * cs.y), t = fmaf(v[p], cs.x, -(u[p] * cs.y));  // turned back
-      x[p] *= rstd, y[p] *= rstd;
-      const float ds = s * x[p], dt = t * y[p];
-      da[0][p] += of ? 0.0f : ds, da[1][p] += of ? ds : 0.0f;
-      db[0][p] += of ? 0.0f : dt, db[1][p] += of ? dt : 0.0f;
-      u[p] = s * (of ? ka[p] : qa[p]), v[p] = t * (of ? kb[p] : qb[p]);
+      u[p] = s[p] * wa[p], v[p] = t[p] * wb[p];
       dot = fmaf(u[p], x[p], fmaf(v[p], y[p], dot));
     }
     dot = head_sum<LANES>(dot) * a.inv;
