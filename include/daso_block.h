@@ -89,7 +89,7 @@ typedef struct daso_attention_args {
   int32_t type;               /* of all rows */
   int32_t sequences;          /* 0..DASO_MAX_SEQUENCES; (tokens / 32 + sequences) * heads < 2^23 */
   uint32_t flags;             /* DASO_ATTENTION_* */
-  float scale;                /* > 0, finite */
+  float scale;                /* > 0, below 2^127 */
   uint32_t reserved;          /* 0 */
   const int64_t* offsets;     /* sequences + 1, device memory, or NULL with sequences == 1: all tokens */
   daso_heads q, k, v;         /* read; k and v have kv_heads */
@@ -105,7 +105,7 @@ int daso_attention(const daso_attention_args* args, hipStream_t stream);
 /* Its gradients: with p = exp(z - lse) and ds_j = p_j * (dout . v_j - dout . out),
  *     dq_i = scale * sum_j ds_j k_j,  dk_j = scale * sum_i ds_j q_i,  dv_j = sum_i p_j dout_i
  * the latter two over all tokens and heads that read key j, in a fixed order; with bf16 operands p and ds are
- * rounded to bf16 for the products. */
+ * rounded to bf16 for the products, and dout . out, which the rounding of out puts off, is set right by sum_j ds_j = 0. */
 int daso_attention_backward_workspace(const daso_attention_args* args, size_t* bytes);
 int daso_attention_backward(const daso_attention_args* args, hipStream_t stream);
 

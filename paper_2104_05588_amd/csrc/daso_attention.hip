@@ -19,7 +19,7 @@ constexpr float kGrowth = 10.0f;
 template <class T, int D>
 constexpr int kForwardPerSimd = sizeof(T) == 2 && D <= 64 ? 3 : sizeof(T) == 2 || D < 128 ? 2 : 1;
 template <class T, int D>
-constexpr int kQueryPerSimd = sizeof(T) == 2 ? (D <= 32 ? 3 : 2) : D <= 64 ? 2 : 1;
+constexpr int kQueryPerSimd = D <= 64 ? 2 : 1;
 template <class T, int D>
 __device__ inline void forward_tile(const Attention& a, const Place& at, char (&lds)[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes]) {
   using K = Kind<T, D>;
@@ -28,6 +28,7 @@ __device__ inline void forward_tile(const Attention& a, const Place& at, char (&
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
   const T *k = head_of<T>(a.k, at.start, at.head / a.share), *v = head_of<T>(a.v, at.start, at.head / a.share);
   char* const room = lds[0][0];
+  static_assert(sizeof lds >= Stage<T, D, kOwn, kThreads>::kBytes, "room for the workgroup's own rows");
   S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
   u4 q[K::kParts];
   {
@@ -143,6 +144,7 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
   const bool there = mine < at.len;
   const T *k = head_of<T>(a.k, at.start, at.head / a.share), *v = head_of<T>(a.v, at.start, at.head / a.share);
   char* const room = lds[0][0];
+  static_assert(sizeof lds >= Stage<T, D, kOwn, kThreads>::kBytes, "room for the workgroup's own rows");
   S ks(k, a.k.token, a.dim), vs(v, a.v.token, a.dim);
   u4 q[K::kParts], g[K::kParts];
   float delta = 0.0f;
@@ -168,38 +170,43 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
   }
   const int64_t stat = at.head * a.tokens + at.start + mine;
   const float lse2 = there ? a.lse[stat] * kLog2e : INFINITY;
-  if (there && lane < 32) a.delta[stat] = delta;
   const int last = a.causal ? min(mine, at.len - 1) : at.len - 1;
   const int keys = a.causal ? min(at.len, at.row + kOwn) : at.len;
   const int whole = sizeof(T) == 2 ? (a.causal ? min(at.len, at.row + 1) : at.len) / kKeys * kKeys : 0;  // as in the forward pass
-  f16v acc[D / 32];
+  // delta is dout . out of the rounded out, so it is off by up to 2^-8 of its terms, and ds_j by p_j times as much, which is more
+  // than the roundings of ds and dq make.  But the sum of ds is zero: what it comes to instead tells how far delta is off.  The
+  // pass by keys gets delta set right, and dq gives back that much of the keys' mean by p, a third product by
+  // keys.  With it dq and dk of 4 x 512 x 16 x 64 are off by 0.0024 of their norm and 0.0033 without, where the two roundings alone
+  // make 0.0023; it is a third of this pass's work (8 x 1024 x 16 x 64 causal in 59 us, 48 without; 8192 x 16 x 128 in 1205, 740).
+  constexpr bool kRounded = sizeof(T) == 2;
+  float off = 0.0f;
+  f16v acc[D / 32], mean[kRounded ? D / 32 : 1];
 #pragma unroll
   for (int b = 0; b < D / 32; ++b) acc[b] = (f16v)0.0f;
-  // The next tile in halves, as in the forward pass, where registers are short: 8192 x 16 x 128 in 730 us against 870 in one piece
-  // with one wavefront a SIMD.  Else in one, which has longer to come: 8192 x 16 x 64 in 419 us against 530.
-  constexpr bool kHalves = D > 96;
-  const auto fetch = [&](int key) {
-    ks.load(key, at.len);
-    if constexpr (!kHalves) vs.load(key, at.len);
-  };
-  const auto turn = [&](int key, int buffer) {
-    if constexpr (kHalves) ks.store(lds[buffer ^ 1][0]), vs.load(key + kKeys, at.len);
-  };
-  const auto keep = [&](int buffer) {
-    if constexpr (!kHalves) ks.store(lds[buffer][0]);
-    vs.store(lds[buffer][1]);
-  };
-  const auto step = [&](int key, int buffer) {
+#pragma unroll
+  for (int b = 0; b < (kRounded ? D / 32 : 1); ++b) mean[b] = (f16v)0.0f;
+  const auto fetch = [&](int key) { ks.load(key, at.len), vs.load(key, at.len); };
+  const auto keep = [&](int buffer) { ks.store(lds[buffer][0]), vs.store(lds[buffer][1]); };
+  const auto step = [&](int buffer) {
 #pragma unroll
     for (int s = 0; s < kSubs; ++s) {
       f16v z = scores<T, D>(lds[buffer][0], s * 32, q, (f16v)0.0f);
       const f16v dp = scores<T, D>(lds[buffer][1], s * 32, g, (f16v)(-delta));
 #pragma unroll
-      for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -lse2)) * dp[r];
-      const typename K::Right ds(z);
+      for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -lse2));
+      if constexpr (kRounded) {
+        const typename K::Right p(z);
+        z *= dp;
+        off += sum_of(z);
+        const typename K::Right ds(z);
 #pragma unroll
-      for (int b = 0; b < D / 32; ++b) K::gather(lds[buffer][0], s * 32, b, ds, acc[b]);
-      if (s == (kSubs - 1) / 2) turn(key, buffer);
+        for (int b = 0; b < D / 32; ++b) K::gather(lds[buffer][0], s * 32, b, ds, p, acc[b], mean[b]);
+      } else {
+        z *= dp;
+        const typename K::Right ds(z);
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) K::gather(lds[buffer][0], s * 32, b, ds, acc[b]);
+      }
     }
   };
   const auto step_part = [&](int key, int buffer) {
@@ -209,12 +216,24 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
       if (from >= keys || (a.causal && from >= first + 32)) break;
       f16v z = scores<T, D>(lds[buffer][0], s * 32, q, (f16v)0.0f);
       const f16v dp = scores<T, D>(lds[buffer][1], s * 32, g, (f16v)(-delta));
-#pragma unroll
-      for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -lse2)) * dp[r];
       const bool part = from + 31 > (a.causal ? min(first, at.len - 1) : at.len - 1);
-      if (part)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) z[r] = from + row_in(r) <= last ? z[r] : 0.0f;
+      for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -lse2));
+      if constexpr (kRounded) {
+        f16v p = z;
+        if (part)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) p[r] = from + row_in(r) <= last ? p[r] : 0.0f;
+        const typename K::Right weights(p);
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) {
+          if (part) K::template gather_part<1>(lds[buffer][0], s * 32, b, weights, last - key, mean[b]);
+          else K::gather(lds[buffer][0], s * 32, b, weights, mean[b]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z[r] = !part || from + row_in(r) <= last ? z[r] * dp[r] : 0.0f;
+      if constexpr (kRounded) off += sum_of(z);
       const typename K::Right ds(z);
 #pragma unroll
       for (int b = 0; b < D / 32; ++b) {
@@ -228,17 +247,23 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
   int key = 0, buffer = 0;
   for (; key < whole; key += kKeys, buffer ^= 1) {
     fetch(key + kKeys);
-    step(key, buffer);
+    step(buffer);
     keep(buffer ^ 1);
     __syncthreads();
   }
   for (; key < keys; key += kKeys, buffer ^= 1) {
     fetch(key + kKeys);
     step_part(key, buffer);
-    turn(key, buffer);
     keep(buffer ^ 1);
     __syncthreads();
   }
+  off = halves_sum(off);
+  if constexpr (kRounded)
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][r] = fmaf(-off, mean[b][r], acc[b][r]);
+  if (there && lane < 32) a.delta[stat] = delta + off;
   put_rows<T, D>(room, (T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, first, at.len, a.dim, acc, a.scale);
 }
 

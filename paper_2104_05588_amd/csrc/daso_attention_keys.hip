@@ -25,6 +25,7 @@ __device__ inline void key_tile(const Attention& a, const Place& at,
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
   const int kv = at.head / a.parts, part = at.head % a.parts, each = a.share / a.parts;
   char* const room = lds[0][0];
+  static_assert(sizeof lds >= Stage<T, D, kOwn, kThreads>::kBytes, "room for the workgroup's own rows");
   u4 k[K::kParts], v[K::kParts];
   {
     const Own<T, D> keys(head_of<T>(a.k, at.start, kv), a.k.token, at.row, at.len, a.dim);

@@ -28,7 +28,6 @@ template <class T>
 constexpr int kTile = sizeof(T) == 2 ? 64 : 32;  // rows of a tile in LDS
 using product::bhalf8;
 using product::half4;
-using product::half8;
 
 struct Rows {
   void* p;
@@ -251,17 +250,14 @@ struct Kind<uint16_t, D> {
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(tile, row, b, j), right.of[j], acc, 0, 0, 0);
   }
-  // Columns 32 b.. of 32 rows, read ahead.
-  struct Left {
-    bhalf8 of[2];
-    __device__ void read(const char* tile, int row, int b) {
+  // The same for two right operands at a time.
+  __device__ static void gather(const char* tile, int row, int b, const Right& right, const Right& other, f16v& acc, f16v& more) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) of[j] = turned(tile, row, b, j);
+    for (int j = 0; j < 2; ++j) {
+      const bhalf8 left = turned(tile, row, b, j);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(left, right.of[j], acc, 0, 0, 0);
+      more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(left, other.of[j], more, 0, 0, 0);
     }
-  };
-  __device__ static void gather(const Left& left, const Right& right, f16v& acc) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(left.of[j], right.of[j], acc, 0, 0, 0);
   }
   // The same where a column sees row i only if SIGN * i <= limit: what is no number in a row counts only in columns that see it.
   template <int SIGN>

@@ -102,7 +102,7 @@ int check_rotary(const daso_rotary_args& s, bool backward) {
 int check_attention_sizes(const daso_attention_args& s) {
   if (s.tokens < 0 || s.tokens > DASO_MAX_TOKENS || !heads_ok(s.heads) || !heads_ok(s.kv_heads) || s.heads % s.kv_heads != 0)
     return DASO_EINVAL;
-  if (!dim_ok(s.dim) || !known(s.type) || !(s.scale > 0.0f) || !std::isfinite(s.scale)) return DASO_EINVAL;
+  if (!dim_ok(s.dim) || !known(s.type) || !(s.scale > 0.0f) || !std::isfinite(2.0f * s.scale)) return DASO_EINVAL;
   if ((s.flags & ~(DASO_ATTENTION_CAUSAL | DASO_ATTENTION_ZERO_Q | DASO_ATTENTION_ZERO_K | DASO_ATTENTION_ZERO_V)) != 0 || s.reserved != 0 || s.sequences < 0 || s.sequences > DASO_MAX_SEQUENCES)
     return DASO_EINVAL;
   return (s.tokens / 32 + s.sequences) * s.heads < (int64_t(1) << 23) ? DASO_OK : DASO_EINVAL;

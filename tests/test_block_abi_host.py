@@ -104,7 +104,7 @@ def test_attention_rejects(lib):
                 v=h(2, 2), out=h(3), lse=A + 21 * MB, dout=h(4), dq=h(5), dk=h(6, 2), dv=h(7, 2), workspace=A + 30 * MB, workspace_bytes=MB)
     both = [(dict(tokens=-1), EINVAL), (dict(tokens=(1 << 24) + 1), EINVAL), (dict(heads=3), EINVAL), (dict(kv_heads=0), EINVAL),
             (dict(heads=2048), EINVAL), (dict(dim=4), EINVAL), (dict(dim=132), EINVAL), (dict(dim=136), EINVAL), (dict(type=3), EINVAL),
-            (dict(scale=0.0), EINVAL), (dict(scale=-1.0), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(scale=float("nan")), EINVAL),
+            (dict(scale=0.0), EINVAL), (dict(scale=-1.0), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(scale=3e38), EINVAL), (dict(scale=float("nan")), EINVAL),
             (dict(flags=16), EINVAL), (dict(reserved=1), EINVAL), (dict(sequences=-1), EINVAL), (dict(sequences=(1 << 20) + 1), EINVAL),
             (dict(tokens=1 << 24, heads=16, kv_heads=16), EINVAL), (dict(offsets=None), EINVAL), (dict(offsets=A + 20 * MB + 4), EALIGN),
             (dict(q=rows(None, 256, 64)), EINVAL), (dict(v=rows(None, 128, 64)), EINVAL), (dict(out=rows(None, 256, 64)), EINVAL),

@@ -376,6 +376,24 @@ def test_attention_of_many_sequences_and_other_layouts():
     assert torch.equal(out3, out) and all(torch.equal(a, b) for a, b in zip(got, grads))
 
 
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_gradients_of_bf16_are_off_by_their_own_roundings(dim, causal):
+    """A rounding to bf16 is off by at most 2^-8 of a value in [1, 2) times its power of two, evenly: by 2^-8 / sqrt(3) times
+    sqrt(E m^-2) = 0.74 of the norm, where the logarithm of m is spread evenly; that is 0.00166.  dq and dk have two of them, of ds
+    and their own (0.0024), dv of p and its own, out the same; a tenth more for the sample.  A delta of the rounded out, which is a
+    third one of dq and dk, makes 0.0031 and is not allowed here."""
+    n, heads = 512, 2
+    q, k, v, dout = attention_case(n, heads, heads, dim, BF16, 77 + dim)
+    out, lse, grads = both_ways(q, k, v, dout, None, causal)
+    qh, kh, vh, gh = (np64(t) for t in (q, k, v, dout))
+    c = 1 / np.sqrt(dim)
+    want = [O.attention(qh, kh, vh, None, causal, c)[0], *O.attention_backward(gh, qh, kh, vh, None, causal, c)]
+    for what, got, exact in zip(("out", "dq", "dk", "dv"), (out, *grads), want):
+        off = np.linalg.norm(np64(got.cpu()) - exact) / np.linalg.norm(exact)
+        assert off < 1.1 * np.sqrt(2) * 0.00166, (what, off)
+
+
 def test_attention_gradients_against_differences():
     """fp32, along random directions: (f(x + e d) - f(x - e d)) / 2e is off by e^2 f''' and rounding / e."""
     announce("differences")
