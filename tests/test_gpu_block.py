@@ -376,6 +376,22 @@ def test_attention_of_many_sequences_and_other_layouts():
     assert torch.equal(out3, out) and all(torch.equal(a, b) for a, b in zip(got, grads))
 
 
+@pytest.mark.parametrize("ends", [[0, 100, 40000, 40001, 40100], [0, 3000, 3000, 17000, 41000], [0] + [1000 * (i + 1) for i in range(40)]])
+def test_long_sequences_of_one_head_are_each_by_itself(ends):
+    """More tiles of a sequence than the order of their work is kept for, more sequences, and few of them: the same bits as by themselves."""
+    announce("long sequences", ends)
+    n, dim = ends[-1], 16
+    q, k, v, dout = (t.cuda() for t in attention_case(n, 1, 1, dim, BF16, 5))
+    off = torch.tensor(ends, device="cuda")
+    out, lse = daso.packed_attention(q, k, v, off)
+    grads = daso.packed_attention_backward(dout, q, k, v, out, lse, off)
+    for a, b in zip(ends, ends[1:]):
+        o, l = daso.packed_attention(q[a:b], k[a:b], v[a:b])
+        assert torch.equal(o, out[a:b]) and torch.equal(l, lse[:, a:b]), (a, b)
+        for got, one in zip(grads, daso.packed_attention_backward(dout[a:b], q[a:b], k[a:b], v[a:b], o, l)):
+            assert torch.equal(one, got[a:b]), (a, b)
+
+
 @pytest.mark.parametrize("dim", [32, 64, 96, 128])
 @pytest.mark.parametrize("causal", [True, False])
 def test_attention_gradients_of_bf16_are_off_by_their_own_roundings(dim, causal):
