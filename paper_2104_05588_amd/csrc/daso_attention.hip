@@ -27,7 +27,10 @@ constexpr float kGrowth = 10.0f;
 template <class T, int D>
 constexpr int kForwardPerSimd = sizeof(T) == 2 && D <= 64 ? 3 : sizeof(T) == 2 || D < 128 ? 2 : 1;
 template <class T, int D>
-constexpr int kQueryPerSimd = D <= 64 ? 2 : 1;
+constexpr int kQueryPerSimd = D <= 64 || (sizeof(T) == 2 && D == 96) ? 2 : 1;
+// Rows of a tile of its keys.
+template <class T, int D>
+constexpr int kQueryKeys = D == 96 ? 32 : kTile<T>;
 
 template <class T, int D>
 __device__ inline void forward_tile(const Attention& a, const Place& at, char (&lds)[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes]) {
@@ -145,9 +148,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kForwa
 }
 
 template <class T, int D>
-__device__ inline void query_tile(const Attention& a, const Place& at, char (&lds)[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes]) {
+__device__ inline void query_tile(const Attention& a, const Place& at, char (&lds)[2][2][Stage<T, D, kQueryKeys<T, D>, kThreads>::kBytes]) {
   using K = Kind<T, D>;
-  constexpr int kKeys = kTile<T>, kSubs = kKeys / 32;
+  constexpr int kKeys = kQueryKeys<T, D>, kSubs = kKeys / 32;
   using S = Stage<T, D, kKeys, kThreads>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = at.row + wave * 32, mine = first + (lane & 31);
   const bool there = mine < at.len;
@@ -184,8 +187,8 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
   const int whole = sizeof(T) == 2 ? (a.causal ? min(at.len, at.row + 1) : at.len) / kKeys * kKeys : 0;  // as in the forward pass
   // delta is dout . out of the rounded out, so it is off by up to 2^-8 of its terms, and ds_j by p_j times as much, which is more
   // than the roundings of ds and dq make.  But the sum of ds is zero: what it comes to instead tells how far delta is off.  The
-  // pass by keys gets delta set right, and dq gives back that much of the keys' mean by p, a third product by
-  // keys.  With it dq and dk of 8 x 1024 x 16 x 64, causal, are off by 0.0024 of their norm and by 0.0031 without, where the two
+  // pass by keys gets delta set right, and dq gives back that much of the keys' mean by p, a fourth product.
+  // With it dq and dk of 8 x 1024 x 16 x 64, causal, are off by 0.0024 of their norm and by 0.0031 without, where the two
   // roundings alone make 0.0023; it is a third of this pass's work (8 x 1024 x 16 x 64 causal in 59 us, 48 without; 8192 x 16 x 128 in 1205, 740).
   constexpr bool kRounded = sizeof(T) == 2;
   float off = 0.0f;
@@ -278,7 +281,7 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
 
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kQueryPerSimd<T, D>, kQueryPerSimd<T, D>))) void query_kernel(Attention a) {
-  __shared__ __attribute__((aligned(16))) char lds[2][2][Stage<T, D, kTile<T>, kThreads>::kBytes];
+  __shared__ __attribute__((aligned(16))) char lds[2][2][Stage<T, D, kQueryKeys<T, D>, kThreads>::kBytes];
   Place at;
   const Found found = place_of<kOwn, true>(a, a.heads, &at);
   if (found == kSequence) return query_tile<T, D>(a, at, lds);
