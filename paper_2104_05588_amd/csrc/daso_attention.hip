@@ -10,7 +10,7 @@
 // wavefronts.  A workgroup of four wavefronts shares the tiles of 64 keys (32 in fp32): its own 128 rows are
 // in registers, so what is read from LDS is the tile's alone, and the next tile is on its way meanwhile.
 // 8192 x 16 x 64, not causal: 375 us forward (0.73 PFLOP/s), 530 by queries (1.04 with the mean's product), 660 by keys (0.83);
-// 8192 x 16 x 128: 585 (0.94), 1240 (0.89), 1380 (0.80).
+// 8192 x 16 x 128: 585 (0.94), 1129 (0.97), 1380 (0.80).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -23,12 +23,12 @@ namespace {
 
 constexpr float kGrowth = 10.0f;
 // Wavefronts a SIMD that the registers are dealt for: as many as leave no spills in the loop over whole tiles, which cost more than a
-// wavefront (by queries with 96 elements: 970 us for 8192 x 16 with one, 1375 with two).
+// wavefront (by queries with 96 elements and tiles of 64 keys: 970 us for 8192 x 16 with one, 1375 with two).
 template <class T, int D>
 constexpr int kForwardPerSimd = sizeof(T) == 2 && D <= 64 ? 3 : sizeof(T) == 2 || D < 128 ? 2 : 1;
 template <class T, int D>
 constexpr int kQueryPerSimd = D <= 64 || (sizeof(T) == 2 && D == 96) ? 2 : 1;
-// Rows of a tile of its keys.
+// Rows of a tile of its keys: with 96 elements 32, which leaves registers for two wavefronts a SIMD, 792 us.
 template <class T, int D>
 constexpr int kQueryKeys = D == 96 ? 32 : kTile<T>;
 
@@ -189,8 +189,8 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
   // than the roundings of ds and dq make.  But the sum of ds is zero: what it comes to instead tells how far delta is off.  The
   // pass by keys gets delta set right, and dq gives back that much of the keys' mean by p, a fourth product.
   // With it dq and dk of 8 x 1024 x 16 x 64, causal, are off by 0.0024 of their norm and by 0.0031 without, where the two
-  // roundings alone make 0.0023; it is a third of this pass's work (8 x 1024 x 16 x 64 causal in 59 us, 48 without; 8192 x 16 x 128 in 1205, 740).
-  constexpr bool kRounded = sizeof(T) == 2;
+  // roundings alone make 0.0023; it is a third of this pass's work (8 x 1024 x 16 x 64 causal in 59 us, 48 without; 8192 x 16 x 128 in 1129, 740).
+  constexpr bool kRounded = sizeof(T) == 2, kAlone = kRounded && kQueryPerSimd<T, D> == 1;
   float off = 0.0f;
   f16v acc[D / 32], mean[kRounded ? D / 32 : 1];
 #pragma unroll
@@ -203,7 +203,30 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
 #pragma unroll
     for (int s = 0; s < kSubs; ++s) {
       f16v z = scores<T, D>(lds[buffer][0], s * 32, q, (f16v)0.0f);
-      const f16v dp = scores<T, D>(lds[buffer][1], s * 32, g, (f16v)(-delta));
+      f16v dp = (f16v)(-delta);
+      if constexpr (kAlone) {
+        // one wavefront a SIMD: the powers are taken while the matrix cores work on dp, and ds while they work on the mean
+        // (8192 x 16 x 128 in 1129 us, 1277 in the order below)
+        Parts<T, D> rows;
+        rows.read(lds[buffer][1], s * 32);
+        pin();
+#pragma unroll
+        for (int j = 0; j < K::kParts; ++j) {
+          dp = K::multiply(rows.of[j], g[j], dp);
+#pragma unroll
+          for (int r = j * 16 / K::kParts; r < (j + 1) * 16 / K::kParts; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -lse2));
+          pin();
+        }
+        const typename K::Right p(z);
+        const typename K::Left columns(lds[buffer][0], s * 32);
+        columns.gather(p, mean);
+        z *= dp;
+        off += sum_of(z);
+        const typename K::Right ds(z);
+        columns.gather(ds, acc);
+        continue;
+      }
+      dp = scores<T, D>(lds[buffer][1], s * 32, g, dp);
 #pragma unroll
       for (int r = 0; r < 16; ++r) z[r] = exp2_fast(fmaf(z[r], a.scale2, -lse2));
       if constexpr (kRounded) {

@@ -250,6 +250,22 @@ struct Kind<uint16_t, D> {
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(tile, row, b, j), right.of[j], acc, 0, 0, 0);
   }
+  // All columns of 32 rows, for several right operands one after the other.
+  struct Left {
+    bhalf8 of[D / 32][2];
+    __device__ Left(const char* tile, int row) {
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) of[b][j] = turned(tile, row, b, j);
+    }
+    __device__ void gather(const Right& right, f16v (&acc)[D / 32]) const {
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(of[b][j], right.of[j], acc[b], 0, 0, 0);
+    }
+  };
   // The same for two right operands at a time.
   __device__ static void gather(const char* tile, int row, int b, const Right& right, const Right& other, f16v& acc, f16v& more) {
 #pragma unroll
