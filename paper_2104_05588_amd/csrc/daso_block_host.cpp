@@ -12,11 +12,13 @@ namespace host {
 namespace {
 
 // A buffer as rows that do not overlap, twice: as its tokens' (or its heads') rows whole, and, where all (token, head) rows
-// lie a multiple of one distance apart, as those rows themselves (else as the first).
+// lie a multiple of one distance apart, as those rows themselves (else as the first).  And the distances of neighbouring tokens
+// and heads, 0 where there is one of them.
 struct Rows {
   Block whole, each;
+  int64_t token, head;
 };
-Rows line(const void* p, int64_t n, size_t esz) { return {flat(p, n, esz), flat(p, n, esz)}; }
+Rows line(const void* p, int64_t n, size_t esz) { return {flat(p, n, esz), flat(p, n, esz), 0, 0}; }
 
 // Whether the rows lie as daso_heads says, and how.
 bool rows_of_heads(const daso_heads& h, int64_t tokens, int64_t heads, int64_t dim, size_t esz, Rows* to) {
@@ -28,7 +30,7 @@ bool rows_of_heads(const daso_heads& h, int64_t tokens, int64_t heads, int64_t d
   if (tokens == 1 || ts >= token) to->whole = rows_of(h.data, tokens, ts, token, esz);
   else if (heads == 1 || hs >= head) to->whole = rows_of(h.data, heads, hs, head, esz);
   else return false;
-  to->each = to->whole;
+  to->each = to->whole, to->token = ts, to->head = hs;
   if (heads > 1 && tokens > 1 && ts % hs == 0) to->each = rows_of(h.data, tokens * heads, hs, dim, esz);
   else if (heads > 1 && tokens > 1 && hs % ts == 0) to->each = rows_of(h.data, tokens * heads, ts, dim, esz);
   return true;
@@ -36,14 +38,19 @@ bool rows_of_heads(const daso_heads& h, int64_t tokens, int64_t heads, int64_t d
 
 bool meet(const Rows& a, const Rows& b) { return overlap(a.whole, b.whole) && !beside(a.each, b.each); }
 
-// Outputs against inputs and each other.  The first `in_place` outputs may be the input of the same number, row for row
-// (of the same row length too, which the other stride makes).
+// The same rows for the same tokens and heads.  (Both distances: with as many tokens as heads a buffer with the two
+// exchanged has the same rows, which are other tokens'.)
+bool same_rows(const Rows& a, const Rows& b) {
+  return a.whole.p == b.whole.p && a.whole.esz == b.whole.esz && a.token == b.token && a.head == b.head;
+}
+
+// Outputs against inputs and each other.  The first `in_place` outputs may be the input of the same number, row for row.
 int check_rows(std::initializer_list<Rows> outputs, std::initializer_list<Rows> inputs, int in_place) {
   int k = 0;
   for (const Rows* o = outputs.begin(); o != outputs.end(); ++o, ++k) {
     int i = 0;
     for (const Rows& in : inputs) {
-      const bool allowed = i == k && k < in_place && same(o->whole, in.whole) && o->whole.row == in.whole.row;
+      const bool allowed = i == k && k < in_place && same_rows(*o, in);
       if (!allowed && meet(*o, in)) return DASO_EALIAS;
       ++i;
     }

@@ -97,6 +97,27 @@ def test_rotary_rejects(lib):
         assert fn(None, None) == EINVAL
 
 
+def test_rotary_in_place_is_of_the_same_distances(lib):
+    """With tokens and heads exchanged the same bytes are other tokens' rows: no output may lie so over its input."""
+    no_gpu()
+    for n, kv in ((4, 4), (7, 7), (3, 2)):
+        token, head = (n * 64, 64), (64, n * 64)
+        apart = lambda i, s: rows(A + i * MB, *s)  # noqa: E731
+        base = dict(tokens=n, heads=n, kv_heads=kv, dim=64, rotated=64, type=1, eps=1e-6, positions=A + 20 * MB, frequencies=A + 21 * MB,
+                    q=apart(0, token), k=apart(1, token), q_out=apart(2, token), k_out=apart(3, token), dq_out=apart(4, token),
+                    dk_out=apart(5, token), dq=apart(6, token), dk=apart(7, token), dq_weight=A + 24 * MB, workspace=A + 30 * MB,
+                    workspace_bytes=0)
+        refused(lib.daso_head_norm_rotary, K.daso_rotary_args, base, [
+            (dict(q_out=apart(0, head)), EALIAS), (dict(q=apart(0, head), q_out=apart(0, token)), EALIAS), (dict(k_out=apart(1, head)), EALIAS)])
+        # in place with the same distances comes as far as a workspace that is too small
+        refused(lib.daso_head_norm_rotary_backward, K.daso_rotary_args, base, [
+            (dict(dq=apart(4, head)), EALIAS), (dict(dk=apart(5, head)), EALIAS), (dict(dq_out=apart(4, head), dq=apart(4, head)), ENOSPACE),
+            (dict(dq=apart(4, token), dk=apart(5, token)), ENOSPACE)])
+    # 3 tokens 100 apart, or 2 heads: both are rows of 24 elements 100 apart
+    mixed = dict(base, tokens=3, heads=2, kv_heads=1, dim=8, rotated=8, q=rows(A, 100, 16), k=rows(A + MB, 8, 8))
+    refused(lib.daso_head_norm_rotary, K.daso_rotary_args, mixed, [(dict(q_out=rows(A, 8, 100)), EALIAS)])
+
+
 def test_attention_rejects(lib):
     no_gpu()
     h = lambda i, n=4: rows(A + i * MB, n * 64, 64)  # noqa: E731

@@ -26,3 +26,16 @@ def test_block_host_code_under_asan_and_ubsan(tmp_path):
     assert res.returncode == 0, res.stderr[-4000:]
     assert "runtime error" not in res.stderr and "AddressSanitizer" not in res.stderr, res.stderr[-4000:]
     assert "block host checks ok" in res.stdout
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_accepted_rows_touch_no_other_rows(tmp_path):
+    exe = tmp_path / "block_alias_checks"
+    cmd = ["g++", "-std=c++17", "-O2", "-Wall", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+           "-I", "/opt/rocm/include", os.path.join(CSRC, "daso_block_host.cpp"), os.path.join(CSRC, "daso_train_host.cpp"),
+           os.path.join(ROOT, "tests", "c", "block_alias_checks.cpp"), "-o", str(exe)]
+    built = subprocess.run(cmd, capture_output=True, text=True)
+    assert built.returncode == 0, built.stderr[-4000:]
+    res = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, res.stderr[-4000:]
+    assert "block alias checks ok" in res.stdout
