@@ -308,7 +308,9 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, ORDER>)) void backward_kerne
     known = token;
 #pragma unroll
     for (int p = 0; p < 8; ++p) sum = fmaf(x[p], x[p], fmaf(y[p], y[p], sum));
-    const float rstd = 1.0f / sqrtf(fmaf(head_sum<LANES>(sum), a.inv, a.eps));
+    // (lanes beyond the last head hold zeros, which without eps are no numbers once divided by their norm: their part of the
+    // weights' sums is to be 0)
+    const float rstd = h < a.all ? 1.0f / sqrtf(fmaf(head_sum<LANES>(sum), a.inv, a.eps)) : 0.0f;
     read_pairs(table + in * kLaneFloats, wa, wb);
 #pragma unroll
     for (int p = 0; p < 8; ++p) {  // turned back
