@@ -37,8 +37,9 @@ typedef struct daso_heads {
  *     n = x * rstd * weight,  rstd = 1 / sqrt(sum x^2 / dim + eps)
  *     y_a = n_a cos t - n_b sin t,  y_b = n_b cos t + n_a sin t,  t = position * frequency_j
  * for the pairs (a, b) = (j, j + rotated / 2) or, with DASO_ROTARY_INTERLEAVED, (2j, 2j + 1),
- * j < rotated / 2; elements from `rotated` on are y = n.  In 32 bits, rounded once to the type;
- * the angle is taken in 64 bits, so that far positions turn as exactly as near ones. */
+ * j < rotated / 2; elements from `rotated` on are y = n.  In 32 bits, rounded once to the type; squares that would
+ * leave their range are scaled, so that heads of any finite size have their norm (and without eps any but zero).
+ * The angle is taken in 64 bits, so that far positions turn as exactly as near ones. */
 typedef struct daso_rotary_args {
   int64_t tokens;
   int32_t heads, kv_heads;    /* 1..DASO_MAX_HEADS each */

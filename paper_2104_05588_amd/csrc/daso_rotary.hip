@@ -204,6 +204,30 @@ __device__ inline float head_sum(float v) {
   return v;
 }
 
+// 1 / sqrt(mean square + eps) of a head's elements x and y, whose mean square is `mean`.  Squares of elements beyond 2^64 or
+// below 2^-75 do not fit 32 bits: where any head's mean is far out, the elements are multiplied by a power of two, `scale`, first, and what is
+// returned is of those.  (2^-70 brings the largest to 2^58, and the sum of 128 squares below 2^123; eps goes along.)
+struct Size {
+  float rstd, scale;
+  bool scaled;  // of any head of the wavefront
+};
+template <int LANES>
+__device__ inline Size size_of(const Rotary& a, float mean, float (&x)[8], float (&y)[8]) {
+  Size s = {0.0f, 1.0f, __any(!(mean >= 0x1p-100f && mean <= 0x1p100f)) != 0};
+  if (__builtin_expect(s.scaled, 0)) {
+    s.scale = mean > 0x1p100f ? 0x1p-70f : mean < 0x1p-100f ? 0x1p96f : 1.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      x[p] *= s.scale, y[p] *= s.scale;
+      sum = fmaf(x[p], x[p], fmaf(y[p], y[p], sum));
+    }
+    mean = fmaf(head_sum<LANES>(sum), a.inv, a.eps * s.scale * s.scale);
+  }
+  s.rstd = 1.0f / sqrtf(mean);
+  return s;
+}
+
 // A wavefront's walk: tokens (or shares of them), and within one the heads, 64 / LANES at a time.
 template <int LANES>
 struct Walk {
@@ -255,7 +279,7 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(Rotary a) {
     known = token;
 #pragma unroll
     for (int p = 0; p < 8; ++p) sum = fmaf(x[p], x[p], fmaf(y[p], y[p], sum));
-    const float rstd = 1.0f / sqrtf(fmaf(head_sum<LANES>(sum), a.inv, a.eps));
+    const float rstd = size_of<LANES>(a, fmaf(head_sum<LANES>(sum), a.inv, a.eps), x, y).rstd;
     read_pairs(table + in * kLaneFloats, cosine, sine);
     read_pairs(weights[of] + in * kLaneFloats, wa, wb);
 #pragma unroll
@@ -310,7 +334,8 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, ORDER>)) void backward_kerne
     for (int p = 0; p < 8; ++p) sum = fmaf(x[p], x[p], fmaf(y[p], y[p], sum));
     // (lanes beyond the last head hold zeros, which without eps are no numbers once divided by their norm: their part of the
     // weights' sums is to be 0)
-    const float rstd = h < a.all ? 1.0f / sqrtf(fmaf(head_sum<LANES>(sum), a.inv, a.eps)) : 0.0f;
+    const Size size = size_of<LANES>(a, fmaf(head_sum<LANES>(sum), a.inv, a.eps), x, y);
+    const float rstd = h < a.all ? size.rstd : 0.0f;
     read_pairs(table + in * kLaneFloats, wa, wb);
 #pragma unroll
     for (int p = 0; p < 8; ++p) {  // turned back
@@ -340,6 +365,9 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, ORDER>)) void backward_kerne
     dot = head_sum<LANES>(dot) * a.inv;
 #pragma unroll
     for (int p = 0; p < 8; ++p) x[p] = rstd * fmaf(-x[p], dot, u[p]), y[p] = rstd * fmaf(-y[p], dot, v[p]);
+    if (__builtin_expect(size.scaled, 0))
+#pragma unroll
+      for (int p = 0; p < 8; ++p) x[p] *= size.scale, y[p] *= size.scale;
     if (h < a.all)
       Raw<T, ORDER>::store((T*)a.to[of].p + token * a.to[of].token + (h - (of ? a.heads : 0)) * a.to[of].head, at, x, y);
   }
