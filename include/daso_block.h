@@ -81,8 +81,8 @@ int daso_head_norm_rotary_backward(const daso_rotary_args* args, hipStream_t str
  *     z_j = scale * q_i . k_j,  lse = log sum exp z_j,  out = sum exp(z_j - lse) v_j
  * Token strides are at most 2 * DASO_MAX_SIDE.  Nothing of a token that i does not see counts, whatever it holds.  Sums and statistics are in 32 bits; with
  * bf16 operands exp(z - max) is rounded to bf16 for its product with v.  offsets ascend from 0; a pair
- * that does not, or that passes `tokens`, is taken as an empty sequence.  The rows of tokens in no
- * sequence are not written but where a flag asks for zeros.  An infinite or NaN v_j may give NaN where the formula gives an infinity. */
+ * that does not, that passes `tokens` or that begins before the end of an earlier one is taken as an empty
+ * sequence, so that no two share a token.  The rows of tokens in no sequence are not written but where a flag asks for zeros.  An infinite or NaN v_j may give NaN where the formula gives an infinity. */
 typedef struct daso_attention_args {
   int64_t tokens;             /* <= DASO_MAX_TOKENS */
   int32_t heads, kv_heads;    /* 1..DASO_MAX_HEADS, heads a multiple of kv_heads */

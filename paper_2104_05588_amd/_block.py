@@ -196,7 +196,8 @@ def packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
     [tokens, kv_heads, dim], whose heads are shared by heads / kv_heads neighbouring query heads: out, of q's shape, and the
     log-sum-exp of the scores, fp32 [heads, tokens].  bf16 or fp32, a head's elements contiguous, dim a multiple of 8 up to
     128.  offsets (int64, on the device) holds the first token of each sequence and, last, where they end; without it
-    all tokens are one sequence.  Rows of tokens behind the last sequence are left as they are; in
+    all tokens are one sequence.  Pairs of offsets that fall, pass the tokens or begin before the end of an earlier one are empty
+    sequences.  Rows of tokens behind the last sequence are left as they are; in
     an out made here they are zeros; lse's follow out's.
     scale is 1 / sqrt(dim) unless given."""
     a = _attention_args(q, k, v, offsets, causal, scale)

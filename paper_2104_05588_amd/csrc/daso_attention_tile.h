@@ -73,6 +73,37 @@ constexpr int kSorted = 32;  // sequences, at most, whose tiles are taken in the
 // 64 forward in 154 us, 182 where each sequence begins with its heaviest tile.
 // kRest: a tile of the rows behind the last sequence.
 enum Found { kNone, kSequence, kRest };
+
+// The 64 pairs of offsets from `base` on, a lane's as from..to: empty where a pair falls or leaves the tokens and, once some pair has (`odd`),
+// where it begins before the end of one before it, so that no two sequences share a row.  Pairs that all ascend need no look at each other.
+// `end`: the last end so far.
+struct Pairs {
+  int64_t from, to;
+  __device__ Pairs(const Attention& a, int base, bool& odd, int& end) {
+    const int lane = threadIdx.x & 63;
+    from = to = 0;
+    if (base + lane < a.sequences) from = a.offsets[base + lane], to = a.offsets[base + lane + 1];
+    const bool fits = from >= 0 && to >= from && to <= a.tokens;
+    if (!fits) to = from = 0;
+    odd |= __any(!fits) != 0;
+    int upto = to > from ? static_cast<int>(to) : 0;
+    if (__builtin_expect(odd, 0)) {
+#pragma unroll
+      for (int s = 1; s < 64; s <<= 1) {
+        const int v = __shfl_up(upto, s);
+        if (lane >= s) upto = max(upto, v);
+      }
+      int before = __shfl_up(upto, 1);
+      before = max(lane == 0 ? 0 : before, end);
+      if (from < before) to = from = 0;
+      end = max(end, __builtin_amdgcn_readlane(upto, 63));
+    } else {
+      const uint64_t some = __ballot(upto > 0);
+      if (some != 0) end = __builtin_amdgcn_readlane(upto, 63 - __builtin_clzll(some));
+    }
+  }
+};
+
 template <int ROWS, bool QUERIES>
 __device__ inline Found place_of(const Attention& a, int heads, Place* at) {
   const int id = blockIdx.x;
@@ -94,11 +125,11 @@ __device__ inline Found place_of(const Attention& a, int heads, Place* at) {
     return index < tiles ? kSequence : kNone;
   }
   const int lane = threadIdx.x & 63;
-  int before = 0;
+  int before = 0, end = 0;
+  bool odd = false;
   for (int base = 0; base < a.sequences; base += 64) {
-    int64_t from = 0, to = 0;
-    if (base + lane < a.sequences) from = a.offsets[base + lane], to = a.offsets[base + lane + 1];
-    if (!(from >= 0 && to >= from && to <= a.tokens)) to = from = 0;
+    const Pairs pairs(a, base, odd, end);
+    const int64_t from = pairs.from, to = pairs.to;
     const int mine = (static_cast<int>(to - from) + ROWS - 1) / ROWS;
     if (a.causal && a.sorted && a.sequences <= kSorted) {
       // A tile's work is its place from the light end of its sequence, 1, 2, ..  more[j]: the tiles of more work than lane +

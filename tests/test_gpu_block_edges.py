@@ -6,7 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import paper_2104_05588_amd as daso  # noqa: E402
-from tests.test_gpu_block import BF16, F32, check_rotary, rotary_case  # noqa: E402
+from tests.test_gpu_block import BF16, F32, attention_case, check_attention, check_rotary, rotary_case  # noqa: E402
 from tests.test_gpu_train import announce  # noqa: E402
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(), reason="no GPU")]
@@ -53,3 +53,44 @@ def test_heads_of_any_size_have_their_norm(dtype, heads, kv, dim, inter, size, e
     dxq, dxk, dqw, dkw = daso.head_norm_rotary_backward(dq.cuda(), dk.cuda(), q.cuda(), k.cuda(), *args, eps=eps, interleaved=inter)
     check_rotary(q, dq, at, qw, freq, inter, yq, dxq, dqw, dtype, eps=eps)
     check_rotary(k, dk, at, kw, freq, inter, yk, dxk, dkw, dtype, eps=eps)
+
+
+# --------------------------------------------------------------- attention
+def sequences_of(offsets, n):
+    """Pairs that ascend within the tokens and begin behind all such pairs before them."""
+    out, end = [], 0
+    for a, b in zip(offsets, offsets[1:]):
+        if 0 <= a < b <= n:
+            if a >= end:
+                out.append((a, b))
+            end = max(end, b)
+    return out
+
+
+SHARED = [  # offsets that come back into sequences before them
+    (150, [0, 100, 50, 150]), (500, [0, 300, 0, 300, 0, 500]), (500, [200, 300, 100, 400, 350, 500, 400, 480]),
+    (1000, [7 * i for i in range(80)] + [300 + 7 * i for i in range(100)]), (400, [0, 400, 399, 400, 0, 1]),
+    (900, [10, 500] + [400, 600] * 40 + [0, 880, 890, 890, 0, 10])]
+
+
+@pytest.mark.parametrize("n,offsets", SHARED)
+@pytest.mark.parametrize("heads,kv,dim,dtype,causal", [(8, 8, 16, BF16, True), (3, 1, 72, F32, False)])
+def test_pairs_that_come_back_into_a_sequence_are_none(n, offsets, heads, kv, dim, dtype, causal):
+    """No token is in two sequences; each sequence is as by itself, and rows in none are left as they were."""
+    announce("pairs that come back", n, offsets[:8], heads, kv, dim, dtype, causal)
+    seqs = sequences_of(offsets, n)
+    host = attention_case(n, heads, kv, dim, dtype, n)
+    rest = torch.ones(n, dtype=torch.bool)
+    for a, b in seqs:
+        rest[a:b] = False
+    q, k, v, dout = (t.cuda() for t in host)
+    off, gone = torch.tensor(offsets, device="cuda"), rest.cuda()
+    out, lse = torch.full_like(q, 7), torch.full((heads, n), 7.0, device="cuda")
+    daso.packed_attention(q, k, v, off, causal, out=out, lse=lse)
+    grads = daso.packed_attention_backward(dout, q, k, v, out, lse, off, causal, dq=torch.full_like(q, 7), dk=torch.full_like(k, 7),
+                                           dv=torch.full_like(v, 7))
+    assert (out[gone] == 7).all() and (lse[:, gone] == 7).all() and all((t[gone] == 7).all() for t in grads)
+    for a, b in seqs[:3] + seqs[3::29] + seqs[-2:]:
+        check_attention(*(t[a:b] for t in host), None, causal, None, out[a:b], lse[:, a:b], [t[a:b] for t in grads], dtype)
+        alone, lse_alone = daso.packed_attention(q[a:b], k[a:b], v[a:b], None, causal)
+        assert torch.equal(alone, out[a:b]) and torch.equal(lse_alone, lse[:, a:b])
