@@ -70,7 +70,7 @@ int daso_head_norm_rotary_backward_workspace(const daso_rotary_args* args, size_
 int daso_head_norm_rotary_backward(const daso_rotary_args* args, hipStream_t stream);
 
 #define DASO_ATTENTION_CAUSAL 1u
-/* Zeros in the rows of tokens from the last offset on (else those rows are not written): */
+/* Zeros in the rows of tokens in no sequence (else those rows are not written): */
 #define DASO_ATTENTION_ZERO_Q 2u /* of out and lse, or of dq */
 #define DASO_ATTENTION_ZERO_K 4u /* of dk */
 #define DASO_ATTENTION_ZERO_V 8u /* of dv */
@@ -82,7 +82,8 @@ int daso_head_norm_rotary_backward(const daso_rotary_args* args, hipStream_t str
  * Token strides are at most 2 * DASO_MAX_SIDE.  Nothing of a token that i does not see counts, whatever it holds.  Sums and statistics are in 32 bits; with
  * bf16 operands exp(z - max) is rounded to bf16 for its product with v.  offsets ascend from 0; a pair
  * that does not, that passes `tokens` or that begins before the end of an earlier one is taken as an empty
- * sequence, so that no two share a token.  The rows of tokens in no sequence are not written but where a flag asks for zeros.  An infinite or NaN v_j may give NaN where the formula gives an infinity. */
+ * sequence, so that no two share a token.  The rows of tokens in no sequence, whichever they are, are not written but
+ * where a flag asks for zeros.  An infinite or NaN v_j may give NaN where the formula gives an infinity. */
 typedef struct daso_attention_args {
   int64_t tokens;             /* <= DASO_MAX_TOKENS */
   int32_t heads, kv_heads;    /* 1..DASO_MAX_HEADS, heads a multiple of kv_heads */

@@ -197,8 +197,8 @@ def packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
     log-sum-exp of the scores, fp32 [heads, tokens].  bf16 or fp32, a head's elements contiguous, dim a multiple of 8 up to
     128.  offsets (int64, on the device) holds the first token of each sequence and, last, where they end; without it
     all tokens are one sequence.  Pairs of offsets that fall, pass the tokens or begin before the end of an earlier one are empty
-    sequences.  Rows of tokens behind the last sequence are left as they are; in
-    an out made here they are zeros; lse's follow out's.
+    sequences.  Rows of tokens in no sequence, as those behind the last, are left as they are; in an out made here they are zeros;
+    lse's follow out's.
     scale is 1 / sqrt(dim) unless given."""
     a = _attention_args(q, k, v, offsets, causal, scale)
     with T._on(stream):
@@ -218,7 +218,7 @@ def packed_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tens
                               dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
                               stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """dq, dk and dv from the gradient dout of what packed_attention gave (out and lse) for the same arguments.  They may be
-    given, for instance as parts of one gradient of a joint projection: then the rows of tokens behind the last sequence are left as
+    given, for instance as parts of one gradient of a joint projection: then the rows of tokens in no sequence are left as
     they are, else they are zeros."""
     a = _attention_args(q, k, v, offsets, causal, scale)
     a.out, a.dout = _heads(out, q.shape, (q.dtype,), "out"), _heads(dout, q.shape, (q.dtype,), "dout")

@@ -143,8 +143,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kForwa
   const Found found = place_of<kOwn, true>(a, a.heads, &at);
   if (found == kSequence) return forward_tile<T, D>(a, at, lds);
   if (found == kNone || !a.zero_q) return;
-  zero_rows((T*)head_of<T>(a.out, at.start, at.head), a.out.token, at, a.dim);
-  zero_rows(a.lse + at.head * a.tokens + at.start, 1, at, 1);
+  over_rest<kOwn>(a, at, [&](int from, int to) {
+    zero_rows((T*)head_of<T>(a.out, at.start, at.head), a.out.token, from, to, a.dim);
+    zero_rows(a.lse + at.head * a.tokens + at.start, 1, from, to, 1);
+  });
 }
 
 template <class T, int D>
@@ -309,7 +311,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kQuery
   const Found found = place_of<kOwn, true>(a, a.heads, &at);
   if (found == kSequence) return query_tile<T, D>(a, at, lds);
   if (found == kNone || !a.zero_q) return;
-  zero_rows((T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, at, a.dim);
+  over_rest<kOwn>(a, at, [&](int from, int to) { zero_rows((T*)head_of<T>(a.dq, at.start, at.head), a.dq.token, from, to, a.dim); });
 }
 
 // ------------------------------------------------------------------------- host

@@ -152,8 +152,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kKeyPe
   if (found == kSequence) return key_tile<T, D>(a, at, lds, stats);
   if (found == kNone || at.head % a.parts != 0) return;
   at.head /= a.parts;
-  if (a.zero_k) zero_rows((T*)head_of<T>(a.dk, at.start, at.head), a.dk.token, at, a.dim);
-  if (a.zero_v) zero_rows((T*)head_of<T>(a.dv, at.start, at.head), a.dv.token, at, a.dim);
+  if (!a.zero_k && !a.zero_v) return;
+  over_rest<kOwn>(a, at, [&](int from, int to) {
+    if (a.zero_k) zero_rows((T*)head_of<T>(a.dk, at.start, at.head), a.dk.token, from, to, a.dim);
+    if (a.zero_v) zero_rows((T*)head_of<T>(a.dv, at.start, at.head), a.dv.token, from, to, a.dim);
+  });
 }
 
 // dk and dv of 32 rows from the parts, in order.

@@ -38,7 +38,7 @@ struct Attention {
   int64_t tokens;
   const int64_t* offsets;  // or null: one sequence of all tokens
   int32_t sequences, heads, kv_heads, share;  // share: query heads of a key head
-  int32_t dim, causal, zero_q, zero_k, zero_v;  // zeros behind the last sequence
+  int32_t dim, causal, zero_q, zero_k, zero_v;  // zeros in rows of no sequence
   int32_t tiles, sorted;  // tiles: of a head, at most
   float scale, scale2;  // scale2 = scale * log2 e
   Rows q, k, v, out, dout, dq, dk, dv;
@@ -49,10 +49,11 @@ struct Attention {
   float* partial;
 };
 
-// What a workgroup works on: rows `row`.. of the sequence of `len` tokens from `start` on.
+// What a workgroup works on: rows `row`.. of the sequence of `len` tokens from `start` on.  Of rows in no sequence (kRest) those from
+// `row` on, or, with `apart`, of all tokens' rows those in no sequence of every tile `apart` rows from the one before.
 struct Place {
   int64_t start;
-  int32_t len, row, head;
+  int32_t len, row, head, apart;
 };
 
 __device__ inline int64_t read_lane(int64_t v, int lane) {
@@ -71,12 +72,14 @@ constexpr int kSorted = 32;  // sequences, at most, whose tiles are taken in the
 // order of their work, the most first.  Else, whose keys would not fit the L2s together, head by head and sequence
 // by sequence, from another tile on in each, so that no part of an XCD is dealt the heavy ones alone: 32 x 1024 tokens of 16 heads of
 // 64 forward in 154 us, 182 where each sequence begins with its heaviest tile.
-// kRest: a tile of the rows behind the last sequence.
+// kRest: rows in no sequence.  They are those behind the last one, a tile each for the workgroups that are left, or, where
+// offsets begin later than at 0 or some pair is no sequence, all that these workgroups find between the sequences.  (One is left
+// at least: n sequences apart from each other have no more than tokens / ROWS + n tiles.)
 enum Found { kNone, kSequence, kRest };
 
-// The 64 pairs of offsets from `base` on, a lane's as from..to: empty where a pair falls or leaves the tokens and, once some pair has (`odd`),
-// where it begins before the end of one before it, so that no two sequences share a row.  Pairs that all ascend need no look at each other.
-// `end`: the last end so far.
+// The 64 pairs of offsets from `base` on, a lane's as from..to: empty where a pair falls or leaves the tokens and, once some
+// pair has (`odd`), where it begins before the end of one before it, so that no two sequences share a row.  Pairs that all ascend
+// need no look at each other.  `end`: the last end so far.
 struct Pairs {
   int64_t from, to;
   __device__ Pairs(const Attention& a, int base, bool& odd, int& end) {
@@ -178,11 +181,34 @@ __device__ inline Found place_of(const Attention& a, int heads, Place* at) {
     }
     before += __builtin_amdgcn_readlane(upto, 63);
   }
-  at->start = a.offsets[a.sequences];
-  if (at->start < 0 || at->start > a.tokens) return kNone;
+  odd |= a.offsets[0] != 0;
+  at->start = odd ? 0 : end;
   at->len = static_cast<int32_t>(a.tokens - at->start);
   at->row = (index - before) * ROWS;
+  at->apart = odd ? (a.tiles - before) * ROWS : 0;
   return at->row < at->len ? kRest : kNone;
+}
+
+// Calls zero(from, to) for runs of at most ROWS of the workgroup's rows in no sequence, counted from at.start.
+template <int ROWS, class F>
+__device__ inline void over_rest(const Attention& a, const Place& at, F zero) {
+  if (at.apart == 0) return zero(at.row, min(at.row + ROWS, at.len));
+  const auto gap = [&](int from, int to) {
+    int row = at.row;
+    if (from > row) row += (from - row) / at.apart * at.apart;
+    for (; row < to; row += at.apart) zero(max(row, from), min(row + ROWS, to));
+  };
+  int done = 0, end = 0;
+  bool odd = true;
+  for (int base = 0; base < a.sequences; base += 64) {
+    const Pairs pairs(a, base, odd, end);
+    for (uint64_t left = __ballot(pairs.to > pairs.from); left != 0; left &= left - 1) {
+      const int l = __builtin_ctzll(left);
+      gap(done, __builtin_amdgcn_readlane(static_cast<int>(pairs.from), l));
+      done = __builtin_amdgcn_readlane(static_cast<int>(pairs.to), l);
+    }
+  }
+  gap(done, at.len);
 }
 
 __device__ inline float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -522,11 +548,10 @@ __device__ inline void put_own(float* row, const f16v (&acc)[D / 32], float fact
              acc[b][4 * g + 3] * factor);
 }
 
-// Zeros in the tile's rows.
+// Zeros in rows from..to.
 template <class T>
-__device__ inline void zero_rows(T* p, int64_t stride, const Place& at, int dim) {
-  for (int i = threadIdx.x; i < kOwn * dim; i += kThreads)
-    if (at.row + i / dim < at.len) p[(at.row + i / dim) * stride + i % dim] = T(0);
+__device__ inline void zero_rows(T* p, int64_t stride, int from, int to, int dim) {
+  for (int i = threadIdx.x; i < (to - from) * dim; i += kThreads) p[(from + i / dim) * stride + i % dim] = T(0);
 }
 
 template <class T>

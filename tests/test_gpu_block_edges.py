@@ -67,30 +67,55 @@ def sequences_of(offsets, n):
     return out
 
 
+APART = [  # tokens and offsets whose sequences share no token, but leave some out
+    (100, [30, 80]), (5, [3]), (5, [-1]), (300, [1 << 50]), (300, [0, 40, 301]), (300, [17, 17, 170, 171, 999]), (200, [-7, 20, 60, 200]),
+    (700, [0, 130, 1 << 40, 140, 400, -1, 400, 640]), (13000, [100 + 129 * i for i in range(101)]),
+    (1000, [5 * i for i in range(70)] + [-1] + [400 + 2 * i for i in range(130)]), (600, [1, 1, 1]), (4000, [3000, 3300])]
 SHARED = [  # offsets that come back into sequences before them
     (150, [0, 100, 50, 150]), (500, [0, 300, 0, 300, 0, 500]), (500, [200, 300, 100, 400, 350, 500, 400, 480]),
     (1000, [7 * i for i in range(80)] + [300 + 7 * i for i in range(100)]), (400, [0, 400, 399, 400, 0, 1]),
     (900, [10, 500] + [400, 600] * 40 + [0, 880, 890, 890, 0, 10])]
 
 
-@pytest.mark.parametrize("n,offsets", SHARED)
-@pytest.mark.parametrize("heads,kv,dim,dtype,causal", [(8, 8, 16, BF16, True), (3, 1, 72, F32, False)])
-def test_pairs_that_come_back_into_a_sequence_are_none(n, offsets, heads, kv, dim, dtype, causal):
-    """No token is in two sequences; each sequence is as by itself, and rows in none are left as they were."""
-    announce("pairs that come back", n, offsets[:8], heads, kv, dim, dtype, causal)
+def no_sequence(n, offsets, heads, kv, dim, dtype, causal):
+    """Rows in no sequence are zeros in tensors made by the call, whatever memory they get, and left alone in given ones; each sequence
+    is as by itself."""
+    announce("rows in no sequence", n, offsets[:8], heads, kv, dim, dtype, causal)
     seqs = sequences_of(offsets, n)
     host = attention_case(n, heads, kv, dim, dtype, n)
     rest = torch.ones(n, dtype=torch.bool)
     for a, b in seqs:
         rest[a:b] = False
+    for t in host:
+        t[rest] = float("nan")
     q, k, v, dout = (t.cuda() for t in host)
-    off, gone = torch.tensor(offsets, device="cuda"), rest.cuda()
-    out, lse = torch.full_like(q, 7), torch.full((heads, n), 7.0, device="cuda")
-    daso.packed_attention(q, k, v, off, causal, out=out, lse=lse)
-    grads = daso.packed_attention_backward(dout, q, k, v, out, lse, off, causal, dq=torch.full_like(q, 7), dk=torch.full_like(k, 7),
-                                           dv=torch.full_like(v, 7))
-    assert (out[gone] == 7).all() and (lse[:, gone] == 7).all() and all((t[gone] == 7).all() for t in grads)
+    off = torch.tensor(offsets, device="cuda")
+    spoiled = [torch.full((n, h, dim), 7.0, dtype=dtype, device="cuda") for h in (heads, heads, kv, kv)] + [torch.full((heads, n), 7.0, device="cuda")]
+    del spoiled  # what the allocator hands out next
+    out, lse = daso.packed_attention(q, k, v, off, causal)
+    grads = daso.packed_attention_backward(dout, q, k, v, out, lse, off, causal)
+    gone = rest.cuda()
+    assert not out[gone].any() and not lse[:, gone].any() and not any(t[gone].any() for t in grads)
     for a, b in seqs[:3] + seqs[3::29] + seqs[-2:]:
         check_attention(*(t[a:b] for t in host), None, causal, None, out[a:b], lse[:, a:b], [t[a:b] for t in grads], dtype)
         alone, lse_alone = daso.packed_attention(q[a:b], k[a:b], v[a:b], None, causal)
         assert torch.equal(alone, out[a:b]) and torch.equal(lse_alone, lse[:, a:b])
+    to, stats = torch.full_like(q, 7), torch.full_like(lse, 7)
+    daso.packed_attention(q, k, v, off, causal, out=to, lse=stats)
+    given = daso.packed_attention_backward(dout, q, k, v, out, lse, off, causal, dq=torch.full_like(q, 7), dk=torch.full_like(k, 7),
+                                           dv=torch.full_like(v, 7))
+    assert (to[gone] == 7).all() and (stats[:, gone] == 7).all() and all((t[gone] == 7).all() for t in given)
+    assert torch.equal(to[~gone], out[~gone]) and torch.equal(stats[:, ~gone], lse[:, ~gone])
+    assert all(torch.equal(t[~gone], g[~gone]) for t, g in zip(given, grads))
+
+
+@pytest.mark.parametrize("n,offsets", APART)
+@pytest.mark.parametrize("heads,kv,dim,dtype,causal", [(8, 8, 16, BF16, True), (3, 1, 72, F32, False)])
+def test_rows_between_sequences_are_zeros_in_tensors_made_here(n, offsets, heads, kv, dim, dtype, causal):
+    no_sequence(n, offsets, heads, kv, dim, dtype, causal)
+
+
+@pytest.mark.parametrize("n,offsets", SHARED)
+@pytest.mark.parametrize("heads,kv,dim,dtype,causal", [(8, 8, 16, BF16, True), (3, 1, 72, F32, False)])
+def test_pairs_that_come_back_into_a_sequence_are_none(n, offsets, heads, kv, dim, dtype, causal):
+    no_sequence(n, offsets, heads, kv, dim, dtype, causal)
