@@ -103,3 +103,53 @@ def test_clipping_to_a_large_norm_steps_as_without():
         node.step(tokens, tokens[::-1], LM.Sequences(lay, 2, 33))
     a, b = (node.params[:lay.rest] for node in nodes)
     assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("vocab,d,blocks,heads,kv,rows,length", [(211, 64, 2, 4, 2, 3, 70), (300, 96, 1, 2, 2, 2, 129)])
+def test_gradients_of_an_fp32_model_against_autograd(vocab, d, blocks, heads, kv, rows, length):
+    """A model whose matrices are fp32 throughout has no roundings that a missing or wrong term could hide behind: a product of at most 384
+    terms is off by 384 * 2^-24 < 2^-15 of its terms, other steps by less; 16 of them a block and pass, as in bf16."""
+    print(f"fp32 attention model's gradients {vocab} {d} {blocks} {heads} {kv} {rows} {length}", flush=True)
+    lay = LM.Layout(vocab, d, blocks, heads, kv)
+    flat = lay.init(5)
+    gen = torch.Generator().manual_seed(6)
+    n = rows * length
+    tokens, targets = torch.randint(vocab, (n,), generator=gen), torch.randint(vocab, (n,), generator=gen)
+    targets[::7] = -100
+    exact = flat.double().requires_grad_()
+    want_loss = plain_loss(lay, exact, tokens, targets, rows)
+    want, = torch.autograd.grad(want_loss, exact)
+    grad = torch.full((lay.n,), 7.0, device="cuda")
+    loss = LM.gradients(lay, flat.cuda(), flat.cuda(), tokens.cuda(), targets.cuda(), grad, LM.Sequences(lay, rows, length))
+    tol = 2.0 ** -15 * 16 * (3 * blocks + 1)
+    assert abs(float(loss.double().sum()) / int((targets != -100).sum()) - float(want_loss.detach())) <= tol * float(want_loss.detach())
+    for name in lay.spans:
+        g, e = lay.view(grad, name).double().cpu(), lay.view(want, name)
+        assert float((g - e).norm()) <= tol * float(e.norm()), name
+
+
+@pytest.mark.gpu
+def test_a_small_clip_is_the_steps_norm():
+    """The replicas' mean gradient is longer than the clip, and the step takes it scaled to that."""
+    print("a small clip", flush=True)
+    lay, clip = LM.Layout(60, 64, 1, 4, 2), 1e-3
+    gen = torch.Generator("cuda").manual_seed(2)
+    tokens = [torch.randint(60, (3 * 40,), generator=gen, device="cuda") for _ in range(2)]
+    at = LM.Sequences(lay, 3, 40)
+    node = LM.Node(lay, 3, 2, clip=clip)
+    before, want = node.params.clone(), torch.zeros(lay.n, dtype=torch.float64, device="cuda")
+    for x, t in zip(tokens, tokens[::-1]):
+        grad = torch.zeros(lay.n, device="cuda")
+        LM.gradients(lay, node.params, node.wire, x, t, grad, at)
+        want += grad.double() / 2
+    long = float(want.norm())
+    assert long > 10 * clip
+    node.step(tokens, tokens[::-1], at)
+    # the mean's, the factor's and the scaled value's roundings, of 2^-24 each; index_add's order may differ in the embedding
+    got = node.grads[0].double()
+    assert float((got - want * (clip / (long + 1e-6))).norm()) <= clip * 2.0 ** -16
+    assert abs(float(got.norm()) - clip * long / (long + 1e-6)) <= clip * 2.0 ** -20
+    # plain SGD of the first step: lr 1, momentum from zero
+    k = lay.rest
+    assert float((before[:k] - got[:k].float() - node.params[:k]).abs().max()) <= 2.0 ** -22 * float(before[:k].abs().max())
