@@ -146,7 +146,8 @@ def head_norm_rotary_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: tor
                               dq_weight: Optional[torch.Tensor] = None, dk_weight: Optional[torch.Tensor] = None,
                               stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
     """dq, dk, dq_weight and dk_weight from the gradients dq_out and dk_out of what head_norm_rotary gave for q and k.  dq
-    and dk may be dq_out and dk_out; the weights' gradients are fp32 [dim], and may be views of a flat gradient buffer."""
+    and dk may be dq_out and dk_out; the weights' gradients are fp32 [dim], may be views of a flat gradient buffer, and are computed in any
+    case: without weights, for ones."""
     a = _rotary_args(q, k, positions, frequencies, q_weight, k_weight, eps, interleaved)
     dim = a.dim
     a.dq_out, a.dk_out = _heads(dq_out, q.shape, (q.dtype,), "dq_out"), _heads(dk_out, k.shape, (q.dtype,), "dk_out")
@@ -198,7 +199,8 @@ def packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
     128.  offsets (int64, on the device) holds the first token of each sequence and, last, where they end; without it
     all tokens are one sequence.  Pairs of offsets that fall, pass the tokens or begin before the end of an earlier one are empty
     sequences.  Rows of tokens in no sequence, as those behind the last, are left as they are; in an out made here they are zeros;
-    lse's follow out's.
+    lse's follow out's.  Meant for sequences of dozens of tokens and more, some thousands at most: short ones cost as much as ones of 128
+    tokens, and beyond that the time grows with the square of their number.
     scale is 1 / sqrt(dim) unless given."""
     a = _attention_args(q, k, v, offsets, causal, scale)
     with T._on(stream):
@@ -279,7 +281,7 @@ def gradient_norm(grads: Sequence[torch.Tensor], tensors: Optional[Sequence[Tupl
 def clip_gradients(grads: Sequence[torch.Tensor], max_norm: float, tensors: Optional[Sequence[Tuple[int, int]]] = None,
                    out: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The mean of the replicas' flat fp32 gradient buffers, scaled down to max_norm where its norm over all tensors is larger:
-    out = mean * min(1, max_norm / (norm + eps)), and what gradient_norm returns.  out is the first buffer unless given, and
+    out = mean * min(1, max_norm / (norm + eps)), and what gradient_norm returns.  max_norm and eps are taken as fp32.  out is the first buffer unless given, and
     may be any of them; a step then takes it as the gradient of one replica.  Elements outside the tensors stay as
     they are."""
     return _clip(grads, max_norm, tensors, grads[0] if out is None and len(grads) else out, eps, stream)

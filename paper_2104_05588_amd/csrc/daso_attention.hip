@@ -5,12 +5,14 @@
 // by queries (dq, and sum dout out, which the other reads), one by keys (dk and dv, over all query heads of the key
 // head).
 //
-// Bound by the matrix cores and the exponents together: a power takes a wavefront 8 cycles, the 16 of a lane's scores 128, where
-// the two products of 32 x 32 scores of 64 elements take 128 (a SIMD) as well, and the two overlap in part, from different
-// wavefronts.  A workgroup of four wavefronts shares the tiles of 64 keys (32 in fp32): its own 128 rows are
+// Bound by vector instructions and the matrix cores together, which overlap little, from different wavefronts.  Forward, the two
+// products of 32 x 32 scores of 64 elements take a SIMD 256 cycles (1024 operations each) and the vector instructions 458,
+// 128 of them for the 16 powers, 8 each; counted are 684 in all.  With 128 elements 512 and 537, of 1134.  By queries, with the
+// mean's product, 512 and 486 of 918, and with 128 elements and one wavefront a SIMD 1024 and 771 of 2394.  LDS is read for less than half of
+// the time in all of them.  A workgroup of four wavefronts shares the tiles of 64 keys (32 in fp32): its own 128 rows are
 // in registers, so what is read from LDS is the tile's alone, and the next tile is on its way meanwhile.
-// 8192 x 16 x 64, not causal: 375 us forward (0.73 PFLOP/s), 530 by queries (1.04 with the mean's product), 660 by keys (0.83);
-// 8192 x 16 x 128: 585 (0.94), 1129 (0.97), 1380 (0.80).
+// 8192 x 16 x 64, not causal, on two machines: 340 and 353 us forward (0.81 and 0.78 PFLOP/s), 489 and 510 by queries (1.12 and 1.08 with the
+// mean's product); 8192 x 16 x 128: 566 and 585 (0.97 and 0.94), 1047 and 1072 (1.05 and 1.03).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -28,7 +30,7 @@ template <class T, int D>
 constexpr int kForwardPerSimd = sizeof(T) == 2 && D <= 64 ? 3 : sizeof(T) == 2 || D < 128 ? 2 : 1;
 template <class T, int D>
 constexpr int kQueryPerSimd = D <= 64 || (sizeof(T) == 2 && D == 96) ? 2 : 1;
-// Rows of a tile of its keys: with 96 elements 32, which leaves registers for two wavefronts a SIMD, 792 us.
+// Rows of a tile of its keys: with 96 elements 32, which leaves registers for two wavefronts a SIMD, 710 to 743 us.
 template <class T, int D>
 constexpr int kQueryKeys = D == 96 ? 32 : kTile<T>;
 
@@ -191,7 +193,8 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
   // than the roundings of ds and dq make.  But the sum of ds is zero: what it comes to instead tells how far delta is off.  The
   // pass by keys gets delta set right, and dq gives back that much of the keys' mean by p, a fourth product.
   // With it dq and dk of 8 x 1024 x 16 x 64, causal, are off by 0.0024 of their norm and by 0.0031 without, where the two
-  // roundings alone make 0.0023; it is a third of this pass's work (8 x 1024 x 16 x 64 causal in 59 us, 48 without; 8192 x 16 x 128 in 1129, 740).
+  // roundings alone make 0.0023; it is a third of this pass's work (8 x 1024 x 16 x 64 causal 48 to 59 us and 8192 x 16 x 128 740 to 1129 when it came, with clocks not yet
+  // settled; 54 to 57 and 1047 to 1072 now).
   constexpr bool kRounded = sizeof(T) == 2, kAlone = kRounded && kQueryPerSimd<T, D> == 1;
   float off = 0.0f;
   f16v acc[D / 32], mean[kRounded ? D / 32 : 1];
@@ -208,7 +211,7 @@ __device__ inline void query_tile(const Attention& a, const Place& at, char (&ld
       f16v dp = (f16v)(-delta);
       if constexpr (kAlone) {
         // one wavefront a SIMD: the powers are taken while the matrix cores work on dp, and ds while they work on the mean
-        // (8192 x 16 x 128 in 1129 us, 1277 in the order below)
+        // (8192 x 16 x 128 in 1129 us, 1277 in the order below, one run against the other)
         Parts<T, D> rows;
         rows.read(lds[buffer][1], s * 32);
         pin();

@@ -1,9 +1,11 @@
 // Attention over packed sequences, the backward pass by keys (daso_block.h): a wavefront has 32 keys and walks over the queries
 // that see them, of all query heads of the key head.
 //
-// Four products of 32 x 32 scores against two exponents' cycles of the forward pass, so the matrix cores bound it; dk and dv
-// of a wavefront take 32 registers for each 32 elements, its keys and values 32 more, which leaves one wavefront a SIMD with 128 elements, 1380 us
-// for 8192 x 16 x 128, not causal (0.80 PFLOP/s), and two with fewer: 660 us for 8192 x 16 x 64 (0.83).
+// Four products of 32 x 32 scores, 512 cycles of a SIMD's matrix cores for 64 elements and 1024 for 128, beside the forward pass's 16 powers a
+// lane, 128 cycles of 476 and 744 in vector instructions, and 457 and 781 in LDS; counted are 1221 and 3247 in all, so that none of them
+// alone bounds it: they wait for each other.  dk and dv of a wavefront take 32 registers for each 32 elements, its keys and values 32 more,
+// which leaves one wavefront a SIMD with 128 elements, 1387 us for 8192 x 16 x 128, not causal (0.79 PFLOP/s), and two with
+// fewer: 569 and 590 us on two machines for 8192 x 16 x 64 (0.97 and 0.93).
 #include <hip/hip_runtime.h>
 
 #include "daso_attention_tile.h"

@@ -293,8 +293,8 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(Rotary a) {
   }
 }
 
-// Registers for four wavefronts a SIMD, three where rows are wider or in runs of four: 16384 tokens of 40 heads of 128 in 114 us,
-// with the weights in registers and two wavefronts 120, with three 130.
+// Registers for four wavefronts a SIMD, three where rows are wider or in runs of four: 16384 tokens of 40 heads of 128 in 114 us
+// (108 where the clocks have settled), with the weights in registers and two wavefronts 120, with three 130.
 template <class T, Order ORDER>
 constexpr int kPerSimd = sizeof(T) == 2 && ORDER != kFours ? 4 : 3;
 template <class T, int LANES, Order ORDER>
