@@ -129,7 +129,8 @@ def head_norm_rotary(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, 
     """The root-mean-square norm of each head of q [tokens, heads, dim] and k [tokens, kv_heads, dim] (bf16 or fp32, a
     head's elements contiguous, dim a multiple of 8 up to 128), and its rotation by the token's position (int64 [tokens])
     times the frequencies (float64, a multiple of 4 of them; see rotary_frequencies): of the pairs (j, j + rotated / 2), or
-    neighbours if `interleaved`.  The weights are fp32 [dim].  out_q and out_k may be q and k."""
+    neighbours if `interleaved`.  The weights are fp32 [dim].  out_q and out_k may be q and k, with the same strides.  Not recorded by
+    autograd, whatever the inputs require: head_norm_rotary_backward gives the gradients."""
     a = _rotary_args(q, k, positions, frequencies, q_weight, k_weight, eps, interleaved)
     with T._on(stream):
         out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out_q is None else out_q
@@ -201,7 +202,8 @@ def packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
     sequences.  Rows of tokens in no sequence, as those behind the last, are left as they are; in an out made here they are zeros;
     lse's follow out's.  Meant for sequences of dozens of tokens and more, some thousands at most: short ones cost as much as ones of 128
     tokens, and beyond that the time grows with the square of their number.
-    scale is 1 / sqrt(dim) unless given."""
+    scale is 1 / sqrt(dim) unless given.  Not recorded by autograd, whatever the inputs require: packed_attention_backward gives the
+    gradients."""
     a = _attention_args(q, k, v, offsets, causal, scale)
     with T._on(stream):
         if out is None:
